@@ -40,7 +40,11 @@ typedef enum {
     E3_ERR_LAUNCH = -7     /* the HIP runtime refused a launch (see hipGetLastError) */
 } e3_status;
 
-typedef enum { E3_F32 = 0, E3_BF16 = 1 } e3_dtype;
+typedef enum {
+    E3_F32 = 0,
+    E3_BF16 = 1,
+    E3_E4M3 = 2            /* 8-bit floating point (OCP e4m3): the elements of an e3_cache only */
+} e3_dtype;
 
 /*
  * Column partition of the two-level sampler (see e3_sample_entropy).  Columns
@@ -382,6 +386,105 @@ int e3_allocate_budgets(const double* k, int32_t B, int32_t G, int32_t G_min, in
  */
 int e3_budget_bounds(int32_t G, int32_t passes_done, int32_t step, int32_t G_min_limit,
                      int32_t G_max_limit, int32_t* G_min_out, int32_t* G_max_out);
+
+/* ------------------------------------------------------------------------------------
+ * The decode step in front of the sampler: a paged cache of keys and values, the
+ * attention of rollouts that share their question's prompt, the verification of drafted
+ * tokens.  (Section 4.1 gives every question its own number of rollouts, all of the same
+ * prompt: the groups are the CSR groups that e3_grpo_advantages takes.)
+ * ------------------------------------------------------------------------------------ */
+
+/*
+ * A paged cache (the struct itself is host memory, the arrays are device memory):
+ *   k  [num_pages][kv_heads][page_size][head_dim]
+ *   v  [num_pages][kv_heads][page_size / 8][head_dim][8]     (eight tokens of a column together)
+ * of bf16, or of e4m3 codes with one exponent per token and head in
+ *   k_scale, v_scale  [num_pages][kv_heads][page_size] uint8  (NULL for bf16):
+ * element = code * 2^(scale - 127).  Token s of the cache ("slot") is token s % page_size of
+ * page s / page_size.
+ * page_size is a power of two of at least 32, head_dim 64 or 128 (else E3_ERR_SHAPE); k and v
+ * are 16-byte, the scales 8-byte aligned (else E3_ERR_ALIGN).
+ */
+typedef struct {
+    void* k;
+    void* v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int64_t num_pages;
+    int32_t page_size, kv_heads, head_dim;
+    int32_t dtype;                 /* E3_BF16 or E3_E4M3 */
+} e3_cache;
+
+/*
+ * Write the keys and values of `tokens` tokens into the cache, quantising them where it holds
+ * 8 bits.  Per token, head and tensor, x being the head_dim elements:
+ *   a = largest finite |x_i|,   e = smallest integer in [-126, 127] with a <= 448 * 2^e,
+ *   code_i = e4m3(x_i * 2^-e), nearest, ties to even,   scale byte = e + 127.
+ * Scaling by a power of two is exact, nothing saturates, and values that are read back and
+ * written again keep their bits (but for magnitudes from 2^128 (1 - 2^-5) on, which round to
+ * 2^128 and read back as inf).  Elements that are not finite become the NaN code and do
+ * not enter a.  In a bf16 cache fp32 input is rounded (nearest, ties to even).
+ *
+ * k, v      [tokens][kv_heads][head_dim] of dtype (E3_BF16 / E3_F32), strides in elements,
+ *           columns next to each other; base and strides multiples of 16 bytes (E3_ERR_ALIGN).
+ * slots     [tokens] int64: where each goes.  A slot outside the cache (negative, say: padding)
+ *           is skipped.  Slots are expected to differ within a call; which of two tokens with one
+ *           slot is kept is not specified (elements and scale may then be of different tokens).
+ * tokens == 0 is a no-op.
+ */
+int e3_cache_append(const e3_cache* cache, const void* k, const void* v, int dtype, int64_t tokens,
+                    int64_t k_token_stride, int64_t k_head_stride,
+                    int64_t v_token_stride, int64_t v_head_stride,
+                    const int64_t* slots, void* hip_stream);
+
+/*
+ * Read tokens back: k_out, v_out [tokens][kv_heads][head_dim] contiguous, of dtype (E3_BF16 /
+ * E3_F32), 16-byte aligned.  Exact in fp32, and in bf16 down to its smallest normal number.
+ * A slot outside the cache reads as zeros.
+ */
+int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
+                  void* k_out, void* v_out, int dtype, void* hip_stream);
+
+/*
+ * Attention of one decode step.  Row r belongs to group g (group_offsets[g] <= r <
+ * group_offsets[g + 1]) and attends to the group's prefix, all of it, and to its own tokens, of
+ * which the last `queries` are the step's own: query t sees the first
+ * row_lens[r] - (queries - 1 - t).
+ *   s_j = scale q . k_j,   out = sum_j softmax(s)_j v_j,   lse = ln sum_j exp(s_j)
+ * Query head h reads key head h / (q_heads / kv_heads).  A query without any key (prefix and own
+ * tokens empty) gives 0 and -inf.  The prefix is read once for all rows of the group.
+ *
+ * q             [rows][queries][q_heads][head_dim] bf16, strides in elements, columns next to
+ *               each other; base and strides multiples of 16 bytes (E3_ERR_ALIGN).
+ * rows, queries, q_heads   q_heads a multiple of kv_heads (E3_ERR_SHAPE); one query per row is
+ *               the ordinary step, more are drafted tokens to be verified.
+ * group_offsets [num_groups + 1] int32, group_offsets[num_groups] = rows (the caller's contract);
+ *               NULL with num_groups == 0: no prefixes.  A row in no group has none.
+ * prefix_pages  [num_groups][prefix_width] int32, prefix_lens [num_groups] int32 (tokens).
+ * row_pages     [rows][row_width] int32, row_lens [rows] int32 (tokens, the step's included).
+ *               Lengths are cut to what the tables can hold; a page id outside the cache
+ *               hides its tokens.  Table entries behind a length are not read.  Whatever the cache
+ *               holds behind a length (NaN included) has no influence.
+ * scale         host, finite and > 0 (E3_ERR_VALUE).
+ * out           [rows][queries][q_heads][head_dim] bf16, contiguous, 16-byte aligned.
+ * lse_out       [rows][queries][q_heads] fp32 or NULL.
+ * workspace     device, 256-byte aligned (E3_ERR_ALIGN), at least
+ *               e3_prefix_attention_workspace_bytes() (else E3_ERR_WORKSPACE); contents on entry
+ *               ignored, no state between calls, to be used by one call at a time.
+ * Scores, maxima, sums and the output's sums in fp32; the weights enter the product with V with
+ * sixteen bits.  Where the keys are cut into runs depends on the lengths, so a row in another
+ * batch may differ in the last bits; the same call gives the same bits.
+ * e3_prefix_attention_workspace_bytes: host only; 0 for a shape that is not served.
+ */
+size_t e3_prefix_attention_workspace_bytes(int64_t rows, int64_t queries, int64_t q_heads, int64_t kv_heads,
+                                           int64_t head_dim, int64_t num_groups);
+int e3_prefix_attention(const e3_cache* cache, const void* q, int64_t rows, int64_t queries, int64_t q_heads,
+                        int64_t q_row_stride, int64_t q_token_stride, int64_t q_head_stride,
+                        const int32_t* group_offsets, int64_t num_groups,
+                        const int32_t* prefix_pages, int64_t prefix_width, const int32_t* prefix_lens,
+                        const int32_t* row_pages, int64_t row_width, const int32_t* row_lens,
+                        float scale, void* out, float* lse_out,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -14,7 +14,7 @@ import ctypes as C
 import importlib.machinery
 import importlib.util
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -22,7 +22,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libe3.so")
 NATIVE_PATH = os.path.join(HERE, "_native.so")
 
-E3_F32, E3_BF16 = 0, 1
+E3_F32, E3_BF16, E3_E4M3 = 0, 1, 2
 E3_OK = 0
 E3_TILE_CHUNK, E3_TILE_LANES, E3_TILE_DEPTH = 8, 64, 8
 E3_NOALLOC_MAX_ROWS = 1024
@@ -32,7 +32,8 @@ EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_
            "e3_logprob_entropy", "e3_logprob_entropy_advantages",
            "e3_grpo_advantages", "e3_temperature_update", "e3_difficulty_ranks",
            "e3_allocate_budgets", "e3_budget_bounds", "e3_logprob_entropy_gap",
-           "e3_temperature_update_gap", "e3_grpo_objective", "e3_read_probe",
+           "e3_temperature_update_gap", "e3_grpo_objective", "e3_cache_append", "e3_cache_read",
+           "e3_prefix_attention", "e3_prefix_attention_workspace_bytes", "e3_read_probe",
            "e3_time_next_launch", "e3_launch_plan", "e3_launch_plan_of")
 
 _NATIVE_CALLS = ("e3_grpo_advantages", "e3_grpo_objective", "e3_workspace_bytes", "e3_sample_entropy",
@@ -113,6 +114,15 @@ def lib() -> C.CDLL:
         L.e3_allocate_budgets.restype = C.c_int
         L.e3_budget_bounds.argtypes = [i32, i32, i32, i32, i32, vp, vp]
         L.e3_budget_bounds.restype = C.c_int
+        L.e3_cache_append.argtypes = [vp, vp, vp, C.c_int, i64, i64, i64, i64, i64, vp, vp]
+        L.e3_cache_append.restype = C.c_int
+        L.e3_cache_read.argtypes = [vp, vp, i64, vp, vp, C.c_int, vp]
+        L.e3_cache_read.restype = C.c_int
+        L.e3_prefix_attention_workspace_bytes.argtypes = [i64] * 6
+        L.e3_prefix_attention_workspace_bytes.restype = C.c_size_t
+        L.e3_prefix_attention.argtypes = [vp, vp, i64, i64, i64, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, f32,
+                                          vp, vp, vp, C.c_size_t, vp]
+        L.e3_prefix_attention.restype = C.c_int
         _bind_native(L)                           # may raise: nothing is loaded then
         _lib = L
     return _lib
@@ -618,3 +628,161 @@ def e3_grpo_objective(logp_new: torch.Tensor, logp_old: torch.Tensor, seq_offset
     if rc != E3_OK:
         raise E3Error(rc, "e3_grpo_objective")
     return J, seq_mean, terms
+
+
+class E3Cache(NamedTuple):
+    """A paged cache of keys and values (e3_cache in include/e3.h): k [pages, heads, page, D], v [pages, heads, page / 8, D, 8]
+    of torch.bfloat16, or of torch.float8_e4m3fn with the exponent bytes k_scale, v_scale [pages, heads, page]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+class _CacheStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("num_pages", C.c_int64), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+def new_cache(num_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype: torch.dtype = torch.float8_e4m3fn,
+              device="cuda") -> E3Cache:
+    """Allocate an empty cache.  dtype: torch.float8_e4m3fn (8 bits, quantised as it is written) or torch.bfloat16."""
+    if dtype not in (torch.float8_e4m3fn, torch.bfloat16):
+        raise TypeError(f"unsupported cache dtype {dtype}")
+    if page_size < 32 or page_size & (page_size - 1):
+        raise ValueError("page_size must be a power of two of at least 32")
+    k = torch.zeros((num_pages, kv_heads, page_size, head_dim), dtype=dtype, device=device)
+    v = torch.zeros((num_pages, kv_heads, page_size // 8, head_dim, 8), dtype=dtype, device=device)
+    if dtype is torch.bfloat16:
+        return E3Cache(k, v)
+    scales = [torch.zeros((num_pages, kv_heads, page_size), dtype=torch.uint8, device=device) for _ in range(2)]
+    return E3Cache(k, v, *scales)
+
+
+def _cache(cache) -> _CacheStruct:
+    k, v, ks, vs = cache
+    if k.dim() != 4 or not k.is_cuda:
+        raise ValueError("a cache's keys must be [pages, heads, page, D] on the GPU")
+    pages, heads, page, D = k.shape
+    dev = k.device
+    if k.dtype is torch.bfloat16:
+        dt = E3_BF16
+    elif k.dtype is torch.float8_e4m3fn:
+        dt = E3_E4M3
+    else:
+        raise TypeError(f"unsupported cache dtype {k.dtype}")
+    if v.dtype is not k.dtype or v.device != dev or v.shape != (pages, heads, page // 8, D, 8):
+        raise ValueError("a cache's values must be [pages, heads, page / 8, D, 8] of the keys' type and device")
+    if not k.is_contiguous() or not v.is_contiguous():
+        raise ValueError("a cache's tensors must be contiguous")
+    for t, name in ((ks, "k_scale"), (vs, "v_scale")):
+        if (t is None) != (dt == E3_BF16):
+            raise ValueError(f"{name} belongs to an 8-bit cache, and to no other")
+        if t is not None and (t.dtype is not torch.uint8 or t.shape != (pages, heads, page) or t.device != dev
+                              or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous uint8 tensor [pages, heads, page] on {dev}")
+    return _CacheStruct(_ptr(k), _ptr(v), _ptr(ks), _ptr(vs), pages, page, heads, D, dt)
+
+
+_FLOATS = {torch.bfloat16: E3_BF16, torch.float32: E3_F32}
+
+
+def _float_type(dtype) -> int:
+    if dtype not in _FLOATS:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return _FLOATS[dtype]
+
+
+def e3_cache_append(cache: E3Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Write keys and values [tokens, heads, D] (bf16 or fp32, any strides with columns next to each other) to the slots
+    (int64 [tokens]; negative: skipped) of the cache."""
+    c = _cache(cache)
+    dev = cache[0].device
+    dt = _float_type(k.dtype)
+    n = slots.shape[0]
+    for t, name in ((k, "k"), (v, "v")):
+        if t.dtype is not k.dtype or t.shape != (n, c.kv_heads, c.head_dim) or t.device != dev or (n and t.stride(2) != 1):
+            raise ValueError(f"{name} must be a {k.dtype} tensor [{n}, {c.kv_heads}, {c.head_dim}] with unit column stride on {dev}")
+    _check(slots, torch.int64, n, "slots", dev)
+    rc = lib().e3_cache_append(C.byref(c), _ptr(k), _ptr(v), dt, n, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+                               _ptr(slots), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_cache_append")
+
+
+def e3_cache_read(cache: E3Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
+                  k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """Returns (k, v) [tokens, heads, D] of the slots (int64 [tokens]; outside the cache: zeros) in bf16 or fp32."""
+    c = _cache(cache)
+    dev = cache[0].device
+    n = slots.shape[0]
+    _check(slots, torch.int64, n, "slots", dev)
+    outs = []
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is None:
+            t = torch.empty((n, c.kv_heads, c.head_dim), dtype=dtype, device=dev)
+        elif t.dtype is not dtype or t.shape != (n, c.kv_heads, c.head_dim) or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor [{n}, {c.kv_heads}, {c.head_dim}] on {dev}")
+        outs.append(t)
+    rc = lib().e3_cache_read(C.byref(c), _ptr(slots), n, _ptr(outs[0]), _ptr(outs[1]), _float_type(dtype), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_cache_read")
+    return outs[0], outs[1]
+
+
+def e3_prefix_attention_workspace_bytes(rows: int, queries: int, q_heads: int, kv_heads: int, head_dim: int, num_groups: int) -> int:
+    """Host-only; 0 for a shape that is not served."""
+    return int(lib().e3_prefix_attention_workspace_bytes(rows, queries, q_heads, kv_heads, head_dim, num_groups))
+
+
+def _table(t: torch.Tensor, n: int, name: str, device) -> int:
+    if t.dtype is not torch.int32 or t.dim() != 2 or t.shape[0] != n or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{n}, pages] on {device}")
+    return t.shape[1]
+
+
+def e3_prefix_attention(q: torch.Tensor, cache: E3Cache, group_offsets: Optional[torch.Tensor],
+                        prefix_pages: Optional[torch.Tensor], prefix_lens: Optional[torch.Tensor],
+                        row_pages: torch.Tensor, row_lens: torch.Tensor, scale: float,
+                        out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, want_lse: bool = True):
+    """Attention of a decode step: q bf16 [rows, queries, q_heads, D]; row r of group g (group_offsets int32 [groups + 1], None:
+    no prefixes) sees the group's prefix (prefix_pages int32 [groups, width], prefix_lens int32 [groups]) and its own
+    tokens (row_pages, row_lens), query t all but its last queries - 1 - t.  Returns (out bf16 like q, lse fp32 [rows, queries,
+    q_heads] or None).  workspace: a tensor of e3_prefix_attention_workspace_bytes(), or None to allocate one."""
+    c = _cache(cache)
+    dev = cache[0].device
+    if q.dim() != 4 or q.dtype is not torch.bfloat16 or q.device != dev or q.shape[3] != c.head_dim or (q.numel() and q.stride(3) != 1):
+        raise ValueError(f"q must be a bf16 tensor [rows, queries, q_heads, {c.head_dim}] with unit column stride on {dev}")
+    rows, T, q_heads, D = q.shape
+    groups = 0 if group_offsets is None else group_offsets.shape[0] - 1
+    prefix_width = 0
+    if group_offsets is not None:
+        _check(group_offsets, torch.int32, groups + 1, "group_offsets", dev)
+        if prefix_pages is None or prefix_lens is None:
+            raise ValueError("groups need prefix_pages and prefix_lens")
+        prefix_width = _table(prefix_pages, groups, "prefix_pages", dev)
+        _check(prefix_lens, torch.int32, groups, "prefix_lens", dev)
+    row_width = _table(row_pages, rows, "row_pages", dev)
+    _check(row_lens, torch.int32, rows, "row_lens", dev)
+    if out is None:
+        out = torch.empty((rows, T, q_heads, D), dtype=torch.bfloat16, device=dev)
+    elif out.dtype is not torch.bfloat16 or out.shape != q.shape or out.device != dev or not out.is_contiguous():
+        raise ValueError(f"out must be a contiguous bf16 tensor {tuple(q.shape)} on {dev}")
+    if lse_out is None:
+        lse_out = torch.empty((rows, T, q_heads), dtype=torch.float32, device=dev) if want_lse else None
+    elif lse_out.dtype is not torch.float32 or lse_out.shape != q.shape[:3] or lse_out.device != dev or not lse_out.is_contiguous():
+        raise ValueError(f"lse_out must be a contiguous fp32 tensor {tuple(q.shape[:3])} on {dev}")
+    if workspace is None:
+        need = e3_prefix_attention_workspace_bytes(rows, T, q_heads, c.kv_heads, D, groups)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    rc = lib().e3_prefix_attention(C.byref(c), _ptr(q), rows, T, q_heads, q.stride(0), q.stride(1), q.stride(2),
+                                   _ptr(group_offsets) if groups else None, groups, _ptr(prefix_pages), prefix_width,
+                                   _ptr(prefix_lens), _ptr(row_pages), row_width, _ptr(row_lens), float(scale),
+                                   _ptr(out), _ptr(lse_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_prefix_attention")
+    return out, lse_out
