@@ -486,6 +486,55 @@ int e3_prefix_attention(const e3_cache* cache, const void* q, int64_t rows, int6
                         float scale, void* out, float* lse_out,
                         void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Verification of drafted tokens (speculative sampling) with what a rollout keeps of every token.
+ * A row brings `drafts` drafted tokens x_0 .. and the target's logits at drafts + 1 positions
+ * (position t: given x_0 .. x_{t-1}).
+ *   p_t = softmax(z_t / tau_r),   q_t = softmax(d_t / tau'_r), or the point mass on x_t when there are
+ *         no draft logits (drafts looked up rather than sampled)
+ *   draft t is accepted while u_t q_t(x_t) < p_t(x_t);   n = number of accepted drafts
+ *   the token after them ~ (p_n - q_n)+ / sum (p_n - q_n)+ if draft n was rejected,  ~ p_n if none was
+ *   (if p_n exceeds q_n nowhere, rounding aside they are equal: ~ p_n).
+ * u_t is the uniform of e3_sample_entropy's map at Philox stream 5, index t; the draw is its two-level
+ * race with r_i = (p_i - q_i)+ for exp(a_i), streams 6 (tiles) and 7 (columns):
+ *   T* = argmax_T (sum_{i in T} r_i) / E_T,   token = argmax_{i in T*} r_i / E_i.
+ * Random numbers are thus given by seed and row_base + r; a new step takes a new seed (or row_base).
+ *
+ * logits        [rows][drafts + 1][V] of dtype (E3_F32 / E3_BF16), strides in elements; base and
+ *               strides multiples of 16 bytes (E3_ERR_ALIGN), position_stride >= V.
+ * draft_logits  [rows][drafts][V] of the same dtype, or NULL.
+ * draft_tokens  [rows][drafts] int32 (NULL only when drafts == 0).  An id outside [0, V) is rejected.
+ * draft_lens    [rows] int32 or NULL: drafts of each row (cut to 0 .. drafts); positions behind a
+ *               row's last draft and the one after it are not read.
+ * drafts        0 .. E3_MAX_DRAFTS.
+ * tau_rows, tau_scalar  as for e3_sample_entropy;  draft_tau_rows [rows] or NULL: the drafts'
+ *               temperature, NULL: the target's.
+ * accepted_out  [rows] int32 = n.
+ * token_out     [rows][drafts + 1] int32: the n drafts and the token after them, then -1.
+ * logp_out, entropy_out  [rows][drafts + 1] fp32 or NULL: ln p_t of token t and the entropy of p_t for
+ *               the n + 1 tokens, then 0: what e3_sample_entropy reports of a sampled token.
+ * A logit of -inf, or of -1e30 and less, has no probability.  A position whose target logits hold
+ * NaN or +inf, or no finite value, is rejected with an unspecified token in [0, V) and NaN outputs;
+ * one whose draft logits do is rejected and drawn from p.
+ * V             at most 1,040,384.
+ * workspace     device, 256-byte aligned (E3_ERR_ALIGN), at least e3_verify_workspace_bytes()
+ *               (else E3_ERR_WORKSPACE); contents on entry ignored, no state between calls, to be
+ *               used by one call at a time.
+ * Sums in fp32 per lane, merged in fp64; decisions in fp64.  A row whose decision or race lies within
+ * fp32 rounding may fall the other way in a batch of another size; the same call gives the
+ * same bits.
+ */
+#define E3_MAX_DRAFTS 63
+size_t e3_verify_workspace_bytes(int64_t rows, int32_t drafts, int64_t V);
+int e3_verify_drafts(const void* logits, int dtype, int64_t rows, int32_t drafts, int64_t V,
+                     int64_t row_stride, int64_t position_stride,
+                     const int32_t* draft_tokens, const int32_t* draft_lens,
+                     const void* draft_logits, int64_t draft_row_stride, int64_t draft_position_stride,
+                     const float* tau_rows, float tau_scalar, const float* draft_tau_rows,
+                     uint64_t seed, uint64_t row_base,
+                     int32_t* accepted_out, int32_t* token_out, float* logp_out, float* entropy_out,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,6 +26,7 @@ E3_F32, E3_BF16, E3_E4M3 = 0, 1, 2
 E3_OK = 0
 E3_TILE_CHUNK, E3_TILE_LANES, E3_TILE_DEPTH = 8, 64, 8
 E3_NOALLOC_MAX_ROWS = 1024
+E3_MAX_DRAFTS = 63
 
 EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_entropy_noalloc",
            "e3_sample_restricted", "e3_sample_restricted_ws", "e3_restricted_workspace_bytes",
@@ -33,7 +34,8 @@ EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_
            "e3_grpo_advantages", "e3_temperature_update", "e3_difficulty_ranks",
            "e3_allocate_budgets", "e3_budget_bounds", "e3_logprob_entropy_gap",
            "e3_temperature_update_gap", "e3_grpo_objective", "e3_cache_append", "e3_cache_read",
-           "e3_prefix_attention", "e3_prefix_attention_workspace_bytes", "e3_read_probe",
+           "e3_prefix_attention", "e3_prefix_attention_workspace_bytes", "e3_verify_drafts",
+           "e3_verify_workspace_bytes", "e3_read_probe",
            "e3_time_next_launch", "e3_launch_plan", "e3_launch_plan_of")
 
 _NATIVE_CALLS = ("e3_grpo_advantages", "e3_grpo_objective", "e3_workspace_bytes", "e3_sample_entropy",
@@ -123,6 +125,11 @@ def lib() -> C.CDLL:
         L.e3_prefix_attention.argtypes = [vp, vp, i64, i64, i64, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, f32,
                                           vp, vp, vp, C.c_size_t, vp]
         L.e3_prefix_attention.restype = C.c_int
+        L.e3_verify_workspace_bytes.argtypes = [i64, i32, i64]
+        L.e3_verify_workspace_bytes.restype = C.c_size_t
+        L.e3_verify_drafts.argtypes = [vp, C.c_int, i64, i32, i64, i64, i64, vp, vp, vp, i64, i64, vp, f32, vp, u64, u64,
+                                       vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.e3_verify_drafts.restype = C.c_int
         _bind_native(L)                           # may raise: nothing is loaded then
         _lib = L
     return _lib
@@ -786,3 +793,66 @@ def e3_prefix_attention(q: torch.Tensor, cache: E3Cache, group_offsets: Optional
     if rc != E3_OK:
         raise E3Error(rc, "e3_prefix_attention")
     return out, lse_out
+
+
+def e3_verify_workspace_bytes(rows: int, drafts: int, V: int) -> int:
+    """Host-only; 0 for a shape that is not served."""
+    return int(lib().e3_verify_workspace_bytes(rows, drafts, V))
+
+
+def _positions(t: torch.Tensor, name: str, dtype, shape, device) -> Tuple[int, int]:
+    if t.dtype is not dtype or t.dim() != 3 or tuple(t.shape) != tuple(shape) or t.device != device or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} with unit column stride on {device}")
+    # a dimension of one has no stride of its own: torch may report anything
+    V = t.shape[2]
+    pitch = t.stride(1) if t.shape[1] > 1 else -(-V // 8) * 8
+    return (t.stride(0) if t.shape[0] > 1 else pitch * t.shape[1]), pitch
+
+
+def e3_verify_drafts(logits: torch.Tensor, draft_tokens: Optional[torch.Tensor], draft_logits: Optional[torch.Tensor],
+                     draft_lens: Optional[torch.Tensor], tau_rows: Optional[torch.Tensor], tau_scalar: float,
+                     seed: int, row_base: int = 0, draft_tau_rows: Optional[torch.Tensor] = None,
+                     accepted_out: Optional[torch.Tensor] = None, token_out: Optional[torch.Tensor] = None,
+                     logp_out: Optional[torch.Tensor] = None, entropy_out: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None):
+    """Verify drafted tokens: logits [rows, drafts + 1, V], draft_tokens int32 [rows, drafts], draft_logits [rows, drafts, V] or None
+    (drafts without a distribution).  Returns (accepted int32 [rows], token int32 [rows, drafts + 1], logp fp32, entropy fp32 of the
+    same shape).  workspace: a tensor of e3_verify_workspace_bytes(), or None to allocate one."""
+    if logits.dim() != 3 or not logits.is_cuda:
+        raise ValueError("logits must be [rows, drafts + 1, V] on the GPU")
+    dt = _float_type(logits.dtype)
+    rows, positions, V = logits.shape
+    drafts, dev = positions - 1, logits.device
+    row_stride, position_stride = _positions(logits, "logits", logits.dtype, (rows, positions, V), dev)
+    draft_strides = (0, 0)
+    if draft_logits is not None:
+        draft_strides = _positions(draft_logits, "draft_logits", logits.dtype, (rows, drafts, V), dev)
+    if draft_tokens is not None or drafts > 0:
+        if (draft_tokens is None or draft_tokens.dtype is not torch.int32 or tuple(draft_tokens.shape) != (rows, drafts)
+                or not draft_tokens.is_contiguous() or draft_tokens.device != dev):
+            raise ValueError(f"draft_tokens must be a contiguous int32 tensor [{rows}, {drafts}] on {dev}")
+    _check(draft_lens, torch.int32, rows, "draft_lens", dev)
+    _check(tau_rows, torch.float32, rows, "tau_rows", dev)
+    _check(draft_tau_rows, torch.float32, rows, "draft_tau_rows", dev)
+    if accepted_out is None:
+        accepted_out = torch.empty(rows, dtype=torch.int32, device=dev)
+    else:
+        _check(accepted_out, torch.int32, rows, "accepted_out", dev)
+    outs = []
+    for t, dtype, name in ((token_out, torch.int32, "token_out"), (logp_out, torch.float32, "logp_out"), (entropy_out, torch.float32, "entropy_out")):
+        if t is None:
+            t = torch.empty((rows, positions), dtype=dtype, device=dev)
+        elif t.dtype is not dtype or tuple(t.shape) != (rows, positions) or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor [{rows}, {positions}] on {dev}")
+        outs.append(t)
+    if workspace is None:
+        workspace = torch.empty(e3_verify_workspace_bytes(rows, drafts, V), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    rc = lib().e3_verify_drafts(_ptr(logits), dt, rows, drafts, V, row_stride, position_stride, _ptr(draft_tokens), _ptr(draft_lens),
+                                _ptr(draft_logits), *draft_strides, _ptr(tau_rows), float(tau_scalar), _ptr(draft_tau_rows),
+                                int(seed), int(row_base), _ptr(accepted_out), *(_ptr(t) for t in outs), _ptr(workspace),
+                                workspace.numel() * workspace.element_size(), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_verify_drafts")
+    return (accepted_out, *outs)

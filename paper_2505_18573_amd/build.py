@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libe3.so")
 NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["e3_api.hip", "vocab_pass.hip", "restricted.hip", "restricted_select.hip", "probe.hip", "advantages.hip", "objective.hip",
-           "decode_api.hip", "kv_cache.hip", "prefix_attention.hip",
+           "decode_api.hip", "kv_cache.hip", "prefix_attention.hip", "verify.hip",
            "scheduler.cpp", "budget.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -5,6 +5,8 @@
 
 #include "../../include/e3.h"
 #include "kv_cache.h"
+#include "verify.h"
+#include "vocab_pass.h"
 
 namespace {
 
@@ -114,5 +116,50 @@ extern "C" int e3_prefix_attention(const e3_cache* cache, const void* q, int64_t
     a.prefix_width = (int32_t)prefix_width; a.row_width = (int32_t)row_width;
     a.scale = scale; a.out = static_cast<uint16_t*>(out); a.lse = lse_out;
     const hipError_t err = e3::launch_prefix_attention(view, a, workspace, static_cast<hipStream_t>(hip_stream));
+    return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
+}
+
+static bool verify_dims(int64_t rows, int32_t drafts, int64_t V)
+{
+    return rows >= 0 && drafts >= 0 && drafts <= E3_MAX_DRAFTS && V >= 1 && V <= 0x7FFFFFFF - 8192 && e3::vocab_pass_fits(V) &&
+           rows * (drafts + 1) <= 0x7FFFFFFF;
+}
+
+extern "C" size_t e3_verify_workspace_bytes(int64_t rows, int32_t drafts, int64_t V)
+{
+    return rows > 0 && rows <= 0x7FFFFFFF && verify_dims(rows, drafts, V) ? e3::verify_workspace_bytes(rows, drafts, V) : 0;
+}
+
+extern "C" int e3_verify_drafts(const void* logits, int dtype, int64_t rows, int32_t drafts, int64_t V,
+                                int64_t row_stride, int64_t position_stride,
+                                const int32_t* draft_tokens, const int32_t* draft_lens,
+                                const void* draft_logits, int64_t draft_row_stride, int64_t draft_position_stride,
+                                const float* tau_rows, float tau_scalar, const float* draft_tau_rows,
+                                uint64_t seed, uint64_t row_base,
+                                int32_t* accepted_out, int32_t* token_out, float* logp_out, float* entropy_out,
+                                void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    static_assert(E3_MAX_DRAFTS == e3::kMaxDrafts, "one lane per position");
+    if (dtype != E3_F32 && dtype != E3_BF16) return E3_ERR_DTYPE;
+    if (rows > 0x7FFFFFFF || !verify_dims(rows, drafts, V) || position_stride < V) return E3_ERR_SHAPE;
+    if (draft_logits != nullptr && drafts > 0 && draft_position_stride < V) return E3_ERR_SHAPE;
+    if (tau_rows == nullptr && !(std::isfinite(tau_scalar) && tau_scalar > 0.0f)) return E3_ERR_VALUE;
+    if (rows == 0) return E3_OK;
+    if (logits == nullptr || accepted_out == nullptr || token_out == nullptr || (draft_tokens == nullptr && drafts > 0)) return E3_ERR_NULL;
+    const size_t need = e3::verify_workspace_bytes(rows, drafts, V);
+    if (workspace == nullptr || workspace_bytes < need) return E3_ERR_WORKSPACE;
+    const int64_t per = dtype == E3_F32 ? 4 : 8;                    // elements in 16 bytes
+    if (!aligned(logits, 16) || !aligned(draft_logits, 16) || !aligned(workspace, 256) || row_stride % per || position_stride % per ||
+        draft_row_stride % per || draft_position_stride % per)
+        return E3_ERR_ALIGN;
+    e3::VerifyArgs a{};
+    a.logits = logits; a.draft_logits = drafts > 0 ? draft_logits : nullptr;
+    a.rows = rows; a.V = V; a.row_stride = row_stride; a.position_stride = position_stride;
+    a.draft_row_stride = draft_row_stride; a.draft_position_stride = draft_position_stride;
+    a.drafts = drafts; a.draft_tokens = draft_tokens; a.draft_lens = draft_lens;
+    a.tau_rows = tau_rows; a.tau_scalar = tau_scalar; a.draft_tau_rows = draft_tau_rows;
+    a.seed = seed; a.row_base = row_base;
+    a.accepted_out = accepted_out; a.token_out = token_out; a.logp_out = logp_out; a.entropy_out = entropy_out;
+    const hipError_t err = e3::launch_verify(a, dtype == E3_BF16, workspace, static_cast<hipStream_t>(hip_stream));
     return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
 }
