@@ -7,12 +7,13 @@
 // (O scaled by 2^{m - m'}), so the keys may be cut anywhere: into prefix and own tokens, and either into runs.  A
 // prefix is read once for all rows of its group, whose queries form the columns of one product.
 //
-// Three launches:
-//   plan     one workgroup looks at the lengths (device memory: they change with every step) and lists the tasks: a run
-//            of tokens of one prefix or one row, a key head, a tile of queries.  Runs are of one length, chosen so that
-//            the tasks fill the card some times over.
-//   attend   workgroups of four waves take tasks; each wave takes every fourth step of 32 tokens of the run and keeps
-//            its own (m, l, O) in registers; the four join through LDS and leave one partial result in the workspace.
+// Two launches:
+//   attend   workgroups of four waves.  Each looks at all lengths first (device memory: they change with every step) and
+//            cuts every prefix and row ("unit") into runs of one length, chosen so that the tasks fill the card some times
+//            over; a task is a run, a key head and a tile of queries.  The waves of a task share its queries by tiles of
+//            16 (one, two or four of them) and, as far as there are fewer tiles than waves, its steps of 32 tokens; each
+//            keeps its own (m, l, O) in registers.  Waves with the same queries join through LDS, and every task leaves one
+//            partial result in the workspace.
 //   join     a wave per row, query and head joins the partial results of its prefix and its own tokens.
 //
 // Registers instead of LDS: S^T = K Q^T puts the queries on the matrix instruction's columns, so a lane holds one
@@ -43,21 +44,26 @@ constexpr float kNoScore = -3.0e38f;            // running maximum before any sc
 constexpr float kSlack = 8.0f;                  // scores may pass the running maximum by this (2^8) before it moves
 constexpr int kTargetTasks = 2048;              // tasks that one long run is cut into, all prefixes and rows together
 
-struct Task { int32_t unit, item, from, to; };  // item: key head + heads * query tile; tokens [from, to)
-
 // What the host fixes of a call; the workspace's parts lie behind one another.
 struct AttendShape {
     int32_t R, M;                               // query heads per key head; queries of a row and key head (T * R)
-    int32_t row_tile, prefix_tile;              // queries of a task (16 or 32 or 64)
-    int32_t row_tiles;                          // tiles of a row
-    int32_t row_slot;                           // queries a row's task leaves results of
+    int32_t units;                              // groups, then rows
+    int32_t row_slot, prefix_slot;              // queries that a task of either kind leaves results of, at most
     int64_t max_row_tasks, max_prefix_tasks;
-    int64_t at_tasks, at_row, at_prefix, at_group, at_ml, at_o, bytes;     // byte offsets (at_o: fp32 [rows of D])
+    int64_t at_first, at_ml, at_o, bytes;       // byte offsets (at_o: fp32 [results][D])
 };
 
-struct PlanHead { int32_t run, prefix_tasks, row_tasks, pad; };
+struct PlanHead { int32_t run, prefix_tasks; };
 
 static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Query tiles of 16 that a task's waves share: as many as a unit's queries fill, up to one per wave.
+__host__ __device__ __forceinline__ int query_waves(int64_t queries) { return queries <= 16 ? 1 : queries <= 32 ? 2 : 4; }
+__host__ __device__ __forceinline__ int64_t query_tiles(int64_t queries)
+{
+    const int per = 16 * query_waves(queries);
+    return (queries + per - 1) / per;
+}
 
 static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int64_t groups, AttendShape& s)
 {
@@ -65,23 +71,16 @@ static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads
     const int64_t M = T * s.R;
     if (M > (1 << 16)) return false;
     s.M = (int32_t)M;
-    // A row's queries in as few tiles as possible, since each reads the row's keys once more; a prefix has the queries
-    // of many rows, at least two tiles' worth for one read.
-    const int tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    s.row_tile = 16 * tiles;
-    s.prefix_tile = 16 * (tiles < 2 ? 2 : tiles);
-    s.row_tiles = (int32_t)((M + s.row_tile - 1) / s.row_tile);
-    s.row_slot = (int32_t)(M < s.row_tile ? M : s.row_tile);
-    s.max_row_tasks = heads * rows * s.row_tiles + kTargetTasks;
-    s.max_prefix_tasks = groups > 0 ? heads * (rows * M / s.prefix_tile + groups) + kTargetTasks : 0;
+    s.units = (int32_t)(groups + rows);
+    s.row_slot = (int32_t)(M < 64 ? M : 64);
+    s.prefix_slot = (int32_t)(rows * M < 64 ? rows * M : 64);
+    s.max_row_tasks = heads * rows * query_tiles(M) + kTargetTasks;
+    s.max_prefix_tasks = groups > 0 ? heads * (rows * M / 64 + groups) + kTargetTasks : 0;
     const int64_t tasks = s.max_row_tasks + s.max_prefix_tasks;
-    const int64_t slots = s.max_row_tasks * s.row_slot + s.max_prefix_tasks * s.prefix_tile;
+    const int64_t slots = s.max_row_tasks * s.row_slot + s.max_prefix_tasks * s.prefix_slot;
     if (tasks > (int64_t)1 << 30 || slots > ((int64_t)1 << 31) - 1) return false;
-    s.at_tasks = 256;
-    s.at_row = up(s.at_tasks + tasks * (int64_t)sizeof(Task), 256);
-    s.at_prefix = up(s.at_row + rows * 8, 256);
-    s.at_group = up(s.at_prefix + groups * 8, 256);
-    s.at_ml = up(s.at_group + rows * 4, 256);
+    s.at_first = 256;
+    s.at_ml = up(s.at_first + (int64_t)s.units * 4, 256);
     s.at_o = up(s.at_ml + slots * 8, 256);
     s.bytes = up(s.at_o + slots * D * 4, 256);
     return true;
@@ -94,10 +93,40 @@ size_t prefix_attention_workspace_bytes(int64_t rows, int64_t T, int64_t q_heads
 }
 
 // ---------------------------------------------------------------- plan
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 64 * kAttendWaves;
 
-// exclusive prefix sums over the workgroup; the total to everyone
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* lds, int64_t* total)
+__device__ __forceinline__ int clamp_len(int n, int64_t most) { return n < 0 ? 0 : n > most ? (int)most : n; }
+// tokens that a table of `width` pages can name
+__device__ __forceinline__ int64_t table_tokens(int width, int page_size)
+{
+    const int64_t n = (int64_t)width * page_size;
+    return n > 0x7FFFFF00 ? 0x7FFFFF00 : n;
+}
+
+// A group's prefix or a row's own tokens.
+struct Unit {
+    int len, row0;                              // tokens; the first row that sees them
+    int64_t queries;                            // per key head
+};
+__device__ __forceinline__ Unit unit_at(const AttentionArgs& a, const AttendShape& s, int page_size, int u)
+{
+    Unit x;
+    if (u < a.groups) {
+        x.row0 = clamp_len(a.group_offsets[u], a.rows);
+        const int n = clamp_len(a.group_offsets[u + 1], a.rows) - x.row0;
+        x.len = n > 0 ? clamp_len(a.prefix_lens[u], table_tokens(a.prefix_width, page_size)) : 0;
+        x.queries = (int64_t)(n > 0 ? n : 0) * s.M;
+    } else {
+        x.row0 = u - a.groups;
+        x.len = clamp_len(a.row_lens[x.row0], table_tokens(a.row_width, page_size));
+        x.queries = s.M;
+    }
+    return x;
+}
+__device__ __forceinline__ int runs_of(int len, int run) { return (int)(((int64_t)len + run - 1) / run); }
+
+// sums over the waves of a workgroup that come before the thread's own lane, and over all
+__device__ __forceinline__ int64_t workgroup_scan(int64_t v, int64_t* lds, int64_t* total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t x = v;
@@ -110,7 +139,8 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* lds, int64_t* 
     if (lane == 63) lds[wave] = x;
     __syncthreads();
     int64_t before = 0, all = 0;
-    for (int i = 0; i < kPlanThreads / 64; ++i) {
+#pragma unroll
+    for (int i = 0; i < kAttendWaves; ++i) {
         if (i < wave) before += lds[i];
         all += lds[i];
     }
@@ -118,81 +148,91 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* lds, int64_t* 
     return before + x - v;
 }
 
-__device__ __forceinline__ int clamp_len(int n, int64_t most) { return n < 0 ? 0 : n > most ? (int)most : n; }
-// tokens that a table of `width` pages can name
-__device__ __forceinline__ int64_t table_tokens(int width, int page_size)
+// Every thread sums up a share of successive units; `first` [kPlanThreads] gets each share's first task.
+struct Plan {
+    int share, run, tasks, prefix_tasks;
+};
+__device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, int64_t* lds, int* first)
 {
-    const int64_t n = (int64_t)width * page_size;
-    return n > 0x7FFFFF00 ? 0x7FFFFF00 : n;
+    Plan p;
+    p.share = (s.units + kPlanThreads - 1) / kPlanThreads;
+    const int u0 = (int)threadIdx.x * p.share;
+    const int u1 = u0 + p.share < s.units ? u0 + p.share : s.units;
+    int64_t tokens = 0, total;
+    for (int u = u0; u < u1; ++u) {
+        const Unit x = unit_at(a, s, page_size, u);
+        tokens += x.len * query_tiles(x.queries);
+    }
+    workgroup_scan(tokens, lds, &total);
+    const int64_t run = (total * heads / kTargetTasks + kRun) / kRun * kRun;
+    p.run = (int)(run < 0x40000000 ? run : 0x40000000);
+    int64_t tasks = 0, prefix = 0;
+    for (int u = u0; u < u1; ++u) {
+        const Unit x = unit_at(a, s, page_size, u);
+        const int64_t n = runs_of(x.len, p.run) * query_tiles(x.queries) * heads;
+        tasks += n;
+        if (u < a.groups) prefix += n;
+    }
+    // both counts in one word (each below 2^31, see attend_shape)
+    const int64_t before = workgroup_scan(prefix << 32 | tasks, lds, &total);
+    first[threadIdx.x] = (int)(before & 0x7FFFFFFF);
+    p.tasks = (int)(total & 0x7FFFFFFF);
+    p.prefix_tasks = (int)(total >> 32);
+    __syncthreads();
+    return p;
 }
 
-__global__ __launch_bounds__(kPlanThreads)
-void attend_plan_kernel(AttentionArgs a, AttendShape s, int heads, int page_size, char* ws)
+struct Task {
+    int unit, head, tile, from, to;             // tokens [from, to)
+    bool leads;                                 // the unit's first task
+    Unit of;
+};
+__device__ __forceinline__ Task task_at(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, const Plan& p,
+                                        const int* first, int i)
 {
-    __shared__ int64_t lds[kPlanThreads / 64];
-    const int64_t row_most = table_tokens(a.row_width, page_size), prefix_most = table_tokens(a.prefix_width, page_size);
-    auto row_len = [&](int r) { return clamp_len(a.row_lens[r], row_most); };
-    auto prefix_len = [&](int g) { return clamp_len(a.prefix_lens[g], prefix_most); };
-    auto first_row = [&](int g) { return clamp_len(a.group_offsets[g], a.rows); };
-    auto prefix_tiles = [&](int g) {
-        const int n = first_row(g + 1) - first_row(g);
-        return n > 0 ? (int)(((int64_t)n * s.M + s.prefix_tile - 1) / s.prefix_tile) : 0;
-    };
-    Task* tasks = reinterpret_cast<Task*>(ws + s.at_tasks);
-    int2* row_plan = reinterpret_cast<int2*>(ws + s.at_row);          // first task, runs
-    int2* prefix_plan = reinterpret_cast<int2*>(ws + s.at_prefix);
-    int32_t* group_of = reinterpret_cast<int32_t*>(ws + s.at_group);
-
-    int64_t mine = 0, total, carry;
-    for (int r = threadIdx.x; r < a.rows; r += kPlanThreads) {
-        mine += (int64_t)row_len(r) * s.row_tiles;
-        group_of[r] = -1;
-    }
-    for (int g = threadIdx.x; g < a.groups; g += kPlanThreads) mine += (int64_t)prefix_len(g) * prefix_tiles(g);
-    block_scan(mine * heads, lds, &total);
-    int64_t run = (total / kTargetTasks + kRun) / kRun * kRun;
-    if (run > 0x40000000) run = 0x40000000;
-
-    // group_of[] = -1 above is written by the thread that may be overtaken here: same workgroup, barrier in block_scan
-    carry = 0;
-    for (int g0 = 0; g0 < a.groups; g0 += kPlanThreads) {
-        const int g = g0 + (int)threadIdx.x;
-        const int len = g < a.groups ? prefix_len(g) : 0, tiles = g < a.groups ? prefix_tiles(g) : 0;
-        const int runs = (int)((len + run - 1) / run);
-        int64_t at = block_scan((int64_t)runs * tiles * heads, lds, &total) + carry;
-        carry += total;
-        if (g < a.groups) {
-            // (groups that overlap could exceed the list: those beyond it have no prefix)
-            const bool fits = at + (int64_t)runs * tiles * heads <= s.max_prefix_tasks;
-            prefix_plan[g] = fits ? int2{(int)at, runs} : int2{0, 0};
-            for (int item = 0; fits && item < tiles * heads; ++item)
-                for (int c = 0; c < runs; ++c, ++at)
-                    tasks[at] = Task{-1 - g, item, (int)(c * run), (int)((c + 1) * run < len ? (c + 1) * run : len)};
-            for (int r = first_row(g); r < first_row(g + 1); ++r) group_of[r] = g;
+    const int lane = threadIdx.x & 63;
+    // the last share that begins at or before task i
+    int below = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanThreads / 64; ++k) below += (int)__popcll(__ballot(first[k * 64 + lane] <= i));
+    const int share = below - 1;
+    int at = __builtin_amdgcn_readfirstlane(first[share]);
+    Task t{};
+    t.unit = -1;
+    for (int u0 = share * p.share; u0 < s.units && u0 < (share + 1) * p.share; u0 += 64) {
+        const int u = u0 + lane;
+        Unit x{};
+        int n = 0;
+        if (u < s.units && u < (share + 1) * p.share) {
+            x = unit_at(a, s, page_size, u);
+            n = (int)(runs_of(x.len, p.run) * query_tiles(x.queries) * heads);
         }
-    }
-    const int64_t prefix_tasks = carry = carry < s.max_prefix_tasks ? carry : s.max_prefix_tasks;
-    for (int r0 = 0; r0 < a.rows; r0 += kPlanThreads) {
-        const int r = r0 + (int)threadIdx.x;
-        const int len = r < a.rows ? row_len(r) : 0;
-        const int runs = (int)((len + run - 1) / run);
-        int64_t at = block_scan((int64_t)runs * s.row_tiles * heads, lds, &total) + carry;
-        carry += total;
-        if (r < a.rows) {
-            row_plan[r] = int2{(int)(at - prefix_tasks), runs};
-            for (int item = 0; item < s.row_tiles * heads; ++item)
-                for (int c = 0; c < runs; ++c, ++at)
-                    tasks[at] = Task{r, item, (int)(c * run), (int)((c + 1) * run < len ? (c + 1) * run : len)};
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(sum, d);
+            if (lane >= d) sum += y;
         }
+        const unsigned long long behind = __ballot(at + sum > i);
+        if (behind != 0ull) {
+            const int l = (int)__builtin_ctzll(behind);
+            t.unit = u0 + l;
+            const int rank = i - (at + __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(n, l));
+            t.of.len = __builtin_amdgcn_readlane(x.len, l);
+            t.of.row0 = __builtin_amdgcn_readlane(x.row0, l);
+            t.of.queries = __builtin_amdgcn_readlane((int)x.queries, l);
+            const int runs = runs_of(t.of.len, p.run);
+            const int item = rank / runs, c = rank % runs;
+            t.head = item % heads;
+            t.tile = item / heads;
+            t.from = c * p.run;
+            t.to = t.from + p.run < t.of.len ? t.from + p.run : t.of.len;
+            t.leads = rank == 0;
+            break;
+        }
+        at += __builtin_amdgcn_readlane(sum, 63);
     }
-    if (threadIdx.x == 0) {
-        PlanHead h;
-        h.run = (int)run;
-        h.prefix_tasks = (int)prefix_tasks;
-        h.row_tasks = (int)(carry - prefix_tasks);
-        h.pad = 0;
-        *reinterpret_cast<PlanHead*>(ws) = h;
-    }
+    return t;
 }
 
 // ---------------------------------------------------------------- attend
@@ -302,14 +342,14 @@ struct StepData {
     __device__ __forceinline__ float v_factor(int j) const { return __uint_as_float(((vs[j >> 2] >> (8 * (j & 3))) & 0xFFu) << 23); }
 };
 
-template <int D, bool kFp8, int kTiles>
+template <int D, bool kFp8>
 struct Attend {
     using Data = StepData<D, kFp8>;
     static constexpr int kBlocks = D / 16, kSteps = D / 32;
-    bf16x8 q[kTiles][kSteps];
-    f32x4 o[kTiles][kBlocks];
-    float m[kTiles], l[kTiles];
-    int limit[kTiles];                          // tokens the lane's query sees (of the prefix, of the row)
+    bf16x8 q[kSteps];
+    f32x4 o[kBlocks];
+    float m, l;
+    int limit;                                  // tokens the lane's query sees (of the prefix, of the row)
 
     // One step.  `at`: its first token; every query sees at least `sure` tokens, none more than `most`.
     __device__ __forceinline__ void step(Data& d, int at, int sure, int most, float c, int lane)
@@ -317,131 +357,111 @@ struct Attend {
         const int g = lane >> 4;
         const bool tail = at + kStep > sure;                              // uniform
         if (tail) d.clear_from(most - at - 8 * g);
-        f32x4 s[kTiles][2];
+        f32x4 s[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) s[n][0] = s[n][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) s[t] = mfma(d.key(t, i), q[i], s[t]);
+        float x[8];
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const bf16x8 key = d.key(t, i);
+        for (int j = 0; j < 8; ++j) {
+            x[j] = s[j >> 2][j & 3] * (kFp8 ? c * d.k_factor(j) : c);
+            if (tail) x[j] = at + 8 * g + j < limit ? x[j] : -INFINITY;
+        }
+        float top = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+        if (__any(top > m + kSlack)) {
+            // the queries' maxima over the four lanes that hold their scores
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float to = fmaxf(m, top);
+            const float f = __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= f;
 #pragma unroll
-                for (int n = 0; n < kTiles; ++n) s[n][t] = mfma(key, q[n][i], s[n][t]);
-            }
-        bf16x8 p[kTiles], rest[kTiles];
+            for (int b = 0; b < kBlocks; ++b) o[b] *= f;
+        }
+        bf16x8 p, rest;
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = s[n][j >> 2][j & 3] * (kFp8 ? c * d.k_factor(j) : c);
-                if (tail) x[j] = at + 8 * g + j < limit[n] ? x[j] : -INFINITY;
-            }
-            float top = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
-            if (__any(top > m[n] + kSlack)) {
-                // the queries' maxima over the four lanes that hold their scores
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float to = fmaxf(m[n], top);
-                const float f = __builtin_amdgcn_exp2f(m[n] - to);
-                m[n] = to;
-                l[n] *= f;
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) o[n][b] *= f;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float e = __builtin_amdgcn_exp2f(x[j] - m[n]);
-                l[n] += e;
-                const float w = kFp8 ? e * d.v_factor(j) : e;
-                p[n][j] = (__bf16)w;
-                rest[n][j] = (__bf16)(w - (float)p[n][j]);
-            }
+        for (int j = 0; j < 8; ++j) {
+            const float e = __builtin_amdgcn_exp2f(x[j] - m);
+            l += e;
+            const float w = kFp8 ? e * d.v_factor(j) : e;
+            p[j] = (__bf16)w;
+            rest[j] = (__bf16)(w - (float)p[j]);
         }
         // Tokens that some queries see and others do not: a weight of zero keeps them out, unless the value is no
-        // number.  Then the queries take turns, each with the others' tokens cleared.
+        // number.  Then the queries take turns, those that see most first, and what the next do not see is cleared.
         if (__builtin_expect(tail && sure < most && __any(d.unbounded()), 0)) {
-            for (int have = sure; have <= most; ++have) {
-                Data only = d;
-                only.clear_from(have - at - 8 * g);
+            const int end = at + kStep;
+            const int mine = limit < at ? at : limit < end ? limit : end;
+            for (int have = most < end ? most : end; have >= (sure > at ? sure : at); --have) {
+                d.clear_from(have - at - 8 * g);
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                    for (int n = 0; n < kTiles; ++n) {
-                        const f32x4 r = mfma(only.value(b), rest[n], mfma(only.value(b), p[n], o[n][b]));
-                        if (limit[n] == have) o[n][b] = r;
-                    }
+                for (int b = 0; b < kBlocks; ++b) {
+                    const f32x4 r = mfma(d.value(b), rest, mfma(d.value(b), p, o[b]));
+                    if (mine == have) o[b] = r;
+                }
             }
             return;
         }
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             const bf16x8 value = d.value(b);
-#pragma unroll
-            for (int n = 0; n < kTiles; ++n) o[n][b] = mfma(value, rest[n], mfma(value, p[n], o[n][b]));
+            o[b] = mfma(value, rest, mfma(value, p, o[b]));
         }
     }
 
-    // kPrefix: task.unit is -1 - group; otherwise a row.  `head`, `tile` of the task.
-    template <bool kPrefix>
+    // A task.  lds: (m, l) of all waves, then O of two waves.
     __device__ __forceinline__ void run(const CacheView& c, const AttentionArgs& a, const AttendShape& sh, const Task& task,
-                                        float* lds, float2* ml_out, float* o_out, int slot_rows)
+                                        float* lds, float2* ml_out, float* o_out)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int col = lane & 15, g = lane >> 4;
-        const int unit = kPrefix ? -1 - task.unit : task.unit;
-        const int head = task.item % c.heads, tile = task.item / c.heads;
-        int row0 = unit, queries = sh.M, len, sure;
-        const int32_t* pages;
-        if (kPrefix) {
-            row0 = clamp_len(a.group_offsets[unit], a.rows);
-            queries *= clamp_len(a.group_offsets[unit + 1], a.rows) - row0;
-            pages = a.prefix_pages + (int64_t)unit * a.prefix_width;
-            len = sure = clamp_len(a.prefix_lens[unit], table_tokens(a.prefix_width, c.page_size));
-        } else {
-            pages = a.row_pages + (int64_t)unit * a.row_width;
-            len = clamp_len(a.row_lens[unit], table_tokens(a.row_width, c.page_size));
-            sure = len - (a.T - 1) > 0 ? len - (a.T - 1) : 0;
-        }
-        // queries: column n of tile i is query first + 16 i + n
-        const int first = tile * (16 * kTiles);
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            const int qi = first + 16 * i + col;
+        const bool prefix = task.unit < a.groups;
+        const int queries = (int)task.of.queries, len = task.of.len;
+        const int qw = query_waves(queries), qs = qw == 1 ? 0 : qw == 2 ? 1 : 2;
+        const int tile = wave & (qw - 1), share = wave >> qs, shares = kAttendWaves >> qs;
+        const int sure = prefix ? len : len - (a.T - 1) > 0 ? len - (a.T - 1) : 0;
+        const int32_t* pages = prefix ? a.prefix_pages + (int64_t)task.unit * a.prefix_width
+                                      : a.row_pages + (int64_t)task.of.row0 * a.row_width;
+        // queries: column n is query first + n
+        const int first = (task.tile * qw + tile) * 16;
+        {
+            const int qi = first + col;
             const bool is = qi < queries;
-            const int row = row0 + (is ? qi / sh.M : 0), in_row = is ? qi % sh.M : 0;
-            const int t = in_row / sh.R, h = head * sh.R + in_row % sh.R;
+            const int row = task.of.row0 + (is ? qi / sh.M : 0), in_row = is ? qi % sh.M : 0;
+            const int t = in_row / sh.R, h = task.head * sh.R + in_row % sh.R;
             const uint16_t* qp = a.q + row * a.q_row_stride + t * a.q_token_stride + h * a.q_head_stride;
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 u32x4 w = *reinterpret_cast<const u32x4*>(qp + Data::key_column(s, g));
                 if (!is) w = u32x4{0, 0, 0, 0};
-                q[i][s] = __builtin_bit_cast(bf16x8, w);
+                q[s] = __builtin_bit_cast(bf16x8, w);
             }
             const int own = len - (a.T - 1 - t);
-            limit[i] = kPrefix ? len : own > 0 ? own : 0;
-            m[i] = kNoScore;
-            l[i] = 0.0f;
+            limit = prefix ? len : own > 0 ? own : 0;
+            m = kNoScore;
+            l = 0.0f;
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[i][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
         const float scale = a.scale * kLog2eF;
 
-        // tokens [from, to) of the run; the wave's steps are 4 apart.  A page that the cache does not have is not seen.
-        const int to = task.to;
+        // tokens [from, to) of the run.  A page that the cache does not have is not seen.
+        const int to = task.to, apart = shares * kStep;
         auto page_at = [&](int at) { return at < to ? pages[at >> c.page_shift] : -1; };
         auto row_of = [&](int page, int at) {
             const int64_t p = (uint32_t)page < (uint64_t)c.num_pages ? page : 0;
-            return (p * c.heads + head) * c.page_size + (at & (c.page_size - 1));
+            return (p * c.heads + task.head) * c.page_size + (at & (c.page_size - 1));
         };
-        int at = task.from + wave * kStep;
-        if (at < to) {
+        int at = task.from + share * kStep;
+        if (at < to && first < queries) {
             Data cur, next;
-            int page = page_at(at), page_next = page_at(at + kRun);
+            int page = page_at(at), page_next = page_at(at + apart);
             cur.load(c, row_of(page, at), lane);
-            for (; at < to; at += kRun) {
-                const int page_after = page_at(at + 2 * kRun);
-                if (at + kRun < to) next.load(c, row_of(page_next, at + kRun), lane);
+            for (; at < to; at += apart) {
+                const int page_after = page_at(at + 2 * apart);
+                if (at + apart < to) next.load(c, row_of(page_next, at + apart), lane);
                 if ((uint32_t)page < (uint64_t)c.num_pages) step(cur, at, sure, len, scale, lane);
                 cur = next;
                 page = page_next;
@@ -449,95 +469,77 @@ struct Attend {
             }
         }
 
-        // Join the four waves.  l is spread over the four lanes of a query.
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            l[i] += __shfl_xor(l[i], 16);
-            l[i] += __shfl_xor(l[i], 32);
-        }
-        constexpr int kMl = kAttendWaves * 16 * kTiles;                    // lds: (m, l) of all waves, then O of two waves
+        // Join the waves that have the same queries.  l is spread over the four lanes of a query.
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
         float2* ml = reinterpret_cast<float2*>(lds);
-        f32x4* part = reinterpret_cast<f32x4*>(lds + 2 * kMl);             // [2][kTiles * kBlocks][64]
-        __syncthreads();                                                   // the last task's results are read
-        if (g == 0) {
+        f32x4* part = reinterpret_cast<f32x4*>(lds + 2 * kAttendWaves * 16);               // [2][kBlocks][64]
+        float all_m = m, all_l = l;
+        auto give = [&](int slot) {
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) ml[wave * 16 * kTiles + 16 * i + col] = float2{m[i], l[i]};
-        }
-        __syncthreads();
-        float all_m[kTiles], all_l[kTiles];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            float2 w[kAttendWaves];
-            all_m[i] = kNoScore;
-#pragma unroll
-            for (int k = 0; k < kAttendWaves; ++k) {
-                w[k] = ml[k * 16 * kTiles + 16 * i + col];
-                all_m[i] = fmaxf(all_m[i], w[k].x);
-            }
-            all_l[i] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kAttendWaves; ++k) all_l[i] = fmaf(w[k].y, __builtin_amdgcn_exp2f(w[k].x - all_m[i]), all_l[i]);
-            const float f = __builtin_amdgcn_exp2f(m[i] - all_m[i]);
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[i][b] *= f;
-        }
-        auto give = [&](int to_slot) {
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) part[(to_slot * kTiles * kBlocks + i * kBlocks + b) * 64 + lane] = o[i][b];
+            for (int b = 0; b < kBlocks; ++b) part[(slot * kBlocks + b) * 64 + lane] = o[b];
         };
-        auto take = [&](int from_slot) {
+        auto take = [&](int slot) {
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) o[i][b] += part[(from_slot * kTiles * kBlocks + i * kBlocks + b) * 64 + lane];
+            for (int b = 0; b < kBlocks; ++b) o[b] += part[(slot * kBlocks + b) * 64 + lane];
         };
-        if (wave >= 2) give(wave - 2);
-        __syncthreads();
-        if (wave < 2) take(wave);
-        __syncthreads();
-        if (wave == 1) give(0);
-        __syncthreads();
-        if (wave == 0) {
-            take(0);
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-                const int slot = 16 * i + col;
-                if (first + slot >= queries || slot >= slot_rows) continue;
-                if (g == 0) ml_out[slot] = float2{all_m[i], all_l[i]};
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) o_out[(int64_t)slot * D + Data::column(b, 4 * g + k)] = o[i][b][k];
+        if (shares > 1) {                                                  // uniform over the workgroup
+            __syncthreads();                                               // the last task's results are read
+            if (g == 0) ml[wave * 16 + col] = float2{m, l};
+            __syncthreads();
+            all_m = kNoScore;
+            for (int k = 0; k < shares; ++k) all_m = fmaxf(all_m, ml[(tile + k * qw) * 16 + col].x);
+            all_l = 0.0f;
+            for (int k = 0; k < shares; ++k) {
+                const float2 w = ml[(tile + k * qw) * 16 + col];
+                all_l = fmaf(w.y, __builtin_amdgcn_exp2f(w.x - all_m), all_l);
             }
+            const float f = __builtin_amdgcn_exp2f(m - all_m);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[b] *= f;
+            if (wave >= 2) give(wave - 2);
+            __syncthreads();
+            if (wave < 2) take(wave);
+            if (shares == 4) {
+                __syncthreads();
+                if (wave == 1) give(0);
+                __syncthreads();
+                if (wave == 0) take(0);
+            }
+        }
+        if (share == 0 && first + col < queries) {
+            const int slot = tile * 16 + col;
+            if (g == 0) ml_out[slot] = float2{all_m, all_l};
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o_out[(int64_t)slot * D + Data::column(b, 4 * g + k)] = o[b][k];
         }
     }
 };
 
-template <int D, int kTiles>
-constexpr int attend_lds_floats() { return 2 * kAttendWaves * 16 * kTiles + 2 * kTiles * (D / 16) * 64 * 4; }
-
-template <int D, bool kFp8, int kRowTiles, int kPrefixTiles>
-__global__ __launch_bounds__(64 * kAttendWaves)
+template <int D, bool kFp8>
+__global__ __launch_bounds__(64 * kAttendWaves, 2)
 void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
 {
-    __shared__ __align__(16) float lds[attend_lds_floats<D, kPrefixTiles>()];
-    const PlanHead head = *reinterpret_cast<const PlanHead*>(ws);
-    const Task* tasks = reinterpret_cast<const Task*>(ws + s.at_tasks);
+    __shared__ __align__(16) float lds[2 * kAttendWaves * 16 + 2 * (D / 16) * 64 * 4];
+    __shared__ int64_t sums[kAttendWaves];
+    __shared__ int firsts[kPlanThreads];
+    const Plan plan = make_plan(a, s, c.heads, c.page_size, sums, firsts);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<PlanHead*>(ws) = PlanHead{plan.run, plan.prefix_tasks};
+    int32_t* unit_first = reinterpret_cast<int32_t*>(ws + s.at_first);
     float2* ml = reinterpret_cast<float2*>(ws + s.at_ml);
     float* o = reinterpret_cast<float*>(ws + s.at_o);
-    for (int i = blockIdx.x; i < head.prefix_tasks + head.row_tasks; i += gridDim.x) {
-        const Task task = tasks[i];
-        if (i < head.prefix_tasks) {
-            const int64_t slot = s.max_row_tasks * s.row_slot + (int64_t)i * s.prefix_tile;
-            Attend<D, kFp8, kPrefixTiles> x;
-            x.template run<true>(c, a, s, task, lds, ml + slot, o + slot * D, s.prefix_tile);
-        } else {
-            const int64_t slot = (int64_t)(i - head.prefix_tasks) * s.row_slot;
-            Attend<D, kFp8, kRowTiles> x;
-            x.template run<false>(c, a, s, task, lds, ml + slot, o + slot * D, s.row_slot);
-        }
+    // (groups that overlap, against the contract, could exceed the results' places)
+    const int prefix_tasks = plan.prefix_tasks < s.max_prefix_tasks ? plan.prefix_tasks : (int)s.max_prefix_tasks;
+    for (int i = blockIdx.x; i < plan.tasks; i += gridDim.x) {
+        if (i >= prefix_tasks && i < plan.prefix_tasks) continue;
+        const Task task = task_at(a, s, c.heads, c.page_size, plan, firsts, i);
+        if (task.leads && threadIdx.x == 0) unit_first[task.unit] = i;
+        const int64_t slot = i < prefix_tasks ? s.max_row_tasks * s.row_slot + (int64_t)i * s.prefix_slot
+                                              : (int64_t)(i - plan.prefix_tasks) * s.row_slot;
+        Attend<D, kFp8> x;
+        x.run(c, a, s, task, lds, ml + slot, o + slot * D);
     }
 }
 
@@ -545,25 +547,31 @@ void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
 // A wave per (row, key head, query): the partial results of the prefix's runs, then those of the row's.
 template <int D>
 __global__ __launch_bounds__(256)
-void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, const char* ws)
+void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size, const char* ws)
 {
     constexpr int kCols = D / 64;
     const int lane = threadIdx.x & 63;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= (int64_t)a.rows * heads * s.M) return;
     const int in_row = (int)(at % s.M), head = (int)(at / s.M % heads), row = (int)(at / s.M / heads);
-    const int2* row_plan = reinterpret_cast<const int2*>(ws + s.at_row);
-    const int2* prefix_plan = reinterpret_cast<const int2*>(ws + s.at_prefix);
-    const int group = reinterpret_cast<const int32_t*>(ws + s.at_group)[row];
+    const PlanHead plan = *reinterpret_cast<const PlanHead*>(ws);
+    const int32_t* unit_first = reinterpret_cast<const int32_t*>(ws + s.at_first);
     const float2* ml = reinterpret_cast<const float2*>(ws + s.at_ml);
     const float* o = reinterpret_cast<const float*>(ws + s.at_o);
+    // the row's group: the last one that begins at or before it
+    int group = -1;
+    for (int g0 = 0; g0 < a.groups; g0 += 64) {
+        const int n = (int)__popcll(__ballot(g0 + lane < a.groups && a.group_offsets[g0 + lane < a.groups ? g0 + lane : 0] <= row));
+        group += n;
+        if (n < 64) break;
+    }
 
     float m = kNoScore, l = 0.0f, acc[kCols] = {};
     // results at slots first + i * apart, i < n
     auto join = [&](int64_t first, int64_t apart, int n) {
         for (int i0 = 0; i0 < n; i0 += 64) {
             const int many = n - i0 < 64 ? n - i0 : 64;
-            float2 mine = lane < many ? ml[first + (i0 + lane) * apart] : float2{kNoScore, 0.0f};
+            const float2 mine = lane < many ? ml[first + (i0 + lane) * apart] : float2{kNoScore, 0.0f};
             const float top = wave_max(mine.x);
             const float to = fmaxf(m, top);
             const float f = __builtin_amdgcn_exp2f(m - to);
@@ -571,26 +579,48 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, const char* w
             l *= f;
 #pragma unroll
             for (int j = 0; j < kCols; ++j) acc[j] *= f;
-            const float w = __builtin_amdgcn_exp2f(mine.x - to);           // 0 beyond `many` once any score is there
+            const float w = lane < many ? __builtin_amdgcn_exp2f(mine.x - to) : 0.0f;
             l += (float)wave_sum((double)(mine.y * w));
-            for (int i = 0; i < many; ++i) {
-                const float wi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i));
-                const float* p = o + (first + (i0 + i) * apart) * D + lane * kCols;
+            // eight results in flight; past the last one its place is read again with no weight
+            for (int i = 0; i < many; i += 8) {
+                float p[8][kCols];
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) acc[j] = fmaf(wi, p[j], acc[j]);
+                for (int k = 0; k < 8; ++k) {
+                    const int at_i = i + k < many ? i + k : many - 1;
+                    const float* from = o + (first + (i0 + at_i) * apart) * D + lane * kCols;
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) p[k][j] = from[j];
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float wk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i + k < 64 ? i + k : 63));
+                    if (i + k < many) {
+#pragma unroll
+                        for (int j = 0; j < kCols; ++j) acc[j] = fmaf(wk, p[k][j], acc[j]);
+                    }
+                }
             }
         }
     };
     if (group >= 0) {
-        const int2 plan = prefix_plan[group];
-        const int qi = (row - clamp_len(a.group_offsets[group], a.rows)) * s.M + in_row;
-        const int64_t item = (int64_t)(qi / s.prefix_tile) * heads + head;
-        join(s.max_row_tasks * s.row_slot + (plan.x + item * plan.y) * s.prefix_tile + qi % s.prefix_tile, s.prefix_tile, plan.y);
+        const Unit x = unit_at(a, s, page_size, group);
+        const int runs = runs_of(x.len, plan.run);
+        const int64_t qi = (int64_t)(row - x.row0) * s.M + in_row;
+        if (runs > 0 && qi < x.queries) {
+            const int per = 16 * query_waves(x.queries);
+            const int64_t first = unit_first[group] + (qi / per * heads + head) * runs;
+            if (first >= 0 && first + runs <= s.max_prefix_tasks)          // (see attend_kernel)
+                join(s.max_row_tasks * s.row_slot + first * s.prefix_slot + qi % per, s.prefix_slot, runs);
+        }
     }
     {
-        const int2 plan = row_plan[row];
-        const int64_t item = (int64_t)(in_row / s.row_tile) * heads + head;
-        join((plan.x + item * plan.y) * s.row_slot + in_row % s.row_tile, s.row_slot, plan.y);
+        const Unit x = unit_at(a, s, page_size, a.groups + row);
+        const int runs = runs_of(x.len, plan.run);
+        if (runs > 0) {
+            const int per = 16 * query_waves(x.queries);
+            const int64_t first = unit_first[a.groups + row] - plan.prefix_tasks + (in_row / per * heads + head) * runs;
+            join(first * s.row_slot + in_row % per, s.row_slot, runs);
+        }
     }
     const int t = in_row / s.R, h = head * s.R + in_row % s.R;
     const int64_t where = ((int64_t)row * a.T + t) * a.q_heads + h;
@@ -607,15 +637,14 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, const char* w
     if (a.lse && lane == 0) a.lse[where] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (float)kLn2;
 }
 
-template <int D, bool kFp8, int kRowTiles, int kPrefixTiles>
+template <int D, bool kFp8>
 static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, const AttendShape& s, char* ws, hipStream_t stream)
 {
-    attend_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, s, c.heads, c.page_size, ws);
     const int64_t most = s.max_row_tasks + s.max_prefix_tasks;
     const int64_t groups = (int64_t)compute_units() * 2;
-    attend_kernel<D, kFp8, kRowTiles, kPrefixTiles><<<(uint32_t)(most < groups ? most : groups), 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
+    attend_kernel<D, kFp8><<<(uint32_t)(most < groups ? most : groups), 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
     const int64_t waves = (int64_t)a.rows * c.heads * s.M;
-    attend_join_kernel<D><<<(uint32_t)((waves + 3) / 4), 256, 0, stream>>>(a, s, c.heads, ws);
+    attend_join_kernel<D><<<(uint32_t)((waves + 3) / 4), 256, 0, stream>>>(a, s, c.heads, c.page_size, ws);
     return hipGetLastError();
 }
 
@@ -624,15 +653,8 @@ hipError_t launch_prefix_attention(const CacheView& c, const AttentionArgs& a, v
     AttendShape s;
     if (!attend_shape(a.rows, a.T, a.q_heads, c.heads, c.dim, a.groups, s)) return hipErrorInvalidValue;
     char* ws = static_cast<char*>(workspace);
-    auto by_tiles = [&](auto d, auto fp8) {
-        constexpr int D = decltype(d)::value;
-        constexpr bool kFp8 = decltype(fp8)::value;
-        if (s.row_tile == 16) return launch_attend<D, kFp8, 1, 2>(c, a, s, ws, stream);
-        if (s.row_tile == 32) return launch_attend<D, kFp8, 2, 2>(c, a, s, ws, stream);
-        return launch_attend<D, kFp8, 4, 4>(c, a, s, ws, stream);
-    };
-    auto by_type = [&](auto d) { return c.fp8 ? by_tiles(d, std::true_type{}) : by_tiles(d, std::false_type{}); };
-    return c.dim == 128 ? by_type(std::integral_constant<int, 128>{}) : by_type(std::integral_constant<int, 64>{});
+    if (c.dim == 128) return c.fp8 ? launch_attend<128, true>(c, a, s, ws, stream) : launch_attend<128, false>(c, a, s, ws, stream);
+    return c.fp8 ? launch_attend<64, true>(c, a, s, ws, stream) : launch_attend<64, false>(c, a, s, ws, stream);
 }
 
 }  // namespace e3
