@@ -261,7 +261,7 @@ struct StepData {
     u32x2 ks, vs;                                                       // scale bytes of tokens 8 g .. 8 g + 7
 
     // `row`: index of the step's first token among the rows of D elements
-    __device__ __forceinline__ void load(const CacheView& c, int64_t row, int lane)
+    __device__ __forceinline__ void load_keys(const CacheView& c, int64_t row, int lane)
     {
         const int m = lane & 15, g = lane >> 4;
         constexpr int kElem = kFp8 ? 1 : 2;
@@ -270,13 +270,16 @@ struct StepData {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) k[t][i] = stream_load(reinterpret_cast<const u32x4*>(kp + t * 4 * (D * kElem) + i * 64));
+        if (kFp8) ks = *reinterpret_cast<const u32x2*>(c.k_scale + row + g * 8);
+    }
+    __device__ __forceinline__ void load_values(const CacheView& c, int64_t row, int lane)
+    {
+        const int m = lane & 15, g = lane >> 4;
+        constexpr int kElem = kFp8 ? 1 : 2;
         const char* vp = static_cast<const char*>(c.v) + row * (D * kElem) + g * (8 * D * kElem) + m * 16;
 #pragma unroll
         for (int i = 0; i < kVLoads; ++i) v[i] = stream_load(reinterpret_cast<const u32x4*>(vp + i * 256));
-        if (kFp8) {
-            ks = *reinterpret_cast<const u32x2*>(c.k_scale + row + g * 8);
-            vs = *reinterpret_cast<const u32x2*>(c.v_scale + row + g * 8);
-        }
+        if (kFp8) vs = *reinterpret_cast<const u32x2*>(c.v_scale + row + g * 8);
     }
     // K of score tile t, columns of k-step s
     __device__ __forceinline__ bf16x8 key(int t, int s) const
@@ -302,12 +305,17 @@ struct StepData {
     // tokens of the lane's eight from the n-th on become zeros, in V and in both scales
     __device__ __forceinline__ void clear_from(int n)
     {
+        clear_values_from(n);
+        if (kFp8) ks &= u32x2{n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u,
+                              n >= 8 ? 0xFFFFFFFFu : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1u};
+    }
+    __device__ __forceinline__ void clear_values_from(int n)
+    {
         if (kFp8) {
             const uint32_t lo = n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
             const uint32_t hi = n >= 8 ? 0xFFFFFFFFu : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1u;
 #pragma unroll
             for (int i = 0; i < kVLoads; ++i) v[i] &= u32x4{lo, hi, lo, hi};
-            ks &= u32x2{lo, hi};
             vs &= u32x2{lo, hi};
         } else {
             u32x4 mask;
@@ -351,11 +359,13 @@ struct Attend {
     float m, l;
     int limit;                                  // tokens the lane's query sees (of the prefix, of the row)
 
-    // One step.  `at`: its first token; every query sees at least `sure` tokens, none more than `most`.
-    __device__ __forceinline__ void step(Data& d, int at, int sure, int most, float c, int lane)
+    // One step.  `at`: its first token; every query sees at least `sure` tokens, none more than `most`.  The keys' registers
+    // are given to the next step (`next`: where it lies) as soon as the scores are there, the values' at the end.
+    __device__ __forceinline__ void step(Data& d, const CacheView& cache, int64_t next, int at, int sure, int most, float c, int lane)
     {
         const int g = lane >> 4;
         const bool tail = at + kStep > sure;                              // uniform
+        const int see = limit < most ? limit : most;
         if (tail) d.clear_from(most - at - 8 * g);
         f32x4 s[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
@@ -366,8 +376,9 @@ struct Attend {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             x[j] = s[j >> 2][j & 3] * (kFp8 ? c * d.k_factor(j) : c);
-            if (tail) x[j] = at + 8 * g + j < limit ? x[j] : -INFINITY;
+            if (tail) x[j] = at + 8 * g + j < see ? x[j] : -INFINITY;
         }
+        d.load_keys(cache, next, lane);
         float top = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
         if (__any(top > m + kSlack)) {
             // the queries' maxima over the four lanes that hold their scores
@@ -395,20 +406,21 @@ struct Attend {
             const int end = at + kStep;
             const int mine = limit < at ? at : limit < end ? limit : end;
             for (int have = most < end ? most : end; have >= (sure > at ? sure : at); --have) {
-                d.clear_from(have - at - 8 * g);
+                d.clear_values_from(have - at - 8 * g);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
                     const f32x4 r = mfma(d.value(b), rest, mfma(d.value(b), p, o[b]));
                     if (mine == have) o[b] = r;
                 }
             }
-            return;
-        }
+        } else {
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const bf16x8 value = d.value(b);
-            o[b] = mfma(value, rest, mfma(value, p, o[b]));
+            for (int b = 0; b < kBlocks; ++b) {
+                const bf16x8 value = d.value(b);
+                o[b] = mfma(value, rest, mfma(value, p, o[b]));
+            }
         }
+        d.load_values(cache, next, lane);
     }
 
     // A task.  lds: (m, l) of all waves, then O of two waves.
@@ -456,14 +468,17 @@ struct Attend {
         };
         int at = task.from + share * kStep;
         if (at < to && first < queries) {
-            Data cur, next;
+            Data d;
             int page = page_at(at), page_next = page_at(at + apart);
-            cur.load(c, row_of(page, at), lane);
+            d.load_keys(c, row_of(page, at), lane);
+            d.load_values(c, row_of(page, at), lane);
             for (; at < to; at += apart) {
                 const int page_after = page_at(at + 2 * apart);
-                if (at + apart < to) next.load(c, row_of(page_next, at + apart), lane);
-                if ((uint32_t)page < (uint64_t)c.num_pages) step(cur, at, sure, len, scale, lane);
-                cur = next;
+                // behind the last step: a page of the cache again, for nothing
+                const int64_t next = row_of(page_next, at + apart);
+                // (a page that the cache does not have: no token of the step is seen)
+                const bool there = (uint32_t)page < (uint64_t)c.num_pages;
+                step(d, c, next, at, there ? sure : -1, there ? len : -1, scale, lane);
                 page = page_next;
                 page_next = page_after;
             }
