@@ -8,12 +8,14 @@
 // prefix is read once for all rows of its group, whose queries form the columns of one product.
 //
 // Two launches:
-//   attend   workgroups of four waves.  Each looks at all lengths first (device memory: they change with every step) and
-//            cuts every prefix and row ("unit") into runs of one length, chosen so that the tasks fill the card some times
-//            over; a task is a run, a key head and a tile of queries.  The waves of a task share its queries by tiles of
-//            16 (one, two or four of them) and, as far as there are fewer tiles than waves, its steps of 32 tokens; each
-//            keeps its own (m, l, O) in registers.  Waves with the same queries join through LDS, and every task leaves one
-//            partial result in the workspace.
+//   attend   workgroups of four waves, as many as are resident together.  Each looks at all lengths first (device
+//            memory: they change with every step).  A prefix or a row's own tokens ("unit"), a key head and a tile of
+//            queries are an item; the items lie behind one another, measured in the steps of 32 tokens that a wave has to
+//            take, and every workgroup takes an equal stretch of that line, whichever items it falls into.  The waves of
+//            an item share its queries by tiles of 16 (one, two or four of them) and, as far as there are fewer tiles than
+//            waves, its steps; each keeps its own (m, l, O) in registers.  Waves with the same queries join through LDS,
+//            and the part of an item in a stretch leaves one partial result in the workspace.  (Runs of one length dealt
+//            round robin before: rows of 1 to 6000 tokens left the workgroups 1.6 times the mean at worst.)
 //   join     a wave per row, query and head joins the partial results of its prefix and its own tokens.
 //
 // Registers instead of LDS: S^T = K Q^T puts the queries on the matrix instruction's columns, so a lane holds one
@@ -39,21 +41,19 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 32;                       // tokens of a wave's step
 constexpr int kAttendWaves = 4;
-constexpr int kRun = kStep * kAttendWaves;      // a run is a multiple of this
 constexpr float kNoScore = -3.0e38f;            // running maximum before any score
 constexpr float kSlack = 8.0f;                  // scores may pass the running maximum by this (2^8) before it moves
-constexpr int kTargetTasks = 2048;              // tasks that one long run is cut into, all prefixes and rows together
-
 // What the host fixes of a call; the workspace's parts lie behind one another.
 struct AttendShape {
     int32_t R, M;                               // query heads per key head; queries of a row and key head (T * R)
     int32_t units;                              // groups, then rows
     int32_t row_slot, prefix_slot;              // queries that a task of either kind leaves results of, at most
-    int64_t max_row_tasks, max_prefix_tasks;
+    int32_t workgroups;
+    int64_t row_slots, prefix_slots;            // places for the partial results of rows, of prefixes
     int64_t at_first, at_ml, at_o, bytes;       // byte offsets (at_o: fp32 [results][D])
 };
 
-struct PlanHead { int32_t run, prefix_tasks; };
+struct PlanHead { int64_t steps; int32_t parts, prefix_items; };
 
 static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -65,6 +65,9 @@ __host__ __device__ __forceinline__ int64_t query_tiles(int64_t queries)
     return (queries + per - 1) / per;
 }
 
+// Workgroups per compute unit, which are waves per SIMD, that the registers allow.
+constexpr int attend_occupancy(int64_t D, bool fp8) { return D == 64 ? (fp8 ? 4 : 3) : fp8 ? 3 : 2; }
+
 static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int64_t groups, AttendShape& s)
 {
     s.R = (int32_t)(q_heads / heads);
@@ -74,13 +77,14 @@ static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads
     s.units = (int32_t)(groups + rows);
     s.row_slot = (int32_t)(M < 64 ? M : 64);
     s.prefix_slot = (int32_t)(rows * M < 64 ? rows * M : 64);
-    s.max_row_tasks = heads * rows * query_tiles(M) + kTargetTasks;
-    s.max_prefix_tasks = groups > 0 ? heads * (rows * M / 64 + groups) + kTargetTasks : 0;
-    const int64_t tasks = s.max_row_tasks + s.max_prefix_tasks;
-    const int64_t slots = s.max_row_tasks * s.row_slot + s.max_prefix_tasks * s.prefix_slot;
-    if (tasks > (int64_t)1 << 30 || slots > ((int64_t)1 << 31) - 1) return false;
+    // an item, or a part of it, per place: no more parts than items and workgroups together
+    s.workgroups = compute_units() * attend_occupancy(D, true);
+    s.row_slots = heads * rows * query_tiles(M) + s.workgroups;
+    s.prefix_slots = groups > 0 ? heads * (rows * M / 64 + groups) + s.workgroups : 0;
+    const int64_t slots = s.row_slots * s.row_slot + s.prefix_slots * s.prefix_slot;
+    if (s.row_slots + s.prefix_slots > (int64_t)1 << 30 || slots > ((int64_t)1 << 31) - 1) return false;
     s.at_first = 256;
-    s.at_ml = up(s.at_first + (int64_t)s.units * 4, 256);
+    s.at_ml = up(s.at_first + (int64_t)s.units * 8, 256);
     s.at_o = up(s.at_ml + slots * 8, 256);
     s.bytes = up(s.at_o + slots * D * 4, 256);
     return true;
@@ -103,12 +107,20 @@ __device__ __forceinline__ int64_t table_tokens(int width, int page_size)
     return n > 0x7FFFFF00 ? 0x7FFFFF00 : n;
 }
 
+// The same in every lane: kept in scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    return (int64_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v);
+}
+
 // A group's prefix or a row's own tokens.
 struct Unit {
     int len, row0;                              // tokens; the first row that sees them
     int64_t queries;                            // per key head
+    int items, steps;                           // (tile, key head) pairs, and a wave's steps in each; 0: nothing to do
 };
-__device__ __forceinline__ Unit unit_at(const AttentionArgs& a, const AttendShape& s, int page_size, int u)
+__device__ __forceinline__ Unit unit_at(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, int u)
 {
     Unit x;
     if (u < a.groups) {
@@ -121,119 +133,128 @@ __device__ __forceinline__ Unit unit_at(const AttentionArgs& a, const AttendShap
         x.len = clamp_len(a.row_lens[x.row0], table_tokens(a.row_width, page_size));
         x.queries = s.M;
     }
+    const int apart = kStep * kAttendWaves / query_waves(x.queries);           // tokens of a round of the waves that share the steps
+    x.items = x.len > 0 ? (int)(query_tiles(x.queries) * heads) : 0;
+    x.steps = x.len > 0 ? (int)(((int64_t)x.len + apart - 1) / apart) : 0;
     return x;
 }
-__device__ __forceinline__ int runs_of(int len, int run) { return (int)(((int64_t)len + run - 1) / run); }
 
-// sums over the waves of a workgroup that come before the thread's own lane, and over all
-__device__ __forceinline__ int64_t workgroup_scan(int64_t v, int64_t* lds, int64_t* total)
+// exclusive sums of two counts over the workgroup's threads, and the totals
+__device__ __forceinline__ void workgroup_scan(int64_t& v, int64_t& w, int64_t* lds, int64_t* total_v, int64_t* total_w)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t x = v;
+    int64_t x = v, y = w;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
+        const int64_t xs = __shfl_up(x, d), ys = __shfl_up(y, d);
+        if (lane >= d) { x += xs; y += ys; }
     }
+    if (lane == 63) { lds[2 * wave] = x; lds[2 * wave + 1] = y; }
     __syncthreads();
-    if (lane == 63) lds[wave] = x;
-    __syncthreads();
-    int64_t before = 0, all = 0;
+    int64_t before_x = 0, before_y = 0, all_x = 0, all_y = 0;
 #pragma unroll
     for (int i = 0; i < kAttendWaves; ++i) {
-        if (i < wave) before += lds[i];
-        all += lds[i];
+        if (i < wave) { before_x += lds[2 * i]; before_y += lds[2 * i + 1]; }
+        all_x += lds[2 * i];
+        all_y += lds[2 * i + 1];
     }
-    *total = all;
-    return before + x - v;
+    *total_v = all_x;
+    *total_w = all_y;
+    v = before_x + x - v;
+    w = before_y + y - w;
 }
 
-// Every thread sums up a share of successive units; `first` [kPlanThreads] gets each share's first task.
+// Every thread sums up a share of successive units; `first` gets each share's first step.
 struct Plan {
-    int share, run, tasks, prefix_tasks;
+    int share, prefix_items, parts;             // units of a share; items of all prefixes; stretches
+    int64_t steps;
 };
-__device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, int64_t* lds, int* first)
+__device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, int64_t* lds,
+                                          int64_t* first, int* first_item)
 {
     Plan p;
     p.share = (s.units + kPlanThreads - 1) / kPlanThreads;
     const int u0 = (int)threadIdx.x * p.share;
     const int u1 = u0 + p.share < s.units ? u0 + p.share : s.units;
-    int64_t tokens = 0, total;
+    int64_t steps = 0, items = 0, total, prefix = 0;                           // items: of prefixes in the upper half
     for (int u = u0; u < u1; ++u) {
-        const Unit x = unit_at(a, s, page_size, u);
-        tokens += x.len * query_tiles(x.queries);
+        const Unit x = unit_at(a, s, heads, page_size, u);
+        steps += (int64_t)x.items * x.steps;
+        items += x.items;
+        if (u < a.groups) prefix += x.items;
     }
-    workgroup_scan(tokens, lds, &total);
-    const int64_t run = (total * heads / kTargetTasks + kRun) / kRun * kRun;
-    p.run = (int)(run < 0x40000000 ? run : 0x40000000);
-    int64_t tasks = 0, prefix = 0;
-    for (int u = u0; u < u1; ++u) {
-        const Unit x = unit_at(a, s, page_size, u);
-        const int64_t n = runs_of(x.len, p.run) * query_tiles(x.queries) * heads;
-        tasks += n;
-        if (u < a.groups) prefix += n;
-    }
-    // both counts in one word (each below 2^31, see attend_shape)
-    const int64_t before = workgroup_scan(prefix << 32 | tasks, lds, &total);
-    first[threadIdx.x] = (int)(before & 0x7FFFFFFF);
-    p.tasks = (int)(total & 0x7FFFFFFF);
-    p.prefix_tasks = (int)(total >> 32);
+    items |= prefix << 32;
+    workgroup_scan(steps, items, lds, &total, &prefix);
+    first[threadIdx.x] = steps;
+    first_item[threadIdx.x] = (int)(uint32_t)items;
+    total = uniform(total);
+    p.steps = total;
+    p.prefix_items = uniform((int)(prefix >> 32));
+    p.parts = total < (int64_t)gridDim.x ? (int)total : (int)gridDim.x;
     __syncthreads();
     return p;
+}
+// stretch w: steps [begin_of(w), begin_of(w + 1)); and the stretch that holds a step
+__device__ __forceinline__ int64_t begin_of(int w, int64_t steps, int parts) { return w * steps / parts; }
+__device__ __forceinline__ int part_of(int64_t step, int64_t steps, int parts) { return (int)(((step + 1) * parts + steps - 1) / steps) - 1; }
+
+// The unit that holds a step, with the unit's first step and item; uniform.
+struct Place {
+    int unit, item;
+    int64_t step;
+    Unit of;
+};
+__device__ __forceinline__ Unit uniform(const Unit& x)
+{
+    return Unit{uniform(x.len), uniform(x.row0), uniform(x.queries), uniform(x.items), uniform(x.steps)};
+}
+__device__ __forceinline__ Place place_of(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, const Plan& p,
+                                          const int64_t* first, const int* first_item, int64_t step)
+{
+    const int lane = threadIdx.x & 63;
+    // the last share that begins at or before the step
+    int below = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanThreads / 64; ++k) below += (int)__popcll(__ballot(first[k * 64 + lane] <= step));
+    const int share = uniform(below) - 1;
+    Place r{};
+    r.unit = -1;
+    r.step = uniform(first[share]);
+    r.item = uniform(first_item[share]);
+    for (int u0 = share * p.share; u0 < s.units && u0 < (share + 1) * p.share; u0 += 64) {
+        const int u = u0 + lane;
+        Unit x{};
+        if (u < s.units && u < (share + 1) * p.share) x = unit_at(a, s, heads, page_size, u);
+        const int64_t mine = (int64_t)x.items * x.steps;
+        int64_t sum = mine;
+        int items = x.items;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t y = __shfl_up(sum, d);
+            const int z = __shfl_up(items, d);
+            if (lane >= d) { sum += y; items += z; }
+        }
+        const unsigned long long behind = __ballot(r.step + sum > step);
+        const int l = behind != 0ull ? (int)__builtin_ctzll(behind) : 63;
+        const int64_t upto = uniform(__shfl(sum, l)), own = uniform(__shfl(mine, l));
+        const int items_upto = __builtin_amdgcn_readlane(items, l), own_items = __builtin_amdgcn_readlane(x.items, l);
+        if (behind != 0ull) {
+            r.unit = u0 + l;
+            r.step += upto - own;
+            r.item += items_upto - own_items;
+            break;
+        }
+        r.step += upto;
+        r.item += items_upto;
+    }
+    if (r.unit >= 0) r.of = uniform(unit_at(a, s, heads, page_size, r.unit));
+    return r;
 }
 
 struct Task {
     int unit, head, tile, from, to;             // tokens [from, to)
-    bool leads;                                 // the unit's first task
     Unit of;
 };
-__device__ __forceinline__ Task task_at(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, const Plan& p,
-                                        const int* first, int i)
-{
-    const int lane = threadIdx.x & 63;
-    // the last share that begins at or before task i
-    int below = 0;
-#pragma unroll
-    for (int k = 0; k < kPlanThreads / 64; ++k) below += (int)__popcll(__ballot(first[k * 64 + lane] <= i));
-    const int share = below - 1;
-    int at = __builtin_amdgcn_readfirstlane(first[share]);
-    Task t{};
-    t.unit = -1;
-    for (int u0 = share * p.share; u0 < s.units && u0 < (share + 1) * p.share; u0 += 64) {
-        const int u = u0 + lane;
-        Unit x{};
-        int n = 0;
-        if (u < s.units && u < (share + 1) * p.share) {
-            x = unit_at(a, s, page_size, u);
-            n = (int)(runs_of(x.len, p.run) * query_tiles(x.queries) * heads);
-        }
-        int sum = n;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(sum, d);
-            if (lane >= d) sum += y;
-        }
-        const unsigned long long behind = __ballot(at + sum > i);
-        if (behind != 0ull) {
-            const int l = (int)__builtin_ctzll(behind);
-            t.unit = u0 + l;
-            const int rank = i - (at + __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(n, l));
-            t.of.len = __builtin_amdgcn_readlane(x.len, l);
-            t.of.row0 = __builtin_amdgcn_readlane(x.row0, l);
-            t.of.queries = __builtin_amdgcn_readlane((int)x.queries, l);
-            const int runs = runs_of(t.of.len, p.run);
-            const int item = rank / runs, c = rank % runs;
-            t.head = item % heads;
-            t.tile = item / heads;
-            t.from = c * p.run;
-            t.to = t.from + p.run < t.of.len ? t.from + p.run : t.of.len;
-            t.leads = rank == 0;
-            break;
-        }
-        at += __builtin_amdgcn_readlane(sum, 63);
-    }
-    return t;
-}
 
 // ---------------------------------------------------------------- attend
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
@@ -269,7 +290,7 @@ struct StepData {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) k[t][i] = stream_load(reinterpret_cast<const u32x4*>(kp + t * 4 * (D * kElem) + i * 64));
+            for (int i = 0; i < kLoads; ++i) k[t][i] = (*reinterpret_cast<const u32x4*>(kp + t * 4 * (D * kElem) + i * 64));
         if (kFp8) ks = *reinterpret_cast<const u32x2*>(c.k_scale + row + g * 8);
     }
     __device__ __forceinline__ void load_values(const CacheView& c, int64_t row, int lane)
@@ -278,7 +299,7 @@ struct StepData {
         constexpr int kElem = kFp8 ? 1 : 2;
         const char* vp = static_cast<const char*>(c.v) + row * (D * kElem) + g * (8 * D * kElem) + m * 16;
 #pragma unroll
-        for (int i = 0; i < kVLoads; ++i) v[i] = stream_load(reinterpret_cast<const u32x4*>(vp + i * 256));
+        for (int i = 0; i < kVLoads; ++i) v[i] = (*reinterpret_cast<const u32x4*>(vp + i * 256));
         if (kFp8) vs = *reinterpret_cast<const u32x2*>(c.v_scale + row + g * 8);
     }
     // K of score tile t, columns of k-step s
@@ -305,17 +326,12 @@ struct StepData {
     // tokens of the lane's eight from the n-th on become zeros, in V and in both scales
     __device__ __forceinline__ void clear_from(int n)
     {
-        clear_values_from(n);
-        if (kFp8) ks &= u32x2{n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u,
-                              n >= 8 ? 0xFFFFFFFFu : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1u};
-    }
-    __device__ __forceinline__ void clear_values_from(int n)
-    {
         if (kFp8) {
             const uint32_t lo = n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
             const uint32_t hi = n >= 8 ? 0xFFFFFFFFu : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1u;
 #pragma unroll
             for (int i = 0; i < kVLoads; ++i) v[i] &= u32x4{lo, hi, lo, hi};
+            ks &= u32x2{lo, hi};
             vs &= u32x2{lo, hi};
         } else {
             u32x4 mask;
@@ -325,26 +341,33 @@ struct StepData {
             for (int i = 0; i < kVLoads; ++i) v[i] &= mask;
         }
     }
-    // whether the lane holds a value (or a scale) that is no finite number
+    // all bits of the elements of two (bf16) or four (codes) that are no finite number
+    static __device__ __forceinline__ uint32_t unbounded_in(uint32_t w)
+    {
+        if (kFp8) return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;   // 0x7F, 0xFF: the sum carries
+        return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+    }
+    // whether the lane holds a value that is no finite number
     __device__ __forceinline__ bool unbounded() const
     {
-        bool bad = false;
-        if (kFp8) {
+        uint32_t bad = 0;
 #pragma unroll
-            for (int i = 0; i < kVLoads; ++i)
+        for (int i = 0; i < kVLoads; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)                              // a byte of 0x7F or 0xFF: + 1 carries into its top bit
-                    bad |= (((v[i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+            for (int j = 0; j < 4; ++j) bad |= unbounded_in(v[i][j]);
+        return bad != 0;
+    }
+    // such values of `from` as ones, all others as zeros; they are zeros in `from` afterwards
+    __device__ __forceinline__ void take_unbounded(StepData& from)
+    {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bad |= ((vs[j >> 2] >> (8 * (j & 3))) & 0xFFu) == 0xFFu;
-        } else {
+        for (int i = 0; i < kVLoads; ++i)
 #pragma unroll
-            for (int i = 0; i < kVLoads; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    bad |= (v[i][j] & 0x7F80u) == 0x7F80u || (v[i][j] & 0x7F800000u) == 0x7F800000u;
-        }
-        return bad;
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t bad = unbounded_in(from.v[i][j]);
+                v[i][j] = bad & (kFp8 ? 0x38383838u : 0x3F803F80u);
+                from.v[i][j] &= ~bad;
+            }
     }
     __device__ __forceinline__ float k_factor(int j) const { return __uint_as_float(((ks[j >> 2] >> (8 * (j & 3))) & 0xFFu) << 23); }
     __device__ __forceinline__ float v_factor(int j) const { return __uint_as_float(((vs[j >> 2] >> (8 * (j & 3))) & 0xFFu) << 23); }
@@ -401,24 +424,24 @@ struct Attend {
             rest[j] = (__bf16)(w - (float)p[j]);
         }
         // Tokens that some queries see and others do not: a weight of zero keeps them out, unless the value is no
-        // number.  Then the queries take turns, those that see most first, and what the next do not see is cleared.
+        // finite number.  Such values leave the product, and one more counts those that a query sees.
         if (__builtin_expect(tail && sure < most && __any(d.unbounded()), 0)) {
-            const int end = at + kStep;
-            const int mine = limit < at ? at : limit < end ? limit : end;
-            for (int have = most < end ? most : end; have >= (sure > at ? sure : at); --have) {
-                d.clear_values_from(have - at - 8 * g);
+            bf16x8 seen;
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    const f32x4 r = mfma(d.value(b), rest, mfma(d.value(b), p, o[b]));
-                    if (mine == have) o[b] = r;
-                }
-            }
-        } else {
+            for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(at + 8 * g + j < see ? 1.0f : 0.0f);
+            Data ones;
+            ones.take_unbounded(d);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
-                const bf16x8 value = d.value(b);
-                o[b] = mfma(value, rest, mfma(value, p, o[b]));
+                const f32x4 count = mfma(ones.value(b), seen, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[b][k] = count[k] > 0.0f ? __builtin_nanf("") : o[b][k];
             }
+        }
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const bf16x8 value = d.value(b);
+            o[b] = mfma(value, rest, mfma(value, p, o[b]));
         }
         d.load_values(cache, next, lane);
     }
@@ -534,27 +557,58 @@ struct Attend {
 };
 
 template <int D, bool kFp8>
-__global__ __launch_bounds__(64 * kAttendWaves, 2)
+__global__ __launch_bounds__(64 * kAttendWaves, attend_occupancy(D, kFp8))
 void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
 {
     __shared__ __align__(16) float lds[2 * kAttendWaves * 16 + 2 * (D / 16) * 64 * 4];
-    __shared__ int64_t sums[kAttendWaves];
-    __shared__ int firsts[kPlanThreads];
-    const Plan plan = make_plan(a, s, c.heads, c.page_size, sums, firsts);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<PlanHead*>(ws) = PlanHead{plan.run, plan.prefix_tasks};
-    int32_t* unit_first = reinterpret_cast<int32_t*>(ws + s.at_first);
+    __shared__ int64_t sums[2 * kAttendWaves];
+    __shared__ int64_t firsts[kPlanThreads];
+    __shared__ int first_items[kPlanThreads];
+    const Plan plan = make_plan(a, s, c.heads, c.page_size, sums, firsts, first_items);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<PlanHead*>(ws) = PlanHead{plan.steps, plan.parts, plan.prefix_items};
+    const int part = blockIdx.x;
+    if (part >= plan.parts) return;
+    int2* unit_first = reinterpret_cast<int2*>(ws + s.at_first);
     float2* ml = reinterpret_cast<float2*>(ws + s.at_ml);
     float* o = reinterpret_cast<float*>(ws + s.at_o);
-    // (groups that overlap, against the contract, could exceed the results' places)
-    const int prefix_tasks = plan.prefix_tasks < s.max_prefix_tasks ? plan.prefix_tasks : (int)s.max_prefix_tasks;
-    for (int i = blockIdx.x; i < plan.tasks; i += gridDim.x) {
-        if (i >= prefix_tasks && i < plan.prefix_tasks) continue;
-        const Task task = task_at(a, s, c.heads, c.page_size, plan, firsts, i);
-        if (task.leads && threadIdx.x == 0) unit_first[task.unit] = i;
-        const int64_t slot = i < prefix_tasks ? s.max_row_tasks * s.row_slot + (int64_t)i * s.prefix_slot
-                                              : (int64_t)(i - plan.prefix_tasks) * s.row_slot;
-        Attend<D, kFp8> x;
-        x.run(c, a, s, task, lds, ml + slot, o + slot * D);
+    int64_t at = begin_of(part, plan.steps, plan.parts);
+    const int64_t end = begin_of(part + 1, plan.steps, plan.parts);
+    Place u = place_of(a, s, c.heads, c.page_size, plan, firsts, first_items, at);
+    while (at < end && u.unit >= 0) {
+        const int off = (int)(at - u.step);                                    // in the unit
+        const int item = off / u.of.steps, from = off % u.of.steps;
+        const int n = end - at < u.of.steps - from ? (int)(end - at) : u.of.steps - from;
+        const int apart = kStep * kAttendWaves / query_waves(u.of.queries);
+        Task task;
+        task.unit = u.unit;
+        task.head = item % c.heads;
+        task.tile = item / c.heads;
+        task.from = from * apart;
+        task.to = u.of.len - task.from < n * apart ? u.of.len : task.from + n * apart;
+        task.of = u.of;
+        if (off == 0 && threadIdx.x == 0) unit_first[u.unit] = int2{(int)u.step, u.item};
+        const bool prefix = u.unit < a.groups;
+        const int64_t place = part + u.item + item - (prefix ? 0 : plan.prefix_items);
+        // (groups that overlap, against the contract, could exceed the places)
+        if (place < (prefix ? s.prefix_slots : s.row_slots)) {
+            const int64_t slot = prefix ? s.row_slots * s.row_slot + place * s.prefix_slot : place * s.row_slot;
+            Attend<D, kFp8> x;
+            x.run(c, a, s, task, lds, ml + slot, o + slot * D);
+        }
+        at += n;
+        if (at < end && item + 1 == u.of.items && from + n == u.of.steps) {
+            const int next = u.unit + 1;
+            Unit x{};
+            if (next < s.units) x = uniform(unit_at(a, s, c.heads, c.page_size, next));
+            if (x.items > 0) {
+                u.step = at;
+                u.item += u.of.items;
+                u.unit = next;
+                u.of = x;
+            } else {
+                u = place_of(a, s, c.heads, c.page_size, plan, firsts, first_items, at);
+            }
+        }
     }
 }
 
@@ -570,7 +624,7 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
     if (at >= (int64_t)a.rows * heads * s.M) return;
     const int in_row = (int)(at % s.M), head = (int)(at / s.M % heads), row = (int)(at / s.M / heads);
     const PlanHead plan = *reinterpret_cast<const PlanHead*>(ws);
-    const int32_t* unit_first = reinterpret_cast<const int32_t*>(ws + s.at_first);
+    const int2* unit_first = reinterpret_cast<const int2*>(ws + s.at_first);
     const float2* ml = reinterpret_cast<const float2*>(ws + s.at_ml);
     const float* o = reinterpret_cast<const float*>(ws + s.at_o);
     // the row's group: the last one that begins at or before it
@@ -617,26 +671,24 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
             }
         }
     };
+    // the parts of the unit's item that holds query qi
+    auto join_unit = [&](int u, int64_t qi, int64_t region, int64_t places, int per_place, int items_before) {
+        const Unit x = unit_at(a, s, heads, page_size, u);
+        if (x.items == 0 || qi >= x.queries) return;
+        const int per = 16 * query_waves(x.queries);
+        const int item = (int)(qi / per) * heads + head;
+        const int2 at_unit = unit_first[u];
+        const int64_t from = at_unit.x + (int64_t)item * x.steps;
+        const int w0 = part_of(from, plan.steps, plan.parts), w1 = part_of(from + x.steps - 1, plan.steps, plan.parts);
+        const int64_t place = (int64_t)at_unit.y - items_before + item + w0;
+        if (place < 0 || w1 < w0 || place + (w1 - w0) >= places) return;        // (see attend_kernel)
+        join(region + place * per_place + qi % per, per_place, w1 - w0 + 1);
+    };
     if (group >= 0) {
-        const Unit x = unit_at(a, s, page_size, group);
-        const int runs = runs_of(x.len, plan.run);
-        const int64_t qi = (int64_t)(row - x.row0) * s.M + in_row;
-        if (runs > 0 && qi < x.queries) {
-            const int per = 16 * query_waves(x.queries);
-            const int64_t first = unit_first[group] + (qi / per * heads + head) * runs;
-            if (first >= 0 && first + runs <= s.max_prefix_tasks)          // (see attend_kernel)
-                join(s.max_row_tasks * s.row_slot + first * s.prefix_slot + qi % per, s.prefix_slot, runs);
-        }
+        const int64_t qi = (int64_t)(row - clamp_len(a.group_offsets[group], a.rows)) * s.M + in_row;
+        join_unit(group, qi, s.row_slots * s.row_slot, s.prefix_slots, s.prefix_slot, 0);
     }
-    {
-        const Unit x = unit_at(a, s, page_size, a.groups + row);
-        const int runs = runs_of(x.len, plan.run);
-        if (runs > 0) {
-            const int per = 16 * query_waves(x.queries);
-            const int64_t first = unit_first[a.groups + row] - plan.prefix_tasks + (in_row / per * heads + head) * runs;
-            join(first * s.row_slot + in_row % per, s.row_slot, runs);
-        }
-    }
+    join_unit(a.groups + row, in_row, 0, s.row_slots, s.row_slot, plan.prefix_items);
     const int t = in_row / s.R, h = head * s.R + in_row % s.R;
     const int64_t where = ((int64_t)row * a.T + t) * a.q_heads + h;
     const bool none = l == 0.0f && m == kNoScore;                          // no key at all
@@ -655,9 +707,8 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
 template <int D, bool kFp8>
 static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, const AttendShape& s, char* ws, hipStream_t stream)
 {
-    const int64_t most = s.max_row_tasks + s.max_prefix_tasks;
-    const int64_t groups = (int64_t)compute_units() * 2;
-    attend_kernel<D, kFp8><<<(uint32_t)(most < groups ? most : groups), 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
+    const int workgroups = compute_units() * attend_occupancy(D, kFp8);
+    attend_kernel<D, kFp8><<<workgroups, 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
     const int64_t waves = (int64_t)a.rows * c.heads * s.M;
     attend_join_kernel<D><<<(uint32_t)((waves + 3) / 4), 256, 0, stream>>>(a, s, c.heads, c.page_size, ws);
     return hipGetLastError();
