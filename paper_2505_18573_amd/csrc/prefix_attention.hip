@@ -10,13 +10,13 @@
 // Two launches:
 //   attend   workgroups of four waves, as many as are resident together.  Each looks at all lengths first (device
 //            memory: they change with every step).  A prefix or a row's own tokens ("unit"), a key head and a tile of
-//            queries are an item; the items lie behind one another, measured in the steps of 32 tokens that a wave has to
-//            take, and every workgroup takes an equal stretch of that line, whichever items it falls into.  The waves of
-//            an item share its queries by tiles of 16 (one, two or four of them) and, as far as there are fewer tiles than
-//            waves, its steps; each keeps its own (m, l, O) in registers.  Waves with the same queries join through LDS,
-//            and the part of an item in a stretch leaves one partial result in the workspace.  (Runs of one length dealt
-//            round robin before: rows of 1 to 6000 tokens left the workgroups 1.6 times the mean at worst.)
-//   join     a wave per row, query and head joins the partial results of its prefix and its own tokens.
+//            queries are an item.  Items of at most 16 queries are one wave's work, larger ones (64 queries at most) a
+//            workgroup's, whose waves bring the keys into LDS for each other.  Items of either kind lie behind one another
+//            on a line, measured in a wave's steps of 32 tokens and a few more for the item itself, and every wave
+//            (workgroup) takes an equal stretch of its line, whichever items it falls into.  What it has of an item, (m, l, O),
+//            stays in registers and is left in the workspace as one partial result.  (Runs of one length dealt round robin
+//            before: rows of 1 to 6000 tokens gave the busiest workgroup 1.6 times the mean.)
+//   join     a workgroup per row and key head joins the partial results of its prefix and its own tokens.
 //
 // Registers instead of LDS: S^T = K Q^T puts the queries on the matrix instruction's columns, so a lane holds one
 // query's scores and the softmax needs hardly any exchange; and since a sum over tokens may be taken in any order, row
@@ -41,23 +41,31 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 32;                       // tokens of a wave's step
 constexpr int kAttendWaves = 4;
+#ifndef E3_ITEM_COST
+#define E3_ITEM_COST 4
+#endif
+constexpr int kItemCost = E3_ITEM_COST;         // what an item costs besides its steps, in steps
+constexpr int kWaveQueries = 16;                // an item of so many is a wave's
 constexpr float kNoScore = -3.0e38f;            // running maximum before any score
 constexpr float kSlack = 8.0f;                  // scores may pass the running maximum by this (2^8) before it moves
+
+enum { kByGroup = 0, kByWave = 1 };             // the two lines
+
 // What the host fixes of a call; the workspace's parts lie behind one another.
 struct AttendShape {
     int32_t R, M;                               // query heads per key head; queries of a row and key head (T * R)
     int32_t units;                              // groups, then rows
-    int32_t row_slot, prefix_slot;              // queries that a task of either kind leaves results of, at most
-    int32_t workgroups;
-    int64_t row_slots, prefix_slots;            // places for the partial results of rows, of prefixes
-    int64_t at_first, at_ml, at_o, bytes;       // byte offsets (at_o: fp32 [results][D])
+    int32_t slot[2];                            // queries that an item of either line leaves results of, at most
+    int64_t slots[2];                           // places for its partial results
+    int64_t at_items, at_ml, at_o, bytes;       // byte offsets (at_items: Parts; at_o: fp32 [results][D])
 };
 
-struct PlanHead { int64_t steps; int32_t parts, prefix_items; };
+// Where the partial results of an item lie: `first` and the places behind it.
+struct Parts { int32_t first, count; };
 
 static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Query tiles of 16 that a task's waves share: as many as a unit's queries fill, up to one per wave.
+// Tiles of 16 queries that the waves of a workgroup share: as many as a unit's queries fill, up to one per wave.
 __host__ __device__ __forceinline__ int query_waves(int64_t queries) { return queries <= 16 ? 1 : queries <= 32 ? 2 : 4; }
 __host__ __device__ __forceinline__ int64_t query_tiles(int64_t queries)
 {
@@ -65,8 +73,16 @@ __host__ __device__ __forceinline__ int64_t query_tiles(int64_t queries)
     return (queries + per - 1) / per;
 }
 
+// The unit's first item in the list of items: rows first, a fixed number of tiles each; a group of n rows has n * M / 64 tiles or
+// one more.  The key heads of a tile lie next to each other.
+__device__ __forceinline__ int64_t first_item(const AttendShape& s, int rows, int heads, bool prefix, int group, int row0)
+{
+    const int64_t of_rows = query_tiles(s.M);
+    return heads * (prefix ? rows * of_rows + (int64_t)row0 * s.M / 64 + group : row0 * of_rows);
+}
+
 // Workgroups per compute unit, which are waves per SIMD, that the registers allow.
-constexpr int attend_occupancy(int64_t D, bool fp8) { return D == 64 ? (fp8 ? 4 : 3) : fp8 ? 3 : 2; }
+constexpr int attend_occupancy(int64_t D, bool fp8) { return D == 64 ? 3 : 2; }
 
 static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int64_t groups, AttendShape& s)
 {
@@ -75,18 +91,20 @@ static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads
     if (M > (1 << 16)) return false;
     s.M = (int32_t)M;
     s.units = (int32_t)(groups + rows);
-    s.row_slot = (int32_t)(M < 64 ? M : 64);
-    s.prefix_slot = (int32_t)(rows * M < 64 ? rows * M : 64);
-    // an item, or a part of it, per place: no more parts than items and workgroups together
-    s.workgroups = compute_units() * attend_occupancy(D, true);
-    s.row_slots = heads * rows * query_tiles(M) + s.workgroups;
-    s.prefix_slots = groups > 0 ? heads * (rows * M / 64 + groups) + s.workgroups : 0;
-    const int64_t slots = s.row_slots * s.row_slot + s.prefix_slots * s.prefix_slot;
-    if (s.row_slots + s.prefix_slots > (int64_t)1 << 30 || slots > ((int64_t)1 << 31) - 1) return false;
-    s.at_first = 256;
-    s.at_ml = up(s.at_first + (int64_t)s.units * 8, 256);
-    s.at_o = up(s.at_ml + slots * 8, 256);
-    s.bytes = up(s.at_o + slots * D * 4, 256);
+    // an item, or a part of it, per place: no more parts than items and workers together
+    const int64_t workgroups = compute_units() * attend_occupancy(D, true);
+    const int64_t most = groups > 0 ? rows * M : M;               // queries of a unit
+    s.slot[kByGroup] = (int32_t)(most < 64 ? most : 64);
+    s.slot[kByWave] = (int32_t)(most < 16 ? most : 16);
+    s.slots[kByGroup] = most > kWaveQueries
+        ? workgroups + heads * ((M > kWaveQueries ? rows * query_tiles(M) : 0) + (groups > 0 ? rows * M / 64 + groups : 0)) : 0;
+    s.slots[kByWave] = workgroups * kAttendWaves + heads * ((M > kWaveQueries ? 0 : rows) + groups);
+    const int64_t places = s.slots[0] * s.slot[0] + s.slots[1] * s.slot[1];
+    if (s.slots[0] + s.slots[1] > (int64_t)1 << 30 || places > ((int64_t)1 << 31) - 1) return false;
+    s.at_items = 0;
+    s.at_ml = up(heads * (rows * query_tiles(M) + (groups > 0 ? rows * M / 64 + groups : 0)) * (int64_t)sizeof(Parts), 256);
+    s.at_o = up(s.at_ml + places * 8, 256);
+    s.bytes = up(s.at_o + places * D * 4, 256);
     return true;
 }
 
@@ -118,8 +136,10 @@ __device__ __forceinline__ int64_t uniform(int64_t v)
 struct Unit {
     int len, row0;                              // tokens; the first row that sees them
     int64_t queries;                            // per key head
-    int items, steps;                           // (tile, key head) pairs, and a wave's steps in each; 0: nothing to do
+    int items, steps;                           // (tile, key head) pairs, and a wave's steps in each with kItemCost; 0: nothing to do
+    int line;
 };
+__device__ __forceinline__ int round_tokens(int64_t queries) { return queries <= kWaveQueries ? kStep : kStep * kAttendWaves / query_waves(queries); }
 __device__ __forceinline__ Unit unit_at(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, int u)
 {
     Unit x;
@@ -133,64 +153,74 @@ __device__ __forceinline__ Unit unit_at(const AttentionArgs& a, const AttendShap
         x.len = clamp_len(a.row_lens[x.row0], table_tokens(a.row_width, page_size));
         x.queries = s.M;
     }
-    const int apart = kStep * kAttendWaves / query_waves(x.queries);           // tokens of a round of the waves that share the steps
+    const int apart = round_tokens(x.queries);
+    x.line = x.queries <= kWaveQueries ? kByWave : kByGroup;
     x.items = x.len > 0 ? (int)(query_tiles(x.queries) * heads) : 0;
-    x.steps = x.len > 0 ? (int)(((int64_t)x.len + apart - 1) / apart) : 0;
+    x.steps = x.len > 0 ? (int)(((int64_t)x.len + apart - 1) / apart) + kItemCost : 0;
     return x;
 }
-
-// exclusive sums of two counts over the workgroup's threads, and the totals
-__device__ __forceinline__ void workgroup_scan(int64_t& v, int64_t& w, int64_t* lds, int64_t* total_v, int64_t* total_w)
+__device__ __forceinline__ Unit uniform(const Unit& x)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t x = v, y = w;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t xs = __shfl_up(x, d), ys = __shfl_up(y, d);
-        if (lane >= d) { x += xs; y += ys; }
-    }
-    if (lane == 63) { lds[2 * wave] = x; lds[2 * wave + 1] = y; }
-    __syncthreads();
-    int64_t before_x = 0, before_y = 0, all_x = 0, all_y = 0;
-#pragma unroll
-    for (int i = 0; i < kAttendWaves; ++i) {
-        if (i < wave) { before_x += lds[2 * i]; before_y += lds[2 * i + 1]; }
-        all_x += lds[2 * i];
-        all_y += lds[2 * i + 1];
-    }
-    *total_v = all_x;
-    *total_w = all_y;
-    v = before_x + x - v;
-    w = before_y + y - w;
+    return Unit{uniform(x.len), uniform(x.row0), uniform(x.queries), uniform(x.items), uniform(x.steps), uniform(x.line)};
 }
 
-// Every thread sums up a share of successive units; `first` gets each share's first step.
+// Every thread sums up a share of successive units; `first` gets each share's first step and item on either line.
 struct Plan {
-    int share, prefix_items, parts;             // units of a share; items of all prefixes; stretches
-    int64_t steps;
+    int share;                                  // units of a share
+    int64_t steps[2];
+    int parts[2];                               // stretches
 };
-__device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, int64_t* lds,
-                                          int64_t* first, int* first_item)
+struct PlanLds {
+    int64_t first[2][kPlanThreads];
+    int first_item[2][kPlanThreads];
+    int64_t sums[kAttendWaves][3];
+};
+__device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, PlanLds& lds)
 {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Plan p;
     p.share = (s.units + kPlanThreads - 1) / kPlanThreads;
     const int u0 = (int)threadIdx.x * p.share;
     const int u1 = u0 + p.share < s.units ? u0 + p.share : s.units;
-    int64_t steps = 0, items = 0, total, prefix = 0;                           // items: of prefixes in the upper half
+    int64_t own[3] = {0, 0, 0};                                                // steps of both lines; items, those of waves in the upper half
     for (int u = u0; u < u1; ++u) {
         const Unit x = unit_at(a, s, heads, page_size, u);
-        steps += (int64_t)x.items * x.steps;
-        items += x.items;
-        if (u < a.groups) prefix += x.items;
+        const int64_t steps = (int64_t)x.items * x.steps;
+        own[0] += x.line == kByGroup ? steps : 0;
+        own[1] += x.line == kByWave ? steps : 0;
+        own[2] += x.line == kByWave ? (int64_t)x.items << 32 : x.items;
     }
-    items |= prefix << 32;
-    workgroup_scan(steps, items, lds, &total, &prefix);
-    first[threadIdx.x] = steps;
-    first_item[threadIdx.x] = (int)(uint32_t)items;
-    total = uniform(total);
-    p.steps = total;
-    p.prefix_items = uniform((int)(prefix >> 32));
-    p.parts = total < (int64_t)gridDim.x ? (int)total : (int)gridDim.x;
+    int64_t sum[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        sum[k] = own[k];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t y = __shfl_up(sum[k], d);
+            if (lane >= d) sum[k] += y;
+        }
+        if (lane == 63) lds.sums[wave][k] = sum[k];
+        sum[k] -= own[k];
+    }
+    __syncthreads();
+    int64_t all[3] = {0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kAttendWaves; ++i)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            if (i < wave) sum[k] += lds.sums[i][k];
+            all[k] += lds.sums[i][k];
+        }
+    lds.first[0][threadIdx.x] = sum[0];
+    lds.first[1][threadIdx.x] = sum[1];
+    lds.first_item[0][threadIdx.x] = (int)(uint32_t)sum[2];
+    lds.first_item[1][threadIdx.x] = (int)(sum[2] >> 32);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int64_t most = (int64_t)gridDim.x * (k == kByWave ? kAttendWaves : 1);
+        p.steps[k] = uniform(all[k]);
+        p.parts[k] = (int)(p.steps[k] < most ? p.steps[k] : most);
+    }
     __syncthreads();
     return p;
 }
@@ -198,36 +228,33 @@ __device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendSh
 __device__ __forceinline__ int64_t begin_of(int w, int64_t steps, int parts) { return w * steps / parts; }
 __device__ __forceinline__ int part_of(int64_t step, int64_t steps, int parts) { return (int)(((step + 1) * parts + steps - 1) / steps) - 1; }
 
-// The unit that holds a step, with the unit's first step and item; uniform.
+// The unit that holds a step of a line, with the unit's first step and item; uniform.
 struct Place {
     int unit, item;
     int64_t step;
     Unit of;
 };
-__device__ __forceinline__ Unit uniform(const Unit& x)
-{
-    return Unit{uniform(x.len), uniform(x.row0), uniform(x.queries), uniform(x.items), uniform(x.steps)};
-}
 __device__ __forceinline__ Place place_of(const AttentionArgs& a, const AttendShape& s, int heads, int page_size, const Plan& p,
-                                          const int64_t* first, const int* first_item, int64_t step)
+                                          const PlanLds& lds, int line, int64_t step)
 {
     const int lane = threadIdx.x & 63;
     // the last share that begins at or before the step
     int below = 0;
 #pragma unroll
-    for (int k = 0; k < kPlanThreads / 64; ++k) below += (int)__popcll(__ballot(first[k * 64 + lane] <= step));
+    for (int k = 0; k < kPlanThreads / 64; ++k) below += (int)__popcll(__ballot(lds.first[line][k * 64 + lane] <= step));
     const int share = uniform(below) - 1;
     Place r{};
     r.unit = -1;
-    r.step = uniform(first[share]);
-    r.item = uniform(first_item[share]);
+    r.step = uniform(lds.first[line][share]);
+    r.item = uniform(lds.first_item[line][share]);
     for (int u0 = share * p.share; u0 < s.units && u0 < (share + 1) * p.share; u0 += 64) {
         const int u = u0 + lane;
         Unit x{};
         if (u < s.units && u < (share + 1) * p.share) x = unit_at(a, s, heads, page_size, u);
-        const int64_t mine = (int64_t)x.items * x.steps;
-        int64_t sum = mine;
-        int items = x.items;
+        int items = x.line == line ? x.items : 0;
+        const int own_items = items;
+        const int64_t own = (int64_t)items * x.steps;
+        int64_t sum = own;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int64_t y = __shfl_up(sum, d);
@@ -236,16 +263,14 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a, const AttendSh
         }
         const unsigned long long behind = __ballot(r.step + sum > step);
         const int l = behind != 0ull ? (int)__builtin_ctzll(behind) : 63;
-        const int64_t upto = uniform(__shfl(sum, l)), own = uniform(__shfl(mine, l));
-        const int items_upto = __builtin_amdgcn_readlane(items, l), own_items = __builtin_amdgcn_readlane(x.items, l);
+        r.step += uniform(__shfl(sum, l));
+        r.item += __builtin_amdgcn_readlane(items, l);
         if (behind != 0ull) {
             r.unit = u0 + l;
-            r.step += upto - own;
-            r.item += items_upto - own_items;
+            r.step -= uniform(__shfl(own, l));
+            r.item -= __builtin_amdgcn_readlane(own_items, l);
             break;
         }
-        r.step += upto;
-        r.item += items_upto;
     }
     if (r.unit >= 0) r.of = uniform(unit_at(a, s, heads, page_size, r.unit));
     return r;
@@ -301,6 +326,34 @@ struct StepData {
 #pragma unroll
         for (int i = 0; i < kVLoads; ++i) v[i] = (*reinterpret_cast<const u32x4*>(vp + i * 256));
         if (kFp8) vs = *reinterpret_cast<const u32x2*>(c.v_scale + row + g * 8);
+    }
+    // A step in LDS: every lane's registers as they are, 64 lanes next to each other.
+    static constexpr int kImage = (2 * kLoads + kVLoads) * 64 * 16 + (kFp8 ? 2 * 64 * 8 : 0);         // bytes
+    __device__ __forceinline__ void put(char* to, int lane) const
+    {
+        u32x4* w = reinterpret_cast<u32x4*>(to) + lane;
+#pragma unroll
+        for (int i = 0; i < 2 * kLoads; ++i) w[i * 64] = k[i / kLoads][i % kLoads];
+#pragma unroll
+        for (int i = 0; i < kVLoads; ++i) w[(2 * kLoads + i) * 64] = v[i];
+        if (kFp8) {
+            u32x2* e = reinterpret_cast<u32x2*>(to + (2 * kLoads + kVLoads) * 1024) + lane;
+            e[0] = ks;
+            e[64] = vs;
+        }
+    }
+    __device__ __forceinline__ void take(const char* from, int lane)
+    {
+        const u32x4* w = reinterpret_cast<const u32x4*>(from) + lane;
+#pragma unroll
+        for (int i = 0; i < 2 * kLoads; ++i) k[i / kLoads][i % kLoads] = w[i * 64];
+#pragma unroll
+        for (int i = 0; i < kVLoads; ++i) v[i] = w[(2 * kLoads + i) * 64];
+        if (kFp8) {
+            const u32x2* e = reinterpret_cast<const u32x2*>(from + (2 * kLoads + kVLoads) * 1024) + lane;
+            ks = e[0];
+            vs = e[64];
+        }
     }
     // K of score tile t, columns of k-step s
     __device__ __forceinline__ bf16x8 key(int t, int s) const
@@ -383,8 +436,9 @@ struct Attend {
     int limit;                                  // tokens the lane's query sees (of the prefix, of the row)
 
     // One step.  `at`: its first token; every query sees at least `sure` tokens, none more than `most`.  The keys' registers
-    // are given to the next step (`next`: where it lies) as soon as the scores are there, the values' at the end.
-    __device__ __forceinline__ void step(Data& d, const CacheView& cache, int64_t next, int at, int sure, int most, float c, int lane)
+    // are free for the next step's (next_keys) as soon as the scores are there, the values' (next_values) at the end.
+    template <typename Keys, typename Values>
+    __device__ __forceinline__ void step(Data& d, int at, int sure, int most, float c, int lane, Keys next_keys, Values next_values)
     {
         const int g = lane >> 4;
         const bool tail = at + kStep > sure;                              // uniform
@@ -401,7 +455,7 @@ struct Attend {
             x[j] = s[j >> 2][j & 3] * (kFp8 ? c * d.k_factor(j) : c);
             if (tail) x[j] = at + 8 * g + j < see ? x[j] : -INFINITY;
         }
-        d.load_keys(cache, next, lane);
+        next_keys();
         float top = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
         if (__any(top > m + kSlack)) {
             // the queries' maxima over the four lanes that hold their scores
@@ -443,188 +497,245 @@ struct Attend {
             const bf16x8 value = d.value(b);
             o[b] = mfma(value, rest, mfma(value, p, o[b]));
         }
-        d.load_values(cache, next, lane);
+        next_values();
     }
 
-    // A task.  lds: (m, l) of all waves, then O of two waves.
-    __device__ __forceinline__ void run(const CacheView& c, const AttentionArgs& a, const AttendShape& sh, const Task& task,
-                                        float* lds, float2* ml_out, float* o_out)
+    // The queries of a wave: column n is query first + n of the unit.
+    __device__ __forceinline__ void begin(const AttentionArgs& a, const AttendShape& sh, const Task& task, int first, int lane)
+    {
+        const int col = lane & 15, g = lane >> 4;
+        const int qi = first + col;
+        const bool is = qi < task.of.queries;
+        const int row = task.of.row0 + (is ? qi / sh.M : 0), in_row = is ? qi % sh.M : 0;
+        const int t = in_row / sh.R, h = task.head * sh.R + in_row % sh.R;
+        const uint16_t* qp = a.q + row * a.q_row_stride + t * a.q_token_stride + h * a.q_head_stride;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            u32x4 w = *reinterpret_cast<const u32x4*>(qp + Data::key_column(s, g));
+            if (!is) w = u32x4{0, 0, 0, 0};
+            q[s] = __builtin_bit_cast(bf16x8, w);
+        }
+        const int own = task.of.len - (a.T - 1 - t);
+        limit = task.unit < a.groups ? task.of.len : own > 0 ? own : 0;
+        m = kNoScore;
+        l = 0.0f;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // The partial result: l is spread over the four lanes of a query until here.
+    __device__ __forceinline__ void leave(int queries, float2* ml_out, float* o_out, int lane)
+    {
+        const int col = lane & 15, g = lane >> 4;
+        if (col >= queries) return;
+        if (g == 0) ml_out[col] = float2{m, l};
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o_out[(int64_t)col * D + Data::column(b, 4 * g + k)] = o[b][k];
+    }
+    // every query of the unit sees so many of its tokens
+    static __device__ __forceinline__ int seen_by_all(const AttentionArgs& a, const Task& task)
+    {
+        const int n = task.of.len - (a.T - 1);
+        return task.unit < a.groups ? task.of.len : n > 0 ? n : 0;
+    }
+    static __device__ __forceinline__ const int32_t* pages_of(const AttentionArgs& a, const Task& task)
+    {
+        return task.unit < a.groups ? a.prefix_pages + (int64_t)task.unit * a.prefix_width
+                                    : a.row_pages + (int64_t)task.of.row0 * a.row_width;
+    }
+    // Where the step at token `at` lies.  A page that the cache does not have is not seen; page 0 is read in its place.
+    static __device__ __forceinline__ int64_t row_of(const CacheView& c, const Task& task, int page, int at)
+    {
+        const int64_t p = (uint32_t)page < (uint64_t)c.num_pages ? page : 0;
+        return (p * c.heads + task.head) * c.page_size + (at & (c.page_size - 1));
+    }
+
+    // A wave's task: all of the unit's queries, steps one after the other.
+    __device__ __forceinline__ void direct(const CacheView& c, const AttentionArgs& a, const AttendShape& sh, const Task& task,
+                                           float2* ml_out, float* o_out)
+    {
+        const int lane = threadIdx.x & 63;
+        const int to = task.to, len = task.of.len, sure = seen_by_all(a, task);
+        const int32_t* pages = pages_of(a, task);
+        auto page_at = [&](int at) { return at < to ? pages[at >> c.page_shift] : -1; };
+        int at = task.from;
+        Data d;
+        int page = page_at(at), page_next = page_at(at + kStep);
+        d.load_keys(c, row_of(c, task, page, at), lane);
+        d.load_values(c, row_of(c, task, page, at), lane);
+        begin(a, sh, task, 0, lane);
+        const float scale = a.scale * kLog2eF;
+        for (; at < to; at += kStep) {
+            const int page_after = page_at(at + 2 * kStep);
+            const int64_t next = row_of(c, task, page_next, at + kStep);       // behind the last step: read for nothing
+            const bool there = (uint32_t)page < (uint64_t)c.num_pages;
+            step(d, at, there ? sure : -1, there ? len : -1, scale, lane, [&] { d.load_keys(c, next, lane); },
+                 [&] { d.load_values(c, next, lane); });
+            page = page_next;
+            page_next = page_after;
+        }
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        leave((int)task.of.queries, ml_out, o_out, lane);
+    }
+
+    // A workgroup's task: a tile of 16 queries per wave, or per two waves, which then take steps in turn.  Each wave brings one
+    // step of four into LDS, in registers while the last four are worked on.
+    // lds: four steps and whether their pages exist; then (m, l) of all waves and O of two.
+    static constexpr int kLds = (kAttendWaves * Data::kImage + 16) > (kAttendWaves * 16 * 8 + 2 * kBlocks * 64 * 16)
+                                    ? (kAttendWaves * Data::kImage + 16) : (kAttendWaves * 16 * 8 + 2 * kBlocks * 64 * 16);
+    __device__ __forceinline__ void shared(const CacheView& c, const AttentionArgs& a, const AttendShape& sh, const Task& task,
+                                           char* lds, float2* ml_out, float* o_out)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int col = lane & 15, g = lane >> 4;
-        const bool prefix = task.unit < a.groups;
-        const int queries = (int)task.of.queries, len = task.of.len;
-        const int qw = query_waves(queries), qs = qw == 1 ? 0 : qw == 2 ? 1 : 2;
+        const int qw = task.of.queries <= 32 ? 2 : 4, qs = qw == 2 ? 1 : 2;
         const int tile = wave & (qw - 1), share = wave >> qs, shares = kAttendWaves >> qs;
-        const int sure = prefix ? len : len - (a.T - 1) > 0 ? len - (a.T - 1) : 0;
-        const int32_t* pages = prefix ? a.prefix_pages + (int64_t)task.unit * a.prefix_width
-                                      : a.row_pages + (int64_t)task.of.row0 * a.row_width;
-        // queries: column n is query first + n
-        const int first = (task.tile * qw + tile) * 16;
-        {
-            const int qi = first + col;
-            const bool is = qi < queries;
-            const int row = task.of.row0 + (is ? qi / sh.M : 0), in_row = is ? qi % sh.M : 0;
-            const int t = in_row / sh.R, h = task.head * sh.R + in_row % sh.R;
-            const uint16_t* qp = a.q + row * a.q_row_stride + t * a.q_token_stride + h * a.q_head_stride;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                u32x4 w = *reinterpret_cast<const u32x4*>(qp + Data::key_column(s, g));
-                if (!is) w = u32x4{0, 0, 0, 0};
-                q[s] = __builtin_bit_cast(bf16x8, w);
-            }
-            const int own = len - (a.T - 1 - t);
-            limit = prefix ? len : own > 0 ? own : 0;
-            m = kNoScore;
-            l = 0.0f;
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-        const float scale = a.scale * kLog2eF;
-
-        // tokens [from, to) of the run.  A page that the cache does not have is not seen.
-        const int to = task.to, apart = shares * kStep;
+        const int first = (task.tile * qw + tile) * 16, queries = (int)task.of.queries;
+        const int to = task.to, len = task.of.len, sure = seen_by_all(a, task);
+        const int32_t* pages = pages_of(a, task);
         auto page_at = [&](int at) { return at < to ? pages[at >> c.page_shift] : -1; };
-        auto row_of = [&](int page, int at) {
-            const int64_t p = (uint32_t)page < (uint64_t)c.num_pages ? page : 0;
-            return (p * c.heads + task.head) * c.page_size + (at & (c.page_size - 1));
-        };
-        int at = task.from + share * kStep;
-        if (at < to && first < queries) {
-            Data d;
-            int page = page_at(at), page_next = page_at(at + apart);
-            d.load_keys(c, row_of(page, at), lane);
-            d.load_values(c, row_of(page, at), lane);
-            for (; at < to; at += apart) {
-                const int page_after = page_at(at + 2 * apart);
-                // behind the last step: a page of the cache again, for nothing
-                const int64_t next = row_of(page_next, at + apart);
-                // (a page that the cache does not have: no token of the step is seen)
-                const bool there = (uint32_t)page < (uint64_t)c.num_pages;
-                step(d, c, next, at, there ? sure : -1, there ? len : -1, scale, lane);
-                page = page_next;
-                page_next = page_after;
+        int* there = reinterpret_cast<int*>(lds + kAttendWaves * Data::kImage);
+        constexpr int kFour = kAttendWaves * kStep;
+        auto nothing = [] {};
+        Data mine;
+        int own = task.from + wave * kStep;
+        int page = page_at(own), page_next = page_at(own + kFour);
+        mine.load_keys(c, row_of(c, task, page, own), lane);
+        mine.load_values(c, row_of(c, task, page, own), lane);
+        begin(a, sh, task, first, lane);
+        const float scale = a.scale * kLog2eF;
+        for (int at = task.from; at < to; at += kFour, own += kFour) {
+            __syncthreads();                                               // the last four (or the last task) are done with
+            mine.put(lds + wave * Data::kImage, lane);
+            if (lane == 0) there[wave] = (uint32_t)page < (uint64_t)c.num_pages;
+            __syncthreads();
+            page = page_next;
+            page_next = page_at(own + 2 * kFour);
+            mine.load_keys(c, row_of(c, task, page, own + kFour), lane);
+            mine.load_values(c, row_of(c, task, page, own + kFour), lane);
+            if (first < queries) {
+                for (int i = share; i < kAttendWaves && at + i * kStep < to; i += shares) {
+                    Data d;
+                    d.take(lds + i * Data::kImage, lane);
+                    const bool is = uniform(there[i]) != 0;
+                    step(d, at + i * kStep, is ? sure : -1, is ? len : -1, scale, lane, nothing, nothing);
+                }
             }
         }
-
-        // Join the waves that have the same queries.  l is spread over the four lanes of a query.
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
-        float2* ml = reinterpret_cast<float2*>(lds);
-        f32x4* part = reinterpret_cast<f32x4*>(lds + 2 * kAttendWaves * 16);               // [2][kBlocks][64]
-        float all_m = m, all_l = l;
-        auto give = [&](int slot) {
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) part[(slot * kBlocks + b) * 64 + lane] = o[b];
-        };
-        auto take = [&](int slot) {
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] += part[(slot * kBlocks + b) * 64 + lane];
-        };
-        if (shares > 1) {                                                  // uniform over the workgroup
-            __syncthreads();                                               // the last task's results are read
+        if (shares > 1) {                                                  // two waves with the same queries
+            float2* ml = reinterpret_cast<float2*>(lds);
+            f32x4* part = reinterpret_cast<f32x4*>(lds + kAttendWaves * 16 * 8);           // [2][kBlocks][64]
+            __syncthreads();
             if (g == 0) ml[wave * 16 + col] = float2{m, l};
             __syncthreads();
-            all_m = kNoScore;
-            for (int k = 0; k < shares; ++k) all_m = fmaxf(all_m, ml[(tile + k * qw) * 16 + col].x);
-            all_l = 0.0f;
-            for (int k = 0; k < shares; ++k) {
-                const float2 w = ml[(tile + k * qw) * 16 + col];
-                all_l = fmaf(w.y, __builtin_amdgcn_exp2f(w.x - all_m), all_l);
-            }
-            const float f = __builtin_amdgcn_exp2f(m - all_m);
+            const float2 other = ml[(wave ^ qw) * 16 + col];
+            const float all = fmaxf(m, other.x);
+            const float f = __builtin_amdgcn_exp2f(m - all);
+            l = l * f + other.y * __builtin_amdgcn_exp2f(other.x - all);
+            m = all;
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] *= f;
-            if (wave >= 2) give(wave - 2);
+            for (int b = 0; b < kBlocks; ++b) {
+                o[b] *= f;
+                if (share == 1) part[(tile * kBlocks + b) * 64 + lane] = o[b];
+            }
             __syncthreads();
-            if (wave < 2) take(wave);
-            if (shares == 4) {
-                __syncthreads();
-                if (wave == 1) give(0);
-                __syncthreads();
-                if (wave == 0) take(0);
+            if (share == 0) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) o[b] += part[(tile * kBlocks + b) * 64 + lane];
             }
         }
-        if (share == 0 && first + col < queries) {
-            const int slot = tile * 16 + col;
-            if (g == 0) ml_out[slot] = float2{all_m, all_l};
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o_out[(int64_t)slot * D + Data::column(b, 4 * g + k)] = o[b][k];
-        }
+        if (share == 0) leave(queries - first, ml_out + tile * 16, o_out + (int64_t)tile * 16 * D, lane);
     }
 };
 
-template <int D, bool kFp8>
-__global__ __launch_bounds__(64 * kAttendWaves, attend_occupancy(D, kFp8))
-void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
+// The stretch of worker `part` on a line: f(task, place of its result).
+template <int kLine, typename F>
+__device__ __forceinline__ void along_line(const AttentionArgs& a, const AttendShape& s, const CacheView& c, const Plan& plan, const PlanLds& lds,
+                                           Parts* items, int part, F f)
 {
-    __shared__ __align__(16) float lds[2 * kAttendWaves * 16 + 2 * (D / 16) * 64 * 4];
-    __shared__ int64_t sums[2 * kAttendWaves];
-    __shared__ int64_t firsts[kPlanThreads];
-    __shared__ int first_items[kPlanThreads];
-    const Plan plan = make_plan(a, s, c.heads, c.page_size, sums, firsts, first_items);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<PlanHead*>(ws) = PlanHead{plan.steps, plan.parts, plan.prefix_items};
-    const int part = blockIdx.x;
-    if (part >= plan.parts) return;
-    int2* unit_first = reinterpret_cast<int2*>(ws + s.at_first);
-    float2* ml = reinterpret_cast<float2*>(ws + s.at_ml);
-    float* o = reinterpret_cast<float*>(ws + s.at_o);
-    int64_t at = begin_of(part, plan.steps, plan.parts);
-    const int64_t end = begin_of(part + 1, plan.steps, plan.parts);
-    Place u = place_of(a, s, c.heads, c.page_size, plan, firsts, first_items, at);
+    if (part >= plan.parts[kLine]) return;
+    const int lane = threadIdx.x & 63;
+    int64_t at = begin_of(part, plan.steps[kLine], plan.parts[kLine]);
+    const int64_t end = begin_of(part + 1, plan.steps[kLine], plan.parts[kLine]);
+    Place u = place_of(a, s, c.heads, c.page_size, plan, lds, kLine, at);
     while (at < end && u.unit >= 0) {
         const int off = (int)(at - u.step);                                    // in the unit
         const int item = off / u.of.steps, from = off % u.of.steps;
         const int n = end - at < u.of.steps - from ? (int)(end - at) : u.of.steps - from;
-        const int apart = kStep * kAttendWaves / query_waves(u.of.queries);
+        const int apart = round_tokens(u.of.queries);
+        const int real_from = from > kItemCost ? from - kItemCost : 0, real_to = from + n - kItemCost;
         Task task;
         task.unit = u.unit;
         task.head = item % c.heads;
         task.tile = item / c.heads;
-        task.from = from * apart;
-        task.to = u.of.len - task.from < n * apart ? u.of.len : task.from + n * apart;
+        task.from = real_from * apart;
+        task.to = u.of.len < (int64_t)real_to * apart ? u.of.len : real_to * apart;
         task.of = u.of;
-        if (off == 0 && threadIdx.x == 0) unit_first[u.unit] = int2{(int)u.step, u.item};
-        const bool prefix = u.unit < a.groups;
-        const int64_t place = part + u.item + item - (prefix ? 0 : plan.prefix_items);
-        // (groups that overlap, against the contract, could exceed the places)
-        if (place < (prefix ? s.prefix_slots : s.row_slots)) {
-            const int64_t slot = prefix ? s.row_slots * s.row_slot + place * s.prefix_slot : place * s.row_slot;
-            Attend<D, kFp8> x;
-            x.run(c, a, s, task, lds, ml + slot, o + slot * D);
+        const int64_t place = (int64_t)part + u.item + item;
+        if (real_to > 0) {
+            // (groups that overlap, against the contract, could exceed the places)
+            if (from <= kItemCost && lane == 0) {                              // the item's first part
+                const int last = part_of(at - from + u.of.steps - 1, plan.steps[kLine], plan.parts[kLine]);
+                const int64_t i = first_item(s, a.rows, c.heads, u.unit < a.groups, u.unit, u.of.row0) + item;
+                items[i] = Parts{(int)place, place + (last - part) < s.slots[kLine] ? last - part + 1 : 0};
+            }
+            if (place < s.slots[kLine]) f(task, place);
         }
         at += n;
         if (at < end && item + 1 == u.of.items && from + n == u.of.steps) {
             const int next = u.unit + 1;
             Unit x{};
             if (next < s.units) x = uniform(unit_at(a, s, c.heads, c.page_size, next));
-            if (x.items > 0) {
+            if (x.items > 0 && x.line == kLine) {
                 u.step = at;
                 u.item += u.of.items;
                 u.unit = next;
                 u.of = x;
             } else {
-                u = place_of(a, s, c.heads, c.page_size, plan, firsts, first_items, at);
+                u = place_of(a, s, c.heads, c.page_size, plan, lds, kLine, at);
             }
         }
     }
 }
 
+template <int D, bool kFp8>
+__global__ __launch_bounds__(64 * kAttendWaves, attend_occupancy(D, kFp8))
+void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
+{
+    __shared__ __align__(16) char lds[Attend<D, kFp8>::kLds];
+    __shared__ PlanLds plan_lds;
+    const Plan plan = make_plan(a, s, c.heads, c.page_size, plan_lds);
+    Parts* items = reinterpret_cast<Parts*>(ws + s.at_items);
+    float2* ml = reinterpret_cast<float2*>(ws + s.at_ml);
+    float* o = reinterpret_cast<float*>(ws + s.at_o);
+    along_line<kByGroup>(a, s, c, plan, plan_lds, items, blockIdx.x, [&](const Task& task, int64_t place) {
+        const int64_t at = place * s.slot[kByGroup];
+        Attend<D, kFp8> x;
+        x.shared(c, a, s, task, lds, ml + at, o + at * D);
+    });
+    // a workgroup's waves lie far apart on their line: few stretches are spread over all workgroups
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    along_line<kByWave>(a, s, c, plan, plan_lds, items, wave * (int)gridDim.x + (int)blockIdx.x, [&](const Task& task, int64_t place) {
+        const int64_t at = s.slots[kByGroup] * s.slot[kByGroup] + place * s.slot[kByWave];
+        Attend<D, kFp8> x;
+        x.direct(c, a, s, task, ml + at, o + at * D);
+    });
+}
+
 // ---------------------------------------------------------------- join
-// A wave per (row, key head, query): the partial results of the prefix's runs, then those of the row's.
+// A workgroup per (row, key head), its waves take the queries in turn: the partial results of the prefix, then the row's own.
 template <int D>
 __global__ __launch_bounds__(256)
 void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size, const char* ws)
 {
     constexpr int kCols = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= (int64_t)a.rows * heads * s.M) return;
-    const int in_row = (int)(at % s.M), head = (int)(at / s.M % heads), row = (int)(at / s.M / heads);
-    const PlanHead plan = *reinterpret_cast<const PlanHead*>(ws);
-    const int2* unit_first = reinterpret_cast<const int2*>(ws + s.at_first);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = blockIdx.x % heads, row = blockIdx.x / heads;
+    const Parts* items = reinterpret_cast<const Parts*>(ws + s.at_items);
     const float2* ml = reinterpret_cast<const float2*>(ws + s.at_ml);
     const float* o = reinterpret_cast<const float*>(ws + s.at_o);
     // the row's group: the last one that begins at or before it
@@ -635,73 +746,76 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
         if (n < 64) break;
     }
 
-    float m = kNoScore, l = 0.0f, acc[kCols] = {};
-    // results at slots first + i * apart, i < n
-    auto join = [&](int64_t first, int64_t apart, int n) {
-        for (int i0 = 0; i0 < n; i0 += 64) {
-            const int many = n - i0 < 64 ? n - i0 : 64;
-            const float2 mine = lane < many ? ml[first + (i0 + lane) * apart] : float2{kNoScore, 0.0f};
-            const float top = wave_max(mine.x);
-            const float to = fmaxf(m, top);
-            const float f = __builtin_amdgcn_exp2f(m - to);
-            m = to;
-            l *= f;
+    const int64_t prefix_places = s.slots[kByGroup] * s.slot[kByGroup];       // results of the line of workgroups come first
+    const Unit of_row = unit_at(a, s, heads, page_size, a.groups + row);
+    Unit of_prefix{};
+    if (group >= 0) of_prefix = unit_at(a, s, heads, page_size, group);
+    const int64_t row_items = first_item(s, a.rows, heads, false, 0, row) + head;
+    const int64_t prefix_items = first_item(s, a.rows, heads, true, group, of_prefix.row0) + head;
+    const int prefix_query = (row - of_prefix.row0) * s.M;
+
+    for (int in_row = wave; in_row < s.M; in_row += 4) {
+        float m = kNoScore, l = 0.0f, acc[kCols] = {};
+        // results at slots first + i * apart, i < n
+        auto join = [&](int64_t first, int64_t apart, int n) {
+            for (int i0 = 0; i0 < n; i0 += 64) {
+                const int many = n - i0 < 64 ? n - i0 : 64;
+                const float2 mine = lane < many ? ml[first + (i0 + lane) * apart] : float2{kNoScore, 0.0f};
+                const float top = wave_max(mine.x);
+                const float to = fmaxf(m, top);
+                const float f = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= f;
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) acc[j] *= f;
-            const float w = lane < many ? __builtin_amdgcn_exp2f(mine.x - to) : 0.0f;
-            l += (float)wave_sum((double)(mine.y * w));
-            // eight results in flight; past the last one its place is read again with no weight
-            for (int i = 0; i < many; i += 8) {
-                float p[8][kCols];
+                for (int j = 0; j < kCols; ++j) acc[j] *= f;
+                const float w = lane < many ? __builtin_amdgcn_exp2f(mine.x - to) : 0.0f;
+                l += (float)wave_sum((double)(mine.y * w));
+                // eight results in flight; past the last one its place is read again with no weight
+                for (int i = 0; i < many; i += 8) {
+                    float p[8][kCols];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int at_i = i + k < many ? i + k : many - 1;
-                    const float* from = o + (first + (i0 + at_i) * apart) * D + lane * kCols;
+                    for (int k = 0; k < 8; ++k) {
+                        const int at_i = i + k < many ? i + k : many - 1;
+                        const float* from = o + (first + (i0 + at_i) * apart) * D + lane * kCols;
 #pragma unroll
-                    for (int j = 0; j < kCols; ++j) p[k][j] = from[j];
-                }
+                        for (int j = 0; j < kCols; ++j) p[k][j] = from[j];
+                    }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float wk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i + k < 64 ? i + k : 63));
-                    if (i + k < many) {
+                    for (int k = 0; k < 8; ++k) {
+                        const float wk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i + k < 64 ? i + k : 63));
+                        if (i + k < many) {
 #pragma unroll
-                        for (int j = 0; j < kCols; ++j) acc[j] = fmaf(wk, p[k][j], acc[j]);
+                            for (int j = 0; j < kCols; ++j) acc[j] = fmaf(wk, p[k][j], acc[j]);
+                        }
                     }
                 }
             }
-        }
-    };
-    // the parts of the unit's item that holds query qi
-    auto join_unit = [&](int u, int64_t qi, int64_t region, int64_t places, int per_place, int items_before) {
-        const Unit x = unit_at(a, s, heads, page_size, u);
-        if (x.items == 0 || qi >= x.queries) return;
-        const int per = 16 * query_waves(x.queries);
-        const int item = (int)(qi / per) * heads + head;
-        const int2 at_unit = unit_first[u];
-        const int64_t from = at_unit.x + (int64_t)item * x.steps;
-        const int w0 = part_of(from, plan.steps, plan.parts), w1 = part_of(from + x.steps - 1, plan.steps, plan.parts);
-        const int64_t place = (int64_t)at_unit.y - items_before + item + w0;
-        if (place < 0 || w1 < w0 || place + (w1 - w0) >= places) return;        // (see attend_kernel)
-        join(region + place * per_place + qi % per, per_place, w1 - w0 + 1);
-    };
-    if (group >= 0) {
-        const int64_t qi = (int64_t)(row - clamp_len(a.group_offsets[group], a.rows)) * s.M + in_row;
-        join_unit(group, qi, s.row_slots * s.row_slot, s.prefix_slots, s.prefix_slot, 0);
-    }
-    join_unit(a.groups + row, in_row, 0, s.row_slots, s.row_slot, plan.prefix_items);
-    const int t = in_row / s.R, h = head * s.R + in_row % s.R;
-    const int64_t where = ((int64_t)row * a.T + t) * a.q_heads + h;
-    const bool none = l == 0.0f && m == kNoScore;                          // no key at all
-    const float inv = none ? 0.0f : 1.0f / l;
-    uint32_t packed = 0;
+        };
+        // the unit's query qi, and the unit's items for this key head
+        auto join_unit = [&](const Unit& x, int64_t list, int qi) {
+            if (x.items == 0 || qi >= x.queries) return;
+            const int per = 16 * query_waves(x.queries);
+            const Parts parts = items[list + (int64_t)(qi / per) * heads];
+            const int apart = x.line == kByWave ? s.slot[kByWave] : s.slot[kByGroup];
+            join((x.line == kByWave ? prefix_places : 0) + (int64_t)parts.first * apart + qi % per, apart, parts.count);
+        };
+        join_unit(of_prefix, prefix_items, prefix_query + in_row);
+        join_unit(of_row, row_items, in_row);
+
+        const int t = in_row / s.R, h = head * s.R + in_row % s.R;
+        const int64_t where = ((int64_t)row * a.T + t) * a.q_heads + h;
+        const bool none = l == 0.0f && m == kNoScore;                      // no key at all
+        const float inv = none ? 0.0f : 1.0f / l;
+        uint32_t packed = 0;
 #pragma unroll
-    for (int j = 0; j < kCols; ++j) {
-        const __bf16 b = (__bf16)(none ? 0.0f : acc[j] * inv);
-        packed |= (uint32_t)__builtin_bit_cast(uint16_t, b) << (16 * j);
+        for (int j = 0; j < kCols; ++j) {
+            const __bf16 b = (__bf16)(none ? 0.0f : acc[j] * inv);
+            packed |= (uint32_t)__builtin_bit_cast(uint16_t, b) << (16 * j);
+        }
+        if (kCols == 2) reinterpret_cast<uint32_t*>(a.out + where * D)[lane] = packed;
+        else a.out[where * D + lane] = (uint16_t)packed;
+        if (a.lse && lane == 0) a.lse[where] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (float)kLn2;
     }
-    if (kCols == 2) reinterpret_cast<uint32_t*>(a.out + where * D)[lane] = packed;
-    else a.out[where * D + lane] = (uint16_t)packed;
-    if (a.lse && lane == 0) a.lse[where] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (float)kLn2;
 }
 
 template <int D, bool kFp8>
@@ -709,8 +823,7 @@ static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, cons
 {
     const int workgroups = compute_units() * attend_occupancy(D, kFp8);
     attend_kernel<D, kFp8><<<workgroups, 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
-    const int64_t waves = (int64_t)a.rows * c.heads * s.M;
-    attend_join_kernel<D><<<(uint32_t)((waves + 3) / 4), 256, 0, stream>>>(a, s, c.heads, c.page_size, ws);
+    attend_join_kernel<D><<<(uint32_t)(a.rows * c.heads), 256, 0, stream>>>(a, s, c.heads, c.page_size, ws);
     return hipGetLastError();
 }
 
