@@ -727,95 +727,125 @@ void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
 }
 
 // ---------------------------------------------------------------- join
-// A workgroup per (row, key head), its waves take the queries in turn: the partial results of the prefix, then the row's own.
+// The partial results of a query's prefix and of its row's own tokens become its output.  What bounds it is the chain of loads
+// (lengths, list of items, results), so a wave takes several queries at once, D / 4 lanes each with four columns,
+// and asks for (m, l) and O of four parts together.
+constexpr int join_queries(int D) { return 4 * 256 / D; }          // of a workgroup
+
+struct Merged {
+    float m, l;
+    f32x4 o;
+};
+__device__ __forceinline__ void merge(Merged& x, float m, float l, const f32x4& o)
+{
+    const float up = fmaxf(x.m, m);
+    const float f = __builtin_amdgcn_exp2f(x.m - up), g = __builtin_amdgcn_exp2f(m - up);
+    x.m = up;
+    x.l = x.l * f + l * g;
+    x.o = x.o * f + o * g;
+}
+
+// (Eight waves per SIMD: 2048 workgroups, those of 512 rows and four key heads, are then resident together.)
 template <int D>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(256, 8)
 void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size, const char* ws)
 {
-    constexpr int kCols = D / 64;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int kLanes4 = D / 4;                                             // lanes of a query
+    __shared__ float lds[256 / kLanes4][2 + D];
+    const int lane = threadIdx.x & 63;
+    const int sub = threadIdx.x / kLanes4, col = (threadIdx.x % kLanes4) * 4;
     const int head = blockIdx.x % heads, row = blockIdx.x / heads;
     const Parts* items = reinterpret_cast<const Parts*>(ws + s.at_items);
     const float2* ml = reinterpret_cast<const float2*>(ws + s.at_ml);
     const float* o = reinterpret_cast<const float*>(ws + s.at_o);
-    // the row's group: the last one that begins at or before it
+    const int first_query = blockIdx.y * join_queries(D);
+    const int end_query = first_query + join_queries(D) < s.M ? first_query + join_queries(D) : s.M;
+
+    const Unit of_row = uniform(unit_at(a, s, heads, page_size, a.groups + row));
+    // the row's group, the last one that begins at or before it, and its lengths, looked at by all lanes at once
     int group = -1;
+    Unit of_prefix{};
     for (int g0 = 0; g0 < a.groups; g0 += 64) {
-        const int n = (int)__popcll(__ballot(g0 + lane < a.groups && a.group_offsets[g0 + lane < a.groups ? g0 + lane : 0] <= row));
-        group += n;
+        const int g = g0 + lane < a.groups ? g0 + lane : a.groups - 1;
+        const Unit x = unit_at(a, s, heads, page_size, g);
+        const unsigned long long begun = __ballot(g0 + lane < a.groups && a.group_offsets[g] <= row);
+        const int n = (int)__popcll(begun);
+        if (n > 0) {
+            group += n;
+            of_prefix.row0 = __builtin_amdgcn_readlane(x.row0, n - 1);
+            of_prefix.queries = __builtin_amdgcn_readlane((int)x.queries, n - 1);
+            of_prefix.items = __builtin_amdgcn_readlane(x.items, n - 1);
+            of_prefix.line = __builtin_amdgcn_readlane(x.line, n - 1);
+        }
         if (n < 64) break;
     }
-
-    const int64_t prefix_places = s.slots[kByGroup] * s.slot[kByGroup];       // results of the line of workgroups come first
-    const Unit of_row = unit_at(a, s, heads, page_size, a.groups + row);
-    Unit of_prefix{};
-    if (group >= 0) of_prefix = unit_at(a, s, heads, page_size, group);
-    const int64_t row_items = first_item(s, a.rows, heads, false, 0, row) + head;
-    const int64_t prefix_items = first_item(s, a.rows, heads, true, group, of_prefix.row0) + head;
     const int prefix_query = (row - of_prefix.row0) * s.M;
 
-    for (int in_row = wave; in_row < s.M; in_row += 4) {
-        float m = kNoScore, l = 0.0f, acc[kCols] = {};
-        // results at slots first + i * apart, i < n
-        auto join = [&](int64_t first, int64_t apart, int n) {
-            for (int i0 = 0; i0 < n; i0 += 64) {
-                const int many = n - i0 < 64 ? n - i0 : 64;
-                const float2 mine = lane < many ? ml[first + (i0 + lane) * apart] : float2{kNoScore, 0.0f};
-                const float top = wave_max(mine.x);
-                const float to = fmaxf(m, top);
-                const float f = __builtin_amdgcn_exp2f(m - to);
-                m = to;
-                l *= f;
-#pragma unroll
-                for (int j = 0; j < kCols; ++j) acc[j] *= f;
-                const float w = lane < many ? __builtin_amdgcn_exp2f(mine.x - to) : 0.0f;
-                l += (float)wave_sum((double)(mine.y * w));
-                // eight results in flight; past the last one its place is read again with no weight
-                for (int i = 0; i < many; i += 8) {
-                    float p[8][kCols];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int at_i = i + k < many ? i + k : many - 1;
-                        const float* from = o + (first + (i0 + at_i) * apart) * D + lane * kCols;
-#pragma unroll
-                        for (int j = 0; j < kCols; ++j) p[k][j] = from[j];
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float wk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i + k < 64 ? i + k : 63));
-                        if (i + k < many) {
-#pragma unroll
-                            for (int j = 0; j < kCols; ++j) acc[j] = fmaf(wk, p[k][j], acc[j]);
-                        }
-                    }
-                }
-            }
-        };
-        // the unit's query qi, and the unit's items for this key head
-        auto join_unit = [&](const Unit& x, int64_t list, int qi) {
-            if (x.items == 0 || qi >= x.queries) return;
+    // A query's parts: n1 of the prefix, then the row's.
+    struct Found {
+        int n1, n, first1, apart1, first2, apart2;
+        __device__ __forceinline__ int64_t place(int i) const { return i < n1 ? first1 + (int64_t)i * apart1 : first2 + (int64_t)(i - n1) * apart2; }
+    };
+    auto find = [&](int in_row) {
+        auto of = [&](const Unit& x, bool prefix, int qi, int* first, int* apart) {
+            *first = *apart = 0;
+            if (x.items == 0 || qi >= x.queries) return 0;
             const int per = 16 * query_waves(x.queries);
-            const Parts parts = items[list + (int64_t)(qi / per) * heads];
-            const int apart = x.line == kByWave ? s.slot[kByWave] : s.slot[kByGroup];
-            join((x.line == kByWave ? prefix_places : 0) + (int64_t)parts.first * apart + qi % per, apart, parts.count);
+            const Parts parts = items[first_item(s, a.rows, heads, prefix, group, x.row0) + (int64_t)(qi / per) * heads + head];
+            *apart = x.line == kByWave ? s.slot[kByWave] : s.slot[kByGroup];
+            // results of the line of workgroups come first
+            *first = (int)((x.line == kByWave ? s.slots[kByGroup] * s.slot[kByGroup] : 0) + (int64_t)parts.first * *apart + qi % per);
+            return parts.count;
         };
-        join_unit(of_prefix, prefix_items, prefix_query + in_row);
-        join_unit(of_row, row_items, in_row);
-
+        Found f;
+        const int n2 = of(of_row, false, in_row, &f.first2, &f.apart2);
+        f.n1 = of(of_prefix, true, prefix_query + in_row, &f.first1, &f.apart1);
+        f.n = f.n1 + n2;
+        return f;
+    };
+    // parts from, from + apart, ... of a query
+    auto join = [&](const Found& f, int from, int apart) {
+        Merged x{kNoScore, 0.0f, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+        for (int i = from; i < f.n; i += 4 * apart) {
+            float2 w[4];
+            f32x4 p[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t at = f.place(i + k * apart < f.n ? i + k * apart : i);
+                w[k] = ml[at];
+                p[k] = *reinterpret_cast<const f32x4*>(o + at * D + col);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k * apart < f.n) merge(x, w[k].x, w[k].y, p[k]);
+        }
+        return x;
+    };
+    auto write = [&](const Merged& x, int in_row) {
         const int t = in_row / s.R, h = head * s.R + in_row % s.R;
         const int64_t where = ((int64_t)row * a.T + t) * a.q_heads + h;
-        const bool none = l == 0.0f && m == kNoScore;                      // no key at all
-        const float inv = none ? 0.0f : 1.0f / l;
-        uint32_t packed = 0;
+        const bool none = x.l == 0.0f && x.m == kNoScore;                      // no key at all
+        const float inv = none ? 0.0f : 1.0f / x.l;
+        const bf16x2 lo = {(__bf16)(x.o[0] * inv), (__bf16)(x.o[1] * inv)}, hi = {(__bf16)(x.o[2] * inv), (__bf16)(x.o[3] * inv)};
+        *reinterpret_cast<u32x2*>(a.out + where * D + col) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        if (a.lse && col == 0) a.lse[where] = none ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.l)) * (float)kLn2;
+    };
+    // lanes of as many queries as there are; fewer queries have their parts spread over several lots of lanes
+    constexpr int kSubs = 256 / kLanes4;
+    const int queries = end_query - first_query, spread = kSubs / queries;     // uniform, at least one
+    const int query = sub / spread, in_row = first_query + query;
+    Merged x{kNoScore, 0.0f, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+    if (query < queries) x = join(find(in_row), sub % spread, spread);
+    if (spread > 1) {
+        if (col == 0) { lds[sub][0] = x.m; lds[sub][1] = x.l; }
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) {
-            const __bf16 b = (__bf16)(none ? 0.0f : acc[j] * inv);
-            packed |= (uint32_t)__builtin_bit_cast(uint16_t, b) << (16 * j);
-        }
-        if (kCols == 2) reinterpret_cast<uint32_t*>(a.out + where * D)[lane] = packed;
-        else a.out[where * D + lane] = (uint16_t)packed;
-        if (a.lse && lane == 0) a.lse[where] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (float)kLn2;
+        for (int j = 0; j < 4; ++j) lds[sub][2 + col + j] = x.o[j];
+        __syncthreads();
+        if (sub % spread != 0) return;
+        for (int k = sub + 1; k < sub + spread && k < kSubs; ++k)
+            merge(x, lds[k][0], lds[k][1], f32x4{lds[k][2 + col], lds[k][3 + col], lds[k][4 + col], lds[k][5 + col]});
     }
+    if (query < queries) write(x, in_row);
 }
 
 template <int D, bool kFp8>
@@ -823,7 +853,7 @@ static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, cons
 {
     const int workgroups = compute_units() * attend_occupancy(D, kFp8);
     attend_kernel<D, kFp8><<<workgroups, 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
-    attend_join_kernel<D><<<(uint32_t)(a.rows * c.heads), 256, 0, stream>>>(a, s, c.heads, c.page_size, ws);
+    attend_join_kernel<D><<<dim3((uint32_t)(a.rows * c.heads), (uint32_t)((s.M + join_queries(D) - 1) / join_queries(D))), 256, 0, stream>>>(a, s, c.heads, c.page_size, ws);
     return hipGetLastError();
 }
 
