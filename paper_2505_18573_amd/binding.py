@@ -40,7 +40,8 @@ EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_
 
 _NATIVE_CALLS = ("e3_grpo_advantages", "e3_grpo_objective", "e3_workspace_bytes", "e3_sample_entropy",
                  "e3_restricted_workspace_bytes", "e3_sample_restricted_ws", "e3_logprob_entropy_advantages",
-                 "e3_logprob_entropy_gap", "e3_temperature_update")
+                 "e3_logprob_entropy_gap", "e3_temperature_update", "e3_cache_append", "e3_cache_read",
+                 "e3_prefix_attention_workspace_bytes", "e3_prefix_attention", "e3_verify_workspace_bytes", "e3_verify_drafts")
 
 _lib: Optional[C.CDLL] = None
 _native = None                     # the native calls, once they are bound to the loaded library
@@ -164,7 +165,8 @@ def _ordinary(name: str, *args):
 _ENTRY = {"advantages": "e3_grpo_advantages", "objective": "e3_grpo_objective", "sample": "e3_sample_entropy",
           "restricted": "e3_sample_restricted", "logprob": "e3_logprob_entropy",
           "logprob_advantages": "e3_logprob_entropy_advantages", "logprob_gap": "e3_logprob_entropy_gap",
-          "temperature": "e3_temperature_update"}
+          "temperature": "e3_temperature_update", "cache_append": "e3_cache_append", "cache_read": "e3_cache_read",
+          "attention": "e3_prefix_attention", "verify": "e3_verify_drafts"}
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -704,6 +706,8 @@ def _float_type(dtype) -> int:
 def e3_cache_append(cache: E3Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Write keys and values [tokens, heads, D] (bf16 or fp32, any strides with columns next to each other) to the slots
     (int64 [tokens]; negative: skipped) of the cache."""
+    if _ordinary("cache_append", cache, k, v, slots) is not None:
+        return
     c = _cache(cache)
     dev = cache[0].device
     dt = _float_type(k.dtype)
@@ -721,6 +725,10 @@ def e3_cache_append(cache: E3Cache, k: torch.Tensor, v: torch.Tensor, slots: tor
 def e3_cache_read(cache: E3Cache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
                   k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
     """Returns (k, v) [tokens, heads, D] of the slots (int64 [tokens]; outside the cache: zeros) in bf16 or fp32."""
+    if dtype is torch.bfloat16 or dtype is torch.float32:
+        out = _ordinary("cache_read", cache, slots, dtype is torch.bfloat16, k_out, v_out)
+        if out is not None:
+            return out
     c = _cache(cache)
     dev = cache[0].device
     n = slots.shape[0]
@@ -758,6 +766,10 @@ def e3_prefix_attention(q: torch.Tensor, cache: E3Cache, group_offsets: Optional
     no prefixes) sees the group's prefix (prefix_pages int32 [groups, width], prefix_lens int32 [groups]) and its own
     tokens (row_pages, row_lens), query t all but its last queries - 1 - t.  Returns (out bf16 like q, lse fp32 [rows, queries,
     q_heads] or None).  workspace: a tensor of e3_prefix_attention_workspace_bytes(), or None to allocate one."""
+    res = _ordinary("attention", q, cache, group_offsets, prefix_pages, prefix_lens, row_pages, row_lens, scale, out, lse_out,
+                    workspace, want_lse)
+    if res is not None:
+        return res
     c = _cache(cache)
     dev = cache[0].device
     if q.dim() != 4 or q.dtype is not torch.bfloat16 or q.device != dev or q.shape[3] != c.head_dim or (q.numel() and q.stride(3) != 1):
@@ -818,6 +830,10 @@ def e3_verify_drafts(logits: torch.Tensor, draft_tokens: Optional[torch.Tensor],
     """Verify drafted tokens: logits [rows, drafts + 1, V], draft_tokens int32 [rows, drafts], draft_logits [rows, drafts, V] or None
     (drafts without a distribution).  Returns (accepted int32 [rows], token int32 [rows, drafts + 1], logp fp32, entropy fp32 of the
     same shape).  workspace: a tensor of e3_verify_workspace_bytes(), or None to allocate one."""
+    res = _ordinary("verify", logits, draft_tokens, draft_logits, draft_lens, tau_rows, tau_scalar, seed, row_base, draft_tau_rows,
+                    accepted_out, token_out, logp_out, entropy_out, workspace)
+    if res is not None:
+        return res
     if logits.dim() != 3 or not logits.is_cuda:
         raise ValueError("logits must be [rows, drafts + 1, V] on the GPU")
     dt = _float_type(logits.dtype)

@@ -15,6 +15,8 @@
 #include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <array>
+
 #include "../../include/e3.h"
 
 namespace {
@@ -29,6 +31,12 @@ decltype(&e3_sample_restricted_ws) p_restricted;
 decltype(&e3_logprob_entropy_advantages) p_logprob;
 decltype(&e3_logprob_entropy_gap) p_gap;
 decltype(&e3_temperature_update) p_temperature;
+decltype(&e3_cache_append) p_cache_append;
+decltype(&e3_cache_read) p_cache_read;
+decltype(&e3_prefix_attention_workspace_bytes) p_attention_bytes;
+decltype(&e3_prefix_attention) p_attention;
+decltype(&e3_verify_workspace_bytes) p_verify_bytes;
+decltype(&e3_verify_drafts) p_verify;
 PyObject* raw_stream = nullptr;
 
 // A call's arguments as they are read: `ok` falls at the first one that is not ordinary.
@@ -145,6 +153,23 @@ struct Output {
         if (given == Py_None) return make(r, type, n);
         p = r.vector(given, type, n);
         take(given);
+    }
+    // the same for a tensor of any shape
+    template <size_t N>
+    void shaped(Reader& r, PyObject* given, at::ScalarType type, const std::array<int64_t, N>& shape)
+    {
+        if (given != Py_None) {
+            const at::Tensor* t = r.plain(given);
+            if (t == nullptr || t->scalar_type() != type || t->sizes() != at::IntArrayRef(shape.data(), N) || t->device() != r.dev
+                || !t->is_contiguous()) { r.ok = false; return; }
+            p = t->data_ptr();
+            return take(given);
+        }
+        if (!r.ok) return;
+        const at::Tensor t = at::empty(at::IntArrayRef(shape.data(), N), at::TensorOptions().dtype(type).device(r.dev));
+        p = t.data_ptr();
+        object = THPVariable_Wrap(t);
+        if (object == nullptr) { PyErr_Clear(); r.ok = false; }
     }
     PyObject* release() { PyObject* o = object; object = nullptr; return o; }
 };
@@ -394,6 +419,199 @@ PyObject* logprob_gap(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     });
 }
 
+// A cache as binding.py's E3Cache holds it: a tuple of k, v, k_scale, v_scale.
+struct Cache {
+    e3_cache c{};
+    Cache(Reader& r, PyObject* o)
+    {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) { r.ok = false; return; }
+        const at::Tensor* k = r.first(PyTuple_GET_ITEM(o, 0));
+        const at::Tensor* v = r.ok ? r.plain(PyTuple_GET_ITEM(o, 1)) : nullptr;
+        if (!r.ok || k->dim() != 4 || v->dim() != 5 || !k->is_contiguous() || !v->is_contiguous() || v->device() != r.dev
+            || v->scalar_type() != k->scalar_type()) { r.ok = false; return; }
+        const auto ks = k->sizes(), vs = v->sizes();
+        if (vs[0] != ks[0] || vs[1] != ks[1] || vs[2] != ks[2] / 8 || vs[3] != ks[3] || vs[4] != 8) { r.ok = false; return; }
+        const bool fp8 = k->scalar_type() == at::kFloat8_e4m3fn;
+        if (!fp8 && k->scalar_type() != at::kBFloat16) { r.ok = false; return; }
+        for (int i = 1; i < 4; ++i)
+            if (ks[i] != (int32_t)ks[i]) { r.ok = false; return; }
+        c.k = k->data_ptr();
+        c.v = v->data_ptr();
+        for (int i = 0; i < 2; ++i) {
+            PyObject* const scale = PyTuple_GET_ITEM(o, 2 + i);
+            if ((scale == Py_None) == fp8) { r.ok = false; return; }
+            if (!fp8) continue;
+            const at::Tensor* t = r.plain(scale);
+            if (t == nullptr || t->scalar_type() != at::kByte || t->dim() != 3 || t->size(0) != ks[0] || t->size(1) != ks[1] || t->size(2) != ks[2]
+                || t->device() != r.dev || !t->is_contiguous()) { r.ok = false; return; }
+            (i == 0 ? c.k_scale : c.v_scale) = (uint8_t*)t->data_ptr();
+        }
+        c.num_pages = ks[0]; c.kv_heads = (int32_t)ks[1]; c.page_size = (int32_t)ks[2]; c.head_dim = (int32_t)ks[3];
+        c.dtype = fp8 ? E3_E4M3 : E3_BF16;
+    }
+};
+
+int float_type(Reader& r, at::ScalarType t)
+{
+    if (t != at::kBFloat16 && t != at::kFloat) r.ok = false;
+    return t == at::kFloat ? E3_F32 : E3_BF16;
+}
+
+// cache, k, v, slots; True where it was done
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 4) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const Cache cache(r, a[0]);
+        const at::Tensor* k = r.ok ? r.plain(a[1]) : nullptr;
+        const at::Tensor* v = r.ok ? r.plain(a[2]) : nullptr;
+        const at::Tensor* slots = r.ok ? r.plain(a[3]) : nullptr;
+        if (!r.ok || slots->dim() != 1) return unusual();
+        const int64_t n = slots->size(0);
+        const void* ps = r.vector(a[3], at::kLong, n);
+        for (const at::Tensor* t : {k, v})
+            if (t->scalar_type() != k->scalar_type() || t->dim() != 3 || t->size(0) != n || t->size(1) != cache.c.kv_heads
+                || t->size(2) != cache.c.head_dim || t->device() != r.dev || (n > 0 && t->stride(2) != 1)) return unusual();
+        const int type = float_type(r, k->scalar_type());
+        return run(r, [&](void* s) {
+                       return p_cache_append(&cache.c, k->data_ptr(), v->data_ptr(), type, n, k->stride(0), k->stride(1), v->stride(0),
+                                             v->stride(1), (const int64_t*)ps, s);
+                   },
+                   [&]() -> PyObject* { Py_RETURN_TRUE; });
+    });
+}
+
+// cache, slots, whether bf16 (or fp32), k_out, v_out
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 5 || !PyBool_Check(a[2])) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const Cache cache(r, a[0]);
+        const at::Tensor* slots = r.ok ? r.plain(a[1]) : nullptr;
+        if (!r.ok || slots->dim() != 1) return unusual();
+        const int64_t n = slots->size(0);
+        const void* ps = r.vector(a[1], at::kLong, n);
+        const at::ScalarType type = a[2] == Py_True ? at::kBFloat16 : at::kFloat;
+        const std::array<int64_t, 3> shape = {n, cache.c.kv_heads, cache.c.head_dim};
+        Output k, v;
+        k.shaped(r, a[3], type, shape);
+        v.shaped(r, a[4], type, shape);
+        return run(r, [&](void* s) { return p_cache_read(&cache.c, (const int64_t*)ps, n, k.p, v.p, type == at::kFloat ? E3_F32 : E3_BF16, s); },
+                   [&] { return PyTuple_Pack(2, k.object, v.object); });
+    });
+}
+
+// q, cache, group_offsets, prefix_pages, prefix_lens, row_pages, row_lens, scale, out, lse_out, workspace, want_lse
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 12 || !PyBool_Check(a[11])) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const Cache cache(r, a[1]);
+        const at::Tensor* q = r.ok ? r.plain(a[0]) : nullptr;
+        if (!r.ok || q->dim() != 4 || q->scalar_type() != at::kBFloat16 || q->device() != r.dev || q->size(3) != cache.c.head_dim
+            || (q->numel() > 0 && q->stride(3) != 1)) return unusual();
+        const int64_t rows = q->size(0), T = q->size(1), heads = q->size(2), D = q->size(3);
+        auto table = [&](PyObject* o, int64_t n, int64_t* width) -> const int32_t* {
+            const at::Tensor* t = r.plain(o);
+            if (t == nullptr || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != n || !t->is_contiguous()
+                || t->device() != r.dev) { r.ok = false; return nullptr; }
+            *width = t->size(1);
+            return (const int32_t*)t->data_ptr();
+        };
+        int64_t groups = 0, prefix_width = 0, row_width = 0;
+        const void *offsets = nullptr, *prefix_lens = nullptr;
+        const int32_t* prefix_pages = nullptr;
+        if (a[2] != Py_None) {
+            const at::Tensor* off = r.plain(a[2]);
+            if (off == nullptr || off->dim() != 1 || a[3] == Py_None || a[4] == Py_None) return unusual();
+            groups = off->size(0) - 1;
+            offsets = r.vector(a[2], at::kInt, groups + 1);
+            prefix_pages = table(a[3], groups, &prefix_width);
+            prefix_lens = r.vector(a[4], at::kInt, groups);
+        }
+        const int32_t* row_pages = table(a[5], rows, &row_width);
+        if (a[6] == Py_None) return unusual();
+        const void* row_lens = r.vector(a[6], at::kInt, rows);
+        const double scale = r.number(a[7]);
+        if (!r.ok) return unusual();
+        Output out, lse;
+        out.shaped(r, a[8], at::kBFloat16, std::array<int64_t, 4>{rows, T, heads, D});
+        if (a[9] == Py_None && a[11] == Py_False) lse.take(Py_None);
+        else lse.shaped(r, a[9], at::kFloat, std::array<int64_t, 3>{rows, T, heads});
+        const size_t need = a[10] == Py_None ? p_attention_bytes(rows, T, heads, cache.c.kv_heads, D, groups) : 0;
+        const Workspace ws(r, a[10] == Py_False ? Py_True : a[10], need, true);       // False is no workspace here: left to binding.py
+        if (a[10] == Py_None && need > 0 && ws.p == nullptr) return unusual();         // no memory: reported there
+        return run(r, [&](void* s) {
+                       return p_attention(&cache.c, q->data_ptr(), rows, T, heads, q->stride(0), q->stride(1), q->stride(2),
+                                          groups > 0 ? (const int32_t*)offsets : nullptr, groups, prefix_pages, prefix_width, (const int32_t*)prefix_lens,
+                                          row_pages, row_width, (const int32_t*)row_lens, (float)scale, out.p, (float*)lse.p, ws.p, ws.bytes, s);
+                   },
+                   [&] { return PyTuple_Pack(2, out.object, lse.object); });
+    });
+}
+
+// logits, draft_tokens, draft_logits, draft_lens, tau_rows, tau_scalar, seed, row_base, draft_tau_rows, accepted_out, token_out,
+// logp_out, entropy_out, workspace
+PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 14) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const at::Tensor* z = r.first(a[0]);
+        if (!r.ok || z->dim() != 3 || z->size(1) < 1) return unusual();
+        const int type = float_type(r, z->scalar_type());
+        const int64_t rows = z->size(0), positions = z->size(1), V = z->size(2), drafts = positions - 1;
+        if (drafts != (int32_t)drafts) return unusual();
+        // row and position strides, of a dimension of one what binding.py gives
+        auto strides = [&](const at::Tensor* t, int64_t* of_row, int64_t* of_position) {
+            if (V > 1 && t->stride(2) != 1) { r.ok = false; return; }
+            *of_position = t->size(1) > 1 ? t->stride(1) : (V + 7) / 8 * 8;
+            *of_row = rows > 1 ? t->stride(0) : *of_position * t->size(1);
+        };
+        int64_t row_stride = 0, position_stride = 0, draft_row = 0, draft_position = 0;
+        strides(z, &row_stride, &position_stride);
+        const void* d = nullptr;
+        if (a[2] != Py_None) {
+            const at::Tensor* t = r.plain(a[2]);
+            if (t == nullptr || t->scalar_type() != z->scalar_type() || t->dim() != 3 || t->size(0) != rows || t->size(1) != drafts
+                || t->size(2) != V || t->device() != r.dev) return unusual();
+            strides(t, &draft_row, &draft_position);
+            d = t->data_ptr();
+        }
+        const void* tokens = nullptr;
+        if (a[1] != Py_None) {
+            const at::Tensor* t = r.plain(a[1]);
+            if (t == nullptr || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != rows || t->size(1) != drafts || !t->is_contiguous()
+                || t->device() != r.dev) return unusual();
+            tokens = t->data_ptr();
+        } else if (drafts > 0) return unusual();
+        const void* lens = r.vector(a[3], at::kInt, rows);
+        const void* tau = r.vector(a[4], at::kFloat, rows);
+        const double tau_scalar = r.number(a[5]);
+        const uint64_t seed = r.word(a[6]), row_base = r.word(a[7]);
+        const void* draft_tau = r.vector(a[8], at::kFloat, rows);
+        if (!r.ok) return unusual();
+        const std::array<int64_t, 2> shape = {rows, positions};
+        Output accepted, token, logp, entropy;
+        accepted.take_or_make(r, a[9], at::kInt, rows);
+        token.shaped(r, a[10], at::kInt, shape);
+        logp.shaped(r, a[11], at::kFloat, shape);
+        entropy.shaped(r, a[12], at::kFloat, shape);
+        const size_t need = a[13] == Py_None ? p_verify_bytes(rows, (int32_t)drafts, V) : 0;
+        const Workspace ws(r, a[13] == Py_False ? Py_True : a[13], need, true);
+        if (a[13] == Py_None && need > 0 && ws.p == nullptr) return unusual();
+        return run(r, [&](void* s) {
+                       return p_verify(z->data_ptr(), type, rows, (int32_t)drafts, V, row_stride, position_stride, (const int32_t*)tokens,
+                                       (const int32_t*)lens, d, draft_row, draft_position, (const float*)tau, (float)tau_scalar, (const float*)draft_tau,
+                                       seed, row_base, (int32_t*)accepted.p, (int32_t*)token.p, (float*)logp.p, (float*)entropy.p, ws.p, ws.bytes, s);
+                   },
+                   [&] { return PyTuple_Pack(4, accepted.object, token.object, logp.object, entropy.object); });
+    });
+}
+
 // tau_t, H_t, H_init, vocab, t, t_anneal, t_max, eta, tau_min, tau_max
 PyObject* temperature(PyObject*, PyObject* const* a, Py_ssize_t n_args)
 {
@@ -431,6 +649,12 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     get("e3_logprob_entropy_advantages", p_logprob);
     get("e3_logprob_entropy_gap", p_gap);
     get("e3_temperature_update", p_temperature);
+    get("e3_cache_append", p_cache_append);
+    get("e3_cache_read", p_cache_read);
+    get("e3_prefix_attention_workspace_bytes", p_attention_bytes);
+    get("e3_prefix_attention", p_attention);
+    get("e3_verify_workspace_bytes", p_verify_bytes);
+    get("e3_verify_drafts", p_verify);
     if (!all) { PyErr_SetString(PyExc_ValueError, "an entry point is missing"); return nullptr; }
     Py_INCREF(a[1]);
     Py_XSETREF(raw_stream, a[1]);
@@ -450,6 +674,10 @@ PyMethodDef methods[] = {
     {"logprob_advantages", fast(logprob), METH_FASTCALL, nullptr},
     {"logprob_gap", fast(logprob_gap), METH_FASTCALL, nullptr},
     {"temperature", fast(temperature), METH_FASTCALL, nullptr},
+    {"cache_append", fast(cache_append), METH_FASTCALL, nullptr},
+    {"cache_read", fast(cache_read), METH_FASTCALL, nullptr},
+    {"attention", fast(attention), METH_FASTCALL, nullptr},
+    {"verify", fast(verify), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
