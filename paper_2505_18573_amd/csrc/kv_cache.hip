@@ -149,12 +149,17 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
     const int head = (int)(item % per) * kHeads + ((lane & 31) >> (D == 128 ? 5 : 4));
     const bool live = head < c.heads;
     const int safe_head = live ? head : 0;
-    const Window w = look_at(slots, first, tokens, c.num_pages * c.page_size, lane);
-
     auto load = [&](const TokenRows& t, int64_t token, float x[4]) {
         const int64_t safe = token < tokens ? token : tokens - 1;
         load4<kBf16>(static_cast<const char*>(t.base) + (safe * t.token_stride + safe_head * t.head_stride + col) * kIn, x);
     };
+    // rows of the window: keys, and values for those whose block is not filled.  Requested before the slots are known.
+    float xk[4][4], xv[4][4], xb[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load(k, first + 4 * half + i, xk[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load(v, first + 4 * half + i, xv[i]);
+    const Window w = look_at(slots, first, tokens, c.num_pages * c.page_size, lane);
     // codes of four rows, and their scale bytes into the cache
     auto quantise = [&](float x[4][4], const int64_t row[4], const bool ok[4], uint8_t* scales, uint32_t code[4]) {
 #pragma unroll
@@ -171,20 +176,17 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
         }
     };
 
-    // rows of the window: keys all, values those whose block is not filled
-    float xk[4][4], xv[4][4], xb[4][4];
     int64_t row[4], brow[4];
     bool ok[4], single[4], all[4] = {true, true, true, true};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load(k, first + 4 * half + i, xk[i]);
     const bool some_single = ((~w.whole) & 0xFFu) != 0;
-    if (some_single) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load(v, first + 4 * half + i, xv[i]);
-    }
-    if (w.start >= 0) {
+    if (w.start > 0) {                                            // a block that starts with the window is the window
 #pragma unroll
         for (int i = 0; i < 4; ++i) load(v, first + w.start + 4 * half + i, xb[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xb[i][j] = xv[i][j];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
