@@ -104,9 +104,9 @@ __device__ __forceinline__ LaneState empty_state()
     return s;
 }
 
-// Columns [from, to) of a line, dealt to the workgroup's waves in blocks of four sweeps.  `from` is a multiple of 512.
+// Columns [from, to) of a line, dealt to `waves` waves in blocks of four sweeps.  `from` is a multiple of 512.
 template <typename Chunk>
-__device__ __forceinline__ void stream_sums(LaneState& s, const char* line, int64_t from, int64_t to, float c, int lane, int wave)
+__device__ __forceinline__ void stream_sums(LaneState& s, const char* line, int64_t from, int64_t to, float c, int lane, int wave, int waves)
 {
     const int sweeps = (int)((to - from) / kSweepCols);
     const int blocks = sweeps / kBlockSweeps;
@@ -123,8 +123,8 @@ __device__ __forceinline__ void stream_sums(LaneState& s, const char* line, int6
 #pragma unroll
         for (int i = 0; i < kBlockSweeps; ++i) buf[i].load_sweep(line, at0 + ((int64_t)b * kBlockSweeps + i) * kSweepCols);
     }
-    for (; b < blocks; b += kVerifyWaves) {
-        const int next = b + kVerifyWaves < blocks ? b + kVerifyWaves : b;           // the last one again: no branch
+    for (; b < blocks; b += waves) {
+        const int next = b + waves < blocks ? b + waves : b;           // the last one again: no branch
 #pragma unroll
         for (int i = 0; i < kBlockSweeps; ++i) {
             const Chunk cur = buf[i];
@@ -136,13 +136,13 @@ __device__ __forceinline__ void stream_sums(LaneState& s, const char* line, int6
     // sweeps behind the last block, one wave each; then the columns behind the last sweep
     const int left = sweeps - blocks * kBlockSweeps;
     for (int i = 0; i < left; ++i) {
-        if ((blocks + i) % kVerifyWaves != wave) continue;        // uniform
+        if ((blocks + i) % waves != wave) continue;        // uniform
         Chunk ch;
         ch.load_sweep(line, at0 + ((int64_t)blocks * kBlockSweeps + i) * kSweepCols);
         add(ch);
         close_tile<false>(s, 0, 0.0f, true, c, lane);
     }
-    if (from + (int64_t)sweeps * kSweepCols < to && (blocks + left) % kVerifyWaves == wave) {
+    if (from + (int64_t)sweeps * kSweepCols < to && (blocks + left) % waves == wave) {
         const int64_t col = from + (int64_t)sweeps * kSweepCols + lane * kChunk;
         float z[8];
 #pragma unroll
@@ -290,12 +290,12 @@ __device__ __forceinline__ float weight_of(const Residual& r, float zp, float zq
 
 // Level 1 over super-tiles [from, to): the wave's best tile.  kQ: with a draft distribution.
 template <typename Chunk, bool kQ>
-__device__ __forceinline__ Cand stream_race(const VerifyArgs& a, const Residual& r, int64_t row, int from, int to, int lane, int wave)
+__device__ __forceinline__ Cand stream_race(const VerifyArgs& a, const Residual& r, int64_t row, int from, int to, int lane, int wave, int waves)
 {
     const int64_t V = a.V;
     const uint64_t grow = a.row_base + (uint64_t)row;
     Cand best{-1.0f, 0};
-    for (int st = from + wave; st < to; st += kVerifyWaves) {
+    for (int st = from + wave; st < to; st += waves) {
         const int64_t base = (int64_t)st * kSuperCols;
         const bool whole = base + kSuperCols <= V;                // uniform
         const int slot = whole ? Chunk::tile_lane(lane) : lane;
@@ -402,33 +402,21 @@ __device__ __forceinline__ Residual residual_of(const VerifyArgs& a, int64_t row
 }
 
 template <typename Chunk>
-__device__ __forceinline__ Cand race(const VerifyArgs& a, const Residual& r, int64_t row, int from, int to, int lane, int wave)
+__device__ __forceinline__ Cand race(const VerifyArgs& a, const Residual& r, int64_t row, int from, int to, int lane, int wave, int waves)
 {
-    return r.q ? stream_race<Chunk, true>(a, r, row, from, to, lane, wave) : stream_race<Chunk, false>(a, r, row, from, to, lane, wave);
+    return r.q ? stream_race<Chunk, true>(a, r, row, from, to, lane, wave, waves)
+               : stream_race<Chunk, false>(a, r, row, from, to, lane, wave, waves);
 }
 
 // the workgroup's best of the waves' candidates, in every thread
-__device__ __forceinline__ Cand workgroup_best(Cand c, Cand* lds, int lane, int wave)
+__device__ __forceinline__ Cand workgroup_best(Cand c, Cand* lds, int lane, int wave, int waves)
 {
     __syncthreads();
     if (lane == 0) lds[wave] = c;
     __syncthreads();
     Cand best = lds[0];
-    for (int i = 1; i < kVerifyWaves; ++i) best = better(best, lds[i]);
+    for (int i = 1; i < waves; ++i) best = better(best, lds[i]);
     return best;
-}
-
-// Sums of a whole line by the workgroup, in every thread.
-template <typename Chunk>
-__device__ __forceinline__ Line workgroup_line(const char* line, int64_t V, float c, LineSum* lds, int lane, int wave)
-{
-    LaneState s = empty_state();
-    stream_sums<Chunk>(s, line, 0, V, c, lane, wave);
-    const LineSum mine = wave_sums(s);
-    __syncthreads();
-    if (lane == 0) lds[wave] = mine;
-    __syncthreads();
-    return line_of(merge_sums(lds, kVerifyWaves, c, lane), c);
 }
 
 // ---------------------------------------------------------------- kernels
@@ -439,13 +427,17 @@ void verify_clear_kernel(int32_t* flags, int64_t rows)
     if (i < rows) flags[i] = 0x7FFFFFFF;
 }
 
-// A workgroup per (position, row), positions rising.
+// A workgroup per (position, row), positions rising.  Four of its eight waves take the sums of the target's line, four the
+// draft's; all of them the one line where there is no other.
+constexpr int kPairWaves = 8;
+
 template <typename Chunk>
-__global__ __launch_bounds__(kVerifyThreads, Chunk::kElemBytes == 2 ? 5 : 4)
+__global__ __launch_bounds__(64 * kPairWaves, 4)
 void verify_pair_kernel(VerifyArgs a, VerifyShape s, char* ws)
 {
-    __shared__ LineSum sums[kVerifyWaves];
-    __shared__ Cand cands[kVerifyWaves];
+    __shared__ LineSum sums[kPairWaves];
+    __shared__ Line found[2];
+    __shared__ Cand cands[kPairWaves];
     __shared__ int known;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = (int)(blockIdx.x / a.rows);
@@ -456,16 +448,27 @@ void verify_pair_kernel(VerifyArgs a, VerifyShape s, char* ws)
     if (threadIdx.x == 0) known = __hip_atomic_load(&flags[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (known < t) return;                                        // an earlier draft was rejected
-    Line* lines = reinterpret_cast<Line*>(ws + s.at_lines) + row * s.lines;
-    const Line p = workgroup_line<Chunk>(target_line<Chunk>(a, row, t), a.V, target_factor(a, row), sums, lane, wave);
-    Line q = p;
-    const bool last = t == len;
-    if (!last && a.draft_logits)
-        q = workgroup_line<Chunk>(draft_line<Chunk>(a, row, t), a.V, draft_factor(a, row), sums, lane, wave);
-    if (threadIdx.x == 0) {
-        lines[t] = p;
-        if (!last && a.draft_logits) lines[a.drafts + 1 + t] = q;
+    const bool last = t == len, two = !last && a.draft_logits != nullptr;
+    const int half = two ? kPairWaves / 2 : kPairWaves;           // waves of a line
+    const int which = wave >= half ? 1 : 0;
+    {
+        const char* line = which ? draft_line<Chunk>(a, row, t) : target_line<Chunk>(a, row, t);
+        const float c = which ? draft_factor(a, row) : target_factor(a, row);
+        LaneState state = empty_state();
+        stream_sums<Chunk>(state, line, 0, a.V, c, lane, wave - which * half, half);
+        const LineSum mine = wave_sums(state);
+        if (lane == 0) sums[wave] = mine;
+        __syncthreads();
+        if (wave == which * half) {
+            const Line l = line_of(merge_sums(sums + which * half, half, c, lane), c);
+            if (lane == 0) {
+                found[which] = l;
+                reinterpret_cast<Line*>(ws + s.at_lines)[row * s.lines + (which ? a.drafts + 1 : 0) + t] = l;
+            }
+        }
+        __syncthreads();
     }
+    const Line p = found[0], q = found[two ? 1 : 0];
     if (!last) {
         const bool ok = accepts<Chunk>(a, row, t, p, q);          // the same in every thread
         if (ok) return;
@@ -473,7 +476,7 @@ void verify_pair_kernel(VerifyArgs a, VerifyShape s, char* ws)
     }
     const Residual r = residual_of<Chunk>(a, row, t, !last, p, q);
     const int tiles = (int)((a.V + kSuperCols - 1) / kSuperCols);
-    const Cand best = workgroup_best(race<Chunk>(a, r, row, 0, tiles, lane, wave), cands, lane, wave);
+    const Cand best = workgroup_best(race<Chunk>(a, r, row, 0, tiles, lane, wave, kPairWaves), cands, lane, wave, kPairWaves);
     if (threadIdx.x == 0) reinterpret_cast<Cand*>(ws + s.at_cands)[row * s.race_slices + t] = best;
 }
 
@@ -494,7 +497,7 @@ void verify_sums_kernel(VerifyArgs a, VerifyShape s, char* ws)
     const int64_t from = (int64_t)slice * s.slice_cols;
     const int64_t to = from + s.slice_cols < a.V ? from + s.slice_cols : a.V;
     LaneState state = empty_state();
-    stream_sums<Chunk>(state, at, from, to, c, lane, wave);
+    stream_sums<Chunk>(state, at, from, to, c, lane, wave, kVerifyWaves);
     const LineSum mine = wave_sums(state);
     if (lane == 0) sums[wave] = mine;
     __syncthreads();
@@ -543,7 +546,7 @@ void verify_race_kernel(VerifyArgs a, VerifyShape s, char* ws)
     const int tiles = (int)((a.V + kSuperCols - 1) / kSuperCols);
     const int each = (tiles + s.race_slices - 1) / s.race_slices;
     const int from = slice * each, to = from + each < tiles ? from + each : tiles;
-    const Cand best = workgroup_best(race<Chunk>(a, r, row, from, to, lane, wave), cands, lane, wave);
+    const Cand best = workgroup_best(race<Chunk>(a, r, row, from, to, lane, wave, kVerifyWaves), cands, lane, wave, kVerifyWaves);
     if (threadIdx.x == 0) reinterpret_cast<Cand*>(ws + s.at_cands)[row * s.race_slices + slice] = best;
 }
 
@@ -576,7 +579,7 @@ void verify_finish_kernel(VerifyArgs a, VerifyShape s, const char* ws)
         r.q = nullptr;
         r.barred = -1;
         const int tiles = (int)((a.V + kSuperCols - 1) / kSuperCols);
-        best = workgroup_best(race<Chunk>(a, r, row, 0, tiles, lane, wave), cands, lane, wave);
+        best = workgroup_best(race<Chunk>(a, r, row, 0, tiles, lane, wave, kVerifyWaves), cands, lane, wave, kVerifyWaves);
         token = best.q > 0.0f ? race_in_tile<Chunk>(a, r, row, best.idx, lane) : -1;
     }
     if (token < 0) token = 0;                                     // p is no distribution
@@ -603,7 +606,7 @@ static hipError_t launch(const VerifyArgs& a, char* ws, hipStream_t stream)
     const VerifyShape s = verify_shape(a.rows, a.drafts, a.V, a.draft_logits != nullptr);
     if (s.slices == 0) {
         verify_clear_kernel<<<(uint32_t)((a.rows + 255) / 256), 256, 0, stream>>>(reinterpret_cast<int32_t*>(ws + s.at_flags), a.rows);
-        verify_pair_kernel<Chunk><<<(uint32_t)(a.rows * (a.drafts + 1)), kVerifyThreads, 0, stream>>>(a, s, ws);
+        verify_pair_kernel<Chunk><<<(uint32_t)(a.rows * (a.drafts + 1)), 64 * kPairWaves, 0, stream>>>(a, s, ws);
     } else {
         verify_sums_kernel<Chunk><<<(uint32_t)(a.rows * s.lines * s.slices), kVerifyThreads, 0, stream>>>(a, s, ws);
         verify_race_kernel<Chunk><<<(uint32_t)(a.rows * s.race_slices), kVerifyThreads, 0, stream>>>(a, s, ws);
