@@ -17,7 +17,9 @@
 //            the result, so the result does not depend on timing.
 //   slices   few positions: every line is cut into runs of columns, each summed by a workgroup of its own; a second
 //            launch merges, decides and races over slices of the one position that draws.
-// Either way a last launch, a workgroup per row, draws within the winning tile and writes the outputs.
+// Either way a last launch, a workgroup per row, draws within the winning tile and writes the outputs.  (Done by the workgroup of
+// a row that ends last instead, which takes a fence over the card's caches in every workgroup, 512 x 4 drafts took 558
+// us where they take 240.)
 #include "verify.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
@@ -44,7 +46,7 @@ struct VerifyShape {
     int slices;                                                   // 0: pairs
     int slice_cols;                                               // columns of a slice of sums (a multiple of 2048)
     int race_slices;                                              // slices of super-tiles
-    int64_t at_lines, at_sums, at_cands, at_flags, bytes;
+    int64_t at_lines, at_sums, at_cands, at_flags, bytes;        // at_flags: first rejected draft of each row
 };
 
 static int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
@@ -60,8 +62,10 @@ static VerifyShape verify_shape(int64_t rows, int32_t drafts, int64_t V, bool dr
     s.slice_cols = 0;
     s.race_slices = drafts + 1;
     if (units < (int64_t)cus * 2) {
-        const int64_t blocks = (V + 2047) / 2048;                 // of four sweeps
+        // a block of four sweeps for each wave at least
+        const int64_t blocks = (V + 2047) / 2048;
         int64_t per = (blocks * rows * s.lines + want - 1) / want;
+        per = (per + kVerifyWaves - 1) / kVerifyWaves * kVerifyWaves;
         if (per * kMaxSlices < blocks) per = (blocks + kMaxSlices - 1) / kMaxSlices;
         s.slice_cols = (int)(per * 2048);
         s.slices = (int)((blocks + per - 1) / per);
@@ -255,20 +259,34 @@ __device__ __forceinline__ double log_p(float z, const Line& line, float c)
     return ((double)z - (double)line.peak) * (double)c * kLn2 - line.l1p;
 }
 
-// u_t q_t(x_t) < p_t(x_t).  An id outside the vocabulary, or lines that are no distribution: rejected.
+// What a draft's decision needs besides its lines; asked for before the lines are summed.
+struct Drafted {
+    int64_t x;
+    float zp, zq;
+    double u;
+};
 template <typename Chunk>
-__device__ __forceinline__ bool accepts(const VerifyArgs& a, int64_t row, int t, const Line& p, const Line& q)
+__device__ __forceinline__ Drafted drafted_at(const VerifyArgs& a, int64_t row, int t)
 {
-    const int64_t x = draft_token(a, row, t);
-    if (x < 0 || x >= a.V) return false;
+    Drafted d;
+    d.x = draft_token(a, row, t);
+    const int64_t safe = d.x < 0 ? 0 : d.x >= a.V ? a.V - 1 : d.x;
+    d.zp = Chunk::load_one(target_line<Chunk>(a, row, t), safe);
+    d.zq = a.draft_logits ? Chunk::load_one(draft_line<Chunk>(a, row, t), safe) : 0.0f;
     const uint64_t grow = a.row_base + (uint64_t)row;
     uint32_t w[4];
     philox4x32_10((uint32_t)t >> 2, (uint32_t)grow, (uint32_t)(grow >> 32), 5u, (uint32_t)a.seed, (uint32_t)(a.seed >> 32), w);
     const uint32_t word = (t & 3) == 0 ? w[0] : (t & 3) == 1 ? w[1] : (t & 3) == 2 ? w[2] : w[3];
-    const double u = ((double)(word >> 9) + 0.5) * 0x1p-23;
-    const double px = exp(log_p(Chunk::load_one(target_line<Chunk>(a, row, t), x), p, target_factor(a, row)));
-    const double qx = a.draft_logits ? exp(log_p(Chunk::load_one(draft_line<Chunk>(a, row, t), x), q, draft_factor(a, row))) : 1.0;
-    return u * qx < px;
+    d.u = ((double)(word >> 9) + 0.5) * 0x1p-23;
+    return d;
+}
+// u_t q_t(x_t) < p_t(x_t).  An id outside the vocabulary, or lines that are no distribution: rejected.
+__device__ __forceinline__ bool accepts(const VerifyArgs& a, int64_t row, const Drafted& d, const Line& p, const Line& q)
+{
+    if (d.x < 0 || d.x >= a.V) return false;
+    const double px = exp(log_p(d.zp, p, target_factor(a, row)));
+    const double qx = a.draft_logits ? exp(log_p(d.zq, q, draft_factor(a, row))) : 1.0;
+    return d.u * qx < px;
 }
 
 // ---------------------------------------------------------------- race
@@ -288,71 +306,105 @@ __device__ __forceinline__ float weight_of(const Residual& r, float zp, float zq
     return fmaxf(p - q, 0.0f);
 }
 
-// Level 1 over super-tiles [from, to): the wave's best tile.  kQ: with a draft distribution.
+// The lane's share of a tile's mass: sweeps first, first + 1, ... of super-tile st, `sweeps` (one or four) of them, all requested before
+// the first is used.  Complete super-tiles are read in whole sweeps, which leave tile lane `slot` with the lane.
+template <typename Chunk, bool kQ, int kSweeps>
+__device__ __forceinline__ float tile_mass(const VerifyArgs& a, const Residual& r, int st, int sweep, int lane)
+{
+    const int64_t V = a.V;
+    const bool whole = (int64_t)(st + 1) * kSuperCols <= V;       // uniform
+    const int64_t first = (int64_t)st * kSuperCols + (int64_t)sweep * kSweepCols;
+    const int slot = whole ? Chunk::tile_lane(lane) : lane;
+    float mass = 0.0f;
+    auto add = [&](const float* zp, const float* zq, int64_t col) {
+        // (after the exchange of a complete sweep of fp32 an odd lane holds the upper four of its columns first)
+        const int at = (int)(r.barred - col) ^ (whole && Chunk::kHalves == 2 && (lane & 1) ? 4 : 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float w = weight_of(r, zp[j], kQ ? zq[j] : 0.0f, kQ);
+            mass += (!kQ && j == at) ? 0.0f : w;
+        }
+    };
+    if (whole) {
+        Chunk bp[kSweeps], bq[kSweeps];
+#pragma unroll
+        for (int i = 0; i < kSweeps; ++i) {
+            bp[i].load_sweep(r.p, first + i * kSweepCols + Chunk::sweep_col(lane));
+            if (kQ) bq[i].load_sweep(r.q, first + i * kSweepCols + Chunk::sweep_col(lane));
+        }
+#pragma unroll
+        for (int i = 0; i < kSweeps; ++i) {
+            float zp[8], zq[8];
+            bp[i].unpack_sweep(zp, lane);
+            if (kQ) bq[i].unpack_sweep(zq, lane);
+            add(zp, zq, first + i * kSweepCols + slot * kChunk);
+        }
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < kSweeps; ++i) {
+            const int64_t col = first + i * kSweepCols + lane * kChunk;
+            float zp[8], zq[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { zp[j] = -INFINITY; zq[j] = -INFINITY; }
+            if (col + kChunk <= V) {
+                Chunk ch;
+                ch.load(r.p, col);
+                ch.unpack(zp);
+                if (kQ) { ch.load(r.q, col); ch.unpack(zq); }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (col + j < V) { zp[j] = Chunk::load_one(r.p, col + j); if (kQ) zq[j] = Chunk::load_one(r.q, col + j); }
+            }
+            add(zp, zq, col);
+        }
+    }
+    return mass;
+}
+
+// The lane's tile of super-tile st in the race of level 1.
+template <typename Chunk>
+__device__ __forceinline__ Cand tile_entry(const VerifyArgs& a, int64_t row, int st, float mass, int lane)
+{
+    const bool whole = (int64_t)(st + 1) * kSuperCols <= a.V;
+    const int tile = st * kLanes + (whole ? Chunk::tile_lane(lane) : lane);
+    const uint64_t grow = a.row_base + (uint64_t)row;
+    uint32_t w[4];
+    philox4x32_10((uint32_t)tile >> 2, (uint32_t)grow, (uint32_t)(grow >> 32), 6u, (uint32_t)a.seed, (uint32_t)(a.seed >> 32), w);
+    const uint32_t word = (tile & 3) == 0 ? w[0] : (tile & 3) == 1 ? w[1] : (tile & 3) == 2 ? w[2] : w[3];
+    return Cand{mass > 0.0f ? mass * inv_exp_variate(word) : -1.0f, tile};
+}
+
+// Level 1 over super-tiles [from, to), dealt to the waves: the wave's best tile.  kQ: with a draft distribution.
 template <typename Chunk, bool kQ>
 __device__ __forceinline__ Cand stream_race(const VerifyArgs& a, const Residual& r, int64_t row, int from, int to, int lane, int wave, int waves)
 {
-    const int64_t V = a.V;
-    const uint64_t grow = a.row_base + (uint64_t)row;
     Cand best{-1.0f, 0};
     for (int st = from + wave; st < to; st += waves) {
-        const int64_t base = (int64_t)st * kSuperCols;
-        const bool whole = base + kSuperCols <= V;                // uniform
-        const int slot = whole ? Chunk::tile_lane(lane) : lane;
         float mass = 0.0f;
-        auto add = [&](const float* zp, const float* zq, int64_t col) {
-            // (after the exchange of a complete sweep of fp32 an odd lane holds the upper four of its columns first)
-            const int at = (int)(r.barred - col) ^ (whole && Chunk::kHalves == 2 && (lane & 1) ? 4 : 0);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float w = weight_of(r, zp[j], kQ ? zq[j] : 0.0f, kQ);
-                mass += (!kQ && j == at) ? 0.0f : w;
-            }
-        };
-        if (whole) {
 #pragma unroll 1
-            for (int half = 0; half < kDepth / kBlockSweeps; ++half) {
-                const int64_t first = base + half * kBlockSweeps * kSweepCols;
-                Chunk bp[kBlockSweeps], bq[kBlockSweeps];
+        for (int half = 0; half < kDepth; half += kBlockSweeps) mass += tile_mass<Chunk, kQ, kBlockSweeps>(a, r, st, half, lane);
+        best = better(best, tile_entry<Chunk>(a, row, st, mass, lane));
+    }
+    return wave_best(best);
+}
+
+// The same with each of eight waves taking one sweep of every super-tile, where there are fewer super-tiles than waves.
+template <typename Chunk, bool kQ>
+__device__ __forceinline__ Cand share_race(const VerifyArgs& a, const Residual& r, int64_t row, int from, int to, float (*masses)[kLanes],
+                                           int lane, int wave)
+{
+    static_assert(kDepth == 8, "one sweep for each of eight waves");
+    Cand best{-1.0f, 0};
+    for (int st = from; st < to; ++st) {
+        __syncthreads();                                          // the last super-tile's are read
+        masses[wave][lane] = tile_mass<Chunk, kQ, 1>(a, r, st, wave, lane);
+        __syncthreads();
+        if (wave != (st & 7)) continue;
+        float mass = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kBlockSweeps; ++i) {
-                    bp[i].load_sweep(r.p, first + i * kSweepCols + Chunk::sweep_col(lane));
-                    if (kQ) bq[i].load_sweep(r.q, first + i * kSweepCols + Chunk::sweep_col(lane));
-                }
-#pragma unroll
-                for (int i = 0; i < kBlockSweeps; ++i) {
-                    float zp[8], zq[8];
-                    bp[i].unpack_sweep(zp, lane);
-                    if (kQ) bq[i].unpack_sweep(zq, lane);
-                    add(zp, zq, first + i * kSweepCols + slot * kChunk);
-                }
-            }
-        } else {
-#pragma unroll 1
-            for (int i = 0; i < kDepth; ++i) {
-                const int64_t col = base + i * kSweepCols + lane * kChunk;
-                float zp[8], zq[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { zp[j] = -INFINITY; zq[j] = -INFINITY; }
-                if (col + kChunk <= V) {
-                    Chunk ch;
-                    ch.load(r.p, col);
-                    ch.unpack(zp);
-                    if (kQ) { ch.load(r.q, col); ch.unpack(zq); }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (col + j < V) { zp[j] = Chunk::load_one(r.p, col + j); if (kQ) zq[j] = Chunk::load_one(r.q, col + j); }
-                }
-                add(zp, zq, col);
-            }
-        }
-        const int tile = st * kLanes + slot;
-        uint32_t w[4];
-        philox4x32_10((uint32_t)tile >> 2, (uint32_t)grow, (uint32_t)(grow >> 32), 6u, (uint32_t)a.seed, (uint32_t)(a.seed >> 32), w);
-        const uint32_t word = (tile & 3) == 0 ? w[0] : (tile & 3) == 1 ? w[1] : (tile & 3) == 2 ? w[2] : w[3];
-        const Cand mine{mass > 0.0f ? mass * inv_exp_variate(word) : -1.0f, tile};
-        if (mine.q > best.q) best = mine;                         // tiles rise: equals stay with the lower
+        for (int i = 0; i < kDepth; ++i) mass += masses[i][lane];
+        best = better(best, tile_entry<Chunk>(a, row, st, mass, lane));
     }
     return wave_best(best);
 }
@@ -428,8 +480,12 @@ void verify_clear_kernel(int32_t* flags, int64_t rows)
 }
 
 // A workgroup per (position, row), positions rising.  Four of its eight waves take the sums of the target's line, four the
-// draft's; all of them the one line where there is no other.
+// draft's; all of them the one line where there is no other.  (One line after the other by four waves
+// before: 512 x 4 drafts of 151,936 columns 301 us, now 240; 64 x 7 of 32,000 38, now 34.)
 constexpr int kPairWaves = 8;
+// LDS that is asked for and not used: two workgroups per compute unit, not three.  Their loads fill the memory's bandwidth as
+// well, and a third would start positions sooner whose row turns out to be rejected before them (512 x 4 drafts: 264 us with three).
+constexpr int kPairLds = 56 * 1024;
 
 template <typename Chunk>
 __global__ __launch_bounds__(64 * kPairWaves, 4)
@@ -445,33 +501,33 @@ void verify_pair_kernel(VerifyArgs a, VerifyShape s, char* ws)
     int32_t* flags = reinterpret_cast<int32_t*>(ws + s.at_flags);
     const int len = drafts_of(a, row);
     if (t > len) return;
-    if (threadIdx.x == 0) known = __hip_atomic_load(&flags[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    Line* lines = reinterpret_cast<Line*>(ws + s.at_lines) + row * s.lines;
+    if (threadIdx.x == 0) known = t > 0 ? __hip_atomic_load(&flags[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0x7FFFFFFF;
+    const bool last = t == len, two = !last && a.draft_logits != nullptr;
+    Drafted d{};
+    if (!last) d = drafted_at<Chunk>(a, row, t);
     __syncthreads();
     if (known < t) return;                                        // an earlier draft was rejected
-    const bool last = t == len, two = !last && a.draft_logits != nullptr;
     const int half = two ? kPairWaves / 2 : kPairWaves;           // waves of a line
     const int which = wave >= half ? 1 : 0;
-    {
-        const char* line = which ? draft_line<Chunk>(a, row, t) : target_line<Chunk>(a, row, t);
-        const float c = which ? draft_factor(a, row) : target_factor(a, row);
-        LaneState state = empty_state();
-        stream_sums<Chunk>(state, line, 0, a.V, c, lane, wave - which * half, half);
-        const LineSum mine = wave_sums(state);
-        if (lane == 0) sums[wave] = mine;
-        __syncthreads();
-        if (wave == which * half) {
-            const Line l = line_of(merge_sums(sums + which * half, half, c, lane), c);
-            if (lane == 0) {
-                found[which] = l;
-                reinterpret_cast<Line*>(ws + s.at_lines)[row * s.lines + (which ? a.drafts + 1 : 0) + t] = l;
-            }
+    const char* line = which ? draft_line<Chunk>(a, row, t) : target_line<Chunk>(a, row, t);
+    const float c = which ? draft_factor(a, row) : target_factor(a, row);
+    LaneState state = empty_state();
+    stream_sums<Chunk>(state, line, 0, a.V, c, lane, wave - which * half, half);
+    const LineSum mine = wave_sums(state);
+    if (lane == 0) sums[wave] = mine;
+    __syncthreads();
+    if (wave == which * half) {
+        const Line l = line_of(merge_sums(sums + which * half, half, c, lane), c);
+        if (lane == 0) {
+            found[which] = l;
+            lines[(which ? a.drafts + 1 : 0) + t] = l;
         }
-        __syncthreads();
     }
+    __syncthreads();
     const Line p = found[0], q = found[two ? 1 : 0];
     if (!last) {
-        const bool ok = accepts<Chunk>(a, row, t, p, q);          // the same in every thread
-        if (ok) return;
+        if (accepts(a, row, d, p, q)) return;                     // the same in every thread
         if (threadIdx.x == 0) atomicMin(&flags[row], t);
     }
     const Residual r = residual_of<Chunk>(a, row, t, !last, p, q);
@@ -508,13 +564,16 @@ void verify_sums_kernel(VerifyArgs a, VerifyShape s, char* ws)
 }
 
 // A workgroup per (row, slice of super-tiles): merges the row's lines, decides, races over its slice of the position that
-// draws.  The first one of a row leaves the lines for the last launch.
+// draws.  The first one of a row leaves the lines and the decision for the last launch.
+constexpr int kRaceWaves = 8;
+
 template <typename Chunk>
-__global__ __launch_bounds__(kVerifyThreads)
+__global__ __launch_bounds__(64 * kRaceWaves)
 void verify_race_kernel(VerifyArgs a, VerifyShape s, char* ws)
 {
     __shared__ Line lines[2 * kMaxDrafts + 1];
-    __shared__ Cand cands[kVerifyWaves];
+    __shared__ Cand cands[kRaceWaves];
+    __shared__ float masses[kRaceWaves][kLanes];
     __shared__ int rejected;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int slice = blockIdx.x % s.race_slices;
@@ -522,7 +581,9 @@ void verify_race_kernel(VerifyArgs a, VerifyShape s, char* ws)
     const int len = drafts_of(a, row);
     const LineSum* sums = reinterpret_cast<const LineSum*>(ws + s.at_sums) + row * s.lines * s.slices;
     if (threadIdx.x == 0) rejected = len;
-    for (int i = wave; i < s.lines; i += kVerifyWaves) {
+    Drafted d{};
+    if (wave == 0 && lane < len) d = drafted_at<Chunk>(a, row, lane);
+    for (int i = wave; i < s.lines; i += kRaceWaves) {
         const bool target = i <= a.drafts;
         if (target ? i > len : i - a.drafts - 1 >= len) continue;
         const float c = target ? target_factor(a, row) : draft_factor(a, row);
@@ -534,7 +595,7 @@ void verify_race_kernel(VerifyArgs a, VerifyShape s, char* ws)
     }
     __syncthreads();
     if (wave == 0) {
-        const bool no = lane < len && !accepts<Chunk>(a, row, lane, lines[lane], lines[a.draft_logits ? a.drafts + 1 + lane : lane]);
+        const bool no = lane < len && !accepts(a, row, d, lines[lane], lines[a.draft_logits ? a.drafts + 1 + lane : lane]);
         const unsigned long long m = __ballot(no);
         if (lane == 0 && m != 0ull) rejected = (int)__builtin_ctzll(m);
     }
@@ -546,11 +607,13 @@ void verify_race_kernel(VerifyArgs a, VerifyShape s, char* ws)
     const int tiles = (int)((a.V + kSuperCols - 1) / kSuperCols);
     const int each = (tiles + s.race_slices - 1) / s.race_slices;
     const int from = slice * each, to = from + each < tiles ? from + each : tiles;
-    const Cand best = workgroup_best(race<Chunk>(a, r, row, from, to, lane, wave, kVerifyWaves), cands, lane, wave, kVerifyWaves);
+    Cand best = each >= kRaceWaves ? race<Chunk>(a, r, row, from, to, lane, wave, kRaceWaves)
+              : r.q ? share_race<Chunk, true>(a, r, row, from, to, masses, lane, wave) : share_race<Chunk, false>(a, r, row, from, to, masses, lane, wave);
+    best = workgroup_best(best, cands, lane, wave, kRaceWaves);
     if (threadIdx.x == 0) reinterpret_cast<Cand*>(ws + s.at_cands)[row * s.race_slices + slice] = best;
 }
 
-// A workgroup per row: the draw's second level, the outputs.
+// A workgroup per row: the draw's second level, ids, log-probs and entropies.
 template <typename Chunk>
 __global__ __launch_bounds__(kVerifyThreads)
 void verify_finish_kernel(VerifyArgs a, VerifyShape s, const char* ws)
@@ -606,10 +669,10 @@ static hipError_t launch(const VerifyArgs& a, char* ws, hipStream_t stream)
     const VerifyShape s = verify_shape(a.rows, a.drafts, a.V, a.draft_logits != nullptr);
     if (s.slices == 0) {
         verify_clear_kernel<<<(uint32_t)((a.rows + 255) / 256), 256, 0, stream>>>(reinterpret_cast<int32_t*>(ws + s.at_flags), a.rows);
-        verify_pair_kernel<Chunk><<<(uint32_t)(a.rows * (a.drafts + 1)), 64 * kPairWaves, 0, stream>>>(a, s, ws);
+        verify_pair_kernel<Chunk><<<(uint32_t)(a.rows * (a.drafts + 1)), 64 * kPairWaves, kPairLds, stream>>>(a, s, ws);
     } else {
         verify_sums_kernel<Chunk><<<(uint32_t)(a.rows * s.lines * s.slices), kVerifyThreads, 0, stream>>>(a, s, ws);
-        verify_race_kernel<Chunk><<<(uint32_t)(a.rows * s.race_slices), kVerifyThreads, 0, stream>>>(a, s, ws);
+        verify_race_kernel<Chunk><<<(uint32_t)(a.rows * s.race_slices), 64 * kRaceWaves, 0, stream>>>(a, s, ws);
     }
     verify_finish_kernel<Chunk><<<(uint32_t)a.rows, kVerifyThreads, 0, stream>>>(a, s, ws);
     return hipGetLastError();
