@@ -61,7 +61,11 @@ static VerifyShape verify_shape(int64_t rows, int32_t drafts, int64_t V, bool dr
     s.slices = 0;
     s.slice_cols = 0;
     s.race_slices = drafts + 1;
-    if (units < (int64_t)cus * 2) {
+    // Slices below two positions per compute unit (64 x 7 of 32,000 columns take the same time either way, 128 x 4 of 151,936 110 us
+    // as pairs and 122 as slices, 4 x 3 do not fill the card as pairs), and below twelve where lines are short, whose pairs are
+    // mostly waiting (300 x 3 of 10,000: 38.0 as pairs, 32.9 as slices; 1000 x 1 of 1000: 40.1 and 28.7; but 512 x 1 of 32,000
+    // 47.8 and 53.3).
+    if (units < (int64_t)cus * (V <= 16384 ? 12 : 2)) {
         // a block of four sweeps for each wave at least
         const int64_t blocks = (V + 2047) / 2048;
         int64_t per = (blocks * rows * s.lines + want - 1) / want;
