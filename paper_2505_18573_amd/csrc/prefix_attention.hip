@@ -730,7 +730,7 @@ void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
 // The partial results of a query's prefix and of its row's own tokens become its output.  What bounds it is the chain of loads
 // (lengths, list of items, results), so a wave takes several queries at once, D / 4 lanes each with four columns,
 // and asks for (m, l) and O of four parts together.
-constexpr int join_queries(int D) { return 4 * 256 / D; }          // of a workgroup
+constexpr int join_queries(int D) { return 4 * 256 / D; }          // of a workgroup at most
 
 struct Merged {
     float m, l;
@@ -748,7 +748,7 @@ __device__ __forceinline__ void merge(Merged& x, float m, float l, const f32x4& 
 // (Eight waves per SIMD: 2048 workgroups, those of 512 rows and four key heads, are then resident together.)
 template <int D>
 __global__ __launch_bounds__(256, 8)
-void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size, const char* ws)
+void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size, int per_group, const char* ws)
 {
     constexpr int kLanes4 = D / 4;                                             // lanes of a query
     __shared__ float lds[256 / kLanes4][2 + D];
@@ -758,8 +758,8 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
     const Parts* items = reinterpret_cast<const Parts*>(ws + s.at_items);
     const float2* ml = reinterpret_cast<const float2*>(ws + s.at_ml);
     const float* o = reinterpret_cast<const float*>(ws + s.at_o);
-    const int first_query = blockIdx.y * join_queries(D);
-    const int end_query = first_query + join_queries(D) < s.M ? first_query + join_queries(D) : s.M;
+    const int first_query = blockIdx.y * per_group;
+    const int end_query = first_query + per_group < s.M ? first_query + per_group : s.M;
 
     const Unit of_row = uniform(unit_at(a, s, heads, page_size, a.groups + row));
     // the row's group, the last one that begins at or before it, and its lengths, looked at by all lanes at once
@@ -853,7 +853,13 @@ static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, cons
 {
     const int workgroups = compute_units() * attend_occupancy(D, kFp8);
     attend_kernel<D, kFp8><<<workgroups, 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
-    attend_join_kernel<D><<<dim3((uint32_t)(a.rows * c.heads), (uint32_t)((s.M + join_queries(D) - 1) / join_queries(D))), 256, 0, stream>>>(a, s, c.heads, c.page_size, ws);
+    // Queries of a workgroup of the join: fewer where there are few workgroups, whose queries have many parts (12 rows x 8 heads
+    // with a prefix of 32,771: 15.4 us with all four queries together).
+    int per_group = join_queries(D) < s.M ? join_queries(D) : s.M;
+    const int64_t pairs = (int64_t)a.rows * c.heads;
+    while (per_group > 1 && pairs * ((s.M + per_group - 1) / per_group) < compute_units() * 2) per_group = (per_group + 1) / 2;
+    attend_join_kernel<D><<<dim3((uint32_t)pairs, (uint32_t)((s.M + per_group - 1) / per_group)), 256, 0, stream>>>(a, s, c.heads, c.page_size,
+                                                                                                                     per_group, ws);
     return hipGetLastError();
 }
 
