@@ -224,9 +224,14 @@ __device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendSh
     __syncthreads();
     return p;
 }
+// (in 32 bits where they do: a division in 64 takes a hundred instructions more)
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t by)
+{
+    return (uint64_t)(x | by) >> 32 == 0 ? (int64_t)((uint32_t)x / (uint32_t)by) : x / by;
+}
 // stretch w: steps [begin_of(w), begin_of(w + 1)); and the stretch that holds a step
-__device__ __forceinline__ int64_t begin_of(int w, int64_t steps, int parts) { return w * steps / parts; }
-__device__ __forceinline__ int part_of(int64_t step, int64_t steps, int parts) { return (int)(((step + 1) * parts + steps - 1) / steps) - 1; }
+__device__ __forceinline__ int64_t begin_of(int w, int64_t steps, int parts) { return divide(w * steps, parts); }
+__device__ __forceinline__ int part_of(int64_t step, int64_t steps, int parts) { return (int)divide((step + 1) * parts + steps - 1, steps) - 1; }
 
 // The unit that holds a step of a line, with the unit's first step and item; uniform.
 struct Place {
@@ -269,10 +274,15 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a, const AttendSh
             r.unit = u0 + l;
             r.step -= uniform(__shfl(own, l));
             r.item -= __builtin_amdgcn_readlane(own_items, l);
+            r.of.len = __builtin_amdgcn_readlane(x.len, l);
+            r.of.row0 = __builtin_amdgcn_readlane(x.row0, l);
+            r.of.queries = uniform(__shfl(x.queries, l));
+            r.of.items = __builtin_amdgcn_readlane(x.items, l);
+            r.of.steps = __builtin_amdgcn_readlane(x.steps, l);
+            r.of.line = line;
             break;
         }
     }
-    if (r.unit >= 0) r.of = uniform(unit_at(a, s, heads, page_size, r.unit));
     return r;
 }
 
@@ -613,8 +623,10 @@ struct Attend {
             __syncthreads();
             page = page_next;
             page_next = page_at(own + 2 * kFour);
-            mine.load_keys(c, row_of(c, task, page, own + kFour), lane);
-            mine.load_values(c, row_of(c, task, page, own + kFour), lane);
+            if (at + kFour < to) {                                         // uniform: the barriers would wait for loads of nothing
+                mine.load_keys(c, row_of(c, task, page, own + kFour), lane);
+                mine.load_values(c, row_of(c, task, page, own + kFour), lane);
+            }
             if (first < queries) {
                 for (int i = share; i < kAttendWaves && at + i * kStep < to; i += shares) {
                     Data d;
