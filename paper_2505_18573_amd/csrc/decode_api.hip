@@ -41,7 +41,7 @@ extern "C" int e3_cache_append(const e3_cache* cache, const void* k, const void*
     const int rc = check_cache(cache, &view);
     if (rc != E3_OK) return rc;
     if (dtype != E3_F32 && dtype != E3_BF16) return E3_ERR_DTYPE;
-    if (tokens < 0 || tokens * view.heads > kMostTokens) return E3_ERR_SHAPE;
+    if (tokens < 0 || tokens > kMostTokens || tokens * view.heads > kMostTokens) return E3_ERR_SHAPE;
     if (tokens == 0) return E3_OK;
     if (k == nullptr || v == nullptr || slots == nullptr) return E3_ERR_NULL;
     const int64_t per = dtype == E3_F32 ? 4 : 8;                    // elements in 16 bytes
@@ -60,7 +60,7 @@ extern "C" int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_
     const int rc = check_cache(cache, &view);
     if (rc != E3_OK) return rc;
     if (dtype != E3_F32 && dtype != E3_BF16) return E3_ERR_DTYPE;
-    if (tokens < 0 || tokens * view.heads > kMostTokens) return E3_ERR_SHAPE;
+    if (tokens < 0 || tokens > kMostTokens || tokens * view.heads > kMostTokens) return E3_ERR_SHAPE;
     if (tokens == 0) return E3_OK;
     if (k_out == nullptr || v_out == nullptr || slots == nullptr) return E3_ERR_NULL;
     if (!aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(slots, 8)) return E3_ERR_ALIGN;

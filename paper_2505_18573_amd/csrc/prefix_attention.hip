@@ -12,10 +12,11 @@
 //            memory: they change with every step).  A prefix or a row's own tokens ("unit"), a key head and a tile of
 //            queries are an item.  Items of at most 16 queries are one wave's work, larger ones (64 queries at most) a
 //            workgroup's, whose waves bring the keys into LDS for each other.  Items of either kind lie behind one another
-//            on a line, measured in a wave's steps of 32 tokens and a few more for the item itself, and every wave
-//            (workgroup) takes an equal stretch of its line, whichever items it falls into.  What it has of an item, (m, l, O),
-//            stays in registers and is left in the workspace as one partial result.  (Runs of one length dealt round robin
-//            before: rows of 1 to 6000 tokens gave the busiest workgroup 1.6 times the mean.)
+//            on a line, measured in a wave's steps of 32 tokens and a few more for the item itself.  The workgroups are
+//            divided between the two lines, and every wave (workgroup) takes an equal stretch of its line, whichever items it
+//            falls into.  What it has of an item, (m, l, O), stays in registers and is left in the workspace as one partial
+//            result.  (Runs of one length dealt round robin before: rows of 1 to 6000 tokens gave the busiest workgroup 1.6
+//            times the mean.)
 //   join     a workgroup per row and key head joins the partial results of its prefix and its own tokens.
 //
 // Registers instead of LDS: S^T = K Q^T puts the queries on the matrix instruction's columns, so a lane holds one
@@ -28,6 +29,10 @@
 // P enters its product as the sum of two bf16 numbers (sixteen bits of each weight): one alone (eight bits) would double the
 // error that the output's own rounding leaves, and the second product costs nothing where memory is what the kernel
 // waits for.  Everything else between the loads and the output is fp32.
+//
+// What bounds it: reading keys and values, 5.3 TB/s at 512 rows x 28 heads of 128 over 4 key heads with prefixes of 100 to 1000 and 1 to
+// 6000 own tokens (1.63 GB, 320 us; leaving out all products and exponentials changed nothing).  Small batches wait
+// for chains of loads: 2.5 us for the lengths, about 8 us into and out of an item, 5 us for the join.
 #include "kv_cache.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
@@ -41,10 +46,12 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStep = 32;                       // tokens of a wave's step
 constexpr int kAttendWaves = 4;
-#ifndef E3_ITEM_COST
-#define E3_ITEM_COST 4
-#endif
-constexpr int kItemCost = E3_ITEM_COST;         // what an item costs besides its steps, in steps
+// What an item costs besides its steps, in steps (a chain of loads to its page, its keys and its queries).  16 rollouts x 8 with drafts
+// 55.9 us with 2, 51.7 with 4, 53.7 with 8; 512 rows 347.7, 344.2, 345.6.
+constexpr int kItemCost = 4;
+// What a step of the workgroups' line costs against one of the waves' line, which waits for more memory.  512 rows 332 us with 0.6, 334
+// with 1 and 440 with 0.3, where the few workgroups of the prefixes end last; 12 rows with a prefix of 32,771 51.9 with 0.6, 57.6 with 1.
+constexpr float kSharedCost = 0.7f;
 constexpr int kWaveQueries = 16;                // an item of so many is a wave's
 constexpr float kNoScore = -3.0e38f;            // running maximum before any score
 constexpr float kSlack = 8.0f;                  // scores may pass the running maximum by this (2^8) before it moves
@@ -122,7 +129,7 @@ __device__ __forceinline__ int clamp_len(int n, int64_t most) { return n < 0 ? 0
 __device__ __forceinline__ int64_t table_tokens(int width, int page_size)
 {
     const int64_t n = (int64_t)width * page_size;
-    return n > 0x7FFFFF00 ? 0x7FFFFF00 : n;
+    return n > 0x7F000000 ? 0x7F000000 : n;                                    // steps beyond it stay in 32 bits
 }
 
 // The same in every lane: kept in scalar registers.
@@ -168,6 +175,7 @@ __device__ __forceinline__ Unit uniform(const Unit& x)
 struct Plan {
     int share;                                  // units of a share
     int64_t steps[2];
+    int groups;                                 // workgroups that work on the line of workgroups
     int parts[2];                               // stretches
 };
 struct PlanLds {
@@ -215,12 +223,18 @@ __device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendSh
     lds.first[1][threadIdx.x] = sum[1];
     lds.first_item[0][threadIdx.x] = (int)(uint32_t)sum[2];
     lds.first_item[1][threadIdx.x] = (int)(sum[2] >> 32);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int64_t most = (int64_t)gridDim.x * (k == kByWave ? kAttendWaves : 1);
-        p.steps[k] = uniform(all[k]);
-        p.parts[k] = (int)(p.steps[k] < most ? p.steps[k] : most);
-    }
+    p.steps[0] = uniform(all[0]);
+    p.steps[1] = uniform(all[1]);
+    // the workgroups are divided by what the lines cost; four waves of one take four steps of the waves' line at a time
+    const float of_groups = (float)p.steps[kByGroup] * kSharedCost, of_waves = (float)p.steps[kByWave] * (1.0f / kAttendWaves);
+    const int n = (int)gridDim.x;
+    int share = (int)(of_groups / (of_groups + of_waves) * (float)n + 0.5f);
+    if (p.steps[kByWave] > 0 && share > n - 1) share = n - 1;
+    if (p.steps[kByGroup] > 0 && share < 1) share = 1;
+    p.groups = p.steps[kByGroup] == 0 ? 0 : uniform(share);
+    const int64_t waves = (int64_t)(n - p.groups) * kAttendWaves;
+    p.parts[kByGroup] = (int)(p.steps[kByGroup] < p.groups ? p.steps[kByGroup] : p.groups);
+    p.parts[kByWave] = (int)(p.steps[kByWave] < waves ? p.steps[kByWave] : waves);
     __syncthreads();
     return p;
 }
@@ -724,14 +738,18 @@ void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
     Parts* items = reinterpret_cast<Parts*>(ws + s.at_items);
     float2* ml = reinterpret_cast<float2*>(ws + s.at_ml);
     float* o = reinterpret_cast<float*>(ws + s.at_o);
-    along_line<kByGroup>(a, s, c, plan, plan_lds, items, blockIdx.x, [&](const Task& task, int64_t place) {
-        const int64_t at = place * s.slot[kByGroup];
-        Attend<D, kFp8> x;
-        x.shared(c, a, s, task, lds, ml + at, o + at * D);
-    });
+    if ((int)blockIdx.x < plan.groups) {
+        along_line<kByGroup>(a, s, c, plan, plan_lds, items, blockIdx.x, [&](const Task& task, int64_t place) {
+            const int64_t at = place * s.slot[kByGroup];
+            Attend<D, kFp8> x;
+            x.shared(c, a, s, task, lds, ml + at, o + at * D);
+        });
+        return;
+    }
     // a workgroup's waves lie far apart on their line: few stretches are spread over all workgroups
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    along_line<kByWave>(a, s, c, plan, plan_lds, items, wave * (int)gridDim.x + (int)blockIdx.x, [&](const Task& task, int64_t place) {
+    const int part = wave * ((int)gridDim.x - plan.groups) + (int)blockIdx.x - plan.groups;
+    along_line<kByWave>(a, s, c, plan, plan_lds, items, part, [&](const Task& task, int64_t place) {
         const int64_t at = s.slots[kByGroup] * s.slot[kByGroup] + place * s.slot[kByWave];
         Attend<D, kFp8> x;
         x.direct(c, a, s, task, ml + at, o + at * D);
@@ -865,6 +883,8 @@ static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, cons
 {
     const int workgroups = compute_units() * attend_occupancy(D, kFp8);
     attend_kernel<D, kFp8><<<workgroups, 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
     // Queries of a workgroup of the join: fewer where there are few workgroups, whose queries have many parts (12 rows x 8 heads
     // with a prefix of 32,771: 15.4 us with all four queries together).
     int per_group = join_queries(D) < s.M ? join_queries(D) : s.M;

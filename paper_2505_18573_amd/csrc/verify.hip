@@ -673,11 +673,14 @@ static hipError_t launch(const VerifyArgs& a, char* ws, hipStream_t stream)
     const VerifyShape s = verify_shape(a.rows, a.drafts, a.V, a.draft_logits != nullptr);
     if (s.slices == 0) {
         verify_clear_kernel<<<(uint32_t)((a.rows + 255) / 256), 256, 0, stream>>>(reinterpret_cast<int32_t*>(ws + s.at_flags), a.rows);
+        if (const hipError_t err = hipGetLastError(); err != hipSuccess) return err;
         verify_pair_kernel<Chunk><<<(uint32_t)(a.rows * (a.drafts + 1)), 64 * kPairWaves, kPairLds, stream>>>(a, s, ws);
     } else {
         verify_sums_kernel<Chunk><<<(uint32_t)(a.rows * s.lines * s.slices), kVerifyThreads, 0, stream>>>(a, s, ws);
+        if (const hipError_t err = hipGetLastError(); err != hipSuccess) return err;
         verify_race_kernel<Chunk><<<(uint32_t)(a.rows * s.race_slices), 64 * kRaceWaves, 0, stream>>>(a, s, ws);
     }
+    if (const hipError_t err = hipGetLastError(); err != hipSuccess) return err;
     verify_finish_kernel<Chunk><<<(uint32_t)a.rows, kVerifyThreads, 0, stream>>>(a, s, ws);
     return hipGetLastError();
 }
