@@ -52,6 +52,10 @@ constexpr int kItemCost = 4;
 // What a step of the workgroups' line costs against one of the waves' line, which waits for more memory.  512 rows 332 us with 0.6, 334
 // with 1 and 440 with 0.3, where the few workgroups of the prefixes end last; 12 rows with a prefix of 32,771 51.9 with 0.6, 57.6 with 1.
 constexpr float kSharedCost = 0.7f;
+// Steps of a stretch at least, on average: with more the join has fewer parts, with fewer the few steps of a small batch are taken side
+// by side.  One row with 150 + 77 tokens (32 steps) 13.0 us with 1, 13.6 with 2, 15.1 with 4; with 8192 tokens (1048 steps) 24.2,
+// 20.0 and 18.4.
+__device__ __forceinline__ int least_stretch(int64_t steps) { return steps < 512 ? 1 : steps < 1024 ? 2 : 4; }
 constexpr int kWaveQueries = 16;                // an item of so many is a wave's
 constexpr float kNoScore = -3.0e38f;            // running maximum before any score
 constexpr float kSlack = 8.0f;                  // scores may pass the running maximum by this (2^8) before it moves
@@ -233,8 +237,13 @@ __device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendSh
     if (p.steps[kByGroup] > 0 && share < 1) share = 1;
     p.groups = p.steps[kByGroup] == 0 ? 0 : uniform(share);
     const int64_t waves = (int64_t)(n - p.groups) * kAttendWaves;
-    p.parts[kByGroup] = (int)(p.steps[kByGroup] < p.groups ? p.steps[kByGroup] : p.groups);
-    p.parts[kByWave] = (int)(p.steps[kByWave] < waves ? p.steps[kByWave] : waves);
+    const int64_t most[2] = {p.groups, waves};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int least = least_stretch(p.steps[k]);
+        const int64_t enough = (p.steps[k] + least - 1) / least;
+        p.parts[k] = (int)(enough < most[k] ? enough : most[k]);
+    }
     __syncthreads();
     return p;
 }
@@ -760,7 +769,7 @@ void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
 // The partial results of a query's prefix and of its row's own tokens become its output.  What bounds it is the chain of loads
 // (lengths, list of items, results), so a wave takes several queries at once, D / 4 lanes each with four columns,
 // and asks for (m, l) and O of four parts together.
-constexpr int join_queries(int D) { return 4 * 256 / D; }          // of a workgroup at most
+constexpr int join_queries(int D) { return 4 * 256 / D; }          // of a workgroup of 256 at most
 
 struct Merged {
     float m, l;
@@ -886,12 +895,12 @@ static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, cons
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     // Queries of a workgroup of the join: fewer where there are few workgroups, whose queries have many parts (12 rows x 8 heads
-    // with a prefix of 32,771: 15.4 us with all four queries together).
+    // with a prefix of 32,771: the join 8.1 us, and 15.4 with all four queries together).
     int per_group = join_queries(D) < s.M ? join_queries(D) : s.M;
     const int64_t pairs = (int64_t)a.rows * c.heads;
     while (per_group > 1 && pairs * ((s.M + per_group - 1) / per_group) < compute_units() * 2) per_group = (per_group + 1) / 2;
-    attend_join_kernel<D><<<dim3((uint32_t)pairs, (uint32_t)((s.M + per_group - 1) / per_group)), 256, 0, stream>>>(a, s, c.heads, c.page_size,
-                                                                                                                     per_group, ws);
+    const dim3 grid((uint32_t)pairs, (uint32_t)((s.M + per_group - 1) / per_group));
+    attend_join_kernel<D><<<grid, 256, 0, stream>>>(a, s, c.heads, c.page_size, per_group, ws);
     return hipGetLastError();
 }
 
