@@ -360,9 +360,10 @@ struct StepData {
         for (int i = 0; i < kVLoads; ++i) v[i] = (*reinterpret_cast<const u32x4*>(vp + i * 256));
         if (kFp8) vs = *reinterpret_cast<const u32x2*>(c.v_scale + row + g * 8);
     }
-    // A step in LDS: every lane's registers as they are, 64 lanes next to each other.
-    static constexpr int kImage = (2 * kLoads + kVLoads) * 64 * 16 + (kFp8 ? 2 * 64 * 8 : 0);         // bytes
-    __device__ __forceinline__ void put(char* to, int lane) const
+    // A step in LDS: every lane's registers as they are, 64 lanes next to each other, and the factors of its tokens in fp32 (made
+    // once for the four waves that read them: 512 rows of five tokens 306 us, 319 with the bytes).
+    static constexpr int kImage = (2 * kLoads + kVLoads) * 64 * 16 + (kFp8 ? 2 * kStep * 4 : 0);         // bytes
+    __device__ __forceinline__ void put(char* to, float c, int lane) const
     {
         u32x4* w = reinterpret_cast<u32x4*>(to) + lane;
 #pragma unroll
@@ -370,9 +371,14 @@ struct StepData {
 #pragma unroll
         for (int i = 0; i < kVLoads; ++i) w[(2 * kLoads + i) * 64] = v[i];
         if (kFp8) {
-            u32x2* e = reinterpret_cast<u32x2*>(to + (2 * kLoads + kVLoads) * 1024) + lane;
-            e[0] = ks;
-            e[64] = vs;
+            float* e = reinterpret_cast<float*>(to + (2 * kLoads + kVLoads) * 1024) + (lane >> 4) * 8;
+            if ((lane & 15) == 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    e[j] = c * k_factor(j);
+                    e[kStep + j] = v_factor(j);
+                }
+            }
         }
     }
     __device__ __forceinline__ void take(const char* from, int lane)
@@ -382,11 +388,11 @@ struct StepData {
         for (int i = 0; i < 2 * kLoads; ++i) k[i / kLoads][i % kLoads] = w[i * 64];
 #pragma unroll
         for (int i = 0; i < kVLoads; ++i) v[i] = w[(2 * kLoads + i) * 64];
-        if (kFp8) {
-            const u32x2* e = reinterpret_cast<const u32x2*>(from + (2 * kLoads + kVLoads) * 1024) + lane;
-            ks = e[0];
-            vs = e[64];
-        }
+    }
+    // of a step in LDS
+    static __device__ __forceinline__ const float* factors(const char* from, int lane)
+    {
+        return reinterpret_cast<const float*>(from + (2 * kLoads + kVLoads) * 1024) + (lane >> 4) * 8;
     }
     // K of score tile t, columns of k-step s
     __device__ __forceinline__ bf16x8 key(int t, int s) const
@@ -468,15 +474,16 @@ struct Attend {
     float m, l;
     int limit;                                  // tokens the lane's query sees (of the prefix, of the row)
 
-    // One step.  `at`: its first token; every query sees at least `sure` tokens, none more than `most`.  The keys' registers
+    // One step.  `at`: its first token; every query sees at least `sure` tokens, none more than `most`, and the tokens from there
+    // on are cleared.  key_factor, value_factor: what a token's score and weight are multiplied by.  The keys' registers
     // are free for the next step's (next_keys) as soon as the scores are there, the values' (next_values) at the end.
-    template <typename Keys, typename Values>
-    __device__ __forceinline__ void step(Data& d, int at, int sure, int most, float c, int lane, Keys next_keys, Values next_values)
+    template <typename KeyFactor, typename ValueFactor, typename Keys, typename Values>
+    __device__ __forceinline__ void step(Data& d, int at, int sure, int most, int lane, KeyFactor key_factor, ValueFactor value_factor,
+                                         Keys next_keys, Values next_values)
     {
         const int g = lane >> 4;
         const bool tail = at + kStep > sure;                              // uniform
         const int see = limit < most ? limit : most;
-        if (tail) d.clear_from(most - at - 8 * g);
         f32x4 s[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
@@ -485,7 +492,7 @@ struct Attend {
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            x[j] = s[j >> 2][j & 3] * (kFp8 ? c * d.k_factor(j) : c);
+            x[j] = s[j >> 2][j & 3] * key_factor(j);
             if (tail) x[j] = at + 8 * g + j < see ? x[j] : -INFINITY;
         }
         next_keys();
@@ -506,7 +513,7 @@ struct Attend {
         for (int j = 0; j < 8; ++j) {
             const float e = __builtin_amdgcn_exp2f(x[j] - m);
             l += e;
-            const float w = kFp8 ? e * d.v_factor(j) : e;
+            const float w = kFp8 ? e * value_factor(j) : e;
             p[j] = (__bf16)w;
             rest[j] = (__bf16)(w - (float)p[j]);
         }
@@ -603,8 +610,10 @@ struct Attend {
             const int page_after = page_at(at + 2 * kStep);
             const int64_t next = row_of(c, task, page_next, at + kStep);       // behind the last step: read for nothing
             const bool there = (uint32_t)page < (uint64_t)c.num_pages;
-            step(d, at, there ? sure : -1, there ? len : -1, scale, lane, [&] { d.load_keys(c, next, lane); },
-                 [&] { d.load_values(c, next, lane); });
+            const int most = there ? len : -1;
+            if (at + kStep > (there ? sure : -1)) d.clear_from(most - at - 8 * (lane >> 4));
+            step(d, at, there ? sure : -1, most, lane, [&](int j) { return kFp8 ? scale * d.k_factor(j) : scale; },
+                 [&](int j) { return d.v_factor(j); }, [&] { d.load_keys(c, next, lane); }, [&] { d.load_values(c, next, lane); });
             page = page_next;
             page_next = page_after;
         }
@@ -641,8 +650,10 @@ struct Attend {
         const float scale = a.scale * kLog2eF;
         for (int at = task.from; at < to; at += kFour, own += kFour) {
             __syncthreads();                                               // the last four (or the last task) are done with
-            mine.put(lds + wave * Data::kImage, lane);
-            if (lane == 0) there[wave] = (uint32_t)page < (uint64_t)c.num_pages;
+            const bool has = (uint32_t)page < (uint64_t)c.num_pages;
+            if (own + kStep > (has ? sure : -1)) mine.clear_from((has ? len : -1) - own - 8 * g);
+            mine.put(lds + wave * Data::kImage, scale, lane);
+            if (lane == 0) there[wave] = has;
             __syncthreads();
             page = page_next;
             page_next = page_at(own + 2 * kFour);
@@ -655,7 +666,9 @@ struct Attend {
                     Data d;
                     d.take(lds + i * Data::kImage, lane);
                     const bool is = uniform(there[i]) != 0;
-                    step(d, at + i * kStep, is ? sure : -1, is ? len : -1, scale, lane, nothing, nothing);
+                    const float* factors = Data::factors(lds + i * Data::kImage, lane);
+                    step(d, at + i * kStep, is ? sure : -1, is ? len : -1, lane, [&](int j) { return kFp8 ? factors[j] : scale; },
+                         [&](int j) { return factors[kStep + j]; }, nothing, nothing);
                 }
             }
         }
