@@ -465,6 +465,8 @@ int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
  *               Lengths are cut to what the tables can hold; a page id outside the cache
  *               hides its tokens.  Table entries behind a length are not read.  Whatever the cache
  *               holds behind a length (NaN included) has no influence.
+ * Elements that are not finite: one of V makes its column of every query that sees it NaN or
+ *               infinite, one of K or q the queries' rows NaN (a score of -inf is a weight of zero).
  * scale         host, finite and > 0 (E3_ERR_VALUE).
  * out           [rows][queries][q_heads][head_dim] bf16, contiguous, 16-byte aligned.
  * lse_out       [rows][queries][q_heads] fp32 or NULL.

@@ -15,6 +15,10 @@
 // eight tokens of the call fill a block (a prompt does that all along, wherever it starts in the call), the wave
 // in whose window they start has their values transposed in registers and writes the block whole; a token whose
 // block is not filled by its neighbours is written element by element.
+//
+// What bounds it: memory for prompts (60,001 tokens x 4 heads of 128: 123 MB of bf16 into 62 MB of codes 42 us, 4.4 TB/s; back
+// 31 us, 6.0 TB/s, part of the codes still in the memory-side cache), the launch and its chain of two loads (slot, row) for a step's
+// tokens (512: 5.4 us in, 4.3 us back).
 #include "kv_cache.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"

@@ -30,9 +30,11 @@
 // error that the output's own rounding leaves, and the second product costs nothing where memory is what the kernel
 // waits for.  Everything else between the loads and the output is fp32.
 //
-// What bounds it: reading keys and values, 5.3 TB/s at 512 rows x 28 heads of 128 over 4 key heads with prefixes of 100 to 1000 and 1 to
-// 6000 own tokens (1.63 GB, 320 us; leaving out all products and exponentials changed nothing).  Small batches wait
-// for chains of loads: 2.5 us for the lengths, about 8 us into and out of an item, 5 us for the join.
+// What bounds it: reading keys and values, 5.1 TB/s at 512 rows x 28 heads of 128 over 4 key heads with prefixes of 100 to 1000 and 1 to
+// 6000 own tokens (1.63 GB, 322 us; leaving out all products and exponentials changed nothing).  Small batches wait
+// for chains of loads: 2.5 us for the lengths, about 8 us into and out of an item, 5 us for the join.  With several tokens a row
+// the workgroups' line does more work per byte: 512 rows x 5 tokens with 500 + 5 to 2000 take 306 us at 2.0 TB/s, the vector
+// units busy for half of the waves' time (64 of a step's 240 instructions widen codes), the rest of it barriers and LDS.
 #include "kv_cache.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
@@ -49,9 +51,10 @@ constexpr int kAttendWaves = 4;
 // What an item costs besides its steps, in steps (a chain of loads to its page, its keys and its queries).  16 rollouts x 8 with drafts
 // 55.9 us with 2, 51.7 with 4, 53.7 with 8; 512 rows 347.7, 344.2, 345.6.
 constexpr int kItemCost = 4;
-// What a step of the workgroups' line costs against one of the waves' line, which waits for more memory.  512 rows 332 us with 0.6, 334
-// with 1 and 440 with 0.3, where the few workgroups of the prefixes end last; 12 rows with a prefix of 32,771 51.9 with 0.6, 57.6 with 1.
-constexpr float kSharedCost = 0.7f;
+// What a step of the workgroups' line costs against one of the waves' line, which waits for more memory.  12 rows with a
+// prefix of 32,771 tokens 52.3 us with 0.6, 58.2 with 1; 512 rows 332 with 0.5 to 0.7, 333 with 1 and 440 with 0.3, where the few
+// workgroups of the prefixes end last.
+constexpr float kSharedCost = 0.6f;
 // Steps of a stretch at least, on average: with more the join has fewer parts, with fewer the few steps of a small batch are taken side
 // by side.  One row with 150 + 77 tokens (32 steps) 13.0 us with 1, 13.6 with 2, 15.1 with 4; with 8192 tokens (1048 steps) 24.2,
 // 20.0 and 18.4.
