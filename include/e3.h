@@ -430,7 +430,7 @@ typedef struct {
  * slots     [tokens] int64: where each goes.  A slot outside the cache (negative, say: padding)
  *           is skipped.  Slots are expected to differ within a call; which of two tokens with one
  *           slot is kept is not specified (elements and scale may then be of different tokens).
- * tokens == 0 is a no-op.
+ * tokens == 0 is a no-op; tokens * kv_heads is at most 2^28 (E3_ERR_SHAPE), here and in e3_cache_read.
  */
 int e3_cache_append(const e3_cache* cache, const void* k, const void* v, int dtype, int64_t tokens,
                     int64_t k_token_stride, int64_t k_head_stride,
@@ -457,7 +457,7 @@ int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
  * q             [rows][queries][q_heads][head_dim] bf16, strides in elements, columns next to
  *               each other; base and strides multiples of 16 bytes (E3_ERR_ALIGN).
  * rows, queries, q_heads   q_heads a multiple of kv_heads (E3_ERR_SHAPE); one query per row is
- *               the ordinary step, more are drafted tokens to be verified.
+ *               the ordinary step, more are drafted tokens to be verified.  rows * kv_heads below 2^24.
  * group_offsets [num_groups + 1] int32, group_offsets[num_groups] = rows (the caller's contract);
  *               NULL with num_groups == 0: no prefixes.  A row in no group has none.
  * prefix_pages  [num_groups][prefix_width] int32, prefix_lens [num_groups] int32 (tokens).
@@ -508,7 +508,7 @@ int e3_prefix_attention(const e3_cache* cache, const void* q, int64_t rows, int6
  * draft_tokens  [rows][drafts] int32 (NULL only when drafts == 0).  An id outside [0, V) is rejected.
  * draft_lens    [rows] int32 or NULL: drafts of each row (cut to 0 .. drafts); positions behind a
  *               row's last draft and the one after it are not read.
- * drafts        0 .. E3_MAX_DRAFTS.
+ * drafts        0 .. E3_MAX_DRAFTS; rows * (drafts + 1) below 2^23 (E3_ERR_SHAPE).
  * tau_rows, tau_scalar  as for e3_sample_entropy;  draft_tau_rows [rows] or NULL: the drafts'
  *               temperature, NULL: the target's.
  * accepted_out  [rows] int32 = n.

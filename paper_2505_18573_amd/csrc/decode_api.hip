@@ -28,7 +28,7 @@ int check_cache(const e3_cache* c, e3::CacheView* view)
     return E3_OK;
 }
 
-constexpr int64_t kMostTokens = (int64_t)1 << 31;   // of one call: the grid's limit lies far above it
+constexpr int64_t kMostTokens = (int64_t)1 << 28;   // tokens x heads of one call: eight a wave, its threads below 2^32
 
 }  // namespace
 
@@ -122,12 +122,12 @@ extern "C" int e3_prefix_attention(const e3_cache* cache, const void* q, int64_t
 static bool verify_dims(int64_t rows, int32_t drafts, int64_t V)
 {
     return rows >= 0 && drafts >= 0 && drafts <= E3_MAX_DRAFTS && V >= 1 && V <= 0x7FFFFFFF - 8192 && e3::vocab_pass_fits(V) &&
-           rows * (drafts + 1) <= 0x7FFFFFFF;
+           rows * (drafts + 1) < 1 << 23;                            // workgroups of 512: threads below 2^32
 }
 
 extern "C" size_t e3_verify_workspace_bytes(int64_t rows, int32_t drafts, int64_t V)
 {
-    return rows > 0 && rows <= 0x7FFFFFFF && verify_dims(rows, drafts, V) ? e3::verify_workspace_bytes(rows, drafts, V) : 0;
+    return rows > 0 && rows < 1 << 23 && verify_dims(rows, drafts, V) ? e3::verify_workspace_bytes(rows, drafts, V) : 0;
 }
 
 extern "C" int e3_verify_drafts(const void* logits, int dtype, int64_t rows, int32_t drafts, int64_t V,
@@ -141,7 +141,7 @@ extern "C" int e3_verify_drafts(const void* logits, int dtype, int64_t rows, int
 {
     static_assert(E3_MAX_DRAFTS == e3::kMaxDrafts, "one lane per position");
     if (dtype != E3_F32 && dtype != E3_BF16) return E3_ERR_DTYPE;
-    if (rows > 0x7FFFFFFF || !verify_dims(rows, drafts, V) || position_stride < V) return E3_ERR_SHAPE;
+    if (rows >= 1 << 23 || !verify_dims(rows, drafts, V) || position_stride < V) return E3_ERR_SHAPE;
     if (draft_logits != nullptr && drafts > 0 && draft_position_stride < V) return E3_ERR_SHAPE;
     if (tau_rows == nullptr && !(std::isfinite(tau_scalar) && tau_scalar > 0.0f)) return E3_ERR_VALUE;
     if (rows == 0) return E3_OK;

@@ -102,7 +102,7 @@ static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads
 {
     s.R = (int32_t)(q_heads / heads);
     const int64_t M = T * s.R;
-    if (M > (1 << 16)) return false;
+    if (M > (1 << 16) || rows * heads >= (1 << 24)) return false;              // threads of the join: below 2^32
     s.M = (int32_t)M;
     s.units = (int32_t)(groups + rows);
     // an item, or a part of it, per place: no more parts than items and workers together
@@ -728,13 +728,13 @@ __device__ __forceinline__ void along_line(const AttentionArgs& a, const AttendS
         task.of = u.of;
         const int64_t place = (int64_t)part + u.item + item;
         if (real_to > 0) {
-            // (groups that overlap, against the contract, could exceed the places)
+            // (groups that overlap, against the contract, could exceed the places, or the 32 bits that items are counted in)
             if (from <= kItemCost && lane == 0) {                              // the item's first part
                 const int last = part_of(at - from + u.of.steps - 1, plan.steps[kLine], plan.parts[kLine]);
                 const int64_t i = first_item(s, a.rows, c.heads, u.unit < a.groups, u.unit, u.of.row0) + item;
-                items[i] = Parts{(int)place, place + (last - part) < s.slots[kLine] ? last - part + 1 : 0};
+                items[i] = Parts{(int)place, place >= 0 && place + (last - part) < s.slots[kLine] ? last - part + 1 : 0};
             }
-            if (place < s.slots[kLine]) f(task, place);
+            if (place >= 0 && place < s.slots[kLine]) f(task, place);
         }
         at += n;
         if (at < end && item + 1 == u.of.items && from + n == u.of.steps) {

@@ -65,6 +65,14 @@ def test_argument_checks_without_gpu():
     assert append(cache_struct(), dtype=0, strides=(256, 130, 256, 128)) == -4
 
 
+def test_calls_beyond_a_launch_are_refused():
+    # more than 2^28 tokens times heads: the launch would pass 2^32 threads
+    L, c = e3.lib(), cache_struct(heads=16)
+    for tokens in ((1 << 24) + 1, 1 << 28):
+        assert L.e3_cache_append(C.byref(c), 0x1000, 0x2000, 1, tokens, 0, 0, 0, 0, 0x3000, None) == -2
+        assert L.e3_cache_read(C.byref(c), 0x3000, tokens, 0x1000, 0x2000, 1, None) == -2
+
+
 def test_binding_refuses():
     with pytest.raises(TypeError):
         e3.new_cache(2, 64, 1, 64, torch.float16, device="cpu")

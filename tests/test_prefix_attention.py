@@ -42,6 +42,12 @@ def test_argument_checks_without_gpu():
     assert call(rows=0, q=None, out=None, rl=None, ws=None) == 0
 
 
+def test_shapes_beyond_a_launch_are_refused():
+    # 2^24 rows times key heads: the join would pass 2^32 threads
+    assert e3.e3_prefix_attention_workspace_bytes((1 << 23) - 1, 1, 2, 2, 64, 0) > 0
+    assert e3.e3_prefix_attention_workspace_bytes(1 << 23, 1, 2, 2, 64, 0) == 0
+
+
 class Step:
     """One decode step's inputs, and its keys and values in 64 bits."""
 

@@ -108,6 +108,12 @@ def test_argument_checks_without_gpu():
     assert call(rows=0, z=None, x=None, acc=None, tok=None, ws=None) == 0
 
 
+def test_shapes_beyond_a_launch_are_refused():
+    # 2^23 positions: their workgroups would pass 2^32 threads
+    assert e3.e3_verify_workspace_bytes((1 << 21) - 1, 3, 8) > 0
+    assert e3.e3_verify_workspace_bytes(1 << 21, 3, 8) == 0 and e3.e3_verify_workspace_bytes(1 << 23, 0, 8) == 0
+
+
 def test_the_restatement_draws_from_the_target():
     # whatever the drafter, the first token is distributed as p_0, the second (where there is one) as p_1
     rng = np.random.default_rng(0)
