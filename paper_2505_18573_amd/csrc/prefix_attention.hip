@@ -817,14 +817,22 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
     const int end_query = first_query + per_group < s.M ? first_query + per_group : s.M;
 
     const Unit of_row = uniform(unit_at(a, s, heads, page_size, a.groups + row));
-    // the row's group, the last one that begins at or before it, and its lengths, looked at by all lanes at once
-    int group = -1;
+    // The row's group is the last one that begins at or before it.  All lanes look, at a 64th of the groups each until there are no
+    // more than 64 left, whose lengths they ask for as well.  (64 after 64 from the first on before: 512 groups of eight rows
+    // and four key heads 104 us, now 74.)
+    int group = -1, left = a.groups;
+    while (left > 64) {
+        const int apart = (left + 63) / 64, at = lane * apart;
+        const int n = (int)__popcll(__ballot(at < left && a.group_offsets[group + 1 + (at < left ? at : 0)] <= row));
+        if (n == 0) { left = 0; break; }                                       // before the first group
+        group += (n - 1) * apart;
+        left = left - (n - 1) * apart < apart ? left - (n - 1) * apart : apart;
+    }
     Unit of_prefix{};
-    for (int g0 = 0; g0 < a.groups; g0 += 64) {
-        const int g = g0 + lane < a.groups ? g0 + lane : a.groups - 1;
+    if (left > 0) {
+        const int g = group + 1 + (lane < left ? lane : left - 1);
         const Unit x = unit_at(a, s, heads, page_size, g);
-        const unsigned long long begun = __ballot(g0 + lane < a.groups && a.group_offsets[g] <= row);
-        const int n = (int)__popcll(begun);
+        const int n = (int)__popcll(__ballot(lane < left && a.group_offsets[g] <= row));
         if (n > 0) {
             group += n;
             of_prefix.row0 = __builtin_amdgcn_readlane(x.row0, n - 1);
@@ -832,7 +840,6 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
             of_prefix.items = __builtin_amdgcn_readlane(x.items, n - 1);
             of_prefix.line = __builtin_amdgcn_readlane(x.line, n - 1);
         }
-        if (n < 64) break;
     }
     const int prefix_query = (row - of_prefix.row0) * s.M;
 

@@ -157,6 +157,18 @@ def test_no_groups_and_rows_without_any_key(cache_type):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("groups", [64, 65, 130, 4200])
+def test_many_groups(groups):
+    # a row finds its group among more than 64, and more than 64 * 64, of them; most are empty where there are very many
+    sizes = [(g * 7 % 3 if groups < 1000 else int(g % 17 == 3 or g == groups - 1)) for g in range(groups)]
+    prefix = [1 + g * 5 % 40 for g in range(groups)]
+    rows_len = [r % 35 for r in range(sum(sizes))]
+    s = Step(sizes, prefix, rows_len, 1, 3, 1, 64, 64, FP8, seed=groups)
+    out, lse = e3.e3_prefix_attention(s.q.to(DEV), *s.args())
+    s.check(out, lse)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("cache_type,H,prefix,rows_len", [
     (FP8, 8, 40_003, [7, 1200, 0]),          # a long prefix in many runs, joined for every row
     (BF16, 2, 3, [150_017, 20, 33]),         # a long row of its own
