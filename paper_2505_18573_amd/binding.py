@@ -703,6 +703,11 @@ def _float_type(dtype) -> int:
     return _FLOATS[dtype]
 
 
+def _step(t: torch.Tensor, dim: int) -> int:
+    """A dimension's stride; one of a single element has none of its own (torch may report anything)."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
 def e3_cache_append(cache: E3Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Write keys and values [tokens, heads, D] (bf16 or fp32, any strides with columns next to each other) to the slots
     (int64 [tokens]; negative: skipped) of the cache."""
@@ -716,7 +721,7 @@ def e3_cache_append(cache: E3Cache, k: torch.Tensor, v: torch.Tensor, slots: tor
         if t.dtype is not k.dtype or t.shape != (n, c.kv_heads, c.head_dim) or t.device != dev or (n and t.stride(2) != 1):
             raise ValueError(f"{name} must be a {k.dtype} tensor [{n}, {c.kv_heads}, {c.head_dim}] with unit column stride on {dev}")
     _check(slots, torch.int64, n, "slots", dev)
-    rc = lib().e3_cache_append(C.byref(c), _ptr(k), _ptr(v), dt, n, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+    rc = lib().e3_cache_append(C.byref(c), _ptr(k), _ptr(v), dt, n, _step(k, 0), _step(k, 1), _step(v, 0), _step(v, 1),
                                _ptr(slots), _stream(dev))
     if rc != E3_OK:
         raise E3Error(rc, "e3_cache_append")
@@ -798,7 +803,7 @@ def e3_prefix_attention(q: torch.Tensor, cache: E3Cache, group_offsets: Optional
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-    rc = lib().e3_prefix_attention(C.byref(c), _ptr(q), rows, T, q_heads, q.stride(0), q.stride(1), q.stride(2),
+    rc = lib().e3_prefix_attention(C.byref(c), _ptr(q), rows, T, q_heads, _step(q, 0), _step(q, 1), _step(q, 2),
                                    _ptr(group_offsets) if groups else None, groups, _ptr(prefix_pages), prefix_width,
                                    _ptr(prefix_lens), _ptr(row_pages), row_width, _ptr(row_lens), float(scale),
                                    _ptr(out), _ptr(lse_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
@@ -841,8 +846,8 @@ def e3_verify_drafts(logits: torch.Tensor, draft_tokens: Optional[torch.Tensor],
     drafts, dev = positions - 1, logits.device
     row_stride, position_stride = _positions(logits, "logits", logits.dtype, (rows, positions, V), dev)
     draft_strides = (0, 0)
-    if draft_logits is not None:
-        draft_strides = _positions(draft_logits, "draft_logits", logits.dtype, (rows, drafts, V), dev)
+    if draft_logits is not None:                # (without drafts an empty tensor, whose strides say nothing)
+        draft_strides = _positions(draft_logits, "draft_logits", logits.dtype, (rows, drafts, V), dev) if drafts else (0, 0)
     if draft_tokens is not None or drafts > 0:
         if (draft_tokens is None or draft_tokens.dtype is not torch.int32 or tuple(draft_tokens.shape) != (rows, drafts)
                 or not draft_tokens.is_contiguous() or draft_tokens.device != dev):

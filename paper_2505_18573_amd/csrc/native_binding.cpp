@@ -457,6 +457,9 @@ int float_type(Reader& r, at::ScalarType t)
     return t == at::kFloat ? E3_F32 : E3_BF16;
 }
 
+// a dimension's stride; one of a single element has none of its own
+int64_t step_of(const at::Tensor* t, int64_t dim) { return t->size(dim) > 1 ? t->stride(dim) : 0; }
+
 // cache, k, v, slots; True where it was done
 PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
 {
@@ -475,8 +478,8 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
                 || t->size(2) != cache.c.head_dim || t->device() != r.dev || (n > 0 && t->stride(2) != 1)) return unusual();
         const int type = float_type(r, k->scalar_type());
         return run(r, [&](void* s) {
-                       return p_cache_append(&cache.c, k->data_ptr(), v->data_ptr(), type, n, k->stride(0), k->stride(1), v->stride(0),
-                                             v->stride(1), (const int64_t*)ps, s);
+                       return p_cache_append(&cache.c, k->data_ptr(), v->data_ptr(), type, n, step_of(k, 0), step_of(k, 1), step_of(v, 0),
+                                             step_of(v, 1), (const int64_t*)ps, s);
                    },
                    [&]() -> PyObject* { Py_RETURN_TRUE; });
     });
@@ -545,7 +548,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         const Workspace ws(r, a[10] == Py_False ? Py_True : a[10], need, true);       // False is no workspace here: left to binding.py
         if (a[10] == Py_None && need > 0 && ws.p == nullptr) return unusual();         // no memory: reported there
         return run(r, [&](void* s) {
-                       return p_attention(&cache.c, q->data_ptr(), rows, T, heads, q->stride(0), q->stride(1), q->stride(2),
+                       return p_attention(&cache.c, q->data_ptr(), rows, T, heads, step_of(q, 0), step_of(q, 1), step_of(q, 2),
                                           groups > 0 ? (const int32_t*)offsets : nullptr, groups, prefix_pages, prefix_width, (const int32_t*)prefix_lens,
                                           row_pages, row_width, (const int32_t*)row_lens, (float)scale, out.p, (float*)lse.p, ws.p, ws.bytes, s);
                    },
@@ -578,7 +581,7 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n_args)
             const at::Tensor* t = r.plain(a[2]);
             if (t == nullptr || t->scalar_type() != z->scalar_type() || t->dim() != 3 || t->size(0) != rows || t->size(1) != drafts
                 || t->size(2) != V || t->device() != r.dev) return unusual();
-            strides(t, &draft_row, &draft_position);
+            if (drafts > 0) strides(t, &draft_row, &draft_position);
             d = t->data_ptr();
         }
         const void* tokens = nullptr;

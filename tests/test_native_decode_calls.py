@@ -132,3 +132,35 @@ def test_tensors_on_the_host_are_refused(name, monkeypatch):
     for native in (False, True):
         kind, text = _outcome(f, kw, monkeypatch, native)
         assert kind is ValueError and "GPU" in text
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_strides_of_single_elements_do_not_count(native, monkeypatch):
+    # torch may report anything as the stride of a dimension of one
+    e3.lib()
+    if not native:
+        monkeypatch.setattr(e3.binding, "_native", None)
+    g = torch.Generator().manual_seed(4)
+    data = torch.randn(256, generator=g).to(DEV)
+    slots = torch.tensor([5, 6, 9], device=DEV)
+    for shape, strides, heads in (((1, 2, 64), (5, 64, 1), 2), ((3, 1, 64), (64, 3, 1), 1)):
+        x = data.as_strided(shape, strides)
+        caches = [e3.new_cache(1, 32, heads, 64, device=DEV) for _ in range(2)]
+        e3.e3_cache_append(caches[0], x, x, slots[:shape[0]])
+        e3.e3_cache_append(caches[1], x.flatten().reshape(shape), x.flatten().reshape(shape), slots[:shape[0]])
+        for a, b in zip(*caches):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    cache = e3.new_cache(1, 32, 2, 64, torch.bfloat16, device=DEV)
+    e3.e3_cache_append(cache, data[:128].reshape(1, 2, 64), data[128:].reshape(1, 2, 64), torch.zeros(1, dtype=torch.int64, device=DEV))
+    q = data.to(torch.bfloat16).as_strided((1, 1, 4, 64), (13, 7, 64, 1))
+    i32 = lambda t: torch.tensor(t, dtype=torch.int32, device=DEV)
+    args = (cache, None, None, None, i32([[0]]), i32([1]), 0.125)
+    out, lse = e3.e3_prefix_attention(q, *args)
+    want, want_lse = e3.e3_prefix_attention(data.to(torch.bfloat16).reshape(1, 1, 4, 64), *args)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    # no drafts, and an empty tensor of their logits whose strides are odd
+    z = torch.randn((2, 1, 104), generator=g).to(DEV)[..., :101]
+    a = e3.e3_verify_drafts(z, None, torch.empty((2, 0, 101), device=DEV), None, None, 1.0, 3)
+    b = e3.e3_verify_drafts(z, None, None, None, None, 1.0, 3)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
