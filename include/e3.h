@@ -473,8 +473,7 @@ int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
  * workspace     device, 256-byte aligned (E3_ERR_ALIGN), at least
  *               e3_prefix_attention_workspace_bytes() (else E3_ERR_WORKSPACE); contents on entry
  *               ignored, no state between calls, to be used by one call at a time.
- * Scores, maxima, sums and the output's sums in fp32; the weights enter the product with V with
- * sixteen bits.  Where the keys are cut into runs depends on the lengths, so a row in another
+ * Scores, maxima, weights, sums and the output's sums in fp32.  Where the keys are cut into runs depends on the lengths, so a row in another
  * batch may differ in the last bits; the same call gives the same bits.
  * e3_prefix_attention_workspace_bytes: host only; 0 for a shape that is not served.
  */

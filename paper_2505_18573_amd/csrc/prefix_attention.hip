@@ -26,14 +26,15 @@
 // tokens of a column together (kv_cache.h), so V^T comes from memory in that form too.
 //
 // An 8-bit cache is widened to bf16 (exactly) and its powers of two are applied to the scores and to P, both in fp32.
-// P enters its product as the sum of two bf16 numbers (sixteen bits of each weight): one alone (eight bits) would double the
-// error that the output's own rounding leaves, and the second product costs nothing where memory is what the kernel
-// waits for.  Everything else between the loads and the output is fp32.
+// P enters its product as the sum of three bf16 numbers, which hold all 24 bits of an fp32 weight, so everything between the
+// loads and the output's own rounding is fp32.  Two of them (sixteen bits) would leave up to 2^-18 of each weight, visible where
+// the terms of an output cancel; the third product costs nothing where memory is what the kernel waits for (512 rows
+// below: 332.7 us, 333.0 with two), and 8 % where it is not (512 rows x 5 tokens: 329 us, 305 with two).
 //
 // What bounds it: reading keys and values, 5.1 TB/s at 512 rows x 28 heads of 128 over 4 key heads with prefixes of 100 to 1000 and 1 to
 // 6000 own tokens (1.63 GB, 322 us; leaving out all products and exponentials changed nothing).  Small batches wait
 // for chains of loads: 2.5 us for the lengths, about 8 us into and out of an item, 5 us for the join.  With several tokens a row
-// the workgroups' line does more work per byte: 512 rows x 5 tokens with 500 + 5 to 2000 take 306 us at 2.0 TB/s, the vector
+// the workgroups' line does more work per byte: 512 rows x 5 tokens with 500 + 5 to 2000 take 329 us at 1.9 TB/s, the vector
 // units busy for half of the waves' time (64 of a step's 240 instructions widen codes), the rest of it barriers and LDS.
 #include "kv_cache.h"
 #include "vocab_common.h"
@@ -364,7 +365,7 @@ struct StepData {
         if (kFp8) vs = *reinterpret_cast<const u32x2*>(c.v_scale + row + g * 8);
     }
     // A step in LDS: every lane's registers as they are, 64 lanes next to each other, and the factors of its tokens in fp32 (made
-    // once for the four waves that read them: 512 rows of five tokens 306 us, 319 with the bytes).
+    // once for the four waves that read them: with the bytes 512 rows of five tokens take 13 us longer).
     static constexpr int kImage = (2 * kLoads + kVLoads) * 64 * 16 + (kFp8 ? 2 * kStep * 4 : 0);         // bytes
     __device__ __forceinline__ void put(char* to, float c, int lane) const
     {
@@ -511,14 +512,16 @@ struct Attend {
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) o[b] *= f;
         }
-        bf16x8 p, rest;
+        bf16x8 p, rest, last;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float e = __builtin_amdgcn_exp2f(x[j] - m);
             l += e;
             const float w = kFp8 ? e * value_factor(j) : e;
             p[j] = (__bf16)w;
-            rest[j] = (__bf16)(w - (float)p[j]);
+            const float left = w - (float)p[j];
+            rest[j] = (__bf16)left;
+            last[j] = (__bf16)(left - (float)rest[j]);
         }
         // Tokens that some queries see and others do not: a weight of zero keeps them out, unless the value is no
         // finite number.  Such values leave the product, and one more counts those that a query sees.
@@ -538,7 +541,7 @@ struct Attend {
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             const bf16x8 value = d.value(b);
-            o[b] = mfma(value, rest, mfma(value, p, o[b]));
+            o[b] = mfma(value, last, mfma(value, rest, mfma(value, p, o[b])));
         }
         next_values();
     }
