@@ -37,6 +37,7 @@
 // the workgroups' line does more work per byte: 512 rows x 5 tokens with 500 + 5 to 2000 take 329 us at 1.9 TB/s, the vector
 // units busy for half of the waves' time (64 of a step's 240 instructions widen codes), the rest of it barriers and LDS.
 #include "kv_cache.h"
+#include "stretch.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
 
@@ -251,15 +252,6 @@ __device__ __forceinline__ Plan make_plan(const AttentionArgs& a, const AttendSh
     __syncthreads();
     return p;
 }
-// (in 32 bits where they do: a division in 64 takes a hundred instructions more)
-__device__ __forceinline__ int64_t divide(int64_t x, int64_t by)
-{
-    return (uint64_t)(x | by) >> 32 == 0 ? (int64_t)((uint32_t)x / (uint32_t)by) : x / by;
-}
-// stretch w: steps [begin_of(w), begin_of(w + 1)); and the stretch that holds a step
-__device__ __forceinline__ int64_t begin_of(int w, int64_t steps, int parts) { return divide(w * steps, parts); }
-__device__ __forceinline__ int part_of(int64_t step, int64_t steps, int parts) { return (int)divide((step + 1) * parts + steps - 1, steps) - 1; }
-
 // The unit that holds a step of a line, with the unit's first step and item; uniform.
 struct Place {
     int unit, item;
@@ -717,9 +709,8 @@ __device__ __forceinline__ void along_line(const AttentionArgs& a, const AttendS
     const int64_t end = begin_of(part + 1, plan.steps[kLine], plan.parts[kLine]);
     Place u = place_of(a, s, c.heads, c.page_size, plan, lds, kLine, at);
     while (at < end && u.unit >= 0) {
-        const int off = (int)(at - u.step);                                    // in the unit
-        const int item = off / u.of.steps, from = off % u.of.steps;
-        const int n = end - at < u.of.steps - from ? (int)(end - at) : u.of.steps - from;
+        const Piece piece = piece_at(at - u.step, end - at, u.of.steps);
+        const int item = piece.item, from = piece.from, n = piece.n;
         const int apart = round_tokens(u.of.queries);
         const int real_from = from > kItemCost ? from - kItemCost : 0, real_to = from + n - kItemCost;
         Task task;
