@@ -457,7 +457,8 @@ int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
  * q             [rows][queries][q_heads][head_dim] bf16, strides in elements, columns next to
  *               each other; base and strides multiples of 16 bytes (E3_ERR_ALIGN).
  * rows, queries, q_heads   q_heads a multiple of kv_heads (E3_ERR_SHAPE); one query per row is
- *               the ordinary step, more are drafted tokens to be verified.  rows * kv_heads below 2^24.
+ *               the ordinary step, more are drafted tokens to be verified: few of them, since every tile
+ *               of queries reads all of the row's tokens.  rows * kv_heads below 2^24.
  * group_offsets [num_groups + 1] int32, group_offsets[num_groups] = rows (the caller's contract);
  *               NULL with num_groups == 0: no prefixes.  A row in no group has none.
  * prefix_pages  [num_groups][prefix_width] int32, prefix_lens [num_groups] int32 (tokens).
@@ -465,8 +466,10 @@ int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
  *               Lengths are cut to what the tables can hold; a page id outside the cache
  *               hides its tokens.  Table entries behind a length are not read.  Whatever the cache
  *               holds behind a length (NaN included) has no influence.
- * Elements that are not finite: one of V makes its column of every query that sees it NaN or
- *               infinite, one of K or q the queries' rows NaN (a score of -inf is a weight of zero).
+ * Elements that are not finite: one of V, infinite ones too, makes its column of every query that sees it NaN
+ *               (or infinite), one of K or q the queries' rows NaN (a score of -inf is a weight of zero).
+ *               Sums are divided at the end and weights reach 2^8 in them: a sum of 2^128 and more overflows,
+ *               which values of V below 2^119 / (tokens that a query sees) cannot reach.
  * scale         host, finite and > 0 (E3_ERR_VALUE).
  * out           [rows][queries][q_heads][head_dim] bf16, contiguous, 16-byte aligned.
  * lse_out       [rows][queries][q_heads] fp32 or NULL.

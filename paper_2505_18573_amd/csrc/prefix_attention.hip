@@ -98,7 +98,7 @@ __device__ __forceinline__ int64_t first_item(const AttendShape& s, int rows, in
 }
 
 // Workgroups per compute unit, which are waves per SIMD, that the registers allow.
-constexpr int attend_occupancy(int64_t D, bool fp8) { return D == 64 ? 3 : 2; }
+constexpr int attend_occupancy(int64_t D) { return D == 64 ? 3 : 2; }
 
 static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int64_t groups, AttendShape& s)
 {
@@ -108,7 +108,7 @@ static bool attend_shape(int64_t rows, int64_t T, int64_t q_heads, int64_t heads
     s.M = (int32_t)M;
     s.units = (int32_t)(groups + rows);
     // an item, or a part of it, per place: no more parts than items and workers together
-    const int64_t workgroups = compute_units() * attend_occupancy(D, true);
+    const int64_t workgroups = compute_units() * attend_occupancy(D);
     const int64_t most = groups > 0 ? rows * M : M;               // queries of a unit
     s.slot[kByGroup] = (int32_t)(most < 64 ? most : 64);
     s.slot[kByWave] = (int32_t)(most < 16 ? most : 16);
@@ -748,7 +748,7 @@ __device__ __forceinline__ void along_line(const AttentionArgs& a, const AttendS
 }
 
 template <int D, bool kFp8>
-__global__ __launch_bounds__(64 * kAttendWaves, attend_occupancy(D, kFp8))
+__global__ __launch_bounds__(64 * kAttendWaves, attend_occupancy(D))
 void attend_kernel(CacheView c, AttentionArgs a, AttendShape s, char* ws)
 {
     __shared__ __align__(16) char lds[Attend<D, kFp8>::kLds];
@@ -907,7 +907,7 @@ void attend_join_kernel(AttentionArgs a, AttendShape s, int heads, int page_size
 template <int D, bool kFp8>
 static hipError_t launch_attend(const CacheView& c, const AttentionArgs& a, const AttendShape& s, char* ws, hipStream_t stream)
 {
-    const int workgroups = compute_units() * attend_occupancy(D, kFp8);
+    const int workgroups = compute_units() * attend_occupancy(D);
     attend_kernel<D, kFp8><<<workgroups, 64 * kAttendWaves, 0, stream>>>(c, a, s, ws);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
