@@ -35,7 +35,7 @@
 // 6000 own tokens (1.63 GB, 322 us; leaving out all products and exponentials changed nothing).  Small batches wait
 // for chains of loads: 2.5 us for the lengths, about 8 us into and out of an item, 5 us for the join.  With several tokens a row
 // the workgroups' line does more work per byte: 512 rows x 5 tokens with 500 + 5 to 2000 take 329 us at 1.9 TB/s, the vector
-// units busy for half of the waves' time (64 of a step's 240 instructions widen codes), the rest of it barriers and LDS.
+// units busy for half of the waves' time (64 of a step's 270 instructions widen codes), the rest of it barriers and LDS.
 #include "kv_cache.h"
 #include "stretch.h"
 #include "vocab_common.h"
@@ -51,11 +51,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kStep = 32;                       // tokens of a wave's step
 constexpr int kAttendWaves = 4;
 // What an item costs besides its steps, in steps (a chain of loads to its page, its keys and its queries).  16 rollouts x 8 with drafts
-// 55.9 us with 2, 51.7 with 4, 53.7 with 8; 512 rows 347.7, 344.2, 345.6.
+// 55.1 us with 2, 53.4 with 4, 55.8 with 8; 512 rows 336.0, 332.5, 335.6.
 constexpr int kItemCost = 4;
-// What a step of the workgroups' line costs against one of the waves' line, which waits for more memory.  12 rows with a
-// prefix of 32,771 tokens 52.3 us with 0.6, 58.2 with 1; 512 rows 332 with 0.5 to 0.7, 333 with 1 and 440 with 0.3, where the few
-// workgroups of the prefixes end last.
+// What a step of the workgroups' line costs against one of the waves' line, which waits for more memory.  512 rows 331.6 to 333.4 us with
+// 0.5 to 0.7, 335.7 with 1 and 455 with 0.3, where the few workgroups of the prefixes end last; batches with hardly any work on one of the
+// lines take the same with any of them (12 rows with a prefix of 32,771 tokens 50.9 to 52.5).
 constexpr float kSharedCost = 0.6f;
 // Steps of a stretch at least, on average: with more the join has fewer parts, with fewer the few steps of a small batch are taken side
 // by side.  One row with 150 + 77 tokens (32 steps) 13.0 us with 1, 13.6 with 2, 15.1 with 4; with 8192 tokens (1048 steps) 24.2,

@@ -22,8 +22,8 @@
 // us where they take 237.)
 //
 // What bounds it: what passes between the caches and memory for many positions (512 rows x 4 drafts of 151,936 bf16 columns 237 us; the
-// positions behind a rejection left out, about 1.0 GB of 1.4), chains of dependent loads for few: three launches of 6.6, 6.5 and
-// 4.2 us for 4 rows x 3 drafts.
+// positions behind a rejection left out, 0.95 GB of 1.4, and the drawn lines read once more), chains of dependent loads for few: three launches of
+// 6.6, 5.8 and 3.7 us for 4 rows x 3 drafts.
 #include "verify.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
