@@ -446,6 +446,52 @@ int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
                   void* k_out, void* v_out, int dtype, void* hip_stream);
 
 /*
+ * Rotary positions (the struct is host memory, its arrays device memory).  Pair i of rot_dim / 2 is turned by
+ *   theta_i = positions[axis[i]][token] * freqs[i]:   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin.
+ * freqs     [rot_dim / 2] fp64: radians per position.
+ * axis      [rot_dim / 2] uint8, or NULL with axes == 1: which of the token's positions a pair goes by (a text's place; time,
+ *           height and width of a picture's part).  Columns may be given to axes in blocks, in turn or in any other way.  A
+ *           pair whose axis is not below `axes` stays as it is.
+ * rot_dim   columns that are turned, the first ones: a multiple of 16, at most head_dim; those behind are copied.
+ * axes      1 .. E3_MAX_AXES.
+ * neighbours  0: pair i is columns i and i + rot_dim / 2;  1: columns 2 i and 2 i + 1.
+ * Positions are int64, [axes][tokens], rows position_stride elements apart, and may be negative; angles are exact to far below fp32's
+ * rounding for |position| < 2^52.  Sums in fp32, rounded once.
+ */
+#define E3_MAX_AXES 8
+typedef struct {
+    const double* freqs;
+    const uint8_t* axis;
+    int32_t rot_dim, axes, neighbours;
+} e3_rotary;
+
+/*
+ * Turn rows of heads: out = R(theta) x, or with inverse = 1 R(-theta) x, which is R's transpose: the gradient with respect
+ * to x where x stands for the gradient with respect to R x.
+ *
+ * x, out    [tokens][heads][head_dim] of dtype (E3_BF16 / E3_F32), strides in elements, columns next to each other; bases and
+ *           strides multiples of 16 bytes (E3_ERR_ALIGN).  out may be x with the same strides (other strides: E3_ERR_VALUE); they may not
+ *           overlap in any other way.
+ * tokens at most 2^25, heads at most 65,536, head_dim a multiple of 8 from 16 to 1024 (E3_ERR_SHAPE).
+ */
+int e3_rotate(const e3_rotary* rotary, const int64_t* positions, int64_t position_stride, const void* x, int dtype,
+              int64_t tokens, int64_t heads, int64_t head_dim, int64_t x_token_stride, int64_t x_head_stride,
+              void* out, int64_t out_token_stride, int64_t out_head_stride, int inverse, void* hip_stream);
+
+/*
+ * e3_cache_append with the keys turned on the way (in fp32, before they are rounded or quantised), and the same tokens' queries
+ * turned beside them in the same launch.  Values are stored as they are.
+ * q, q_out  [tokens][q_heads][head_dim] of dtype, as x and out of e3_rotate; q_heads == 0: keys and values only, both may be NULL.
+ *           The queries of tokens whose slot is outside the cache are turned too.
+ * tokens    at most 2^25; other arguments as for e3_cache_append and e3_rotate.
+ */
+int e3_cache_append_rotated(const e3_cache* cache, const e3_rotary* rotary, const int64_t* positions, int64_t position_stride,
+                            const void* q, const void* k, const void* v, int dtype, int64_t tokens, int64_t q_heads,
+                            int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride,
+                            int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots,
+                            void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* hip_stream);
+
+/*
  * Attention of one decode step.  Row r belongs to group g (group_offsets[g] <= r <
  * group_offsets[g + 1]) and attends to the group's prefix, all of it, and to its own tokens, of
  * which the last `queries` are the step's own: query t sees the first

@@ -27,6 +27,7 @@ E3_OK = 0
 E3_TILE_CHUNK, E3_TILE_LANES, E3_TILE_DEPTH = 8, 64, 8
 E3_NOALLOC_MAX_ROWS = 1024
 E3_MAX_DRAFTS = 63
+E3_MAX_AXES = 8
 
 EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_entropy_noalloc",
            "e3_sample_restricted", "e3_sample_restricted_ws", "e3_restricted_workspace_bytes",
@@ -34,6 +35,7 @@ EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_
            "e3_grpo_advantages", "e3_temperature_update", "e3_difficulty_ranks",
            "e3_allocate_budgets", "e3_budget_bounds", "e3_logprob_entropy_gap",
            "e3_temperature_update_gap", "e3_grpo_objective", "e3_cache_append", "e3_cache_read",
+           "e3_rotate", "e3_cache_append_rotated",
            "e3_prefix_attention", "e3_prefix_attention_workspace_bytes", "e3_verify_drafts",
            "e3_verify_workspace_bytes", "e3_read_probe",
            "e3_time_next_launch", "e3_launch_plan", "e3_launch_plan_of")
@@ -41,7 +43,8 @@ EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_
 _NATIVE_CALLS = ("e3_grpo_advantages", "e3_grpo_objective", "e3_workspace_bytes", "e3_sample_entropy",
                  "e3_restricted_workspace_bytes", "e3_sample_restricted_ws", "e3_logprob_entropy_advantages",
                  "e3_logprob_entropy_gap", "e3_temperature_update", "e3_cache_append", "e3_cache_read",
-                 "e3_prefix_attention_workspace_bytes", "e3_prefix_attention", "e3_verify_workspace_bytes", "e3_verify_drafts")
+                 "e3_prefix_attention_workspace_bytes", "e3_prefix_attention", "e3_verify_workspace_bytes", "e3_verify_drafts",
+                 "e3_rotate", "e3_cache_append_rotated")
 
 _lib: Optional[C.CDLL] = None
 _native = None                     # the native calls, once they are bound to the loaded library
@@ -131,6 +134,10 @@ def lib() -> C.CDLL:
         L.e3_verify_drafts.argtypes = [vp, C.c_int, i64, i32, i64, i64, i64, vp, vp, vp, i64, i64, vp, f32, vp, u64, u64,
                                        vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.e3_verify_drafts.restype = C.c_int
+        L.e3_rotate.argtypes = [vp, vp, i64, vp, C.c_int, i64, i64, i64, i64, i64, vp, i64, i64, C.c_int, vp]
+        L.e3_rotate.restype = C.c_int
+        L.e3_cache_append_rotated.argtypes = [vp, vp, vp, i64, vp, vp, vp, C.c_int, i64, i64, i64, i64, i64, i64, i64, i64, vp, vp, i64, i64, vp]
+        L.e3_cache_append_rotated.restype = C.c_int
         _bind_native(L)                           # may raise: nothing is loaded then
         _lib = L
     return _lib
@@ -166,7 +173,8 @@ _ENTRY = {"advantages": "e3_grpo_advantages", "objective": "e3_grpo_objective", 
           "restricted": "e3_sample_restricted", "logprob": "e3_logprob_entropy",
           "logprob_advantages": "e3_logprob_entropy_advantages", "logprob_gap": "e3_logprob_entropy_gap",
           "temperature": "e3_temperature_update", "cache_append": "e3_cache_append", "cache_read": "e3_cache_read",
-          "attention": "e3_prefix_attention", "verify": "e3_verify_drafts"}
+          "attention": "e3_prefix_attention", "verify": "e3_verify_drafts", "rotate": "e3_rotate",
+          "append_rotated": "e3_cache_append_rotated"}
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -749,6 +757,112 @@ def e3_cache_read(cache: E3Cache, slots: torch.Tensor, dtype: torch.dtype = torc
     if rc != E3_OK:
         raise E3Error(rc, "e3_cache_read")
     return outs[0], outs[1]
+
+
+class E3Rotary(NamedTuple):
+    """Rotary positions (e3_rotary in include/e3.h): freqs fp64 [pairs], radians per position; axis uint8 [pairs] or None (one axis);
+    neighbours: pairs of columns (2 i, 2 i + 1) instead of (i, i + pairs)."""
+    freqs: torch.Tensor
+    axis: Optional[torch.Tensor] = None
+    neighbours: bool = False
+
+
+class _RotaryStruct(C.Structure):
+    _fields_ = [("freqs", C.c_void_p), ("axis", C.c_void_p), ("rot_dim", C.c_int32), ("axes", C.c_int32), ("neighbours", C.c_int32)]
+
+
+def new_rotary(rot_dim: int, base: float = 10000.0, sections=None, neighbours: bool = False, device="cuda") -> E3Rotary:
+    """Frequencies base^(-2 i / rot_dim) for the rot_dim / 2 pairs.  sections: how many pairs, in order, go by each axis."""
+    if rot_dim < 16 or rot_dim % 16:
+        raise ValueError("rot_dim must be a multiple of 16")
+    pairs = rot_dim // 2
+    freqs = torch.tensor([float(base) ** (-2.0 * i / rot_dim) for i in range(pairs)], dtype=torch.float64)
+    axis = None
+    if sections is not None:
+        if sum(sections) != pairs or min(sections) < 0 or len(sections) > E3_MAX_AXES:
+            raise ValueError(f"sections must be at most {E3_MAX_AXES} numbers of pairs that add up to {pairs}")
+        axis = torch.tensor([a for a, n in enumerate(sections) for _ in range(n)], dtype=torch.uint8).to(device)
+    return E3Rotary(freqs.to(device), axis, neighbours)
+
+
+def _rotary(rotary, positions: torch.Tensor, tokens: int, device) -> Tuple[_RotaryStruct, int]:
+    """The struct, and the stride of the positions' rows."""
+    freqs, axis, neighbours = rotary
+    if freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous() or freqs.device != device:
+        raise ValueError(f"freqs must be a contiguous fp64 vector on {device}")
+    pairs = freqs.shape[0]
+    _check(axis, torch.uint8, pairs, "axis", device)
+    if positions.dtype is not torch.int64 or positions.dim() not in (1, 2) or positions.shape[-1] != tokens or positions.device != device \
+            or (tokens > 1 and positions.stride(-1) != 1):
+        raise ValueError(f"positions must be an int64 tensor [axes, {tokens}] (or [{tokens}]) with unit stride on {device}")
+    axes = positions.shape[0] if positions.dim() == 2 else 1
+    if axis is None and axes != 1:
+        raise ValueError("positions on several axes need the rotary's axis")
+    return _RotaryStruct(_ptr(freqs), _ptr(axis), 2 * pairs, axes, int(bool(neighbours))), positions.stride(0) if axes > 1 else 0
+
+
+def _heads(t: torch.Tensor, name: str, dtype, shape, device) -> None:
+    if t.dtype is not dtype or tuple(t.shape) != tuple(shape) or t.device != device or (t.numel() and t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} with unit column stride on {device}")
+
+
+def e3_rotate(x: torch.Tensor, rotary: E3Rotary, positions: torch.Tensor, out: Optional[torch.Tensor] = None,
+              inverse: bool = False) -> torch.Tensor:
+    """Turn x [tokens, heads, D] (bf16 or fp32, any strides with columns next to each other) by its tokens' positions (int64 [axes,
+    tokens], or [tokens]); inverse: by the opposite angles, which takes a gradient back.  out: like x, x itself allowed."""
+    res = _ordinary("rotate", x, rotary, positions, out, inverse)
+    if res is not None:
+        return res
+    if x.dim() != 3 or not x.is_cuda:
+        raise ValueError("x must be [tokens, heads, D] on the GPU")
+    dt, dev = _float_type(x.dtype), x.device
+    _heads(x, "x", x.dtype, x.shape, dev)
+    n, H, D = x.shape
+    r, stride = _rotary(rotary, positions, n, dev)
+    if out is None:
+        out = torch.empty((n, H, D), dtype=x.dtype, device=dev)
+    else:
+        _heads(out, "out", x.dtype, x.shape, dev)
+    rc = lib().e3_rotate(C.byref(r), _ptr(positions), stride, _ptr(x), dt, n, H, D, _step(x, 0), _step(x, 1), _ptr(out), _step(out, 0),
+                         _step(out, 1), int(bool(inverse)), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_rotate")
+    return out
+
+
+def e3_cache_append_rotated(cache: E3Cache, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, rotary: E3Rotary,
+                            positions: torch.Tensor, slots: torch.Tensor, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """e3_cache_append with the keys turned by their positions (int64 [axes, tokens], or [tokens]) on the way.  Returns the queries q [tokens,
+    q_heads, D] turned as well (in q_out if given, which may be q), or None without queries."""
+    res = _ordinary("append_rotated", cache, q, k, v, rotary, positions, slots, q_out)
+    if res is not None:
+        return None if res is True else res
+    c = _cache(cache)
+    dev = cache[0].device
+    dt = _float_type(k.dtype)
+    n = slots.shape[0]
+    for t, name in ((k, "k"), (v, "v")):
+        _heads(t, name, k.dtype, (n, c.kv_heads, c.head_dim), dev)
+    _check(slots, torch.int64, n, "slots", dev)
+    r, stride = _rotary(rotary, positions, n, dev)
+    q_heads, strides, out_strides = 0, (0, 0), (0, 0)
+    if q is not None:
+        if q.dim() != 3:
+            raise ValueError(f"q must be [{n}, q_heads, {c.head_dim}]")
+        q_heads = q.shape[1]
+        _heads(q, "q", k.dtype, (n, q_heads, c.head_dim), dev)
+        if q_out is None:
+            q_out = torch.empty((n, q_heads, c.head_dim), dtype=k.dtype, device=dev)
+        else:
+            _heads(q_out, "q_out", k.dtype, (n, q_heads, c.head_dim), dev)
+        strides, out_strides = (_step(q, 0), _step(q, 1)), (_step(q_out, 0), _step(q_out, 1))
+    elif q_out is not None:
+        raise ValueError("q_out belongs to q")
+    rc = lib().e3_cache_append_rotated(C.byref(c), C.byref(r), _ptr(positions), stride, _ptr(q), _ptr(k), _ptr(v), dt, n, q_heads, *strides,
+                                       _step(k, 0), _step(k, 1), _step(v, 0), _step(v, 1), _ptr(slots), _ptr(q_out), *out_strides, _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_cache_append_rotated")
+    return q_out
 
 
 def e3_prefix_attention_workspace_bytes(rows: int, queries: int, q_heads: int, kv_heads: int, head_dim: int, num_groups: int) -> int:

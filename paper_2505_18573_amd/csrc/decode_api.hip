@@ -5,6 +5,7 @@
 
 #include "../../include/e3.h"
 #include "kv_cache.h"
+#include "rotary.h"
 #include "verify.h"
 #include "vocab_pass.h"
 
@@ -66,6 +67,76 @@ extern "C" int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_
     if (!aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(slots, 8)) return E3_ERR_ALIGN;
     const hipError_t err = e3::launch_cache_read(view, slots, tokens, k_out, v_out, dtype == E3_BF16,
                                                  static_cast<hipStream_t>(hip_stream));
+    return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
+}
+
+static int check_rotary(const e3_rotary* r, const int64_t* positions, int64_t position_stride, int64_t head_dim, e3::Rotary* view)
+{
+    if (r == nullptr) return E3_ERR_NULL;
+    if (r->rot_dim < 16 || r->rot_dim % 16 || r->rot_dim > head_dim || r->axes < 1 || r->axes > E3_MAX_AXES) return E3_ERR_SHAPE;
+    if (r->neighbours != 0 && r->neighbours != 1) return E3_ERR_VALUE;
+    if (r->freqs == nullptr || (r->axis == nullptr && r->axes > 1)) return E3_ERR_NULL;
+    if (!aligned(r->freqs, 8) || !aligned(positions, 8)) return E3_ERR_ALIGN;
+    view->freqs = r->freqs; view->axis = r->axis; view->positions = positions; view->stride = position_stride;
+    view->rot = r->rot_dim; view->axes = r->axes; view->neighbours = r->neighbours != 0; view->sign = 1.0f;
+    return E3_OK;
+}
+
+constexpr int64_t kMostTurned = (int64_t)1 << 25;   // tokens of one call that turns: its threads stay below 2^32
+
+extern "C" int e3_rotate(const e3_rotary* rotary, const int64_t* positions, int64_t position_stride, const void* x, int dtype,
+                         int64_t tokens, int64_t heads, int64_t head_dim, int64_t x_token_stride, int64_t x_head_stride,
+                         void* out, int64_t out_token_stride, int64_t out_head_stride, int inverse, void* hip_stream)
+{
+    e3::Rotary r;
+    if (dtype != E3_F32 && dtype != E3_BF16) return E3_ERR_DTYPE;
+    if (tokens < 0 || tokens > kMostTurned || heads < 0 || heads > 65536 || head_dim < 16 || head_dim > 1024 || head_dim % 8) return E3_ERR_SHAPE;
+    const int rc = check_rotary(rotary, positions, position_stride, head_dim, &r);
+    if (rc != E3_OK) return rc;
+    if (inverse != 0 && inverse != 1) return E3_ERR_VALUE;
+    if (tokens == 0 || heads == 0) return E3_OK;
+    if (x == nullptr || out == nullptr || positions == nullptr) return E3_ERR_NULL;
+    const int64_t per = dtype == E3_F32 ? 4 : 8;                    // elements in 16 bytes
+    if (!aligned(x, 16) || !aligned(out, 16) || x_token_stride % per || x_head_stride % per || out_token_stride % per || out_head_stride % per)
+        return E3_ERR_ALIGN;
+    // in place: element for element, or a row would be read after another one's result is there
+    if (x == out && ((tokens > 1 && x_token_stride != out_token_stride) || (heads > 1 && x_head_stride != out_head_stride))) return E3_ERR_VALUE;
+    r.sign = inverse ? -1.0f : 1.0f;
+    const e3::TurnArgs a{{x, x_token_stride, x_head_stride}, out, out_token_stride, out_head_stride, tokens, (int32_t)heads, (int32_t)head_dim};
+    const hipError_t err = e3::launch_rotate(a, r, dtype == E3_BF16, static_cast<hipStream_t>(hip_stream));
+    return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
+}
+
+extern "C" int e3_cache_append_rotated(const e3_cache* cache, const e3_rotary* rotary, const int64_t* positions, int64_t position_stride,
+                                       const void* q, const void* k, const void* v, int dtype, int64_t tokens, int64_t q_heads,
+                                       int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride,
+                                       int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots,
+                                       void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* hip_stream)
+{
+    e3::CacheView view;
+    int rc = check_cache(cache, &view);
+    if (rc != E3_OK) return rc;
+    if (dtype != E3_F32 && dtype != E3_BF16) return E3_ERR_DTYPE;
+    if (tokens < 0 || tokens > kMostTurned || tokens * view.heads > kMostTokens || q_heads < 0 || q_heads > 65536) return E3_ERR_SHAPE;
+    e3::Rotary r;
+    rc = check_rotary(rotary, positions, position_stride, view.dim, &r);
+    if (rc != E3_OK) return rc;
+    if (tokens == 0) return E3_OK;
+    if (k == nullptr || v == nullptr || slots == nullptr || positions == nullptr || (q_heads > 0 && (q == nullptr || q_out == nullptr))) return E3_ERR_NULL;
+    const int64_t per = dtype == E3_F32 ? 4 : 8;                    // elements in 16 bytes
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8) || k_token_stride % per || k_head_stride % per || v_token_stride % per ||
+        v_head_stride % per)
+        return E3_ERR_ALIGN;
+    e3::TurnArgs a{};
+    if (q_heads > 0) {
+        if (!aligned(q, 16) || !aligned(q_out, 16) || q_token_stride % per || q_head_stride % per || q_out_token_stride % per || q_out_head_stride % per)
+            return E3_ERR_ALIGN;
+        if (q == q_out && ((tokens > 1 && q_token_stride != q_out_token_stride) || (q_heads > 1 && q_head_stride != q_out_head_stride)))
+            return E3_ERR_VALUE;
+        a = e3::TurnArgs{{q, q_token_stride, q_head_stride}, q_out, q_out_token_stride, q_out_head_stride, tokens, (int32_t)q_heads, view.dim};
+    }
+    const hipError_t err = e3::launch_cache_append_rotated(view, {k, k_token_stride, k_head_stride}, {v, v_token_stride, v_head_stride}, a, r,
+                                                           dtype == E3_BF16, slots, tokens, static_cast<hipStream_t>(hip_stream));
     return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
 }
 

@@ -20,6 +20,7 @@
 // 31 us, 6.0 TB/s, part of the codes still in the memory-side cache), the launch and its chain of two loads (slot, row) for a step's
 // tokens (512: 5.4 us in, 4.3 us back).
 #include "kv_cache.h"
+#include "rotary.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
 
@@ -152,19 +153,18 @@ __device__ __forceinline__ uint32_t deal(uint32_t w, int lane)
     for (int j = 0; j < 4; ++j) out |= (((uint32_t)__shfl((int)w, base + (part >> 2) + L / 4 * j) >> (8 * (part & 3))) & 0xFFu) << (8 * j);
     return out;
 }
-template <int D, bool kFp8, bool kBf16>
-__global__ __launch_bounds__(64 * kCacheWaves)
-void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* slots, int64_t tokens, int64_t items)
+
+// A wave's work: the window that starts at token `first`, head (or pair of heads) `head_item`.  turn(x) may change the keys, x[i] being
+// the lane's four columns of token 4 half + i, once all rows are there.
+template <int D, bool kFp8, bool kBf16, typename Turn>
+__device__ __forceinline__ void append_item(const CacheView& c, const TokenRows& k, const TokenRows& v, const int64_t* slots, int64_t tokens,
+                                            int64_t first, int head_item, Turn turn)
 {
     constexpr int kHeads = 128 / D;                               // heads of a wave
     constexpr int kIn = kBf16 ? 2 : 4;
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    if (item >= items) return;
-    const int per = (c.heads + kHeads - 1) / kHeads;
-    const int64_t first = item / per * kBlockTokens;
     const int half = lane >> 5, part = lane & (D / 4 - 1), col = part * 4;
-    const int head = (int)(item % per) * kHeads + ((lane & 31) >> (D == 128 ? 5 : 4));
+    const int head = head_item * kHeads + ((lane & 31) >> (D == 128 ? 5 : 4));
     const bool live = head < c.heads;
     const int safe_head = live ? head : 0;
     auto load = [&](const TokenRows& t, int64_t token, float x[4]) {
@@ -214,6 +214,7 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
         single[i] = ok[i] && !((w.whole >> (4 * half + i)) & 1u);
     }
 
+    turn(xk);
     if (kFp8) {
         uint8_t* kc = static_cast<uint8_t*>(c.k);
         uint8_t* vc = static_cast<uint8_t*>(c.v);
@@ -271,6 +272,79 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
                     u32x2{pack_bf16(xb[0][j], xb[1][j]), pack_bf16(xb[2][j], xb[3][j])};
         }
     }
+}
+
+template <int D, bool kFp8, bool kBf16>
+__global__ __launch_bounds__(64 * kCacheWaves)
+void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* slots, int64_t tokens, int64_t items)
+{
+    constexpr int kHeads = 128 / D;
+    const int64_t item = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
+    if (item >= items) return;
+    const int per = (c.heads + kHeads - 1) / kHeads;
+    append_item<D, kFp8, kBf16>(c, k, v, slots, tokens, item / per * kBlockTokens, (int)(item % per), [](float (&)[4][4]) {});
+}
+
+// With rotary positions: a workgroup takes a window of eight tokens and makes sine and cosine of every (token, pair) once, for all
+// heads, in LDS.  Workgroups of grid row 0 write keys and values, a wave per head (two of 64 columns), turned in registers before they
+// are quantised; the other rows turn the queries, a share of the heads each.  A lane's four columns are half of four pairs
+// whose other half another lane of the row holds, or two whole pairs.
+constexpr int kAppendThreads = 256;
+template <int D, bool kFp8, bool kBf16>
+__global__ __launch_bounds__(kAppendThreads)
+void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Rotary r, const int64_t* slots, int64_t tokens, int q_heads_each)
+{
+    __shared__ float2 turns[kBlockTokens * D / 2];                // [token][pair]
+    const int64_t first = (int64_t)blockIdx.x * kBlockTokens;
+    const int here = tokens - first < kBlockTokens ? (int)(tokens - first) : kBlockTokens;
+    const int pairs = r.rot / 2;
+    for (int i = threadIdx.x; i < here * pairs; i += kAppendThreads) turns[i] = turn_of(r, first + i / pairs, i % pairs);
+    __syncthreads();
+    if (blockIdx.y > 0) {
+        const int units = units_of(r.rot, D);
+        const int h0 = ((int)blockIdx.y - 1) * q_heads_each, n = (q.heads - h0 < q_heads_each ? q.heads - h0 : q_heads_each) * here * units;
+        for (int i = threadIdx.x; i < n; i += kAppendThreads) {
+            const int u = i % units, rest = i / units, t = rest % here, h = h0 + rest / here;
+            turn_unit<kBf16>(q, r, first + t, h, u, turns + t * pairs);
+        }
+        return;
+    }
+    const int lane = threadIdx.x & 63, half = lane >> 5, part = lane & (D / 4 - 1), col = part * 4;
+    const int base = lane & ~(D / 4 - 1);
+    auto turn = [&](float (&x)[4][4]) {
+        const bool mine = col < r.rot, upper = col >= pairs;
+        // halves: pair of column c is c or c - pairs, its other column pairs away
+        const int other = base + (upper ? part - pairs / 4 : part + pairs / 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = 4 * half + i < here ? 4 * half + i : here - 1;
+            const float2* of = turns + t * pairs;
+            if (r.neighbours) {
+                if (mine) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float2 w = of[col / 2 + j];
+                        const float a = x[i][2 * j], b = x[i][2 * j + 1];
+                        x[i][2 * j] = a * w.x - b * w.y;
+                        x[i][2 * j + 1] = b * w.x + a * w.y;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float y = __shfl(x[i][j], other);
+                    if (mine) {
+                        const float2 w = of[(upper ? col - pairs : col) + j];
+                        x[i][j] = upper ? x[i][j] * w.x + y * w.y : x[i][j] * w.x - y * w.y;
+                    }
+                }
+            }
+        }
+    };
+    constexpr int kHeads = 128 / D;
+    const int per = (c.heads + kHeads - 1) / kHeads;
+    for (int item = threadIdx.x >> 6; item < per; item += kAppendThreads / 64)
+        append_item<D, kFp8, kBf16>(c, k, v, slots, tokens, first, item, turn);
 }
 
 // Reading back: the same windows.  A token whose slot is not in the cache reads as zeros.
@@ -445,6 +519,26 @@ hipError_t launch_cache_append(const CacheView& c, const TokenRows& k, const Tok
     return by_shape(c, in_bf16, [&](auto d, auto fp8, auto bf16) {
         cache_append_kernel<decltype(d)::value, decltype(fp8)::value, decltype(bf16)::value>
             <<<grid, 64 * waves, 0, stream>>>(c, k, v, slots, tokens, items);
+    });
+}
+
+hipError_t launch_cache_append_rotated(const CacheView& c, const TokenRows& k, const TokenRows& v, const TurnArgs& q, const Rotary& r,
+                                       bool in_bf16, const int64_t* slots, int64_t tokens, hipStream_t stream)
+{
+    const int64_t windows = (tokens + kBlockTokens - 1) / kBlockTokens;
+    // The queries' heads are spread over as many workgroups as give every compute unit two, and a thread a unit at least.
+    const int units = units_of(r.rot, c.dim) * (int)(tokens < kBlockTokens ? tokens : kBlockTokens);
+    int groups = 0, each = 1;
+    if (q.heads > 0) {
+        const int64_t want = 2 * (int64_t)compute_units() / windows, most = ((int64_t)q.heads * units + kAppendThreads - 1) / kAppendThreads;
+        groups = (int)(want < 1 ? 1 : want < most ? want : most);
+        each = (q.heads + groups - 1) / groups;
+        groups = (q.heads + each - 1) / each;
+    }
+    const dim3 grid((uint32_t)windows, (uint32_t)(1 + groups));
+    return by_shape(c, in_bf16, [&](auto d, auto fp8, auto bf16) {
+        append_rotated_kernel<decltype(d)::value, decltype(fp8)::value, decltype(bf16)::value>
+            <<<grid, kAppendThreads, 0, stream>>>(c, k, v, q, r, slots, tokens, each);
     });
 }
 

@@ -37,6 +37,8 @@ decltype(&e3_prefix_attention_workspace_bytes) p_attention_bytes;
 decltype(&e3_prefix_attention) p_attention;
 decltype(&e3_verify_workspace_bytes) p_verify_bytes;
 decltype(&e3_verify_drafts) p_verify;
+decltype(&e3_rotate) p_rotate;
+decltype(&e3_cache_append_rotated) p_append_rotated;
 PyObject* raw_stream = nullptr;
 
 // A call's arguments as they are read: `ok` falls at the first one that is not ordinary.
@@ -485,6 +487,109 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     });
 }
 
+// rotary positions as binding.py's E3Rotary holds them (freqs, axis, neighbours), and the tokens' positions
+struct Turns {
+    e3_rotary c{};
+    const int64_t* positions = nullptr;
+    int64_t stride = 0;
+    Turns(Reader& r, PyObject* o, PyObject* of, int64_t tokens)
+    {
+        if (!r.ok || !PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3 || !PyBool_Check(PyTuple_GET_ITEM(o, 2))) { r.ok = false; return; }
+        const at::Tensor* f = r.plain(PyTuple_GET_ITEM(o, 0));
+        const at::Tensor* p = r.ok ? r.plain(of) : nullptr;
+        if (!r.ok || f->dim() != 1 || f->size(0) != (int32_t)f->size(0) || f->size(0) > 1 << 20) { r.ok = false; return; }
+        const int64_t pairs = f->size(0), dims = p->dim();
+        c.freqs = (const double*)r.vector(PyTuple_GET_ITEM(o, 0), at::kDouble, pairs);
+        c.axis = (const uint8_t*)r.vector(PyTuple_GET_ITEM(o, 1), at::kByte, pairs);
+        if (!r.ok || (dims != 1 && dims != 2) || p->scalar_type() != at::kLong || p->size(dims - 1) != tokens || p->device() != r.dev
+            || (tokens > 1 && p->stride(dims - 1) != 1)) { r.ok = false; return; }
+        const int64_t axes = dims == 2 ? p->size(0) : 1;
+        if (axes > 1 << 20 || (c.axis == nullptr && axes != 1)) { r.ok = false; return; }
+        c.rot_dim = (int32_t)(2 * pairs); c.axes = (int32_t)axes; c.neighbours = PyTuple_GET_ITEM(o, 2) == Py_True;
+        positions = (const int64_t*)p->data_ptr();
+        stride = axes > 1 ? p->stride(0) : 0;
+    }
+};
+
+bool unit_columns(const at::Tensor* t) { return t->numel() == 0 || t->size(2) < 2 || t->stride(2) == 1; }
+
+// an output [tokens][heads][D] of any strides with columns next to each other
+const at::Tensor* rows_of_heads(Reader& r, Output& out, PyObject* given, at::ScalarType type, const std::array<int64_t, 3>& shape)
+{
+    if (given == Py_None) {
+        out.shaped(r, given, type, shape);
+        return r.ok ? &THPVariable_Unpack(out.object) : nullptr;
+    }
+    const at::Tensor* t = r.plain(given);
+    if (t == nullptr || t->scalar_type() != type || t->sizes() != at::IntArrayRef(shape.data(), 3) || t->device() != r.dev || !unit_columns(t)) {
+        r.ok = false;
+        return nullptr;
+    }
+    out.p = t->data_ptr();
+    out.take(given);
+    return t;
+}
+
+// x, rotary, positions, out, inverse
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 5 || !PyBool_Check(a[4])) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const at::Tensor* x = r.first(a[0]);
+        if (!r.ok || x->dim() != 3 || !unit_columns(x)) return unusual();
+        const int type = float_type(r, x->scalar_type());
+        const int64_t n = x->size(0), heads = x->size(1), D = x->size(2);
+        const Turns turns(r, a[1], a[2], n);
+        if (!r.ok) return unusual();
+        Output out;
+        const at::Tensor* o = rows_of_heads(r, out, a[3], x->scalar_type(), {n, heads, D});
+        return run(r, [&](void* s) {
+                       return p_rotate(&turns.c, turns.positions, turns.stride, x->data_ptr(), type, n, heads, D, step_of(x, 0), step_of(x, 1), out.p,
+                                       step_of(o, 0), step_of(o, 1), a[4] == Py_True, s);
+                   },
+                   [&] { return out.release(); });
+    });
+}
+
+// cache, q, k, v, rotary, positions, slots, q_out; the turned queries, True where there are none
+PyObject* append_rotated(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 8) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const Cache cache(r, a[0]);
+        const at::Tensor* k = r.ok ? r.plain(a[2]) : nullptr;
+        const at::Tensor* v = r.ok ? r.plain(a[3]) : nullptr;
+        const at::Tensor* slots = r.ok ? r.plain(a[6]) : nullptr;
+        const at::Tensor* q = r.ok && a[1] != Py_None ? r.plain(a[1]) : nullptr;
+        if (!r.ok || slots->dim() != 1 || (q == nullptr && a[7] != Py_None)) return unusual();
+        const int64_t n = slots->size(0);
+        const void* ps = r.vector(a[6], at::kLong, n);
+        for (const at::Tensor* t : {k, v})
+            if (t->scalar_type() != k->scalar_type() || t->dim() != 3 || t->size(0) != n || t->size(1) != cache.c.kv_heads
+                || t->size(2) != cache.c.head_dim || t->device() != r.dev || !unit_columns(t)) return unusual();
+        const int type = float_type(r, k->scalar_type());
+        const Turns turns(r, a[4], a[5], n);
+        if (!r.ok) return unusual();
+        Output out;
+        const at::Tensor* o = nullptr;
+        if (q != nullptr) {
+            if (q->scalar_type() != k->scalar_type() || q->dim() != 3 || q->size(0) != n || q->size(2) != cache.c.head_dim || q->device() != r.dev
+                || !unit_columns(q)) return unusual();
+            o = rows_of_heads(r, out, a[7], k->scalar_type(), {n, q->size(1), q->size(2)});
+            if (!r.ok) return unusual();
+        }
+        return run(r, [&](void* s) {
+                       return p_append_rotated(&cache.c, &turns.c, turns.positions, turns.stride, q ? q->data_ptr() : nullptr, k->data_ptr(),
+                                               v->data_ptr(), type, n, q ? q->size(1) : 0, q ? step_of(q, 0) : 0, q ? step_of(q, 1) : 0,
+                                               step_of(k, 0), step_of(k, 1), step_of(v, 0), step_of(v, 1), (const int64_t*)ps, out.p,
+                                               o ? step_of(o, 0) : 0, o ? step_of(o, 1) : 0, s);
+                   },
+                   [&]() -> PyObject* { if (q == nullptr) Py_RETURN_TRUE; return out.release(); });
+    });
+}
+
 // cache, slots, whether bf16 (or fp32), k_out, v_out
 PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n_args)
 {
@@ -658,6 +763,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     get("e3_prefix_attention", p_attention);
     get("e3_verify_workspace_bytes", p_verify_bytes);
     get("e3_verify_drafts", p_verify);
+    get("e3_rotate", p_rotate);
+    get("e3_cache_append_rotated", p_append_rotated);
     if (!all) { PyErr_SetString(PyExc_ValueError, "an entry point is missing"); return nullptr; }
     Py_INCREF(a[1]);
     Py_XSETREF(raw_stream, a[1]);
@@ -681,6 +788,8 @@ PyMethodDef methods[] = {
     {"cache_read", fast(cache_read), METH_FASTCALL, nullptr},
     {"attention", fast(attention), METH_FASTCALL, nullptr},
     {"verify", fast(verify), METH_FASTCALL, nullptr},
+    {"rotate", fast(rotate), METH_FASTCALL, nullptr},
+    {"append_rotated", fast(append_rotated), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

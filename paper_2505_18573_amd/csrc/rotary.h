@@ -1,0 +1,153 @@
+// Rotary positions: pair i of a head's columns is turned by theta_i = (position on the pair's axis) * f_i.
+//
+//   y1 = x1 cos theta - x2 sin theta,   y2 = x2 cos theta + x1 sin theta;   the gradient: by -theta.
+//
+// Angles: positions reach millions and f_0 is 1, so 32 bits would leave nothing of the angle behind the comma.  In turns
+// (theta / 2 pi) the whole part drops out, and the product is taken in 64 bits with its own rounding error (fused
+// multiply-add), so a position below 2^52 loses nothing; what is left, at most an eighth of a turn after the quadrant is
+// taken off, goes to fp32 and into the Taylor polynomials of sine and cosine (degree 9 and 10: the next terms are below
+// 2^-29 of the result).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kv_cache.h"
+
+namespace e3 {
+
+struct Rotary {
+    const double* freqs;              // [rot / 2] radians per position
+    const uint8_t* axis;              // [rot / 2] or nullptr: axis 0
+    const int64_t* positions;         // [axes][tokens], rows `stride` apart
+    int64_t stride;
+    int32_t rot, axes;
+    bool neighbours;                  // pairs (2 i, 2 i + 1) instead of (i, i + rot / 2)
+    float sign;                       // -1: by the opposite angles
+};
+
+// Queries (or any rows of heads) that are turned: [tokens][heads][dim], columns next to each other.
+struct TurnArgs {
+    TokenRows x;
+    void* out;
+    int64_t out_token_stride, out_head_stride;
+    int64_t tokens;
+    int32_t heads, dim;
+};
+
+hipError_t launch_rotate(const TurnArgs& a, const Rotary& r, bool bf16, hipStream_t stream);
+// keys turned and values as they are into the cache, and, where q.heads > 0, queries turned
+hipError_t launch_cache_append_rotated(const CacheView& c, const TokenRows& k, const TokenRows& v, const TurnArgs& q, const Rotary& r,
+                                       bool in_bf16, const int64_t* slots, int64_t tokens, hipStream_t stream);
+
+// (cos, sin) of pair i at a token
+__device__ __forceinline__ float2 turn_of(const Rotary& r, int64_t token, int i)
+{
+    const int axis = r.axis == nullptr ? 0 : r.axis[i];
+    if (axis >= r.axes) return float2{1.0f, 0.0f};                // no axis: the pair stays as it is
+    const double at = (double)r.positions[axis * r.stride + token], f = r.freqs[i];
+    constexpr double kHi = 0.15915494309189533577, kLo = -9.839338337591243e-18;    // 1 / (2 pi) in two parts
+    const double g = f * kHi, g_rest = fma(f, kHi, -g) + f * kLo;
+    const double p = at * g, p_rest = fma(at, g, -p) + at * g_rest;
+    const double turn = (p - rint(p)) + p_rest;                   // in [-1/2, 1/2], and p_rest
+    const double quarter = rint(turn * 4.0);
+    const float z = (float)(turn - quarter * 0.25) * 6.28318530717958647693f;     // at most pi / 4
+    const float z2 = z * z;
+    float s = 1.0f / 362880.0f, c = -1.0f / 3628800.0f;
+    s = fmaf(s, z2, -1.0f / 5040.0f);
+    s = fmaf(s, z2, 1.0f / 120.0f);
+    s = fmaf(s, z2, -1.0f / 6.0f);
+    s = fmaf(s * z2, z, z);
+    c = fmaf(c, z2, 1.0f / 40320.0f);
+    c = fmaf(c, z2, -1.0f / 720.0f);
+    c = fmaf(c, z2, 1.0f / 24.0f);
+    c = fmaf(c, z2, -0.5f);
+    c = fmaf(c, z2, 1.0f);
+    const int q = (int)quarter;
+    const float cs = (q & 1) ? s : c, sn = (q & 1) ? c : s;
+    return float2{((q + 1) & 2) ? -cs : cs, r.sign * ((q & 2) ? -sn : sn)};
+}
+
+// A unit: up to 16 columns of one token and head, in two vectors of eight; those that are turned hold pairs 8 u .. 8 u + 7.
+template <bool kBf16>
+struct Eight {
+    float x[8];
+    __device__ __forceinline__ void load(const char* p)
+    {
+        if (kBf16) {
+            const uint4 w = *reinterpret_cast<const uint4*>(p);
+            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(v[j] << 16); x[2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u); }
+        } else {
+            const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 16);
+            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        }
+    }
+    __device__ __forceinline__ void store(char* p) const
+    {
+        if (kBf16) {
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                typedef __bf16 pair __attribute__((ext_vector_type(2)));
+                const pair w = {(__bf16)x[2 * j], (__bf16)x[2 * j + 1]};
+                v[j] = __builtin_bit_cast(uint32_t, w);
+            }
+            *reinterpret_cast<uint4*>(p) = uint4{v[0], v[1], v[2], v[3]};
+        } else {
+            *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
+            *reinterpret_cast<float4*>(p + 16) = float4{x[4], x[5], x[6], x[7]};
+        }
+    }
+};
+
+__host__ __device__ __forceinline__ int units_of(int rot, int dim) { return rot / 16 + (dim - rot + 15) / 16; }
+
+// Unit u of (token, head): `turns` the token's (cos, sin) of all pairs.
+template <bool kBf16>
+__device__ __forceinline__ void turn_unit(const TurnArgs& a, const Rotary& r, int64_t token, int head, int u, const float2* turns)
+{
+    constexpr int kSize = kBf16 ? 2 : 4;
+    const char* x = static_cast<const char*>(a.x.base) + (token * a.x.token_stride + head * a.x.head_stride) * kSize;
+    char* out = static_cast<char*>(a.out) + (token * a.out_token_stride + head * a.out_head_stride) * kSize;
+    const int turned = r.rot / 16;
+    if (u >= turned) {                                            // columns behind the turned ones
+        const int col = r.rot + (u - turned) * 16;
+        Eight<kBf16> v;
+        v.load(x + col * kSize);
+        if (col + 8 < a.dim) {
+            Eight<kBf16> w;
+            w.load(x + (col + 8) * kSize);
+            w.store(out + (col + 8) * kSize);
+        }
+        v.store(out + col * kSize);
+        return;
+    }
+    const int at_a = r.neighbours ? 16 * u : 8 * u, at_b = r.neighbours ? at_a + 8 : at_a + r.rot / 2;
+    Eight<kBf16> v, w;
+    v.load(x + at_a * kSize);
+    w.load(x + at_b * kSize);
+    if (r.neighbours) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 t = turns[8 * u + j], s = turns[8 * u + 4 + j];
+            const float v0 = v.x[2 * j], w0 = w.x[2 * j];
+            v.x[2 * j] = v0 * t.x - v.x[2 * j + 1] * t.y;
+            v.x[2 * j + 1] = v.x[2 * j + 1] * t.x + v0 * t.y;
+            w.x[2 * j] = w0 * s.x - w.x[2 * j + 1] * s.y;
+            w.x[2 * j + 1] = w.x[2 * j + 1] * s.x + w0 * s.y;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float2 t = turns[8 * u + j];
+            const float v0 = v.x[j];
+            v.x[j] = v0 * t.x - w.x[j] * t.y;
+            w.x[j] = w.x[j] * t.x + v0 * t.y;
+        }
+    }
+    v.store(out + at_a * kSize);
+    w.store(out + at_b * kSize);
+}
+
+}  // namespace e3

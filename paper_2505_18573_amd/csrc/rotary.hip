@@ -1,0 +1,42 @@
+// Turning rows of heads by their tokens' positions (formulas: rotary.h).
+//
+// A workgroup takes a few tokens with all their heads: sine and cosine of every (token, pair) are made once, by one thread each,
+// and lie in LDS; then a thread takes units of two 16-byte vectors (bf16) that hold eight pairs.  Each element is read and
+// written once, in place where the caller likes, since a unit's two vectors are read before either is written.
+#include "rotary.h"
+#include "vocab_pass.h"
+
+namespace e3 {
+
+constexpr int kTurnThreads = 256;
+constexpr int kTurnMostTokens = 4;
+
+template <bool kBf16>
+__global__ __launch_bounds__(kTurnThreads)
+void rotate_kernel(TurnArgs a, Rotary r, int tokens_each, int heads_each)
+{
+    extern __shared__ float2 turns[];                             // [tokens_each][rot / 2]
+    const int64_t first = (int64_t)blockIdx.x * tokens_each;
+    const int here = a.tokens - first < tokens_each ? (int)(a.tokens - first) : tokens_each;
+    const int pairs = r.rot / 2, units = units_of(r.rot, a.dim);
+    for (int i = threadIdx.x; i < here * pairs; i += kTurnThreads) turns[i] = turn_of(r, first + i / pairs, i % pairs);
+    __syncthreads();
+    const int u = threadIdx.x % units, t = threadIdx.x / units % tokens_each, h0 = threadIdx.x / (units * tokens_each);
+    if (h0 >= heads_each || t >= here) return;
+    for (int h = h0; h < a.heads; h += heads_each) turn_unit<kBf16>(a, r, first + t, h, u, turns + t * pairs);
+}
+
+hipError_t launch_rotate(const TurnArgs& a, const Rotary& r, bool bf16, hipStream_t stream)
+{
+    const int units = units_of(r.rot, a.dim);
+    // One token a workgroup while that gives every compute unit two workgroups at most: a step's few tokens are spread over the card.
+    const int each = a.tokens <= 2 * (int64_t)compute_units() ? 1 : kTurnMostTokens;
+    const int heads_each = kTurnThreads / (each * units);
+    const dim3 grid((uint32_t)((a.tokens + each - 1) / each));
+    const size_t lds = (size_t)each * (r.rot / 2) * sizeof(float2);
+    if (bf16) rotate_kernel<true><<<grid, kTurnThreads, lds, stream>>>(a, r, each, heads_each);
+    else rotate_kernel<false><<<grid, kTurnThreads, lds, stream>>>(a, r, each, heads_each);
+    return hipGetLastError();
+}
+
+}  // namespace e3
