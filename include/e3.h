@@ -537,6 +537,38 @@ int e3_prefix_attention(const e3_cache* cache, const void* q, int64_t rows, int6
                         void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Attention with a sliding window and first tokens that stay visible, for rows of any numbers of queries: new tokens, drafted
+ * ones, prompts or pieces of them, in one call.  Row r brings queries query_offsets[r] .. query_offsets[r + 1] - 1, the last ones of its row_lens[r]
+ * tokens (whose keys are in the cache already); the one that is token p of the row sees token j <= p if
+ *   j > p - window   or   j < sinks.
+ * s_j, out and lse as for e3_prefix_attention.  Query head h reads key head h / (q_heads / kv_heads).  A query that sees nothing (of a row with
+ * fewer tokens than queries) gives 0 and -inf.
+ *
+ * q             [tokens][q_heads][head_dim] bf16, strides in elements, columns next to each other; base and strides multiples of 16
+ *               bytes (E3_ERR_ALIGN).
+ * tokens, q_heads   q_heads a multiple of kv_heads, tokens * q_heads below 2^31, rows * kv_heads below 2^24 (E3_ERR_SHAPE).
+ * query_offsets [rows + 1] int32, from 0 on, not falling, at most `tokens` (the caller's contract).  Rows without queries are allowed; out
+ *               and lse_out of queries behind query_offsets[rows] are left as they are.
+ * row_pages     [rows][row_width] int32, row_lens [rows] int32 (tokens, the queries' own included).  Lengths are cut to what the table can hold;
+ *               a page id outside the cache hides its tokens.  Entries of pages of which no query of the row sees a token are not
+ *               used: such pages may have been given to others.  Whatever the cache holds in tokens that a query does not see
+ *               (NaN included) has no influence on it.
+ * window        at least 1; sinks at least 0 (E3_ERR_VALUE).  A window of any row's length and more is plain causal attention.
+ * Elements that are not finite, scale, out [tokens][q_heads][head_dim], lse_out [tokens][q_heads], workspace (at least
+ *               e3_window_attention_workspace_bytes()): as for e3_prefix_attention.
+ * Scores, maxima, sums and outputs' sums in fp32.  Weights enter their product with all of fp32's bits for rows of at most 32 queries
+ * times (q_heads / kv_heads), with 16 of them at least (off by 2^-17 of themselves) for larger ones.  Where the keys are cut into runs depends on
+ * the whole batch, so a row in another batch may differ in the last bits; the same call gives the same bits.
+ * e3_window_attention_workspace_bytes: host only; 0 for a shape that is not served.
+ */
+size_t e3_window_attention_workspace_bytes(int64_t rows, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim);
+int e3_window_attention(const e3_cache* cache, const void* q, int64_t tokens, int64_t q_heads, int64_t q_token_stride, int64_t q_head_stride,
+                        const int32_t* query_offsets, int64_t rows,
+                        const int32_t* row_pages, int64_t row_width, const int32_t* row_lens,
+                        int64_t window, int64_t sinks, float scale, void* out, float* lse_out,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Verification of drafted tokens (speculative sampling) with what a rollout keeps of every token.
  * A row brings `drafts` drafted tokens x_0 .. and the target's logits at drafts + 1 positions
  * (position t: given x_0 .. x_{t-1}).

@@ -9,7 +9,8 @@ from .binding import (E3_BF16, E3_E4M3, E3_F32, E3Cache, E3Error, E3Rotary, e3_a
                       e3_temperature_update_gap, e3_logprob_entropy, e3_logprob_entropy_advantages,
                       e3_prefix_attention, e3_prefix_attention_workspace_bytes,
                       e3_restricted_workspace_bytes, e3_sample_entropy, e3_sample_entropy_noalloc, e3_sample_restricted, e3_strerror,
-                      e3_temperature_update, e3_verify_drafts, e3_verify_workspace_bytes, e3_workspace_bytes, lib, new_cache, new_rotary, new_workspace)
+                      e3_temperature_update, e3_verify_drafts, e3_verify_workspace_bytes, e3_window_attention,
+                      e3_window_attention_workspace_bytes, e3_workspace_bytes, lib, new_cache, new_rotary, new_workspace)
 
 __all__ = ["E3_BF16", "E3_E4M3", "E3_F32", "E3Cache", "E3Error", "E3Rotary", "e3_allocate_budgets", "e3_budget_bounds", "e3_cache_append",
            "e3_cache_append_rotated", "e3_cache_read", "e3_rotate",
@@ -17,5 +18,6 @@ __all__ = ["E3_BF16", "E3_E4M3", "E3_F32", "E3Cache", "E3Error", "E3Rotary", "e3
            "e3_temperature_update_gap", "e3_logprob_entropy", "e3_logprob_entropy_advantages",
            "e3_prefix_attention", "e3_prefix_attention_workspace_bytes",
            "e3_restricted_workspace_bytes", "e3_sample_entropy", "e3_sample_entropy_noalloc", "e3_sample_restricted", "e3_strerror",
-           "e3_temperature_update", "e3_verify_drafts", "e3_verify_workspace_bytes", "e3_workspace_bytes",
+           "e3_temperature_update", "e3_verify_drafts", "e3_verify_workspace_bytes", "e3_window_attention",
+           "e3_window_attention_workspace_bytes", "e3_workspace_bytes",
            "lib", "new_cache", "new_rotary", "new_workspace"]

@@ -35,7 +35,7 @@ EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_
            "e3_grpo_advantages", "e3_temperature_update", "e3_difficulty_ranks",
            "e3_allocate_budgets", "e3_budget_bounds", "e3_logprob_entropy_gap",
            "e3_temperature_update_gap", "e3_grpo_objective", "e3_cache_append", "e3_cache_read",
-           "e3_rotate", "e3_cache_append_rotated",
+           "e3_rotate", "e3_cache_append_rotated", "e3_window_attention", "e3_window_attention_workspace_bytes",
            "e3_prefix_attention", "e3_prefix_attention_workspace_bytes", "e3_verify_drafts",
            "e3_verify_workspace_bytes", "e3_read_probe",
            "e3_time_next_launch", "e3_launch_plan", "e3_launch_plan_of")
@@ -44,7 +44,7 @@ _NATIVE_CALLS = ("e3_grpo_advantages", "e3_grpo_objective", "e3_workspace_bytes"
                  "e3_restricted_workspace_bytes", "e3_sample_restricted_ws", "e3_logprob_entropy_advantages",
                  "e3_logprob_entropy_gap", "e3_temperature_update", "e3_cache_append", "e3_cache_read",
                  "e3_prefix_attention_workspace_bytes", "e3_prefix_attention", "e3_verify_workspace_bytes", "e3_verify_drafts",
-                 "e3_rotate", "e3_cache_append_rotated")
+                 "e3_rotate", "e3_cache_append_rotated", "e3_window_attention", "e3_window_attention_workspace_bytes")
 
 _lib: Optional[C.CDLL] = None
 _native = None                     # the native calls, once they are bound to the loaded library
@@ -138,6 +138,10 @@ def lib() -> C.CDLL:
         L.e3_rotate.restype = C.c_int
         L.e3_cache_append_rotated.argtypes = [vp, vp, vp, i64, vp, vp, vp, C.c_int, i64, i64, i64, i64, i64, i64, i64, i64, vp, vp, i64, i64, vp]
         L.e3_cache_append_rotated.restype = C.c_int
+        L.e3_window_attention_workspace_bytes.argtypes = [i64] * 5
+        L.e3_window_attention_workspace_bytes.restype = C.c_size_t
+        L.e3_window_attention.argtypes = [vp, vp, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, i64, f32, vp, vp, vp, C.c_size_t, vp]
+        L.e3_window_attention.restype = C.c_int
         _bind_native(L)                           # may raise: nothing is loaded then
         _lib = L
     return _lib
@@ -174,7 +178,7 @@ _ENTRY = {"advantages": "e3_grpo_advantages", "objective": "e3_grpo_objective", 
           "logprob_advantages": "e3_logprob_entropy_advantages", "logprob_gap": "e3_logprob_entropy_gap",
           "temperature": "e3_temperature_update", "cache_append": "e3_cache_append", "cache_read": "e3_cache_read",
           "attention": "e3_prefix_attention", "verify": "e3_verify_drafts", "rotate": "e3_rotate",
-          "append_rotated": "e3_cache_append_rotated"}
+          "append_rotated": "e3_cache_append_rotated", "window": "e3_window_attention"}
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -923,6 +927,51 @@ def e3_prefix_attention(q: torch.Tensor, cache: E3Cache, group_offsets: Optional
                                    _ptr(out), _ptr(lse_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
     if rc != E3_OK:
         raise E3Error(rc, "e3_prefix_attention")
+    return out, lse_out
+
+
+def e3_window_attention_workspace_bytes(rows: int, tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    """Host-only; 0 for a shape that is not served."""
+    return int(lib().e3_window_attention_workspace_bytes(rows, tokens, q_heads, kv_heads, head_dim))
+
+
+def e3_window_attention(q: torch.Tensor, cache: E3Cache, query_offsets: torch.Tensor, row_pages: torch.Tensor, row_lens: torch.Tensor,
+                        window: int, sinks: int, scale: float, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, want_lse: bool = True):
+    """Attention with a sliding window over the cache: q bf16 [tokens, q_heads, D]; row r brings queries query_offsets[r] ..
+    query_offsets[r + 1] - 1 (int32 [rows + 1]), the last ones of its row_lens[r] tokens (int32 [rows], in pages row_pages int32 [rows, width]); the
+    one at position p sees the tokens j <= p with j > p - window or j < sinks.  Returns (out bf16 like q, lse fp32 [tokens, q_heads] or
+    None).  workspace: a tensor of e3_window_attention_workspace_bytes(), or None to allocate one."""
+    res = _ordinary("window", q, cache, query_offsets, row_pages, row_lens, window, sinks, scale, out, lse_out, workspace, want_lse)
+    if res is not None:
+        return res
+    c = _cache(cache)
+    dev = cache[0].device
+    if q.dim() != 3:
+        raise ValueError(f"q must be [tokens, q_heads, {c.head_dim}]")
+    tokens, q_heads, D = q.shape
+    _heads(q, "q", torch.bfloat16, (tokens, q_heads, c.head_dim), dev)
+    rows = query_offsets.shape[0] - 1
+    _check(query_offsets, torch.int32, rows + 1, "query_offsets", dev)
+    row_width = _table(row_pages, rows, "row_pages", dev)
+    _check(row_lens, torch.int32, rows, "row_lens", dev)
+    if out is None:
+        out = torch.empty((tokens, q_heads, D), dtype=torch.bfloat16, device=dev)
+    elif out.dtype is not torch.bfloat16 or out.shape != q.shape or out.device != dev or not out.is_contiguous():
+        raise ValueError(f"out must be a contiguous bf16 tensor {tuple(q.shape)} on {dev}")
+    if lse_out is None:
+        lse_out = torch.empty((tokens, q_heads), dtype=torch.float32, device=dev) if want_lse else None
+    elif lse_out.dtype is not torch.float32 or lse_out.shape != q.shape[:2] or lse_out.device != dev or not lse_out.is_contiguous():
+        raise ValueError(f"lse_out must be a contiguous fp32 tensor {tuple(q.shape[:2])} on {dev}")
+    if workspace is None:
+        workspace = torch.empty(e3_window_attention_workspace_bytes(rows, tokens, q_heads, c.kv_heads, D), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    rc = lib().e3_window_attention(C.byref(c), _ptr(q), tokens, q_heads, _step(q, 0), _step(q, 1), _ptr(query_offsets), rows, _ptr(row_pages),
+                                   row_width, _ptr(row_lens), int(window), int(sinks), float(scale), _ptr(out), _ptr(lse_out), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_window_attention")
     return out, lse_out
 
 

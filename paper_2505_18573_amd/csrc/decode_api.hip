@@ -8,6 +8,7 @@
 #include "rotary.h"
 #include "verify.h"
 #include "vocab_pass.h"
+#include "window_attention.h"
 
 namespace {
 
@@ -187,6 +188,47 @@ extern "C" int e3_prefix_attention(const e3_cache* cache, const void* q, int64_t
     a.prefix_width = (int32_t)prefix_width; a.row_width = (int32_t)row_width;
     a.scale = scale; a.out = static_cast<uint16_t*>(out); a.lse = lse_out;
     const hipError_t err = e3::launch_prefix_attention(view, a, workspace, static_cast<hipStream_t>(hip_stream));
+    return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
+}
+
+static bool window_dims(int64_t rows, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim)
+{
+    return rows >= 0 && rows <= (1 << 24) && tokens >= 0 && tokens <= 0x7FFFFFFF && kv_heads >= 1 && kv_heads <= 65536 && q_heads >= kv_heads &&
+           q_heads <= (1 << 20) && q_heads % kv_heads == 0 && (head_dim == 64 || head_dim == 128);
+}
+
+extern "C" size_t e3_window_attention_workspace_bytes(int64_t rows, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim)
+{
+    if (rows == 0 || tokens == 0 || !window_dims(rows, tokens, q_heads, kv_heads, head_dim)) return 0;
+    return e3::window_attention_workspace_bytes(rows, tokens, q_heads, kv_heads, head_dim);
+}
+
+extern "C" int e3_window_attention(const e3_cache* cache, const void* q, int64_t tokens, int64_t q_heads, int64_t q_token_stride,
+                                   int64_t q_head_stride, const int32_t* query_offsets, int64_t rows,
+                                   const int32_t* row_pages, int64_t row_width, const int32_t* row_lens,
+                                   int64_t window, int64_t sinks, float scale, void* out, float* lse_out,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    e3::CacheView view;
+    const int rc = check_cache(cache, &view);
+    if (rc != E3_OK) return rc;
+    if (!window_dims(rows, tokens, q_heads, view.heads, view.dim) || row_width < 0 || row_width > 0x7FFFFFFF) return E3_ERR_SHAPE;
+    if (!std::isfinite(scale) || !(scale > 0.0f) || window < 1 || sinks < 0) return E3_ERR_VALUE;
+    if (rows == 0 || tokens == 0) return E3_OK;
+    const size_t need = e3::window_attention_workspace_bytes(rows, tokens, q_heads, view.heads, view.dim);
+    if (need == 0) return E3_ERR_SHAPE;
+    if (q == nullptr || out == nullptr || query_offsets == nullptr || row_lens == nullptr || (row_pages == nullptr && row_width > 0)) return E3_ERR_NULL;
+    if (workspace == nullptr || workspace_bytes < need) return E3_ERR_WORKSPACE;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256) || q_token_stride % 8 || q_head_stride % 8) return E3_ERR_ALIGN;
+    constexpr int64_t kMost = 0x7F000000;                           // no sequence is longer
+    e3::WindowArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_token_stride = q_token_stride; a.q_head_stride = q_head_stride;
+    a.tokens = (int32_t)tokens; a.rows = (int32_t)rows; a.q_heads = (int32_t)q_heads;
+    a.offsets = query_offsets; a.row_pages = row_pages; a.row_lens = row_lens; a.row_width = (int32_t)row_width;
+    a.window = (int32_t)(window < kMost ? window : kMost); a.sinks = (int32_t)(sinks < kMost ? sinks : kMost);
+    a.scale = scale; a.out = static_cast<uint16_t*>(out); a.lse = lse_out;
+    const hipError_t err = e3::launch_window_attention(view, a, workspace, static_cast<hipStream_t>(hip_stream));
     return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
 }
 

@@ -38,6 +38,8 @@ decltype(&e3_prefix_attention) p_attention;
 decltype(&e3_verify_workspace_bytes) p_verify_bytes;
 decltype(&e3_verify_drafts) p_verify;
 decltype(&e3_rotate) p_rotate;
+decltype(&e3_window_attention) p_window;
+decltype(&e3_window_attention_workspace_bytes) p_window_bytes;
 decltype(&e3_cache_append_rotated) p_append_rotated;
 PyObject* raw_stream = nullptr;
 
@@ -661,6 +663,42 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     });
 }
 
+// q, cache, query_offsets, row_pages, row_lens, window, sinks, scale, out, lse_out, workspace, want_lse
+PyObject* window(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 12 || !PyBool_Check(a[11])) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const Cache cache(r, a[1]);
+        const at::Tensor* q = r.ok ? r.plain(a[0]) : nullptr;
+        const at::Tensor* offsets = r.ok ? r.plain(a[2]) : nullptr;
+        const at::Tensor* pages = r.ok ? r.plain(a[3]) : nullptr;
+        if (!r.ok || q->dim() != 3 || q->scalar_type() != at::kBFloat16 || q->device() != r.dev || q->size(2) != cache.c.head_dim || !unit_columns(q)
+            || offsets->dim() != 1 || offsets->size(0) < 1 || a[4] == Py_None) return unusual();
+        const int64_t tokens = q->size(0), heads = q->size(1), D = q->size(2), rows = offsets->size(0) - 1;
+        const void* of = r.vector(a[2], at::kInt, rows + 1);
+        if (pages->scalar_type() != at::kInt || pages->dim() != 2 || pages->size(0) != rows || !pages->is_contiguous() || pages->device() != r.dev)
+            return unusual();
+        const void* lens = r.vector(a[4], at::kInt, rows);
+        const int64_t width = r.integer(a[5]), sinks = r.integer(a[6]);
+        const double scale = r.number(a[7]);
+        if (!r.ok) return unusual();
+        Output out, lse;
+        out.shaped(r, a[8], at::kBFloat16, std::array<int64_t, 3>{tokens, heads, D});
+        if (a[9] == Py_None && a[11] == Py_False) lse.take(Py_None);
+        else lse.shaped(r, a[9], at::kFloat, std::array<int64_t, 2>{tokens, heads});
+        const size_t need = a[10] == Py_None ? p_window_bytes(rows, tokens, heads, cache.c.kv_heads, D) : 0;
+        const Workspace ws(r, a[10] == Py_False ? Py_True : a[10], need, true);
+        if (a[10] == Py_None && need > 0 && ws.p == nullptr) return unusual();
+        return run(r, [&](void* s) {
+                       return p_window(&cache.c, q->data_ptr(), tokens, heads, step_of(q, 0), step_of(q, 1), (const int32_t*)of, rows,
+                                       (const int32_t*)pages->data_ptr(), pages->size(1), (const int32_t*)lens, width, sinks, (float)scale, out.p,
+                                       (float*)lse.p, ws.p, ws.bytes, s);
+                   },
+                   [&] { return PyTuple_Pack(2, out.object, lse.object); });
+    });
+}
+
 // logits, draft_tokens, draft_logits, draft_lens, tau_rows, tau_scalar, seed, row_base, draft_tau_rows, accepted_out, token_out,
 // logp_out, entropy_out, workspace
 PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n_args)
@@ -764,6 +802,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     get("e3_verify_workspace_bytes", p_verify_bytes);
     get("e3_verify_drafts", p_verify);
     get("e3_rotate", p_rotate);
+    get("e3_window_attention", p_window);
+    get("e3_window_attention_workspace_bytes", p_window_bytes);
     get("e3_cache_append_rotated", p_append_rotated);
     if (!all) { PyErr_SetString(PyExc_ValueError, "an entry point is missing"); return nullptr; }
     Py_INCREF(a[1]);
@@ -789,6 +829,7 @@ PyMethodDef methods[] = {
     {"attention", fast(attention), METH_FASTCALL, nullptr},
     {"verify", fast(verify), METH_FASTCALL, nullptr},
     {"rotate", fast(rotate), METH_FASTCALL, nullptr},
+    {"window", fast(window), METH_FASTCALL, nullptr},
     {"append_rotated", fast(append_rotated), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -1,0 +1,929 @@
+// Attention over the paged cache with a sliding window and first tokens that stay visible.
+//
+//   row r brings n_r queries, the last n_r of its len_r tokens; the one at position p sees
+//   { j <= p : j > p - window or j < sinks },   s_j = scale q . k_j,   out = sum e^{s_j - m} v_j / l,   lse = m + ln l.
+//
+// The softmax's maximum and sum are running ones, and partial results (m, l, O) over disjoint sets of keys join exactly, so the
+// work may be cut anywhere.  Three launches:
+//   plan     one workgroup makes the list of work: lengths and numbers of queries are device memory.  A row's queries of one key
+//            head (tokens x query heads) are cut into tiles; a tile and a key head are an item, measured in steps of tokens that
+//            any of its queries sees (pages that none sees are never touched) and a little for the item itself.
+//   attend   Items of at most 32 queries are a wave's work: a new token's or a few drafted ones', bound by reading the keys, which go from
+//            memory straight into operand registers.  Larger ones, tiles of 128 queries of prompts, are a workgroup's: bound by
+//            the matrix instructions, the keys pass through LDS once for four waves of 32 queries.  Either kind lies on a line, cut into as
+//            many equal stretches as there are workers, whichever items they fall into.  An item that lies in one
+//            stretch is written out; of one that is cut every worker leaves its part in the workspace.
+//   join     the parts of cut items.
+//
+// Weights times values.  For few queries the weights enter as three bf16 numbers, all 24 bits of an fp32 weight, as memory is what
+// is waited for.  For tiles of prompts they enter as two, 16 bits and more: a weight is off by 2^-17 of itself at most, far below the output's own
+// rounding (2^-9 at best) unless an output's terms cancel to less than a hundredth, while one number alone (2^-9)
+// would add as much error as the output's rounding; the third product would cost a quarter more time.
+#include "attention_step.h"
+#include "stretch.h"
+#include "vocab_pass.h"
+#include "window_attention.h"
+
+namespace e3 {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kWaves = 4;                       // of a workgroup
+constexpr int kFewQueries = 32;                 // an item of so many is a wave's
+constexpr int kTile = 128;                      // queries of a workgroup's item
+constexpr int kBlock = 64;                      // tokens of a workgroup's step
+constexpr int kCost = 2;                        // what an item costs besides its steps, in steps of either kind
+constexpr int kPerUnit = 2;                     // workgroups per compute unit
+constexpr float kBlockCost = 1.0f;              // a workgroup's step against four steps of its waves
+
+enum { kOfGroups = 0, kOfWaves = 1 };           // the two lines
+
+// A tile of a row's queries, all key heads: its place on its line is in steps.
+struct Work {
+    int64_t first;
+    int32_t row, tile, offset, n, len, cost;    // offset, n: the row's queries; cost: steps of one key head, kCost among them
+};
+struct Totals {
+    int64_t steps[2];
+    int32_t count[2];
+};
+// The item that a worker's stretch begins inside of, if the item's first part is the worker's before: parts worker - 1 .. last are joined.
+struct Cut {
+    int32_t work, head, last, unused;           // work: -1 where there is none
+};
+
+struct WindowShape {
+    int32_t R;                                  // query heads per key head
+    int64_t most[2];                            // records of either line
+    int32_t workers[2];                         // at most
+    int64_t at_list[2], at_cuts, at_ml, at_o[2], bytes;
+};
+
+static int64_t up(int64_t x) { return (x + 255) / 256 * 256; }
+
+static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t heads, int64_t D, WindowShape& s)
+{
+    s.R = (int32_t)(q_heads / heads);
+    if (rows * heads >= (1 << 24) || tokens * q_heads > 0x7FFFFFFF) return false;
+    const int groups = compute_units() * kPerUnit;
+    const int64_t queries = tokens * s.R;
+    s.most[kOfGroups] = queries > kFewQueries ? queries / kTile + rows : 0;
+    s.most[kOfWaves] = rows;
+    s.workers[kOfGroups] = s.most[kOfGroups] > 0 ? groups : 0;
+    s.workers[kOfWaves] = groups * kWaves;
+    int64_t at = up(sizeof(Totals));
+    for (int k = 0; k < 2; ++k) { s.at_list[k] = at; at = up(at + s.most[k] * (int64_t)sizeof(Work)); }
+    s.at_cuts = at;
+    at = up(at + (s.workers[0] + s.workers[1]) * (int64_t)sizeof(Cut));
+    // partial results: two places for each worker (what its stretch begins inside of, what it ends inside of)
+    s.at_ml = at;
+    at = up(at + (s.workers[0] * (int64_t)kTile + s.workers[1] * (int64_t)kFewQueries) * 2 * (int64_t)sizeof(float2));
+    s.at_o[kOfGroups] = at;
+    at = up(at + s.workers[0] * (int64_t)kTile * 2 * D * 4);
+    s.at_o[kOfWaves] = at;
+    s.bytes = up(at + s.workers[1] * (int64_t)kFewQueries * 2 * D * 4);
+    return true;
+}
+
+size_t window_attention_workspace_bytes(int64_t rows, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim)
+{
+    WindowShape s;
+    return window_shape(rows, tokens, q_heads, heads, dim, s) ? (size_t)s.bytes : 0;
+}
+
+// ---------------------------------------------------------------- which tokens
+__host__ __device__ __forceinline__ int tiles_of(int64_t queries) { return queries <= kFewQueries ? 1 : (int)((queries + kTile - 1) / kTile); }
+
+// The tokens of a tile's item, in steps of `apart` tokens: first those of the always visible tokens that lie before the
+// window's, then the window's.
+struct Band {
+    int p0, p1;                                 // positions of the tile's first and last query
+    int first_steps, skip;                      // step k is at token (k < first_steps ? k : k + skip) * apart
+    int steps;
+    __device__ __forceinline__ int at(int k, int apart) const { return (k < first_steps ? k : k + skip) * apart; }
+};
+__device__ __forceinline__ Band band_of(int R, int tile, int n, int len, int window, int sinks, int apart)
+{
+    const int64_t queries = (int64_t)n * R;
+    const int64_t q0 = (int64_t)tile * kTile, q1 = queries <= kFewQueries || q0 + kTile > queries ? queries : q0 + kTile;
+    Band b;
+    b.p0 = len - n + (int)(q0 / R);
+    b.p1 = len - n + (int)((q1 - 1) / R);
+    const int hi = b.p1 + 1;                                                   // none sees a token from here on
+    if (hi <= 0) { b.first_steps = b.skip = b.steps = 0; return b; }
+    const int lo = (b.p0 < 0 ? 0 : b.p0) >= window ? b.p0 - window + 1 : 0;    // none sees one before it, but the first ones
+    const int lo_step = lo / apart, kept = sinks < hi ? sinks : hi;
+    const int kept_steps = (int)(((int64_t)kept + apart - 1) / apart);
+    b.first_steps = kept_steps < lo_step ? kept_steps : lo_step;
+    b.skip = lo_step - b.first_steps;
+    b.steps = (int)(((int64_t)hi + apart - 1) / apart) - b.skip;
+    return b;
+}
+
+// ---------------------------------------------------------------- plan
+constexpr int kPlanWaves = 16, kPlanLanes = 64 * kPlanWaves, kPlanRows = 8192;
+
+__global__ __launch_bounds__(kPlanLanes)
+void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, char* ws)
+{
+    __shared__ int offsets_lds[kPlanRows + 1];
+    __shared__ int64_t sums[kPlanWaves][3];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool in_lds = a.rows <= kPlanRows;
+    if (in_lds) {
+        for (int i = threadIdx.x; i <= a.rows; i += kPlanLanes) offsets_lds[i] = clamp_len(a.offsets[i], a.tokens);
+        __syncthreads();
+    }
+    auto offset = [&](int r) { return in_lds ? offsets_lds[r] : clamp_len(a.offsets[r], a.tokens); };
+    // Places for tiles: a row's lie from key(row) on, as many as it can have.
+    auto key = [&](int r) { return (int64_t)offset(r) * s.R / kTile + r; };
+    const int64_t places = (int64_t)a.tokens * s.R / kTile + a.rows;
+    const int64_t share = (places + kPlanLanes - 1) / kPlanLanes;
+    const int64_t begin = threadIdx.x * share, end = begin + share < places ? begin + share : places;
+    const int64_t visible = table_tokens(a.row_width, page_size);
+    // f(line, record) for every tile among the thread's places
+    auto each = [&](auto f) {
+        if (begin >= end) return;
+        int low = 0, high = a.rows;                                            // the last row whose places begin at or before `begin`
+        while (high - low > 1) {
+            const int mid = (low + high) / 2;
+            if (key(mid) <= begin) low = mid;
+            else high = mid;
+        }
+        for (int r = low; r < a.rows && key(r) < end; ++r) {
+            const int off = offset(r), n = offset(r + 1) - off;
+            if (n <= 0) continue;
+            const int64_t k = key(r), queries = (int64_t)n * s.R;
+            const int line = queries <= kFewQueries ? kOfWaves : kOfGroups;
+            const int64_t last = k + tiles_of(queries);
+            const int len = clamp_len(a.row_lens[r], visible);
+            for (int64_t u = k > begin ? k : begin; u < last && u < end; ++u) {
+                Work w;
+                w.first = 0; w.row = r; w.tile = (int)(u - k); w.offset = off; w.n = n; w.len = len;
+                w.cost = kCost + band_of(s.R, w.tile, n, len, a.window, a.sinks, line == kOfWaves ? kStep : kBlock).steps;
+                f(line, w);
+            }
+        }
+    };
+    int64_t own[3] = {0, 0, 0};                                                // steps of both lines; tiles, the waves' in the upper half
+    each([&](int line, const Work& w) {
+        own[0] += line == 0 ? (int64_t)w.cost * heads : 0;
+        own[1] += line == 1 ? (int64_t)w.cost * heads : 0;
+        own[2] += line == 1 ? 1ll << 32 : 1;
+    });
+    int64_t sum[3], all[3] = {0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        sum[k] = own[k];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t y = __shfl_up(sum[k], d);
+            if (lane >= d) sum[k] += y;
+        }
+        if (lane == 63) sums[wave][k] = sum[k];
+        sum[k] -= own[k];
+    }
+    __syncthreads();
+    for (int i = 0; i < kPlanWaves; ++i)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            if (i < wave) sum[k] += sums[i][k];
+            all[k] += sums[i][k];
+        }
+    int64_t at[2] = {sum[0], sum[1]};
+    int64_t index[2] = {sum[2] & 0xFFFFFFFF, sum[2] >> 32};
+    each([&](int line, Work w) {
+        w.first = line == 0 ? at[0] : at[1];
+        const int64_t i = line == 0 ? index[0]++ : index[1]++;
+        if (line == 0) at[0] += (int64_t)w.cost * heads;
+        else at[1] += (int64_t)w.cost * heads;
+        if (i < s.most[line]) reinterpret_cast<Work*>(ws + s.at_list[line])[i] = w;
+    });
+    if (threadIdx.x == 0) {
+        Totals t;
+        // (offsets that fall, against the contract, could give more tiles than there is room for: nothing is done then)
+        const bool fits = (all[2] & 0xFFFFFFFF) <= s.most[0] && (all[2] >> 32) <= s.most[1];
+        t.steps[0] = fits ? all[0] : 0;
+        t.steps[1] = fits ? all[1] : 0;
+        t.count[0] = (int)(all[2] & 0xFFFFFFFF);
+        t.count[1] = (int)(all[2] >> 32);
+        *reinterpret_cast<Totals*>(ws) = t;
+    }
+}
+
+// How the workgroups and stretches are divided, the same in every launch that asks.
+struct Division {
+    int64_t steps[2];
+    int groups;                                 // workgroups of the line of workgroups
+    int parts[2];                               // stretches
+};
+__device__ __forceinline__ Division divide_work(const Totals& t, int workgroups)
+{
+    Division d;
+    d.steps[0] = uniform(t.steps[0]);
+    d.steps[1] = uniform(t.steps[1]);
+    const float of_groups = (float)d.steps[0] * kBlockCost, of_waves = (float)d.steps[1] * (1.0f / kWaves);
+    int share = (int)(of_groups / (of_groups + of_waves) * (float)workgroups + 0.5f);
+    if (d.steps[1] > 0 && share > workgroups - 1) share = workgroups - 1;
+    if (d.steps[0] > 0 && share < 1) share = 1;
+    d.groups = d.steps[0] == 0 ? 0 : uniform(share);
+    const int64_t most[2] = {d.groups, (int64_t)(workgroups - d.groups) * kWaves};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int least = k == kOfGroups ? 4 : d.steps[k] < 512 ? 1 : d.steps[k] < 1024 ? 2 : 4;
+        const int64_t enough = (d.steps[k] + least - 1) / least;
+        d.parts[k] = (int)(enough < most[k] ? enough : most[k]);
+    }
+    return d;
+}
+
+// The last record that begins at or before a step: every lane looks at a 64th of what is left.
+__device__ __forceinline__ int find_work(const Work* list, int count, int64_t step)
+{
+    const int lane = threadIdx.x & 63;
+    int first = 0, left = count;
+    while (left > 1) {
+        const int apart = (left + 63) / 64, at = lane * apart;
+        const int n = (int)__popcll(__ballot(at < left && list[first + (at < left ? at : 0)].first <= step));
+        const int k = n > 0 ? n - 1 : 0;
+        first += k * apart;
+        left = left - k * apart < apart ? left - k * apart : apart;
+    }
+    return uniform(first);
+}
+__device__ __forceinline__ Work uniform(const Work& w)
+{
+    return Work{uniform(w.first), uniform(w.row), uniform(w.tile), uniform(w.offset), uniform(w.n), uniform(w.len), uniform(w.cost)};
+}
+
+// ---------------------------------------------------------------- attend
+struct Piece1 {                                 // of an item: real steps [from, to)
+    int head, from, to;
+    bool whole;
+};
+// A query of a tile: where it lies and what it sees.
+struct Query {
+    int token, head;                            // of q and out
+    int lo, hi;                                 // tokens lo .. hi - 1, and the first ones
+    bool is;
+};
+__device__ __forceinline__ Query query_of(const WindowArgs& a, int R, const Work& w, int head, int64_t index)
+{
+    Query q;
+    q.is = index < (int64_t)w.n * R;
+    const int t = q.is ? (int)(index / R) : 0, h = q.is ? (int)(index % R) : 0;
+    const int p = w.len - w.n + t;
+    q.token = w.offset + t;
+    q.head = head * R + h;
+    q.hi = p < 0 ? 0 : p + 1;
+    q.lo = p >= a.window ? p - a.window + 1 : 0;
+    return q;
+}
+__device__ __forceinline__ int64_t page_row(const CacheView& c, int head, int page, int at)
+{
+    const int64_t p = (uint32_t)page < (uint64_t)c.num_pages ? page : 0;
+    return (p * c.heads + head) * c.page_size + (at & (c.page_size - 1));
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    const bf16x2 p = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, p);
+}
+
+// A wave's item: kTiles columns of 16 queries.  One query's scores lie in one lane column (see prefix attention's step).
+template <int D, bool kFp8, int kTiles>
+struct Few {
+    using Data = StepData<D, kFp8>;
+    static constexpr int kBlocks = D / 16, kSteps = D / 32;
+    bf16x8 q[kTiles][kSteps];
+    f32x4 o[kTiles][kBlocks];
+    float m[kTiles], l[kTiles];
+    int lo[kTiles], hi[kTiles];
+
+    __device__ __forceinline__ void run(const CacheView& c, const WindowArgs& a, int R, const Work& w, const Piece1& piece, float2* ml_out, float* o_out)
+    {
+        const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+        const Band band = band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kStep);
+        const int sure_hi = band.p0 + 1;                                       // every query sees the tokens below it
+        const int sure_lo = band.p1 >= a.window ? band.p1 - a.window + 1 : 0;  // and from here on
+        const int32_t* pages = a.row_pages + (int64_t)w.row * a.row_width;
+        auto page_at = [&](int k) { return k < piece.to ? pages[band.at(k, kStep) >> c.page_shift] : -1; };
+        Data d;
+        int page = page_at(piece.from), page_next = page_at(piece.from + 1);
+        {
+            const int64_t row = page_row(c, piece.head, page, band.at(piece.from, kStep));
+            d.load_keys(c, row, lane);
+            d.load_values(c, row, lane);
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const Query x = query_of(a, R, w, piece.head, t * 16 + col);
+            const uint16_t* qp = a.q + x.token * a.q_token_stride + x.head * a.q_head_stride;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                u32x4 v = *reinterpret_cast<const u32x4*>(qp + Data::key_column(s, g));
+                if (!x.is) v = u32x4{0, 0, 0, 0};
+                q[t][s] = __builtin_bit_cast(bf16x8, v);
+            }
+            lo[t] = x.lo; hi[t] = x.hi;
+            m[t] = kNoScore; l[t] = 0.0f;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        const float scale = a.scale * kLog2eF;
+        for (int k = piece.from; k < piece.to; ++k) {
+            const int at = band.at(k, kStep);
+            const int page_after = page_at(k + 2);
+            const int64_t next = page_row(c, piece.head, page_next, k + 1 < piece.to ? band.at(k + 1, kStep) : 0);   // behind the last: read for nothing
+            const bool there = (uint32_t)page < (uint64_t)c.num_pages;
+            const bool edge = !there || at + kStep > sure_hi || (at < sure_lo && at + kStep > a.sinks);   // uniform: not all see all
+            float x[kTiles][8];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                f32x4 s[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) s[u] = mfma(d.key(u, i), q[t][i], s[u]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[t][j] = s[j >> 2][j & 3] * (kFp8 ? scale * d.k_factor(j) : scale);
+            }
+            d.load_keys(c, next, lane);
+            auto sees = [&](int t, int j) {
+                const int token = at + 8 * g + j;
+                return there && token < hi[t] && (token >= lo[t] || token < a.sinks);
+            };
+            if (edge) {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[t][j] = sees(t, j) ? x[t][j] : -INFINITY;
+            }
+            bf16x8 p[kTiles], rest[kTiles], last[kTiles];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                float top = fmax3(fmax3(x[t][0], x[t][1], x[t][2]), fmax3(x[t][3], x[t][4], x[t][5]), fmaxf(x[t][6], x[t][7]));
+                if (__any(top > m[t] + kSlack)) {
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float to = fmaxf(m[t], top);
+                    const float f = __builtin_amdgcn_exp2f(m[t] - to);
+                    m[t] = to;
+                    l[t] *= f;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) o[t][b] *= f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(x[t][j] - m[t]);
+                    l[t] += e;
+                    float v = kFp8 ? e * d.v_factor(j) : e;
+                    if (kFp8 && edge) v = sees(t, j) ? v : 0.0f;               // a hidden token's scale may be anything
+                    p[t][j] = (__bf16)v;
+                    const float left = v - (float)p[t][j];
+                    rest[t][j] = (__bf16)left;
+                    last[t][j] = (__bf16)(left - (float)rest[t][j]);
+                }
+            }
+            // Tokens that not all queries see: a weight of zero keeps them out, unless the value is no finite number.  Such values
+            // leave the product, and one more counts those that a query sees.
+            if (__builtin_expect(edge && __any(d.unbounded()), 0)) {
+#pragma unroll
+                for (int i = 0; i < Data::kVLoads; ++i) {
+                    u32x4 ones;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t bad = Data::unbounded_in(d.v[i][j]);
+                        ones[j] = bad & (kFp8 ? 0x38383838u : 0x3F803F80u);
+                        d.v[i][j] &= ~bad;
+                    }
+#pragma unroll
+                    for (int u = 0; u < kBlocks / Data::kVLoads; ++u) {
+                        const int b = i * (kBlocks / Data::kVLoads) + u;
+                        const bf16x8 one = kFp8 ? (u ? widen(ones.z, ones.w) : widen(ones.x, ones.y)) : __builtin_bit_cast(bf16x8, ones);
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            bf16x8 seen;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(sees(t, j) ? 1.0f : 0.0f);
+                            const f32x4 count = mfma(one, seen, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) o[t][b][n] = count[n] > 0.0f ? __builtin_nanf("") : o[t][b][n];
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                const bf16x8 value = d.value(b);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) o[t][b] = mfma(value, last[t], mfma(value, rest[t], mfma(value, p[t], o[t][b])));
+            }
+            d.load_values(c, next, lane);
+            page = page_next;
+            page_next = page_after;
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            l[t] += __shfl_xor(l[t], 16);
+            l[t] += __shfl_xor(l[t], 32);
+            const Query x = query_of(a, R, w, piece.head, t * 16 + col);
+            if (!x.is) continue;
+            if (!piece.whole) {
+                if (g == 0) ml_out[t * 16 + col] = float2{m[t], l[t]};
+                float* to = o_out + (int64_t)(t * 16 + col) * D;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to[Data::column(b, 4 * g + i)] = o[t][b][i];
+                continue;
+            }
+            const bool none = l[t] == 0.0f && m[t] == kNoScore;
+            const float inv = none ? 0.0f : 1.0f / l[t];
+            const int64_t where = (int64_t)x.token * a.q_heads + x.head;
+            uint16_t* to = a.out + where * D;
+            if (kFp8) {                                                        // blocks b and b + 1 hold columns in turn
+#pragma unroll
+                for (int b = 0; b < kBlocks; b += 2) {
+                    u32x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = pack2(o[t][b][i] * inv, o[t][b + 1][i] * inv);
+                    *reinterpret_cast<u32x4*>(to + Data::column(b, 4 * g)) = v;
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+                    *reinterpret_cast<u32x2*>(to + Data::column(b, 4 * g)) =
+                        u32x2{pack2(o[t][b][0] * inv, o[t][b][1] * inv), pack2(o[t][b][2] * inv, o[t][b][3] * inv)};
+            }
+            if (a.lse && g == 0) a.lse[where] = none ? -INFINITY : (m[t] + __builtin_amdgcn_logf(l[t])) * (float)kLn2;
+        }
+    }
+};
+
+// A workgroup's item: a wave takes 32 queries, on the columns of 32 x 32 products.  S^T = K Q^T leaves 16 scores of one query in a lane,
+// and since a sum over tokens may be taken in any order, row 8 a + 4 h + b of a score tile is given token 16 (a >> 1) + 8 h + 4 (a & 1) + b:
+// a lane's scores are then tokens 8 h .. 8 h + 7 of either half, what it has to hold of P^T as operand of O^T = V^T P^T.
+// In LDS, twice: keys as rows of 16-byte pieces whose places are turned by the token, so that the lanes of a wave, which read one
+// piece of 32 rows, meet all banks; values as the cache has them, eight tokens of a column together, widened to bf16 where the
+// cache holds codes (once for the four waves; the powers of two are applied in fp32 to scores and weights).
+template <int D, bool kFp8>
+struct Many {
+    static constexpr int kPieces = D / 8;                                      // 16-byte pieces of a row in bf16
+    static constexpr int kKeys = kBlock * D * 2, kValues = kBlock * D * 2;
+    static constexpr int kFactors = 2 * kBlock * 4;
+    static constexpr int kImage = kKeys + kValues + kFactors + 16;             // and four flags
+    static constexpr int kLds = 2 * kImage;
+    static constexpr int kLoads = kFp8 ? kBlock * D / 16 / 256 : kBlock * D / 8 / 256;     // of 16 bytes, a thread's, of K and of V
+    static constexpr int kCols = D / 32, kDeep = D / 16;
+
+    static constexpr int kElem = kFp8 ? 1 : 2;
+
+    u32x4 k[kLoads], v[kLoads];
+    uint32_t factor;
+
+    static __device__ __forceinline__ int turned(int token, int piece)
+    {
+        return piece ^ (kPieces == 16 ? token & 15 : (token >> 1) & 7);
+    }
+    // A block's rows into registers: pages of its two halves.
+    __device__ __forceinline__ void fetch(const CacheView& c, int head, const int page[2], int at)
+    {
+        constexpr int kRow = D * kElem / 16;                                   // pieces of a row in the cache
+        const int64_t row[2] = {page_row(c, head, page[0], at), page_row(c, head, page[1], at + 32)};
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = i * 256 + (int)threadIdx.x, token = x / kRow, piece = x % kRow;
+            const int64_t from = (token < 32 ? row[0] : row[1]) + (token & 31);
+            k[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(c.k) + from * (D * kElem) + piece * 16);
+            // values: a block of eight tokens is as long as eight rows
+            const int half = x / (32 * kRow), in = x % (32 * kRow);
+            v[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(c.v) + row[half] * (D * kElem) + in * 16);
+        }
+        if (kFp8) {
+            const int token = threadIdx.x & 63;
+            const int64_t from = (token < 32 ? row[0] : row[1]) + (token & 31);
+            factor = threadIdx.x < 64 ? c.k_scale[from] : c.v_scale[from];
+        }
+    }
+    static __device__ __forceinline__ u32x4 wide(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(u32x4, widen(lo, hi)); }
+    // ... and into LDS.  `check`: values may be hidden from some queries; those that are no finite numbers become zeros, and flags
+    // tell of them.
+    __device__ __forceinline__ void put(char* image, float scale, bool check)
+    {
+        constexpr int kRow = D * (kFp8 ? 1 : 2) / 16;
+        u32x4* keys = reinterpret_cast<u32x4*>(image);
+        u32x4* values = reinterpret_cast<u32x4*>(image + kKeys);
+        uint32_t bad = 0;
+        if (check) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = StepData<D, kFp8>::unbounded_in(v[i][j]);
+                    v[i][j] &= ~w;
+                    bad |= w;
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = i * 256 + (int)threadIdx.x, token = x / kRow, piece = x % kRow;
+            if (kFp8) {
+                keys[token * kPieces + turned(token, 2 * piece)] = wide(k[i].x, k[i].y);
+                keys[token * kPieces + turned(token, 2 * piece + 1)] = wide(k[i].z, k[i].w);
+                values[2 * x] = wide(v[i].x, v[i].y);
+                values[2 * x + 1] = wide(v[i].z, v[i].w);
+            } else {
+                keys[token * kPieces + turned(token, piece)] = k[i];
+                values[x] = v[i];
+            }
+        }
+        float* factors = reinterpret_cast<float*>(image + kKeys + kValues);
+        if (kFp8 && threadIdx.x < 128) {
+            const float f = __uint_as_float(factor << 23);
+            factors[threadIdx.x] = threadIdx.x < 64 ? f * scale : f;
+        }
+        const bool any = __any(bad != 0);
+        if ((threadIdx.x & 63) == 0) reinterpret_cast<int*>(image + kKeys + kValues + kFactors)[threadIdx.x >> 6] = any;
+    }
+    // Writes to LDS are there for all waves.  Loads from memory stay on their way.
+    static __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+    static __device__ __forceinline__ f32x16 product(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16 zero()
+    {
+        f32x16 z;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+        return z;
+    }
+
+    __device__ __forceinline__ void run(const CacheView& c, const WindowArgs& a, int R, const Work& w, const Piece1& piece, char* lds,
+                                        float2* ml_out, float* o_out)
+    {
+        const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
+        const Band band = band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kBlock);
+        const int32_t* pages = a.row_pages + (int64_t)w.row * a.row_width;
+        // pages of the halves of step s; a half that none of the tile's queries sees may lie behind the table
+        auto page_at = [&](int s, int half) {
+            const int at = s < piece.to ? band.at(s, kBlock) + 32 * half : 0x7FFFFFFF;
+            return at <= band.p1 ? pages[at >> c.page_shift] : -1;
+        };
+        // the wave's queries
+        const int64_t first = (int64_t)w.tile * kTile + wave * 32, queries = (int64_t)w.n * R;
+        const bool busy = first < queries;
+        const int64_t end = first + 32 < queries ? first + 32 : queries;
+        const int p0 = w.len - w.n + (int)(first / R), p1 = w.len - w.n + (int)((end - 1) / R);
+        const int wave_hi = p1 + 1, wave_lo = p0 >= a.window ? p0 - a.window + 1 : 0;          // what any of them sees
+        const int sure_hi = p0 + 1, sure_lo = p1 >= a.window ? p1 - a.window + 1 : 0;          // what all of them see
+        const int tile_sure_hi = band.p0 + 1, tile_sure_lo = band.p1 >= a.window ? band.p1 - a.window + 1 : 0;
+        const Query x = query_of(a, R, w, piece.head, first + col);
+
+        int page[2] = {page_at(piece.from, 0), page_at(piece.from, 1)};
+        int after[2] = {page_at(piece.from + 1, 0), page_at(piece.from + 1, 1)};
+        fetch(c, piece.head, page, band.at(piece.from, kBlock));
+        bf16x8 q[kDeep];
+        {
+            const uint16_t* qp = a.q + x.token * a.q_token_stride + x.head * a.q_head_stride;
+#pragma unroll
+            for (int s = 0; s < kDeep; ++s) {
+                u32x4 u = *reinterpret_cast<const u32x4*>(qp + 16 * s + 8 * h);
+                if (!x.is) u = u32x4{0, 0, 0, 0};
+                q[s] = __builtin_bit_cast(bf16x8, u);
+            }
+        }
+        float m = kNoScore, l = 0.0f;
+        f32x16 o[kCols];
+#pragma unroll
+        for (int b = 0; b < kCols; ++b) o[b] = zero();
+        const float scale = a.scale * kLog2eF;
+        // row of the score tile -> token
+        const int token_of_row = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+
+        meet();                                                                // the last item's blocks are done with
+        for (int s = piece.from; s < piece.to; ++s) {
+            char* image = lds + ((s - piece.from) & 1) * kImage;
+            const int at = band.at(s, kBlock);
+            const bool there[2] = {(uint32_t)page[0] < (uint64_t)c.num_pages, (uint32_t)page[1] < (uint64_t)c.num_pages};
+            const bool whole = there[0] && there[1];
+            const bool check = !(whole && at + kBlock <= tile_sure_hi && (at >= tile_sure_lo || at + kBlock <= a.sinks));
+            put(image, scale, check);
+            const int now[2] = {page[0], page[1]};
+            page[0] = after[0]; page[1] = after[1];
+            if (s + 1 < piece.to) {
+                fetch(c, piece.head, page, band.at(s + 1, kBlock));
+                after[0] = page_at(s + 2, 0); after[1] = page_at(s + 2, 1);
+            }
+            meet();
+            if (!busy || at >= wave_hi || (at + kBlock <= wave_lo && at >= a.sinks)) continue;
+            const bool edge = !(whole && at + kBlock <= sure_hi && (at >= sure_lo || at + kBlock <= a.sinks));
+            const u32x4* keys = reinterpret_cast<const u32x4*>(image);
+            const u32x4* values = reinterpret_cast<const u32x4*>(image + kKeys);
+            const float* factors = reinterpret_cast<const float*>(image + kKeys + kValues);
+            f32x16 t[2] = {zero(), zero()};
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int token = 32 * b + token_of_row;
+                    t[b] = product(__builtin_bit_cast(bf16x8, keys[token * kPieces + turned(token, 2 * i + h)]), q[i], t[b]);
+                }
+            auto sees = [&](int b, int i) {
+                const int token = at + 32 * b + 16 * (i >> 3) + 8 * h + (i & 7);
+                return there[b] && token < x.hi && (token >= x.lo || token < a.sinks);
+            };
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    t[b][i] *= kFp8 ? factors[32 * b + 16 * (i >> 3) + 8 * h + (i & 7)] : scale;
+                    if (edge) t[b][i] = sees(b, i) ? t[b][i] : -INFINITY;
+                }
+            float top = fmaxf(t[0][0], t[1][0]);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 1; i < 15; i += 2) top = fmax3(top, t[b][i], t[b][i + 1]);
+            top = fmax3(top, t[0][15], t[1][15]);
+            if (__any(top > m + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float to = fmaxf(m, top);
+                const float f = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= f;
+#pragma unroll
+                for (int b = 0; b < kCols; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[b][i] *= f;
+            }
+            const int* flags = reinterpret_cast<const int*>(image + kKeys + kValues + kFactors);
+            const bool odd = check && (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {                                  // 16 tokens
+                    bf16x8 p, rest;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float e = __builtin_amdgcn_exp2f(t[b][8 * n + j] - m);
+                        l += e;
+                        float u = e;
+                        if (kFp8) {
+                            u = e * factors[kBlock + 32 * b + 16 * n + 8 * h + j];
+                            if (edge) u = sees(b, 8 * n + j) ? u : 0.0f;       // a hidden token's scale may be anything
+                        }
+                        p[j] = (__bf16)u;
+                        rest[j] = (__bf16)(u - (float)p[j]);
+                    }
+                    const u32x4* of = values + (4 * b + 2 * n + h) * D + col;
+#pragma unroll
+                    for (int d = 0; d < kCols; ++d) {
+                        const bf16x8 value = __builtin_bit_cast(bf16x8, of[32 * d]);
+                        o[d] = product(value, rest, product(value, p, o[d]));
+                    }
+                }
+            if (__builtin_expect(odd, 0)) {
+                // Values that are no finite numbers, hidden from some queries (zeros in LDS): one more product, with what the cache
+                // holds, counts those that a query sees.
+#pragma unroll 1
+                for (int n = 0; n < 4; ++n) {
+                    const bool is = n < 2 ? there[0] : there[1];
+                    const int64_t row = page_row(c, piece.head, n < 2 ? now[0] : now[1], at + 16 * n + 8 * h);
+                    bf16x8 seen;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int token = at + 16 * n + 8 * h + j;
+                        seen[j] = (__bf16)(is && token < x.hi && (token >= x.lo || token < a.sinks) ? 1.0f : 0.0f);
+                    }
+                    const char* from = static_cast<const char*>(c.v) + row * (D * kElem) + col * (8 * kElem);
+#pragma unroll
+                    for (int d = 0; d < kCols; ++d) {
+                        bf16x8 ones;
+                        if (kFp8) {
+                            const u32x2 v = *reinterpret_cast<const u32x2*>(from + d * 256);
+                            ones = widen(StepData<D, true>::unbounded_in(v.x) & 0x38383838u, StepData<D, true>::unbounded_in(v.y) & 0x38383838u);
+                        } else {
+                            u32x4 v = *reinterpret_cast<const u32x4*>(from + d * 512);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) v[j] = StepData<D, false>::unbounded_in(v[j]) & 0x3F803F80u;
+                            ones = __builtin_bit_cast(bf16x8, v);
+                        }
+                        const f32x16 count = product(ones, seen, zero());
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[d][i] = count[i] > 0.0f ? __builtin_nanf("") : o[d][i];
+                    }
+                }
+            }
+        }
+        if (!busy) return;
+        l += __shfl_xor(l, 32);
+        if (!x.is) return;
+        const bool none = l == 0.0f && m == kNoScore;
+        if (!piece.whole) {
+            const int place = wave * 32 + col;
+            if (h == 0) ml_out[place] = float2{m, l};
+            float* to = o_out + (int64_t)place * D + 4 * h;
+#pragma unroll
+            for (int b = 0; b < kCols; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f32x4*>(to + 32 * b + 2 * i) = f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+            return;
+        }
+        const float inv = none ? 0.0f : 1.0f / l;
+        const int64_t where = (int64_t)x.token * a.q_heads + x.head;
+        uint16_t* to = a.out + where * D + 4 * h;
+#pragma unroll
+        for (int b = 0; b < kCols; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<u32x2*>(to + 32 * b + 2 * i) = u32x2{pack2(o[b][i] * inv, o[b][i + 1] * inv), pack2(o[b][i + 2] * inv, o[b][i + 3] * inv)};
+        if (a.lse && h == 0) a.lse[where] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (float)kLn2;
+    }
+};
+
+// The stretch of worker `part`: f(record, piece, which of the worker's two places).
+template <int kLine, typename F>
+__device__ __forceinline__ void along(const Work* list, int count, const Division& d, int heads, int part, Cut* cut, F f)
+{
+    if (part >= d.parts[kLine]) return;
+    int64_t at = begin_of(part, d.steps[kLine], d.parts[kLine]);
+    const int64_t end = begin_of(part + 1, d.steps[kLine], d.parts[kLine]);
+    int i = find_work(list, count, at);
+    Cut found{-1, 0, 0, 0};
+    const int64_t begin = at;
+    while (at < end && i < count) {
+        const Work w = uniform(list[i]);
+        const int64_t offset = at - w.first;
+        const int head = (int)divide(offset, w.cost), from = (int)(offset - (int64_t)head * w.cost);
+        const int n = end - at < w.cost - from ? (int)(end - at) : w.cost - from;
+        Piece1 piece;
+        piece.head = head;
+        piece.from = from > kCost ? from - kCost : 0;
+        piece.to = from + n - kCost;
+        piece.whole = w.cost == kCost ? from == 0 : from <= kCost && from + n == w.cost;
+        if (piece.to < 0) piece.to = 0;
+        if (at == begin && from > kCost) {
+            // the item began before: was its first step the worker's before?
+            const int64_t item = at - from;
+            if (begin_of(part - 1, d.steps[kLine], d.parts[kLine]) <= item + kCost)
+                found = Cut{i, head, part_of(item + w.cost - 1, d.steps[kLine], d.parts[kLine]), 0};
+        }
+        if (piece.to > piece.from || (w.cost == kCost && piece.whole)) f(w, piece, from <= kCost ? 1 : 0);
+        at += n;
+        if (head + 1 == heads && from + n == w.cost) ++i;
+    }
+    if ((threadIdx.x & (kLine == kOfGroups ? 255 : 63)) == 0) *cut = found;
+}
+
+template <int D, bool kFp8>
+__global__ __launch_bounds__(64 * kWaves, kPerUnit)
+void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
+{
+    __shared__ __align__(16) char lds[Many<D, kFp8>::kLds];
+    const Totals totals = *reinterpret_cast<const Totals*>(ws);
+    const int workgroups = (int)gridDim.x;
+    const Division d = divide_work(totals, workgroups);
+    Cut* cuts = reinterpret_cast<Cut*>(ws + s.at_cuts);
+    float2* ml = reinterpret_cast<float2*>(ws + s.at_ml);
+    // Workgroups of one die (dealt in turn to eight) lie next to each other on the line: they read the same keys.
+    const int block = (workgroups & 7) == 0 ? (int)(blockIdx.x & 7) * (workgroups >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
+    if (block < d.groups) {
+        float* o = reinterpret_cast<float*>(ws + s.at_o[kOfGroups]);
+        along<kOfGroups>(reinterpret_cast<const Work*>(ws + s.at_list[kOfGroups]), uniform(totals.count[kOfGroups]), d, c.heads, block, cuts + block,
+                         [&](const Work& w, const Piece1& piece, int which) {
+                             const int64_t place = (2 * block + which) * (int64_t)kTile;
+                             Many<D, kFp8> x;
+                             x.run(c, a, s.R, w, piece, lds, ml + place, o + place * D);
+                         });
+        return;
+    }
+    // a workgroup's waves lie far apart on their line: few stretches are spread over all workgroups
+    const int wave = uniform((int)threadIdx.x >> 6);
+    const int part = wave * (workgroups - d.groups) + block - d.groups;
+    float* o = reinterpret_cast<float*>(ws + s.at_o[kOfWaves]);
+    along<kOfWaves>(reinterpret_cast<const Work*>(ws + s.at_list[kOfWaves]), uniform(totals.count[kOfWaves]), d, c.heads, part, cuts + s.workers[0] + part,
+                    [&](const Work& w, const Piece1& piece, int which) {
+                        const int64_t place = (2 * part + which) * (int64_t)kFewQueries;
+                        float2* ml_out = ml + 2 * (int64_t)s.workers[0] * kTile + place;
+                        if (w.n * s.R <= 16) {
+                            Few<D, kFp8, 1> x;
+                            x.run(c, a, s.R, w, piece, ml_out, o + place * D);
+                        } else {
+                            Few<D, kFp8, 2> x;
+                            x.run(c, a, s.R, w, piece, ml_out, o + place * D);
+                        }
+                    });
+}
+
+// ---------------------------------------------------------------- join
+// A workgroup per worker whose stretch begins inside an item (the first such one of the item) and a few of its queries; D / 4 lanes a query,
+// fewer queries than lots of lanes have their parts spread over several.
+template <int D>
+__global__ __launch_bounds__(256, 8)
+void window_join_kernel(WindowArgs a, WindowShape s, int heads, int workgroups, int group_slices, int wave_slices, const char* ws)
+{
+    constexpr int kLanes4 = D / 4, kSubs = 256 / kLanes4;
+    __shared__ float lds[kSubs][2 + D];
+    const Totals totals = *reinterpret_cast<const Totals*>(ws);
+    const Division d = divide_work(totals, workgroups);
+    const int of_groups = s.workers[kOfGroups] * group_slices;
+    const bool groups = (int)blockIdx.x < of_groups;
+    const int slices = groups ? group_slices : wave_slices;
+    const int block = groups ? (int)blockIdx.x : (int)blockIdx.x - of_groups;
+    const int part = block / slices, slice = block % slices;
+    if (part >= (groups ? d.parts[kOfGroups] : d.parts[kOfWaves])) return;
+    const Cut cut = reinterpret_cast<const Cut*>(ws + s.at_cuts)[(groups ? 0 : s.workers[kOfGroups]) + part];
+    if (cut.work < 0) return;
+    const Work w = reinterpret_cast<const Work*>(ws + s.at_list[groups ? kOfGroups : kOfWaves])[cut.work];
+    const int places = groups ? kTile : kFewQueries, each = places / slices;
+    const int64_t base = groups ? (int64_t)w.tile * kTile : 0, queries = (int64_t)w.n * s.R - base;
+    const int first = slice * each, end = queries < first + each ? (int)queries : first + each;
+    if (first >= end) return;
+    const float2* ml = reinterpret_cast<const float2*>(ws + s.at_ml) + (groups ? 0 : 2 * (int64_t)s.workers[kOfGroups] * kTile);
+    const float* o = reinterpret_cast<const float*>(ws + s.at_o[groups ? kOfGroups : kOfWaves]);
+    const int sub = threadIdx.x / kLanes4, col = (threadIdx.x % kLanes4) * 4;
+    const int parts = cut.last - part + 2;
+    const int wide = end - first < kSubs ? end - first : kSubs, spread = kSubs / wide;         // uniform
+    for (int q0 = first; q0 < end; q0 += wide) {
+        const int query = q0 + sub / spread;
+        const bool is = sub / spread < wide && query < end;
+        float m = kNoScore, l = 0.0f;
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (is) {
+            for (int i = sub % spread; i < parts; i += 4 * spread) {
+                float2 pw[4];
+                f32x4 po[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int j = i + k * spread < parts ? i + k * spread : i;
+                    // the first part lies at the end of the worker's before
+                    const int64_t at = (j == 0 ? 2 * (int64_t)(part - 1) + 1 : 2 * (int64_t)(part + j - 1)) * places + query;
+                    pw[k] = ml[at];
+                    po[k] = *reinterpret_cast<const f32x4*>(o + at * D + col);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i + k * spread < parts) {
+                        const float to = fmaxf(m, pw[k].x);
+                        const float f = __builtin_amdgcn_exp2f(m - to), g = __builtin_amdgcn_exp2f(pw[k].x - to);
+                        m = to;
+                        l = l * f + pw[k].y * g;
+                        x = x * f + po[k] * g;
+                    }
+            }
+        }
+        if (spread > 1) {
+            __syncthreads();
+            if (col == 0) { lds[sub][0] = m; lds[sub][1] = l; }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lds[sub][2 + col + j] = x[j];
+            __syncthreads();
+            if (is && sub % spread == 0) {
+                for (int k = sub + 1; k < sub + spread; ++k) {
+                    const float to = fmaxf(m, lds[k][0]);
+                    const float f = __builtin_amdgcn_exp2f(m - to), g = __builtin_amdgcn_exp2f(lds[k][0] - to);
+                    m = to;
+                    l = l * f + lds[k][1] * g;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = x[j] * f + lds[k][2 + col + j] * g;
+                }
+            }
+        }
+        if (is && sub % spread == 0) {
+            const Query t = query_of(a, s.R, w, cut.head, base + query);
+            const int64_t where = (int64_t)t.token * a.q_heads + t.head;
+            const bool none = l == 0.0f && m == kNoScore;
+            const float inv = none ? 0.0f : 1.0f / l;
+            *reinterpret_cast<u32x2*>(a.out + where * D + col) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
+            if (a.lse && col == 0) a.lse[where] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (float)kLn2;
+        }
+    }
+}
+
+template <int D, bool kFp8>
+static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const WindowShape& s, char* ws, hipStream_t stream)
+{
+    window_plan_kernel<<<1, kPlanLanes, 0, stream>>>(a, s, c.heads, c.page_size, ws);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    const int workgroups = compute_units() * kPerUnit;
+    window_kernel<D, kFp8><<<workgroups, 64 * kWaves, 0, stream>>>(c, a, s, ws);
+    err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    const int group_slices = 16, wave_slices = 4;
+    const int blocks = s.workers[kOfGroups] * group_slices + s.workers[kOfWaves] * wave_slices;
+    window_join_kernel<D><<<blocks, 256, 0, stream>>>(a, s, c.heads, workgroups, group_slices, wave_slices, ws);
+    return hipGetLastError();
+}
+
+hipError_t launch_window_attention(const CacheView& c, const WindowArgs& a, void* workspace, hipStream_t stream)
+{
+    WindowShape s;
+    if (!window_shape(a.rows, a.tokens, a.q_heads, c.heads, c.dim, s)) return hipErrorInvalidValue;
+    char* ws = static_cast<char*>(workspace);
+    if (c.dim == 128) return c.fp8 ? launch_window<128, true>(c, a, s, ws, stream) : launch_window<128, false>(c, a, s, ws, stream);
+    return c.fp8 ? launch_window<64, true>(c, a, s, ws, stream) : launch_window<64, false>(c, a, s, ws, stream);
+}
+
+}  // namespace e3
