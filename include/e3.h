@@ -617,6 +617,60 @@ int e3_verify_drafts(const void* logits, int dtype, int64_t rows, int32_t drafts
                      int32_t* accepted_out, int32_t* token_out, float* logp_out, float* entropy_out,
                      void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Beam search: the best continuations of every sequence over its beams and the vocabulary.
+ *   score(b, v) = scores[b] + z_bv / tau - ln sum_i exp(z_bi / tau)
+ * The `keep` candidates with the largest scores, largest first; equal scores go to the lower beam, then to the lower token.  A finished beam
+ * offers one candidate, eos_token with its score as it is.
+ *
+ * logits        [seqs][beams][V] of dtype (E3_F32 / E3_BF16), strides in elements; base and strides multiples of 16 bytes (E3_ERR_ALIGN),
+ *               beam_stride >= V.  Rows of finished beams and of beams without a finite score are not read.
+ * beams         1 .. E3_MAX_BEAMS;  keep  1 .. E3_MAX_KEEP (twice the beams where finished ones are sorted out behind the call);
+ * V             at most 1,040,384; seqs below 2^22, and logits of at most 2^36 elements or so (E3_ERR_SHAPE: no workspace size).
+ * scores        [seqs][beams] fp32: sums of log-probs so far; -inf (or NaN): the beam offers nothing (all but one in a first step).
+ * tau           host, finite and > 0 (E3_ERR_VALUE).
+ * finished      [seqs][beams] uint8 or NULL, with eos_token in [0, V) (E3_ERR_VALUE).
+ * parent_out, token_out [seqs][keep] int32, score_out [seqs][keep] fp32.  Places without a candidate: -1, -1, -inf.
+ * A logit of -inf, or of -1e30 and less, has no probability and is never chosen.  A beam whose logits hold NaN or +inf (or z / tau beyond
+ * fp32) offers nothing.
+ * Scores are compared in fp64.  Where the order between two beams lies within 2e-6 the sums over their vocabularies are taken in
+ * fp64 as well; beyond, fp32 sums decide, whose error is below that but for rows built to add up roundings.
+ * workspace     device, 256-byte aligned (E3_ERR_ALIGN), at least e3_beam_workspace_bytes() (else E3_ERR_WORKSPACE); contents on entry ignored, no
+ *               state between calls, to be used by one call at a time.
+ */
+#define E3_MAX_BEAMS 32
+#define E3_MAX_KEEP 64
+size_t e3_beam_workspace_bytes(int64_t seqs, int32_t beams, int64_t V);
+int e3_beam_select(const void* logits, int dtype, int64_t seqs, int32_t beams, int64_t V, int64_t seq_stride, int64_t beam_stride,
+                   const float* scores, int32_t keep, float tau, const uint8_t* finished, int32_t eos_token,
+                   int32_t* parent_out, int32_t* token_out, float* score_out,
+                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The beams' pages after a selection: row r of a sequence goes on where its parent was.  Rows of one sequence share the pages that are
+ * full and own the one that their next token goes to (entry row_lens[r] / page_size).  A parent's first child goes on in
+ * that page; every other child takes over the page of a beam without children (there are as many), into which the parent's tokens are to be
+ * copied: by e3_cache_copy, once for every layer's cache.
+ *
+ * parent        [seqs][beams] int32, within the sequence; an entry outside [0, beams) stands for the row itself.
+ * row_pages     [seqs * beams][row_width] int32, row_lens [seqs * beams] int32 (tokens): before.
+ * page_size     as the cache's (E3_ERR_SHAPE).
+ * pages_out, lens_out   after: tables and lengths of the same shape, memory of their own (E3_ERR_VALUE where it is the input's).
+ * src_out, dst_out, counts_out [seqs * beams] int32: for e3_cache_copy; -1, -1, 0 where there is nothing to copy.
+ * A row whose table does not reach its next token has no such page: it has none to give and nothing is copied from it.
+ */
+int e3_beam_reorder(const int32_t* parent, int64_t seqs, int32_t beams, const int32_t* row_pages, int64_t row_width,
+                    const int32_t* row_lens, int32_t page_size, int32_t* pages_out, int32_t* lens_out,
+                    int32_t* src_out, int32_t* dst_out, int32_t* counts_out, void* hip_stream);
+
+/*
+ * Copy the first counts[i] tokens of page src_pages[i] to page dst_pages[i] (keys, values and scales, all heads), rounded up to a multiple
+ * of eight and cut to the page.  Where either page is not in the cache or both are the same nothing is done.  No page may be a
+ * destination twice, nor a source and a destination (the caller's contract).  [n] int32 each; n * kv_heads below 2^24 (E3_ERR_SHAPE).
+ */
+int e3_cache_copy(const e3_cache* cache, const int32_t* src_pages, const int32_t* dst_pages, const int32_t* counts, int64_t n,
+                  void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

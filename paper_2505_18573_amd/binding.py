@@ -28,6 +28,8 @@ E3_TILE_CHUNK, E3_TILE_LANES, E3_TILE_DEPTH = 8, 64, 8
 E3_NOALLOC_MAX_ROWS = 1024
 E3_MAX_DRAFTS = 63
 E3_MAX_AXES = 8
+E3_MAX_BEAMS = 32
+E3_MAX_KEEP = 64
 
 EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_entropy_noalloc",
            "e3_sample_restricted", "e3_sample_restricted_ws", "e3_restricted_workspace_bytes",
@@ -36,6 +38,7 @@ EXPORTS = ("e3_strerror", "e3_workspace_bytes", "e3_sample_entropy", "e3_sample_
            "e3_allocate_budgets", "e3_budget_bounds", "e3_logprob_entropy_gap",
            "e3_temperature_update_gap", "e3_grpo_objective", "e3_cache_append", "e3_cache_read",
            "e3_rotate", "e3_cache_append_rotated", "e3_window_attention", "e3_window_attention_workspace_bytes",
+           "e3_beam_workspace_bytes", "e3_beam_select", "e3_beam_reorder", "e3_cache_copy",
            "e3_prefix_attention", "e3_prefix_attention_workspace_bytes", "e3_verify_drafts",
            "e3_verify_workspace_bytes", "e3_read_probe",
            "e3_time_next_launch", "e3_launch_plan", "e3_launch_plan_of")
@@ -44,7 +47,8 @@ _NATIVE_CALLS = ("e3_grpo_advantages", "e3_grpo_objective", "e3_workspace_bytes"
                  "e3_restricted_workspace_bytes", "e3_sample_restricted_ws", "e3_logprob_entropy_advantages",
                  "e3_logprob_entropy_gap", "e3_temperature_update", "e3_cache_append", "e3_cache_read",
                  "e3_prefix_attention_workspace_bytes", "e3_prefix_attention", "e3_verify_workspace_bytes", "e3_verify_drafts",
-                 "e3_rotate", "e3_cache_append_rotated", "e3_window_attention", "e3_window_attention_workspace_bytes")
+                 "e3_rotate", "e3_cache_append_rotated", "e3_window_attention", "e3_window_attention_workspace_bytes",
+                 "e3_beam_workspace_bytes", "e3_beam_select", "e3_beam_reorder", "e3_cache_copy")
 
 _lib: Optional[C.CDLL] = None
 _native = None                     # the native calls, once they are bound to the loaded library
@@ -142,6 +146,14 @@ def lib() -> C.CDLL:
         L.e3_window_attention_workspace_bytes.restype = C.c_size_t
         L.e3_window_attention.argtypes = [vp, vp, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, i64, f32, vp, vp, vp, C.c_size_t, vp]
         L.e3_window_attention.restype = C.c_int
+        L.e3_beam_workspace_bytes.argtypes = [i64, i32, i64]
+        L.e3_beam_workspace_bytes.restype = C.c_size_t
+        L.e3_beam_select.argtypes = [vp, C.c_int, i64, i32, i64, i64, i64, vp, i32, f32, vp, i32, vp, vp, vp, vp, C.c_size_t, vp]
+        L.e3_beam_select.restype = C.c_int
+        L.e3_beam_reorder.argtypes = [vp, i64, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.e3_beam_reorder.restype = C.c_int
+        L.e3_cache_copy.argtypes = [vp, vp, vp, vp, i64, vp]
+        L.e3_cache_copy.restype = C.c_int
         _bind_native(L)                           # may raise: nothing is loaded then
         _lib = L
     return _lib
@@ -178,7 +190,8 @@ _ENTRY = {"advantages": "e3_grpo_advantages", "objective": "e3_grpo_objective", 
           "logprob_advantages": "e3_logprob_entropy_advantages", "logprob_gap": "e3_logprob_entropy_gap",
           "temperature": "e3_temperature_update", "cache_append": "e3_cache_append", "cache_read": "e3_cache_read",
           "attention": "e3_prefix_attention", "verify": "e3_verify_drafts", "rotate": "e3_rotate",
-          "append_rotated": "e3_cache_append_rotated", "window": "e3_window_attention"}
+          "append_rotated": "e3_cache_append_rotated", "window": "e3_window_attention",
+          "beam_select": "e3_beam_select", "beam_reorder": "e3_beam_reorder", "cache_copy": "e3_cache_copy"}
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -1040,3 +1053,93 @@ def e3_verify_drafts(logits: torch.Tensor, draft_tokens: Optional[torch.Tensor],
     if rc != E3_OK:
         raise E3Error(rc, "e3_verify_drafts")
     return (accepted_out, *outs)
+
+
+def e3_beam_workspace_bytes(seqs: int, beams: int, V: int) -> int:
+    """Host-only; 0 for a shape that is not served."""
+    return int(lib().e3_beam_workspace_bytes(seqs, beams, V))
+
+
+def e3_beam_select(logits: torch.Tensor, scores: torch.Tensor, keep: int, tau: float = 1.0, finished: Optional[torch.Tensor] = None,
+                   eos_token: int = -1, parent_out: Optional[torch.Tensor] = None, token_out: Optional[torch.Tensor] = None,
+                   score_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """The `keep` best continuations of every sequence: logits [seqs, beams, V], scores fp32 [seqs, beams] (sums of log-probs; -inf: none),
+    finished uint8 [seqs, beams] or None (with eos_token).  Returns (parent int32, token int32, score fp32), [seqs, keep] each.
+    workspace: a tensor of e3_beam_workspace_bytes(), or None to allocate one."""
+    res = _ordinary("beam_select", logits, scores, keep, tau, finished, eos_token, parent_out, token_out, score_out, workspace)
+    if res is not None:
+        return res
+    if logits.dim() != 3 or not logits.is_cuda:
+        raise ValueError("logits must be [seqs, beams, V] on the GPU")
+    dt, dev = _float_type(logits.dtype), logits.device
+    seqs, beams, V = logits.shape
+    seq_stride, beam_stride = _positions(logits, "logits", logits.dtype, (seqs, beams, V), dev)
+    for t, dtype, name in ((scores, torch.float32, "scores"), (finished, torch.uint8, "finished")):
+        if t is not None and (t.dtype is not dtype or tuple(t.shape) != (seqs, beams) or t.device != dev or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor [{seqs}, {beams}] on {dev}")
+    outs = []
+    for t, dtype, name in ((parent_out, torch.int32, "parent_out"), (token_out, torch.int32, "token_out"), (score_out, torch.float32, "score_out")):
+        if t is None:
+            t = torch.empty((seqs, max(0, int(keep))), dtype=dtype, device=dev)
+        elif t.dtype is not dtype or tuple(t.shape) != (seqs, keep) or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor [{seqs}, {keep}] on {dev}")
+        outs.append(t)
+    if workspace is None:
+        workspace = torch.empty(e3_beam_workspace_bytes(seqs, beams, V), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    rc = lib().e3_beam_select(_ptr(logits), dt, seqs, beams, V, seq_stride, beam_stride, _ptr(scores), int(keep), float(tau), _ptr(finished),
+                              int(eos_token), *(_ptr(t) for t in outs), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_beam_select")
+    return tuple(outs)
+
+
+def e3_beam_reorder(parent: torch.Tensor, row_pages: torch.Tensor, row_lens: torch.Tensor, page_size: int,
+                    pages_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None, src_out: Optional[torch.Tensor] = None,
+                    dst_out: Optional[torch.Tensor] = None, counts_out: Optional[torch.Tensor] = None):
+    """The beams' page tables after a selection: parent int32 [seqs, beams], row_pages int32 [seqs * beams, width], row_lens int32
+    [seqs * beams].  Returns (row_pages, row_lens, src, dst, counts), the last three (int32 [seqs * beams]) for e3_cache_copy."""
+    res = _ordinary("beam_reorder", parent, row_pages, row_lens, page_size, pages_out, lens_out, src_out, dst_out, counts_out)
+    if res is not None:
+        return res
+    dev = parent.device
+    if parent.dtype is not torch.int32 or parent.dim() != 2 or not parent.is_contiguous() or not parent.is_cuda:
+        raise ValueError("parent must be a contiguous int32 tensor [seqs, beams] on the GPU")
+    seqs, beams = parent.shape
+    rows = seqs * beams
+    width = _table(row_pages, rows, "row_pages", dev)
+    _check(row_lens, torch.int32, rows, "row_lens", dev)
+    if pages_out is None:
+        pages_out = torch.empty((rows, width), dtype=torch.int32, device=dev)
+    elif _table(pages_out, rows, "pages_out", dev) != width:
+        raise ValueError(f"pages_out must be [{rows}, {width}]")
+    outs = []
+    for t, name in ((lens_out, "lens_out"), (src_out, "src_out"), (dst_out, "dst_out"), (counts_out, "counts_out")):
+        if t is None:
+            t = torch.empty(rows, dtype=torch.int32, device=dev)
+        else:
+            _check(t, torch.int32, rows, name, dev)
+        outs.append(t)
+    rc = lib().e3_beam_reorder(_ptr(parent), seqs, beams, _ptr(row_pages), width, _ptr(row_lens), int(page_size), _ptr(pages_out),
+                               *(_ptr(t) for t in outs), _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_beam_reorder")
+    return (pages_out, *outs)
+
+
+def e3_cache_copy(cache: E3Cache, src_pages: torch.Tensor, dst_pages: torch.Tensor, counts: torch.Tensor) -> None:
+    """Copy the first counts[i] tokens (rounded up to a multiple of eight) of page src_pages[i] to page dst_pages[i], int32 [n] each; pages that
+    are not in the cache: nothing."""
+    if _ordinary("cache_copy", cache, src_pages, dst_pages, counts) is not None:
+        return
+    c = _cache(cache)
+    dev = cache[0].device
+    n = src_pages.shape[0]
+    for t, name in ((src_pages, "src_pages"), (dst_pages, "dst_pages"), (counts, "counts")):
+        if t is None:
+            raise ValueError(f"{name} must be given")
+        _check(t, torch.int32, n, name, dev)
+    rc = lib().e3_cache_copy(C.byref(c), _ptr(src_pages), _ptr(dst_pages), _ptr(counts), n, _stream(dev))
+    if rc != E3_OK:
+        raise E3Error(rc, "e3_cache_copy")

@@ -1,0 +1,500 @@
+// Beam search: the best continuations over beams and vocabulary, and the beams' pages after them.
+//
+//   score(b, v) = s_b + z_bv / tau - ln sum_i exp(z_bi / tau),   the `keep` largest of a sequence, ties to the lowest (b, v).
+//
+// Two launches.
+//   stream   Every wave takes a segment of a row, eight 16-byte loads a lane, and leaves sum exp2 (fp32 in a lane, fp64 over the
+//            lanes) and the largest logit of every chunk of 512 columns.  The logits are read once; that is what bounds the call.
+//   select   A workgroup per sequence.  No element outside the `keep` best chunks can be among the `keep` best: each of those
+//            chunks holds one that comes before it (chunks are runs of columns, so this is also right for equal values, where the
+//            lower index comes first).  So the chunks' maxima are ranked first and only `keep` chunks are read again, 1 KB each.
+// Scores are compared in fp64.  Sums taken in fp32 leave ln sum exp off by 1e-7 as a rule (1e-6 at worst), the same for all tokens
+// of a beam, so only the order between beams is in question: where two neighbours of different beams among the results (or the best one left
+// out) are within 2e-6 of each other, the beams' sums are taken again in fp64, by the sequence's workgroup, and the
+// selection is made once more.  (One sequence in some hundreds; it takes 10 us and more for a beam.)
+#include "beam.h"
+#include "vocab_common.h"
+#include "vocab_pass.h"
+
+namespace e3 {
+
+constexpr int kChunkCols = 512;
+constexpr int kVecs = 8;                        // 16-byte vectors of a lane in a segment
+constexpr int kStreamWaves = 4;
+constexpr int kSelectWaves = 16, kSelectThreads = 64 * kSelectWaves;
+constexpr float kNoLogit = -1e30f;              // at or below: no probability
+constexpr double kNear = 2e-6;
+constexpr double kNone = -INFINITY;
+
+template <bool kBf16> struct Segment { static constexpr int kCols = kVecs * 64 * (kBf16 ? 8 : 4), kChunks = kCols / kChunkCols; };
+
+struct Partial { float ref; float unused; double sum; };          // sum of 2^((z - ref) c)
+
+struct BeamShape {
+    int64_t chunks, segments;                   // of a row (segments: of the narrower type)
+    int64_t at_partials, bytes;
+};
+static BeamShape beam_shape(int64_t rows, int64_t V, bool bf16)
+{
+    BeamShape s;
+    const int64_t cols = bf16 ? Segment<true>::kCols : Segment<false>::kCols;
+    s.chunks = (V + kChunkCols - 1) / kChunkCols;
+    s.segments = (V + cols - 1) / cols;
+    s.at_partials = (rows * s.chunks * 4 + 255) / 256 * 256;
+    s.bytes = s.at_partials + rows * s.segments * (int64_t)sizeof(Partial);
+    return s;
+}
+
+size_t beam_workspace_bytes(int64_t seqs, int32_t beams, int64_t V)
+{
+    const BeamShape s = beam_shape(seqs * beams, V, false);
+    // a wave per segment, a workgroup of 1024 threads per sequence: threads of the launches below 2^32
+    return seqs < 1 << 22 && seqs * beams * s.segments < (int64_t)1 << 25 ? (size_t)s.bytes : 0;
+}
+
+__device__ __forceinline__ const char* row_of(const BeamArgs& a, int64_t row, int size)
+{
+    return static_cast<const char*>(a.logits) + (row / a.beams * a.seq_stride + row % a.beams * a.beam_stride) * size;
+}
+__device__ __forceinline__ bool takes_part(float score) { return fabsf(score) < INFINITY; }
+
+// ---------------------------------------------------------------- stream
+template <bool kBf16>
+__global__ __launch_bounds__(64 * kStreamWaves)
+void beam_stream_kernel(BeamArgs a, BeamShape s, float c, char* ws)
+{
+    constexpr int kPer = kBf16 ? 8 : 4, kCols = Segment<kBf16>::kCols, kChunks = Segment<kBf16>::kChunks, kOf = kVecs / kChunks;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * kStreamWaves + (threadIdx.x >> 6);
+    if (item >= a.seqs * a.beams * s.segments) return;
+    const int64_t row = item / s.segments, segment = item % s.segments;
+    if (!takes_part(a.scores[row]) || (a.finished && a.finished[row])) return;
+    const char* p = row_of(a, row, kBf16 ? 2 : 4);
+    const int64_t first = segment * kCols + lane * kPer;
+    const bool tail = (segment + 1) * kCols > a.V;                            // uniform
+    u32x4 w[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const int64_t col = first + (int64_t)i * 64 * kPer;
+        if (!tail || col + kPer <= a.V) {
+            w[i] = stream_load(reinterpret_cast<const u32x4*>(p + col * (kBf16 ? 2 : 4)));
+        } else {                                                               // nothing behind the row is read
+            w[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (col + j < a.V) {
+                    if (kBf16) w[i][j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[col + j] << (16 * (j & 1));
+                    else w[i][j & 3] = reinterpret_cast<const uint32_t*>(p)[col + j];
+                }
+        }
+    }
+    float z[kVecs][kPer], top[kChunks];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            z[i][j] = kBf16 ? __uint_as_float((j & 1) ? w[i][j >> 1] & 0xFFFF0000u : w[i][j >> 1] << 16) : __uint_as_float(w[i][j & 3]);
+            if (tail && first + (int64_t)i * 64 * kPer + j >= a.V) z[i][j] = -INFINITY;
+        }
+        float m = fmaxf(z[i][0], z[i][1]);
+#pragma unroll
+        for (int j = 2; j < kPer; j += 2) m = fmax3(m, z[i][j], z[i][j + 1]);
+        top[i / kOf] = i % kOf == 0 ? m : fmaxf(top[i / kOf], m);
+    }
+    float most = top[0];
+#pragma unroll
+    for (int i = 1; i < kChunks; ++i) most = fmaxf(most, top[i]);
+    // Differences first: z c and the reference's would both be rounded, and far apart for masks such as -1e30.
+    const float ref = fmaxf(most, kNoLogit);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        float part[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) part[j] = __builtin_amdgcn_exp2f((z[i][j] - ref) * c);
+#pragma unroll
+        for (int d = 1; d < kPer; d <<= 1)
+#pragma unroll
+            for (int j = 0; j < kPer; j += 2 * d) part[j] += part[j + d];
+        sum += part[0];
+    }
+    const float up = wave_max(ref);
+    const double all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f((ref - up) * c));
+    float* tops = reinterpret_cast<float*>(ws) + row * s.chunks + segment * kChunks;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const float m = wave_max(top[i]);
+        if (lane == i && segment * kChunks + i < s.chunks) tops[i] = m;
+    }
+    if (lane == 0) reinterpret_cast<Partial*>(ws + s.at_partials)[row * s.segments + segment] = Partial{up, 0.0f, all};
+}
+
+// ---------------------------------------------------------------- select
+// A candidate or a chunk's best one: larger keys come first, of equal ones the lower index.
+struct Entry { double key; int index; };
+
+// The lane that holds the wave's first entry, -1 if there is none (all keys -inf).  Rounding to fp32 keeps the order, so only lanes
+// that are equal there are looked at one by one.
+__device__ __forceinline__ int first_of(const Entry& e)
+{
+    const float f = (float)e.key;
+    const float top = wave_max(f);
+    if (!(top > -INFINITY)) return -1;
+    unsigned long long tied = __ballot(f == top);
+    int best = (int)__builtin_ctzll(tied);
+    tied &= tied - 1;
+    if (tied != 0) {
+        double key = read_lane(e.key, best);
+        int index = __builtin_amdgcn_readlane(e.index, best);
+        for (; tied != 0; tied &= tied - 1) {
+            const int l = (int)__builtin_ctzll(tied);
+            const double k = read_lane(e.key, l);
+            const int i = __builtin_amdgcn_readlane(e.index, l);
+            if (k > key || (k == key && i < index)) { best = l; key = k; index = i; }
+        }
+    }
+    return best;
+}
+
+// 2^x for -1000 < x < 1000 in fp64: the fraction's exponential series, whose next term is below 1e-14.
+__device__ __forceinline__ double exp2_of(double x)
+{
+    const double n = rint(x), t = (x - n) * kLn2;
+    double p = 1.0 / 39916800.0;
+    p = fma(p, t, 1.0 / 3628800.0);
+    p = fma(p, t, 1.0 / 362880.0);
+    p = fma(p, t, 1.0 / 40320.0);
+    p = fma(p, t, 1.0 / 5040.0);
+    p = fma(p, t, 1.0 / 720.0);
+    p = fma(p, t, 1.0 / 120.0);
+    p = fma(p, t, 1.0 / 24.0);
+    p = fma(p, t, 1.0 / 6.0);
+    p = fma(p, t, 0.5);
+    p = fma(p, t, 1.0);
+    p = fma(p, t, 1.0);
+    return __builtin_amdgcn_ldexp(p, (int)n);
+}
+
+template <bool kBf16>
+__device__ __forceinline__ float logit_at(const char* row, int64_t col)
+{
+    return kBf16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[col] << 16) : reinterpret_cast<const float*>(row)[col];
+}
+
+struct SelectLds {
+    double base[kMaxBeams];                     // s_b - ln sum exp, -inf: the beam offers nothing
+    double log2_sum[kMaxBeams];
+    double sums[kSelectWaves];
+    int ends[kMaxBeams];                        // a finished beam
+    Entry of_wave[kSelectWaves + 1][kMaxKeep + 2];
+    Entry chunk[kMaxKeep + 2];
+    double key[kMaxKeep * (kMaxKeep + 1) / 2];  // of chunk r at most keep - r elements
+    int column[kMaxKeep * (kMaxKeep + 1) / 2];
+    int count[kMaxKeep];
+    int chunks_found;
+    uint32_t near;                              // beams whose sums decide
+};
+
+template <bool kBf16>
+__global__ __launch_bounds__(kSelectThreads)
+void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
+{
+    __shared__ SelectLds lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t seq = blockIdx.x, row0 = seq * a.beams;
+    const float* tops = reinterpret_cast<const float*>(ws) + row0 * s.chunks;
+    const double per_logit = 1.0 / (double)a.tau, c = kLog2e * per_logit;
+    const int keep = a.keep, most = (int)s.chunks;
+
+    for (int b = wave; b < a.beams; b += kSelectWaves) {
+        const float score = a.scores[row0 + b];
+        const bool ends = a.finished && a.finished[row0 + b];
+        double base = kNone, total = 0.0;
+        if (takes_part(score)) {
+            if (ends) {
+                base = score;
+            } else {
+                const Partial* parts = reinterpret_cast<const Partial*>(ws + s.at_partials) + (row0 + b) * s.segments;
+                float up = -INFINITY;
+                for (int64_t i = lane; i < s.segments; i += 64) up = fmaxf(up, parts[i].ref);
+                up = wave_max(up);
+                double sum = 0.0;
+                for (int64_t i = lane; i < s.segments; i += 64) sum += parts[i].sum * exp2_of(fmax(((double)parts[i].ref - (double)up) * c, -1000.0));
+                sum = wave_sum(sum);
+                total = (double)up * c + log2(sum);
+                // NaN and +inf make the sum no number; a row without any probability has none
+                if (sum > 0.0 && sum < INFINITY && fabsf(up) < INFINITY) base = score - total * kLn2;
+            }
+        }
+        if (lane == 0) { lds.base[b] = base; lds.log2_sum[b] = total; lds.ends[b] = ends; }
+    }
+    if (threadIdx.x == 0) lds.near = 0;
+    __syncthreads();
+
+    for (int round = 0; round < 2; ++round) {
+        // the best keep + 1 chunks
+        constexpr int kEach = 8;
+        const int entries = a.beams * most;
+        int known = 0;                                                         // in lds.chunk
+        for (int from = 0; from < entries; from += kEach * kSelectThreads) {
+            double key[kEach];
+            Entry mine{kNone, 0};
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int e = from + i * kSelectThreads + (int)threadIdx.x;
+                key[i] = kNone;
+                if (e < entries) {
+                    const int b = e / most;
+                    const double base = lds.base[b];
+                    if (base > kNone) {
+                        if (lds.ends[b]) {
+                            if (e - b * most == a.eos / kChunkCols) key[i] = base;
+                        } else {
+                            const float z = tops[e];
+                            if (z > kNoLogit) key[i] = base + (double)z * per_logit;
+                        }
+                    }
+                }
+                if (key[i] > mine.key) mine = Entry{key[i], e};
+            }
+            int n = 0;
+            for (; n <= keep; ++n) {
+                const int l = first_of(mine);
+                if (l < 0) break;
+                if (lane == l) {
+                    lds.of_wave[wave][n] = mine;
+                    const int taken = mine.index;
+                    mine = Entry{kNone, 0};
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) {
+                        const int e = from + i * kSelectThreads + (int)threadIdx.x;
+                        if (e == taken) key[i] = kNone;
+                        if (key[i] > mine.key) mine = Entry{key[i], e};
+                    }
+                }
+            }
+            if (lane == 0) lds.of_wave[wave][n] = Entry{kNone, 0};
+            if (wave == 0)
+                for (int i = lane; i <= known; i += 64) lds.of_wave[kSelectWaves][i] = i < known ? lds.chunk[i] : Entry{kNone, 0};
+            __syncthreads();
+            if (wave == 0) {                                                   // the waves' lists and what is known, in order
+                int at = 0, out = 0;
+                Entry head = lane <= kSelectWaves ? lds.of_wave[lane][0] : Entry{kNone, 0};
+                for (; out <= keep; ++out) {
+                    const int l = first_of(head);
+                    if (l < 0) break;
+                    if (lane == l) {
+                        lds.chunk[out] = head;
+                        head = lds.of_wave[lane][++at];
+                    }
+                }
+                if (lane == 0) lds.chunks_found = out;
+            }
+            __syncthreads();
+            known = lds.chunks_found;
+        }
+        // their elements
+        const int chunks = known < keep ? known : keep;
+        const double border = chunks == keep ? lds.chunk[keep - 1].key : kNone;      // `keep` candidates reach it
+        for (int r = wave; r < chunks; r += kSelectWaves) {
+            const Entry of = lds.chunk[r];
+            const int b = of.index / most, chunk = of.index % most;
+            const int at = r * keep - r * (r - 1) / 2, room = keep - r;
+            int n = 0;
+            if (lds.ends[b]) {
+                if (lane == 0) { lds.key[at] = of.key; lds.column[at] = a.eos; }
+                n = 1;
+            } else {
+                const char* row = row_of(a, row0 + b, kBf16 ? 2 : 4);
+                const int64_t first = (int64_t)chunk * kChunkCols + lane * 8;
+                const double base = lds.base[b];
+                float z[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] = first + j < a.V ? logit_at<kBf16>(row, first + j) : -INFINITY;
+                for (; n < room; ++n) {
+                    float best = z[0];
+                    int j0 = 0;
+#pragma unroll
+                    for (int j = 1; j < 8; ++j)
+                        if (z[j] > best) { best = z[j]; j0 = j; }
+                    const float top = wave_max(best);
+                    const double key = base + (double)top * per_logit;
+                    if (!(top > kNoLogit) || key < border) break;
+                    const int l = (int)__builtin_ctzll(__ballot(best == top));
+                    if (lane == l) {
+                        lds.key[at + n] = key;
+                        lds.column[at + n] = (int)first + j0;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j == j0) z[j] = -INFINITY;
+                    }
+                }
+            }
+            if (lane == 0) lds.count[r] = n;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            // lane r: the elements of chunk r, best first
+            const int at = lane * keep - lane * (lane - 1) / 2, n = lane < chunks ? lds.count[lane] : 0;
+            const int b = lane < chunks ? lds.chunk[lane].index / most : 0;
+            int i = 0;
+            auto head = [&] { return i < n ? Entry{lds.key[at + i], b * (int)a.V + lds.column[at + i]} : Entry{kNone, 0}; };
+            Entry e = head();
+            double before = INFINITY;
+            int beam_before = -1;
+            uint32_t near = 0;
+            int32_t parent = -1, token = -1;
+            double score = kNone;
+            for (int out = 0; out <= keep; ++out) {
+                const int l = first_of(e);
+                Entry best{kNone, 0};
+                if (l >= 0) best = Entry{read_lane(e.key, l), __builtin_amdgcn_readlane(e.index, l)};
+                if (out == keep && known > keep && lds.chunk[keep].key > best.key) best = Entry{lds.chunk[keep].key, lds.chunk[keep].index / most * (int)a.V};
+                if (!(best.key > kNone)) break;
+                const int of = best.index / (int)a.V;
+                if (of != beam_before && beam_before >= 0 && before - best.key < kNear) near |= 1u << of | 1u << beam_before;
+                before = best.key;
+                beam_before = of;
+                if (out == keep) break;
+                if (lane == out) { parent = of; token = best.index % (int)a.V; score = best.key; }
+                if (lane == l) { ++i; e = head(); }
+            }
+            if (round == 0 && lane == 0) lds.near = near;
+            if ((round == 1 || near == 0) && lane < keep) {
+                a.parent_out[seq * keep + lane] = parent;
+                a.token_out[seq * keep + lane] = token;
+                a.score_out[seq * keep + lane] = (float)score;
+            }
+        }
+        __syncthreads();
+        const uint32_t near = lds.near;
+        if (round == 1 || near == 0) return;
+        for (int b = 0; b < a.beams; ++b) {                                    // uniform
+            if (((near >> b) & 1u) == 0 || lds.ends[b]) continue;
+            const char* row = row_of(a, row0 + b, kBf16 ? 2 : 4);
+            const double total = lds.log2_sum[b];
+            double sum = 0.0;
+            for (int64_t col = threadIdx.x; col < a.V; col += kSelectThreads) {
+                const double x = fma((double)logit_at<kBf16>(row, col), c, -total);
+                if (x > -1000.0) sum += exp2_of(x);
+            }
+            sum = wave_sum(sum);
+            if (lane == 0) lds.sums[wave] = sum;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                double all = 0.0;
+                for (int i = 0; i < kSelectWaves; ++i) all += lds.sums[i];
+                lds.base[b] -= log(all);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+hipError_t launch_beam_select(const BeamArgs& a, bool bf16, void* workspace, hipStream_t stream)
+{
+    const BeamShape s = beam_shape(a.seqs * a.beams, a.V, bf16);
+    char* ws = static_cast<char*>(workspace);
+    const float c = (float)(kLog2e / (double)a.tau);
+    const int64_t items = a.seqs * a.beams * s.segments;
+    const dim3 grid((uint32_t)((items + kStreamWaves - 1) / kStreamWaves));
+    if (bf16) beam_stream_kernel<true><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, ws);
+    else beam_stream_kernel<false><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, ws);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    if (bf16) beam_select_kernel<true><<<(uint32_t)a.seqs, kSelectThreads, 0, stream>>>(a, s, ws);
+    else beam_select_kernel<false><<<(uint32_t)a.seqs, kSelectThreads, 0, stream>>>(a, s, ws);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- the beams' pages
+// The first child of a beam goes on in its last page; every other child takes the last page of a beam without children (there are as
+// many) and needs a copy of what its parent's holds.
+__global__ __launch_bounds__(256)
+void beam_reorder_kernel(ReorderArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row0 = (int64_t)blockIdx.x * a.beams;
+    int parent = -1, donor = -1, at = 0, len = 0, own = -1;
+    if (lane < a.beams) {
+        parent = a.parent[row0 + lane];
+        if (parent < 0 || parent >= a.beams) parent = lane;
+        len = a.row_lens[row0 + lane];
+        len = len < 0 ? 0 : len;
+        at = len / a.page_size;
+        own = at < a.width ? a.row_pages[(row0 + lane) * a.width + at] : -1;   // the page that the row's next token goes to
+    }
+    uint32_t childless = 0, first = 0;
+    for (int p = 0; p < a.beams; ++p) {
+        const uint32_t children = (uint32_t)__ballot(parent == p);
+        if (children != 0) first |= children & (0u - children);
+        else childless |= 1u << p;
+    }
+    const bool other = lane < a.beams && ((first >> lane) & 1u) == 0;
+    const uint32_t others = (uint32_t)__ballot(other);
+    if (other) {                                                               // the j-th of them takes the j-th childless beam's
+        uint32_t left = childless;
+        for (int j = __builtin_popcount(others & ((1u << lane) - 1u)); j > 0; --j) left &= left - 1u;
+        donor = __builtin_ctz(left);
+    }
+    const int from = lane < a.beams ? parent : 0;
+    const int page = __shfl(own, other ? donor : from);                        // of the new row
+    const int source = __shfl(own, from), parent_at = __shfl(at, from), parent_len = __shfl(len, from);
+    if (threadIdx.x < 64 && lane < a.beams) {
+        const int count = parent_len % a.page_size;
+        const bool copy = other && count > 0 && page >= 0 && source >= 0;
+        a.lens_out[row0 + lane] = parent_len;
+        a.src_out[row0 + lane] = copy ? source : -1;
+        a.dst_out[row0 + lane] = copy ? page : -1;
+        a.counts_out[row0 + lane] = copy ? count : 0;
+    }
+    for (int r = threadIdx.x >> 6; r < a.beams; r += 4) {
+        const int p = __builtin_amdgcn_readlane(parent, r), e = __builtin_amdgcn_readlane(parent_at, r), last = __builtin_amdgcn_readlane(page, r);
+        const int32_t* in = a.row_pages + (row0 + p) * a.width;
+        int32_t* out = a.pages_out + (row0 + r) * a.width;
+        for (int i = lane; i < a.width; i += 64) out[i] = i == e ? last : in[i];
+    }
+}
+
+hipError_t launch_beam_reorder(const ReorderArgs& a, hipStream_t stream)
+{
+    beam_reorder_kernel<<<(uint32_t)a.seqs, 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+// A workgroup per page and head: its keys, values and scale bytes are four runs next to each other each.
+__global__ __launch_bounds__(256)
+void cache_copy_kernel(CacheView c, const int32_t* src, const int32_t* dst, const int32_t* counts)
+{
+    const int64_t i = blockIdx.x / (uint32_t)c.heads;
+    const int head = (int)(blockIdx.x % (uint32_t)c.heads);
+    const int from = src[i], to = dst[i];
+    if (from == to || (uint32_t)from >= (uint64_t)c.num_pages || (uint32_t)to >= (uint64_t)c.num_pages) return;
+    int n = counts[i];
+    n = n < 0 ? 0 : n > c.page_size ? c.page_size : (n + 7) & ~7;
+    const int64_t a = ((int64_t)from * c.heads + head) * c.page_size, b = ((int64_t)to * c.heads + head) * c.page_size;
+    const int row = c.dim * (c.fp8 ? 1 : 2);
+    const int64_t vectors = (int64_t)n * row / 16;
+    const u32x4* k0 = reinterpret_cast<const u32x4*>(static_cast<const char*>(c.k) + a * row);
+    const u32x4* v0 = reinterpret_cast<const u32x4*>(static_cast<const char*>(c.v) + a * row);
+    u32x4* k1 = reinterpret_cast<u32x4*>(static_cast<char*>(c.k) + b * row);
+    u32x4* v1 = reinterpret_cast<u32x4*>(static_cast<char*>(c.v) + b * row);
+    for (int64_t j = threadIdx.x; j < vectors; j += 256) {
+        const u32x4 x = k0[j], y = v0[j];
+        k1[j] = x;
+        v1[j] = y;
+    }
+    if (c.fp8)
+        for (int j = threadIdx.x; j < n; j += 256) {
+            c.k_scale[b + j] = c.k_scale[a + j];
+            c.v_scale[b + j] = c.v_scale[a + j];
+        }
+}
+
+hipError_t launch_cache_copy(const CacheView& c, const int32_t* src, const int32_t* dst, const int32_t* counts, int64_t n, hipStream_t stream)
+{
+    cache_copy_kernel<<<(uint32_t)(n * c.heads), 256, 0, stream>>>(c, src, dst, counts);
+    return hipGetLastError();
+}
+
+}  // namespace e3

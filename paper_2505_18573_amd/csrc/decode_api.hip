@@ -4,6 +4,7 @@
 #include <cstdint>
 
 #include "../../include/e3.h"
+#include "beam.h"
 #include "kv_cache.h"
 #include "rotary.h"
 #include "verify.h"
@@ -274,5 +275,67 @@ extern "C" int e3_verify_drafts(const void* logits, int dtype, int64_t rows, int
     a.seed = seed; a.row_base = row_base;
     a.accepted_out = accepted_out; a.token_out = token_out; a.logp_out = logp_out; a.entropy_out = entropy_out;
     const hipError_t err = e3::launch_verify(a, dtype == E3_BF16, workspace, static_cast<hipStream_t>(hip_stream));
+    return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
+}
+
+static bool beam_dims(int64_t seqs, int32_t beams, int64_t V)
+{
+    return seqs >= 0 && seqs < 1 << 24 && beams >= 1 && beams <= E3_MAX_BEAMS && V >= 1 && V <= 1040384;
+}
+
+extern "C" size_t e3_beam_workspace_bytes(int64_t seqs, int32_t beams, int64_t V)
+{
+    return seqs > 0 && beam_dims(seqs, beams, V) ? e3::beam_workspace_bytes(seqs, beams, V) : 0;
+}
+
+extern "C" int e3_beam_select(const void* logits, int dtype, int64_t seqs, int32_t beams, int64_t V, int64_t seq_stride, int64_t beam_stride,
+                              const float* scores, int32_t keep, float tau, const uint8_t* finished, int32_t eos_token,
+                              int32_t* parent_out, int32_t* token_out, float* score_out,
+                              void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    static_assert(E3_MAX_BEAMS == e3::kMaxBeams && E3_MAX_KEEP == e3::kMaxKeep, "one lane per kept candidate");
+    if (dtype != E3_F32 && dtype != E3_BF16) return E3_ERR_DTYPE;
+    if (!beam_dims(seqs, beams, V) || keep < 1 || keep > E3_MAX_KEEP || beam_stride < V) return E3_ERR_SHAPE;
+    if (!(std::isfinite(tau) && tau > 0.0f) || (finished != nullptr && (eos_token < 0 || eos_token >= V))) return E3_ERR_VALUE;
+    if (seqs == 0) return E3_OK;
+    const size_t need = e3::beam_workspace_bytes(seqs, beams, V);
+    if (need == 0) return E3_ERR_SHAPE;
+    if (logits == nullptr || scores == nullptr || parent_out == nullptr || token_out == nullptr || score_out == nullptr) return E3_ERR_NULL;
+    if (workspace == nullptr || workspace_bytes < need) return E3_ERR_WORKSPACE;
+    const int64_t per = dtype == E3_F32 ? 4 : 8;                    // elements in 16 bytes
+    if (!aligned(logits, 16) || !aligned(workspace, 256) || seq_stride % per || beam_stride % per) return E3_ERR_ALIGN;
+    const e3::BeamArgs a{logits, seqs, V, seq_stride, beam_stride, beams, keep, scores, finished, eos_token, tau, parent_out, token_out, score_out};
+    const hipError_t err = e3::launch_beam_select(a, dtype == E3_BF16, workspace, static_cast<hipStream_t>(hip_stream));
+    return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
+}
+
+extern "C" int e3_beam_reorder(const int32_t* parent, int64_t seqs, int32_t beams, const int32_t* row_pages, int64_t row_width,
+                               const int32_t* row_lens, int32_t page_size, int32_t* pages_out, int32_t* lens_out,
+                               int32_t* src_out, int32_t* dst_out, int32_t* counts_out, void* hip_stream)
+{
+    if (seqs < 0 || seqs >= 1 << 24 || beams < 1 || beams > E3_MAX_BEAMS || row_width < 0 || row_width > 0x7FFFFFFF || page_size < 32 ||
+        page_size > (1 << 20) || (page_size & (page_size - 1)) != 0)
+        return E3_ERR_SHAPE;
+    if (seqs == 0) return E3_OK;
+    if (parent == nullptr || row_lens == nullptr || lens_out == nullptr || src_out == nullptr || dst_out == nullptr || counts_out == nullptr ||
+        (row_width > 0 && (row_pages == nullptr || pages_out == nullptr)))
+        return E3_ERR_NULL;
+    // rows are read after others were written
+    if ((row_width > 0 && row_pages == pages_out) || row_lens == lens_out) return E3_ERR_VALUE;
+    const e3::ReorderArgs a{parent, seqs, beams, (int32_t)row_width, page_size, row_pages, row_lens, pages_out, lens_out, src_out, dst_out, counts_out};
+    const hipError_t err = e3::launch_beam_reorder(a, static_cast<hipStream_t>(hip_stream));
+    return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
+}
+
+extern "C" int e3_cache_copy(const e3_cache* cache, const int32_t* src_pages, const int32_t* dst_pages, const int32_t* counts, int64_t n,
+                             void* hip_stream)
+{
+    e3::CacheView view;
+    const int rc = check_cache(cache, &view);
+    if (rc != E3_OK) return rc;
+    if (n < 0 || n >= 1 << 24 || n * view.heads >= 1 << 24) return E3_ERR_SHAPE;   // a workgroup of 256 threads each: below 2^32
+    if (n == 0) return E3_OK;
+    if (src_pages == nullptr || dst_pages == nullptr || counts == nullptr) return E3_ERR_NULL;
+    const hipError_t err = e3::launch_cache_copy(view, src_pages, dst_pages, counts, n, static_cast<hipStream_t>(hip_stream));
     return err == hipSuccess ? E3_OK : E3_ERR_LAUNCH;
 }

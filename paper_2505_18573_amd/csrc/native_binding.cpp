@@ -38,6 +38,10 @@ decltype(&e3_prefix_attention) p_attention;
 decltype(&e3_verify_workspace_bytes) p_verify_bytes;
 decltype(&e3_verify_drafts) p_verify;
 decltype(&e3_rotate) p_rotate;
+decltype(&e3_beam_workspace_bytes) p_beam_bytes;
+decltype(&e3_beam_select) p_beam_select;
+decltype(&e3_beam_reorder) p_beam_reorder;
+decltype(&e3_cache_copy) p_cache_copy;
 decltype(&e3_window_attention) p_window;
 decltype(&e3_window_attention_workspace_bytes) p_window_bytes;
 decltype(&e3_cache_append_rotated) p_append_rotated;
@@ -758,6 +762,93 @@ PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     });
 }
 
+// logits, scores, keep, tau, finished, eos_token, parent_out, token_out, score_out, workspace
+PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 10) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const at::Tensor* z = r.first(a[0]);
+        if (!r.ok || z->dim() != 3) return unusual();
+        const int type = float_type(r, z->scalar_type());
+        const int64_t seqs = z->size(0), beams = z->size(1), V = z->size(2);
+        if ((V > 1 && z->stride(2) != 1) || beams != (int32_t)beams || a[1] == Py_None) return unusual();
+        // of a dimension of one what binding.py gives
+        const int64_t beam_stride = beams > 1 ? z->stride(1) : (V + 7) / 8 * 8;
+        const int64_t seq_stride = seqs > 1 ? z->stride(0) : beam_stride * beams;
+        auto table = [&](PyObject* o, at::ScalarType kind) -> const void* {
+            if (o == Py_None) return nullptr;
+            const at::Tensor* t = r.plain(o);
+            if (t == nullptr || t->scalar_type() != kind || t->dim() != 2 || t->size(0) != seqs || t->size(1) != beams || !t->is_contiguous()
+                || t->device() != r.dev) { r.ok = false; return nullptr; }
+            return t->data_ptr();
+        };
+        const void* scores = table(a[1], at::kFloat);
+        const void* finished = table(a[4], at::kByte);
+        const int32_t keep = r.integer32(a[2]), eos = r.integer32(a[5]);
+        const double tau = r.number(a[3]);
+        if (!r.ok || keep < 1) return unusual();
+        const std::array<int64_t, 2> shape = {seqs, keep};
+        Output parent, token, score;
+        parent.shaped(r, a[6], at::kInt, shape);
+        token.shaped(r, a[7], at::kInt, shape);
+        score.shaped(r, a[8], at::kFloat, shape);
+        const size_t need = a[9] == Py_None ? p_beam_bytes(seqs, (int32_t)beams, V) : 0;
+        const Workspace ws(r, a[9] == Py_False ? Py_True : a[9], need, true);
+        if (a[9] == Py_None && need > 0 && ws.p == nullptr) return unusual();
+        return run(r, [&](void* s) {
+                       return p_beam_select(z->data_ptr(), type, seqs, (int32_t)beams, V, seq_stride, beam_stride, (const float*)scores, keep, (float)tau,
+                                            (const uint8_t*)finished, eos, (int32_t*)parent.p, (int32_t*)token.p, (float*)score.p, ws.p, ws.bytes, s);
+                   },
+                   [&] { return PyTuple_Pack(3, parent.object, token.object, score.object); });
+    });
+}
+
+// parent, row_pages, row_lens, page_size, pages_out, lens_out, src_out, dst_out, counts_out
+PyObject* beam_reorder(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 9) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const at::Tensor* parent = r.first(a[0]);
+        const at::Tensor* pages = r.ok ? r.plain(a[1]) : nullptr;
+        if (!r.ok || parent->dim() != 2 || parent->scalar_type() != at::kInt || !parent->is_contiguous() || parent->size(1) != (int32_t)parent->size(1)
+            || pages->dim() != 2 || pages->scalar_type() != at::kInt || pages->size(0) != parent->numel() || !pages->is_contiguous()
+            || pages->device() != r.dev || a[2] == Py_None) return unusual();
+        const int64_t seqs = parent->size(0), beams = parent->size(1), rows = seqs * beams, width = pages->size(1);
+        const void* lens = r.vector(a[2], at::kInt, rows);
+        const int32_t page = r.integer32(a[3]);
+        if (!r.ok) return unusual();
+        Output out_pages, out[4];
+        out_pages.shaped(r, a[4], at::kInt, std::array<int64_t, 2>{rows, width});
+        for (int i = 0; i < 4; ++i) out[i].take_or_make(r, a[5 + i], at::kInt, rows);
+        return run(r, [&](void* s) {
+                       return p_beam_reorder((const int32_t*)parent->data_ptr(), seqs, (int32_t)beams, (const int32_t*)pages->data_ptr(), width,
+                                             (const int32_t*)lens, page, (int32_t*)out_pages.p, (int32_t*)out[0].p, (int32_t*)out[1].p,
+                                             (int32_t*)out[2].p, (int32_t*)out[3].p, s);
+                   },
+                   [&] { return PyTuple_Pack(5, out_pages.object, out[0].object, out[1].object, out[2].object, out[3].object); });
+    });
+}
+
+// cache, src_pages, dst_pages, counts; True where it was done
+PyObject* cache_copy(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    if (n_args != 4) return unusual();
+    return guarded([&]() -> PyObject* {
+        Reader r;
+        const Cache cache(r, a[0]);
+        const at::Tensor* src = r.ok ? r.plain(a[1]) : nullptr;
+        if (!r.ok || src->dim() != 1 || a[2] == Py_None || a[3] == Py_None) return unusual();
+        const int64_t n = src->size(0);
+        const void* from = r.vector(a[1], at::kInt, n);
+        const void* to = r.vector(a[2], at::kInt, n);
+        const void* counts = r.vector(a[3], at::kInt, n);
+        return run(r, [&](void* s) { return p_cache_copy(&cache.c, (const int32_t*)from, (const int32_t*)to, (const int32_t*)counts, n, s); },
+                   [&]() -> PyObject* { Py_RETURN_TRUE; });
+    });
+}
+
 // tau_t, H_t, H_init, vocab, t, t_anneal, t_max, eta, tau_min, tau_max
 PyObject* temperature(PyObject*, PyObject* const* a, Py_ssize_t n_args)
 {
@@ -802,6 +893,10 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     get("e3_verify_workspace_bytes", p_verify_bytes);
     get("e3_verify_drafts", p_verify);
     get("e3_rotate", p_rotate);
+    get("e3_beam_workspace_bytes", p_beam_bytes);
+    get("e3_beam_select", p_beam_select);
+    get("e3_beam_reorder", p_beam_reorder);
+    get("e3_cache_copy", p_cache_copy);
     get("e3_window_attention", p_window);
     get("e3_window_attention_workspace_bytes", p_window_bytes);
     get("e3_cache_append_rotated", p_append_rotated);
@@ -829,6 +924,9 @@ PyMethodDef methods[] = {
     {"attention", fast(attention), METH_FASTCALL, nullptr},
     {"verify", fast(verify), METH_FASTCALL, nullptr},
     {"rotate", fast(rotate), METH_FASTCALL, nullptr},
+    {"beam_select", fast(beam_select), METH_FASTCALL, nullptr},
+    {"beam_reorder", fast(beam_reorder), METH_FASTCALL, nullptr},
+    {"cache_copy", fast(cache_copy), METH_FASTCALL, nullptr},
     {"window", fast(window), METH_FASTCALL, nullptr},
     {"append_rotated", fast(append_rotated), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
