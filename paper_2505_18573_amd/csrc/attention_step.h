@@ -151,8 +151,11 @@ struct StepData {
     static __device__ __forceinline__ uint32_t unbounded_in(uint32_t w)
     {
         if (kFp8) return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;   // 0x7F, 0xFF: the sum carries
-        return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+        const uint32_t top = exponents_full(w);
+        return (top - (top >> 15)) | top;
     }
+    // the highest bit of each bf16 whose exponent is all ones (the addition carries into it)
+    static __device__ __forceinline__ uint32_t exponents_full(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
     // whether the lane holds a value that is no finite number
     __device__ __forceinline__ bool unbounded() const
     {
@@ -160,7 +163,7 @@ struct StepData {
 #pragma unroll
         for (int i = 0; i < kVLoads; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) bad |= unbounded_in(v[i][j]);
+            for (int j = 0; j < 4; ++j) bad |= kFp8 ? unbounded_in(v[i][j]) : exponents_full(v[i][j]);
         return bad != 0;
     }
     // such values of `from` as ones, all others as zeros; they are zeros in `from` afterwards

@@ -281,8 +281,8 @@ __device__ __forceinline__ Query query_of(const WindowArgs& a, int R, const Work
 }
 __device__ __forceinline__ int64_t page_row(const CacheView& c, int head, int page, int at)
 {
-    const int64_t p = (uint32_t)page < (uint64_t)c.num_pages ? page : 0;
-    return (p * c.heads + head) * c.page_size + (at & (c.page_size - 1));
+    const uint32_t p = (uint32_t)page < (uint64_t)c.num_pages ? (uint32_t)page : 0u;
+    return (int64_t)((((uint64_t)p * (uint32_t)c.heads + (uint32_t)head) << c.page_shift) + (uint32_t)(at & (c.page_size - 1)));
 }
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
@@ -465,89 +465,141 @@ struct Few {
 // and since a sum over tokens may be taken in any order, row 8 a + 4 h + b of a score tile is given token 16 (a >> 1) + 8 h + 4 (a & 1) + b:
 // a lane's scores are then tokens 8 h .. 8 h + 7 of either half, what it has to hold of P^T as operand of O^T = V^T P^T.
 // In LDS, twice: keys as rows of 16-byte pieces whose places are turned by the token, so that the lanes of a wave, which read one
-// piece of 32 rows, meet all banks; values as the cache has them, eight tokens of a column together, widened to bf16 where the
-// cache holds codes (once for the four waves; the powers of two are applied in fp32 to scores and weights).
+// piece of 32 rows, meet all banks; values as the cache has them, eight tokens of a column together.  A 16-bit cache goes there
+// from memory without registers in between, while the block before is worked on; codes pass through registers, widened to bf16
+// (once for the four waves; the powers of two are applied in fp32 to scores and weights).
 template <int D, bool kFp8>
 struct Many {
     static constexpr int kPieces = D / 8;                                      // 16-byte pieces of a row in bf16
     static constexpr int kKeys = kBlock * D * 2, kValues = kBlock * D * 2;
-    static constexpr int kFactors = 2 * kBlock * 4;
-    static constexpr int kImage = kKeys + kValues + kFactors + 16;             // and four flags
-    static constexpr int kLds = 2 * kImage;
-    static constexpr int kLoads = kFp8 ? kBlock * D / 16 / 256 : kBlock * D / 8 / 256;     // of 16 bytes, a thread's, of K and of V
+    static constexpr int kImage = kKeys + kValues;                             // two of them, within the 64 KB that a load into LDS reaches,
+    static constexpr int kFactors = 2 * kBlock * 4, kExtra = kFactors + 16;    // then twice factors and four flags
+    static constexpr int kLds = 2 * (kImage + kExtra);
+    static constexpr int kElem = kFp8 ? 1 : 2;
+    static constexpr int kRow = D * kElem / 16;                                // pieces of a row in the cache
+    static constexpr int kLoads = kBlock * kRow / 256;                         // of 16 bytes, a thread's, of K and of V
     static constexpr int kCols = D / 32, kDeep = D / 16;
 
-    static constexpr int kElem = kFp8 ? 1 : 2;
-
-    u32x4 k[kLoads], v[kLoads];
+    u32x4 k[kFp8 ? kLoads : 1], v[kFp8 ? kLoads : 1];
     uint32_t factor;
 
     static __device__ __forceinline__ int turned(int token, int piece)
     {
         return piece ^ (kPieces == 16 ? token & 15 : (token >> 1) & 7);
     }
-    // A block's rows into registers: pages of its two halves.
-    __device__ __forceinline__ void fetch(const CacheView& c, int head, const int page[2], int at)
+    // 16 bytes a lane from memory, `offset` behind `from`, into LDS, lane after lane from `to` on (from and to the same in all of them).
+    static __device__ __forceinline__ void to_lds(const char* from, uint32_t offset, uint32_t to)
     {
-        constexpr int kRow = D * kElem / 16;                                   // pieces of a row in the cache
-        const int64_t row[2] = {page_row(c, head, page[0], at), page_row(c, head, page[1], at + 32)};
+        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(from), "s"(to) : "memory");
+    }
+    static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    // Writes to LDS are there for all waves.  Loads from memory stay on their way.
+    static __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+    // Where the next block lies: its two halves' rows (the same for all lanes; what a lane takes of them is the same in every block) and the
+    // image that it goes to.
+    const char* keys_at[2];
+    const char* values_at[2];
+    uint32_t image_at;
+    uint32_t of_key, of_value;                                                 // the lane's part
+    __device__ __forceinline__ void begin()
+    {
+        // (the tokens of a thread's loads differ by a multiple of 16, which does not turn its piece)
+        const int x = kFp8 && kLoads == 1 ? threadIdx.x & 127 : threadIdx.x, token = x / kRow, piece = x % kRow;
+        of_key = token * D * kElem + (kFp8 ? piece : turned(token, piece)) * 16;
+        of_value = x * 16;
+    }
+    __device__ __forceinline__ void aim(const CacheView& c, int head, const int page[2], int at)
+    {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int x = i * 256 + (int)threadIdx.x, token = x / kRow, piece = x % kRow;
-            const int64_t from = (token < 32 ? row[0] : row[1]) + (token & 31);
-            k[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(c.k) + from * (D * kElem) + piece * 16);
-            // values: a block of eight tokens is as long as eight rows
-            const int half = x / (32 * kRow), in = x % (32 * kRow);
-            v[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(c.v) + row[half] * (D * kElem) + in * 16);
-        }
-        if (kFp8) {
-            const int token = threadIdx.x & 63;
-            const int64_t from = (token < 32 ? row[0] : row[1]) + (token & 31);
-            factor = threadIdx.x < 64 ? c.k_scale[from] : c.v_scale[from];
+        for (int half = 0; half < 2; ++half) {
+            const int64_t row = uniform(page_row(c, head, page[half], at + 32 * half));
+            keys_at[half] = static_cast<const char*>(c.k) + row * (D * kElem);
+            values_at[half] = static_cast<const char*>(c.v) + row * (D * kElem);
+            if (kFp8 && half == 0) {
+                const int token = threadIdx.x & 63;
+                scales_row = row + (token & 31);
+            } else if (kFp8) {
+                scales_row = (threadIdx.x & 63) < 32 ? scales_row : row + (threadIdx.x & 31);
+            }
         }
     }
-    static __device__ __forceinline__ u32x4 wide(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(u32x4, widen(lo, hi)); }
-    // ... and into LDS.  `check`: values may be hidden from some queries; those that are no finite numbers become zeros, and flags
-    // tell of them.
-    __device__ __forceinline__ void put(char* image, float scale, bool check)
+    int64_t scales_row;                                                        // the row whose scale byte the thread takes
+    // The next block's load i of kAll: codes into registers, 16-bit elements into LDS.
+    static constexpr int kAll = 2 * kLoads + (kFp8 ? 1 : 0);
+    __device__ __forceinline__ void load(const CacheView& c, int i)
     {
-        constexpr int kRow = D * (kFp8 ? 1 : 2) / 16;
+        if (i == 2 * kLoads) {
+            factor = threadIdx.x < 64 ? c.k_scale[scales_row] : c.v_scale[scales_row];
+            return;
+        }
+        const bool key = i < kLoads;
+        const int n = key ? i : i - kLoads;
+        const uint32_t of = key ? of_key : of_value;
+        const int wave = uniform((int)threadIdx.x >> 6);
+        if (kFp8 && kLoads == 1) {                                             // two waves a half
+            const char* at = key ? (wave >= 2 ? keys_at[1] : keys_at[0]) : (wave >= 2 ? values_at[1] : values_at[0]);
+            (key ? k : v)[0] = *reinterpret_cast<const u32x4*>(at + of);
+            return;
+        }
+        constexpr int kOfHalf = kLoads / 2 > 0 ? kLoads / 2 : 1, kTokens = 256 / kRow;         // loads of a half, and the tokens of one
+        const char* at = (key ? keys_at : values_at)[n / kOfHalf] + n % kOfHalf * (kTokens * D * kElem);
+        if (kFp8) (key ? k : v)[n] = *reinterpret_cast<const u32x4*>(at + of);
+        else to_lds(at, of, image_at + (key ? 0 : kKeys) + (n * 256 + wave * 64) * 16);
+    }
+    static __device__ __forceinline__ u32x4 wide(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(u32x4, widen(lo, hi)); }
+    static __device__ __forceinline__ uint32_t clean(u32x4& w)
+    {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t b = StepData<D, kFp8>::unbounded_in(w[j]);
+            w[j] &= ~b;
+            bad |= b;
+        }
+        return bad;
+    }
+    // ... and what was fetched is in LDS as far as this wave goes.  `check`: values may be hidden from some queries; those that are no finite numbers
+    // become zeros, and flags tell of them.
+    __device__ __forceinline__ void put(char* image, char* extra, float scale, bool check)
+    {
         u32x4* keys = reinterpret_cast<u32x4*>(image);
         u32x4* values = reinterpret_cast<u32x4*>(image + kKeys);
         uint32_t bad = 0;
-        if (check) {
+        if (kFp8) {
+            if (check) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
+                for (int i = 0; i < kLoads; ++i) bad |= clean(v[i]);
+            }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t w = StepData<D, kFp8>::unbounded_in(v[i][j]);
-                    v[i][j] &= ~w;
-                    bad |= w;
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int x = i * 256 + (int)threadIdx.x, token = x / kRow, piece = x % kRow;
-            if (kFp8) {
+            for (int i = 0; i < kLoads; ++i) {
+                const int x = i * 256 + (int)threadIdx.x, token = x / kRow, piece = x % kRow;
                 keys[token * kPieces + turned(token, 2 * piece)] = wide(k[i].x, k[i].y);
                 keys[token * kPieces + turned(token, 2 * piece + 1)] = wide(k[i].z, k[i].w);
                 values[2 * x] = wide(v[i].x, v[i].y);
                 values[2 * x + 1] = wide(v[i].z, v[i].w);
-            } else {
-                keys[token * kPieces + turned(token, piece)] = k[i];
-                values[x] = v[i];
+            }
+            float* factors = reinterpret_cast<float*>(extra);
+            if (threadIdx.x < 128) {
+                // (a hidden token's byte may be anything, 255 would be infinite: a weight of zero times it must be zero)
+                const float f = __uint_as_float((factor < 254 ? factor : 254) << 23);
+                factors[threadIdx.x] = threadIdx.x < 64 ? f * scale : f;
+            }
+        } else {
+            landed();
+            if (check) {
+#pragma unroll 1
+                for (int i = 0; i < kLoads; ++i) {                             // what the thread itself has fetched
+                    u32x4 w = values[i * 256 + threadIdx.x];
+                    const uint32_t b = clean(w);
+                    if (b != 0) values[i * 256 + threadIdx.x] = w;
+                    bad |= b;
+                }
             }
         }
-        float* factors = reinterpret_cast<float*>(image + kKeys + kValues);
-        if (kFp8 && threadIdx.x < 128) {
-            const float f = __uint_as_float(factor << 23);
-            factors[threadIdx.x] = threadIdx.x < 64 ? f * scale : f;
-        }
         const bool any = __any(bad != 0);
-        if ((threadIdx.x & 63) == 0) reinterpret_cast<int*>(image + kKeys + kValues + kFactors)[threadIdx.x >> 6] = any;
+        if ((threadIdx.x & 63) == 0) reinterpret_cast<int*>(extra + kFactors)[threadIdx.x >> 6] = any;
     }
-    // Writes to LDS are there for all waves.  Loads from memory stay on their way.
-    static __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
     static __device__ __forceinline__ f32x16 product(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x16 zero()
@@ -558,17 +610,28 @@ struct Many {
         return z;
     }
 
-    __device__ __forceinline__ void run(const CacheView& c, const WindowArgs& a, int R, const Work& w, const Piece1& piece, char* lds,
+    // What the workgroup has ahead of it: pages of the next two blocks and the image that the next one is in; `ready`: it is on its way.
+    int page[2], after[2];
+    int image_of;
+    bool ready;
+    // The first block of an item that follows: `is` where there is one.
+    struct Next {
+        Work w;
+        int head;
+        bool is;
+    };
+    static __device__ __forceinline__ int page_of(const CacheView& c, const WindowArgs& a, const Work& w, const Band& band, int s, int steps, int half)
+    {
+        // a half that none of the tile's queries sees may lie behind the table
+        const int at = s < steps ? band.at(s, kBlock) + 32 * half : 0x7FFFFFFF;
+        return at <= band.p1 ? a.row_pages[(int64_t)w.row * a.row_width + (at >> c.page_shift)] : -1;
+    }
+
+    __device__ __forceinline__ void run(const CacheView& c, const WindowArgs& a, int R, const Work& w, const Piece1& piece, const Next& next, char* lds,
                                         float2* ml_out, float* o_out)
     {
         const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
         const Band band = band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kBlock);
-        const int32_t* pages = a.row_pages + (int64_t)w.row * a.row_width;
-        // pages of the halves of step s; a half that none of the tile's queries sees may lie behind the table
-        auto page_at = [&](int s, int half) {
-            const int at = s < piece.to ? band.at(s, kBlock) + 32 * half : 0x7FFFFFFF;
-            return at <= band.p1 ? pages[at >> c.page_shift] : -1;
-        };
         // the wave's queries
         const int64_t first = (int64_t)w.tile * kTile + wave * 32, queries = (int64_t)w.n * R;
         const bool busy = first < queries;
@@ -578,10 +641,8 @@ struct Many {
         const int sure_hi = p0 + 1, sure_lo = p1 >= a.window ? p1 - a.window + 1 : 0;          // what all of them see
         const int tile_sure_hi = band.p0 + 1, tile_sure_lo = band.p1 >= a.window ? band.p1 - a.window + 1 : 0;
         const Query x = query_of(a, R, w, piece.head, first + col);
+        const uint32_t lds_at = (uint32_t)(uintptr_t)reinterpret_cast<__attribute__((address_space(3))) char*>(reinterpret_cast<uintptr_t>(lds));
 
-        int page[2] = {page_at(piece.from, 0), page_at(piece.from, 1)};
-        int after[2] = {page_at(piece.from + 1, 0), page_at(piece.from + 1, 1)};
-        fetch(c, piece.head, page, band.at(piece.from, kBlock));
         bf16x8 q[kDeep];
         {
             const uint16_t* qp = a.q + x.token * a.q_token_stride + x.head * a.q_head_stride;
@@ -592,59 +653,131 @@ struct Many {
                 q[s] = __builtin_bit_cast(bf16x8, u);
             }
         }
+        // the next item's first pages are asked for now, its first block in this item's last step
+        int next_page[2] = {-1, -1}, next_after[2] = {-1, -1}, next_at = 0;
+        if (next.is) {
+            const Band next_band = band_of(R, next.w.tile, next.w.n, next.w.len, a.window, a.sinks, kBlock);
+            next_at = next_band.at(0, kBlock);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                next_page[half] = page_of(c, a, next.w, next_band, 0, next_band.steps, half);
+                next_after[half] = page_of(c, a, next.w, next_band, 1, next_band.steps, half);
+            }
+        }
+        if (!ready && piece.from < piece.to) {
+            meet();                                                            // the last item's blocks are done with
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                page[half] = page_of(c, a, w, band, piece.from, piece.to, half);
+                after[half] = page_of(c, a, w, band, piece.from + 1, piece.to, half);
+            }
+            image_of = 0;
+            aim(c, piece.head, page, band.at(piece.from, kBlock));
+            image_at = lds_at;
+#pragma unroll
+            for (int i = 0; i < kAll; ++i) load(c, i);
+        }
         float m = kNoScore, l = 0.0f;
         f32x16 o[kCols];
 #pragma unroll
         for (int b = 0; b < kCols; ++b) o[b] = zero();
         const float scale = a.scale * kLog2eF;
-        // row of the score tile -> token
+        // row of the score tile -> token; where its piece h lies (piece 2 i + h: that place with the bits of 2 i turned)
         const int token_of_row = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+        const uint32_t key_row = token_of_row * (D * 2), key_piece = turned(token_of_row, h) * 16;
 
-        meet();                                                                // the last item's blocks are done with
         for (int s = piece.from; s < piece.to; ++s) {
-            char* image = lds + ((s - piece.from) & 1) * kImage;
+            char* image = lds + image_of * kImage;
+            char* extra = lds + 2 * kImage + image_of * kExtra;
+            image_of ^= 1;
             const int at = band.at(s, kBlock);
-            const bool there[2] = {(uint32_t)page[0] < (uint64_t)c.num_pages, (uint32_t)page[1] < (uint64_t)c.num_pages};
+            const int now[2] = {uniform(page[0]), uniform(page[1])};
+            const bool there[2] = {(uint32_t)now[0] < (uint64_t)c.num_pages, (uint32_t)now[1] < (uint64_t)c.num_pages};
             const bool whole = there[0] && there[1];
             const bool check = !(whole && at + kBlock <= tile_sure_hi && (at >= tile_sure_lo || at + kBlock <= a.sinks));
-            put(image, scale, check);
-            const int now[2] = {page[0], page[1]};
-            page[0] = after[0]; page[1] = after[1];
-            if (s + 1 < piece.to) {
-                fetch(c, piece.head, page, band.at(s + 1, kBlock));
-                after[0] = page_at(s + 2, 0); after[1] = page_at(s + 2, 1);
+            put(image, extra, scale, check);
+            // The next block: this item's, or the next one's first.  (Behind the last of all the same block comes once more, for nothing:
+            // the loads lie between products, without branches.)
+            const bool last = s + 1 == piece.to;
+            ready = !last || next.is;
+            if (!last) {
+                page[0] = after[0]; page[1] = after[1];
+                after[0] = page_of(c, a, w, band, s + 2, piece.to, 0);
+                after[1] = page_of(c, a, w, band, s + 2, piece.to, 1);
+            } else if (next.is) {
+                page[0] = next_page[0]; page[1] = next_page[1];
+                after[0] = next_after[0]; after[1] = next_after[1];
             }
-            meet();
-            if (!busy || at >= wave_hi || (at + kBlock <= wave_lo && at >= a.sinks)) continue;
+            if (ready) aim(c, last ? next.head : piece.head, page, last ? next_at : band.at(s + 1, kBlock));
+            image_at = lds_at + image_of * kImage;
+            meet();                                                            // all waves' parts are there, and the other image is done with
+            // Of two workgroups on a compute unit the older one's waves go first and it would end earlier, the other then being alone:
+            // they take turns.
+            if (((s >> 2) ^ (int)(blockIdx.x / (gridDim.x / kPerUnit))) & 1) __builtin_amdgcn_s_setprio(1);
+            else __builtin_amdgcn_s_setprio(0);
             const bool edge = !(whole && at + kBlock <= sure_hi && (at >= sure_lo || at + kBlock <= a.sinks));
-            const u32x4* keys = reinterpret_cast<const u32x4*>(image);
-            const u32x4* values = reinterpret_cast<const u32x4*>(image + kKeys);
-            const float* factors = reinterpret_cast<const float*>(image + kKeys + kValues);
+            const u32x4* values = reinterpret_cast<const u32x4*>(image + kKeys) + h * D + col;
+            const float* factors = reinterpret_cast<const float*>(extra);
+            // Pieces of the keys are asked for six products ahead (left to itself the compiler asks for each right before its product
+            // and waits), the next block's loads, which take the memory units 500 cycles a workgroup, one every other product.
+            static_assert(kAll <= kDeep, "a load every other product");
             f32x16 t[2] = {zero(), zero()};
+            {
+                constexpr int kAhead = 6;
+                bf16x8 piece_of[kAhead];
+                auto ask = [&](int j) {
+                    piece_of[j % kAhead] = *reinterpret_cast<const bf16x8*>(image + key_row + (key_piece ^ (j / 2 * 32)) + j % 2 * (32 * D * 2));
+                };
 #pragma unroll
-            for (int i = 0; i < kDeep; ++i)
+                for (int j = 0; j < kAhead; ++j) ask(j);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int token = 32 * b + token_of_row;
-                    t[b] = product(__builtin_bit_cast(bf16x8, keys[token * kPieces + turned(token, 2 * i + h)]), q[i], t[b]);
+                for (int j = 0; j < 2 * kDeep; ++j) {
+                    t[j % 2] = product(piece_of[j % kAhead], q[j / 2], t[j % 2]);
+                    if (j + kAhead < 2 * kDeep) ask(j + kAhead);
+                    if (j % 2 == 1 && j / 2 < kAll) load(c, j / 2);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-            auto sees = [&](int b, int i) {
-                const int token = at + 32 * b + 16 * (i >> 3) + 8 * h + (i & 7);
-                return there[b] && token < x.hi && (token >= x.lo || token < a.sinks);
-            };
+            }
+            if (!busy || at >= wave_hi || (at + kBlock <= wave_lo && at >= a.sinks)) continue;         // (the loads above are every wave's)
+            if (kFp8) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    t[b][i] *= kFp8 ? factors[32 * b + 16 * (i >> 3) + 8 * h + (i & 7)] : scale;
-                    if (edge) t[b][i] = sees(b, i) ? t[b][i] : -INFINITY;
+                    for (int i = 0; i < 16; ++i) t[b][i] *= factors[32 * b + 16 * (i >> 3) + 8 * h + (i & 7)];
+            }
+            if (edge) {
+                // Token 32 b + 16 (i >> 3) + (i & 7) behind the lane's first one: in the window if from `from` on by less than `n`, else
+                // among the first ones.
+                const int base = at + 8 * h;
+                const int from = x.lo - base, n = x.hi - x.lo;
+                if (at < a.sinks) {                                            // uniform
+                    const int kept = (a.sinks < x.hi ? a.sinks : x.hi) - base;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int k = 32 * b + 16 * (i >> 3) + (i & 7);
+                            t[b][i] = there[b] && ((uint32_t)(k - from) < (uint32_t)n || k < kept) ? t[b][i] : -INFINITY;
+                        }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t most = there[b] ? (uint32_t)n : 0u;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) t[b][i] = (uint32_t)(32 * b + 16 * (i >> 3) + (i & 7) - from) < most ? t[b][i] : -INFINITY;
+                    }
                 }
-            float top = fmaxf(t[0][0], t[1][0]);
+            }
+            float tops[4];
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int k = 0; k < 4; ++k) {
+                tops[k] = t[k >> 1][8 * (k & 1)];
 #pragma unroll
-                for (int i = 1; i < 15; i += 2) top = fmax3(top, t[b][i], t[b][i + 1]);
-            top = fmax3(top, t[0][15], t[1][15]);
+                for (int i = 1; i < 8; ++i) tops[k] = fmaxf(tops[k], t[k >> 1][8 * (k & 1) + i]);
+            }
+            float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+            if (!kFp8) top *= scale;                                           // the scale enters the exponent below
             if (__any(top > m + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float to = fmaxf(m, top);
@@ -656,33 +789,46 @@ struct Many {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[b][i] *= f;
             }
-            const int* flags = reinterpret_cast<const int*>(image + kKeys + kValues + kFactors);
-            const bool odd = check && (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+            // Weights of 16 tokens as two bf16 numbers each, two weights at a time: the next tokens' between the products of these.
+            float sum[2] = {0.0f, 0.0f};
+            u32x4 p[2], rest[2];
+            auto weigh = [&](int n, int j) {
+                float u[2];
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {                                  // 16 tokens
-                    bf16x8 p, rest;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float e = __builtin_amdgcn_exp2f(t[b][8 * n + j] - m);
-                        l += e;
-                        float u = e;
-                        if (kFp8) {
-                            u = e * factors[kBlock + 32 * b + 16 * n + 8 * h + j];
-                            if (edge) u = sees(b, 8 * n + j) ? u : 0.0f;       // a hidden token's scale may be anything
-                        }
-                        p[j] = (__bf16)u;
-                        rest[j] = (__bf16)(u - (float)p[j]);
-                    }
-                    const u32x4* of = values + (4 * b + 2 * n + h) * D + col;
-#pragma unroll
-                    for (int d = 0; d < kCols; ++d) {
-                        const bf16x8 value = __builtin_bit_cast(bf16x8, of[32 * d]);
-                        o[d] = product(value, rest, product(value, p, o[d]));
-                    }
+                for (int g = 0; g < 2; ++g) {
+                    const float y = t[n >> 1][8 * (n & 1) + 2 * j + g];
+                    const float e = __builtin_amdgcn_exp2f(kFp8 ? y - m : fmaf(y, scale, -m));
+                    sum[g] += e;
+                    u[g] = kFp8 ? e * factors[kBlock + 16 * n + 8 * h + 2 * j + g] : e;
                 }
-            if (__builtin_expect(odd, 0)) {
+                uint32_t w2 = pack2(u[0], u[1]);
+                asm("" : "+v"(w2));                                            // (or each half would be rounded once more on its own)
+                p[n & 1][j] = w2;
+                rest[n & 1][j] = pack2(u[0] - __uint_as_float(w2 << 16), u[1] - __uint_as_float(w2 & 0xFFFF0000u));
+            };
+            bf16x8 value[2][kCols];
+            auto ask = [&](int n, int d) { value[n & 1][d] = __builtin_bit_cast(bf16x8, values[2 * n * D + 32 * d]); };
+#pragma unroll
+            for (int d = 0; d < kCols; ++d) ask(0, d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) weigh(0, j);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const bf16x8 pb = __builtin_bit_cast(bf16x8, p[n & 1]), rb = __builtin_bit_cast(bf16x8, rest[n & 1]);
+#pragma unroll
+                for (int d = 0; d < 2 * kCols; ++d) {                          // first all columns with p, then with the rest
+                    o[d % kCols] = product(value[n & 1][d % kCols], d < kCols ? pb : rb, o[d % kCols]);
+                    if (n < 3) {
+                        if (d < kCols) ask(n + 1, d);
+                        if (d % (kCols / 2) == kCols / 2 - 1) weigh(n + 1, d / (kCols / 2));
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            l += sum[0] + sum[1];
+            const int* flags = reinterpret_cast<const int*>(extra + kFactors);
+            if (__builtin_expect(check && (flags[0] | flags[1] | flags[2] | flags[3]) != 0, 0)) {
                 // Values that are no finite numbers, hidden from some queries (zeros in LDS): one more product, with what the cache
                 // holds, counts those that a query sees.
 #pragma unroll 1
@@ -742,7 +888,8 @@ struct Many {
     }
 };
 
-// The stretch of worker `part`: f(record, piece, which of the worker's two places).
+// The stretch of worker `part`: f(record, piece, which of the worker's two places, record and head of what lies behind the piece in the stretch,
+// whether that is an item's first steps).
 template <int kLine, typename F>
 __device__ __forceinline__ void along(const Work* list, int count, const Division& d, int heads, int part, Cut* cut, F f)
 {
@@ -752,8 +899,8 @@ __device__ __forceinline__ void along(const Work* list, int count, const Divisio
     int i = find_work(list, count, at);
     Cut found{-1, 0, 0, 0};
     const int64_t begin = at;
+    Work w = uniform(list[i]);
     while (at < end && i < count) {
-        const Work w = uniform(list[i]);
         const int64_t offset = at - w.first;
         const int head = (int)divide(offset, w.cost), from = (int)(offset - (int64_t)head * w.cost);
         const int n = end - at < w.cost - from ? (int)(end - at) : w.cost - from;
@@ -769,9 +916,14 @@ __device__ __forceinline__ void along(const Work* list, int count, const Divisio
             if (begin_of(part - 1, d.steps[kLine], d.parts[kLine]) <= item + kCost)
                 found = Cut{i, head, part_of(item + w.cost - 1, d.steps[kLine], d.parts[kLine]), 0};
         }
-        if (piece.to > piece.from || (w.cost == kCost && piece.whole)) f(w, piece, from <= kCost ? 1 : 0);
+        // what follows: the same tile's next head, or the next tile
+        const bool done = head + 1 == heads && from + n == w.cost;
+        Work after = w;
+        if (done && i + 1 < count) after = uniform(list[i + 1]);
+        const bool more = at + n < end && from + n == w.cost && (!done || i + 1 < count) && after.cost > kCost && end - (at + n) > kCost;
+        if (piece.to > piece.from || (w.cost == kCost && piece.whole)) f(w, piece, from <= kCost ? 1 : 0, after, done ? 0 : head + 1, more);
         at += n;
-        if (head + 1 == heads && from + n == w.cost) ++i;
+        if (done) { ++i; w = after; }
     }
     if ((threadIdx.x & (kLine == kOfGroups ? 255 : 63)) == 0) *cut = found;
 }
@@ -790,12 +942,15 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
     const int block = (workgroups & 7) == 0 ? (int)(blockIdx.x & 7) * (workgroups >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
     if (block < d.groups) {
         float* o = reinterpret_cast<float*>(ws + s.at_o[kOfGroups]);
+        Many<D, kFp8> x;
+        x.begin();
+        x.ready = false;
         along<kOfGroups>(reinterpret_cast<const Work*>(ws + s.at_list[kOfGroups]), uniform(totals.count[kOfGroups]), d, c.heads, block, cuts + block,
-                         [&](const Work& w, const Piece1& piece, int which) {
+                         [&](const Work& w, const Piece1& piece, int which, const Work& after, int head, bool more) {
                              const int64_t place = (2 * block + which) * (int64_t)kTile;
-                             Many<D, kFp8> x;
-                             x.run(c, a, s.R, w, piece, lds, ml + place, o + place * D);
+                             x.run(c, a, s.R, w, piece, {after, head, more}, lds, ml + place, o + place * D);
                          });
+        Many<D, kFp8>::landed();
         return;
     }
     // a workgroup's waves lie far apart on their line: few stretches are spread over all workgroups
@@ -803,7 +958,7 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
     const int part = wave * (workgroups - d.groups) + block - d.groups;
     float* o = reinterpret_cast<float*>(ws + s.at_o[kOfWaves]);
     along<kOfWaves>(reinterpret_cast<const Work*>(ws + s.at_list[kOfWaves]), uniform(totals.count[kOfWaves]), d, c.heads, part, cuts + s.workers[0] + part,
-                    [&](const Work& w, const Piece1& piece, int which) {
+                    [&](const Work& w, const Piece1& piece, int which, const Work&, int, bool) {
                         const int64_t place = (2 * part + which) * (int64_t)kFewQueries;
                         float2* ml_out = ml + 2 * (int64_t)s.workers[0] * kTile + place;
                         if (w.n * s.R <= 16) {
