@@ -4,10 +4,11 @@
 //   { j <= p : j > p - window or j < sinks },   s_j = scale q . k_j,   out = sum e^{s_j - m} v_j / l,   lse = m + ln l.
 //
 // The softmax's maximum and sum are running ones, and partial results (m, l, O) over disjoint sets of keys join exactly, so the
-// work may be cut anywhere.  Three launches:
+// work may be cut anywhere.  Three launches, two for few rows:
 //   plan     one workgroup makes the list of work: lengths and numbers of queries are device memory.  A row's queries of one key
 //            head (tokens x query heads) are cut into tiles; a tile and a key head are an item, measured in steps of tokens that
-//            any of its queries sees (pages that none sees are never touched) and a little for the item itself.
+//            any of its queries sees (pages that none sees are never touched) and a little for the item itself.  For few rows
+//            every workgroup of the next launch does that for itself.
 //   attend   Items of at most 32 queries are a wave's work: a new token's or a few drafted ones', bound by reading the keys, which go from
 //            memory straight into operand registers.  Larger ones, tiles of 128 queries of prompts, are a workgroup's: bound by
 //            the matrix instructions, the keys pass through LDS once for four waves of 32 queries.  Either kind lies on a line, cut into as
@@ -49,28 +50,32 @@ struct Totals {
 };
 // The item that a worker's stretch begins inside of, if the item's first part is the worker's before: parts worker - 1 .. last are joined.
 struct Cut {
-    int32_t work, head, last, unused;           // work: -1 where there is none
+    int32_t row, tile, offset, n, len, head, last, unused;         // row: -1 where there is none
 };
 
 struct WindowShape {
     int32_t R;                                  // query heads per key head
     int64_t most[2];                            // records of either line
-    int32_t workers[2];                         // at most
+    int32_t workgroups, workers[2];             // workers: at most
     int64_t at_list[2], at_cuts, at_ml, at_o[2], bytes;
 };
 
 static int64_t up(int64_t x) { return (x + 255) / 256 * 256; }
 
-static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t heads, int64_t D, WindowShape& s)
+// `visible`: tokens that any query can see at most, for a workspace that serves every call as many as there are.
+static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t heads, int64_t D, int64_t visible, WindowShape& s)
 {
     s.R = (int32_t)(q_heads / heads);
     if (rows * heads >= (1 << 24) || tokens * q_heads > 0x7FFFFFFF) return false;
-    const int groups = compute_units() * kPerUnit;
+    const int64_t groups = compute_units() * kPerUnit;
     const int64_t queries = tokens * s.R;
     s.most[kOfGroups] = queries > kFewQueries ? queries / kTile + rows : 0;
     s.most[kOfWaves] = rows;
-    s.workers[kOfGroups] = s.most[kOfGroups] > 0 ? groups : 0;
-    s.workers[kOfWaves] = groups * kWaves;
+    // no more workers than steps: a small call's launches are small
+    const int64_t steps = rows * heads * (visible / kStep + 3 + kCost);
+    s.workgroups = (int32_t)(s.most[kOfGroups] == 0 && steps < groups ? steps : groups);
+    s.workers[kOfGroups] = s.most[kOfGroups] > 0 ? s.workgroups : 0;
+    s.workers[kOfWaves] = s.workgroups * kWaves;
     int64_t at = up(sizeof(Totals));
     for (int k = 0; k < 2; ++k) { s.at_list[k] = at; at = up(at + s.most[k] * (int64_t)sizeof(Work)); }
     s.at_cuts = at;
@@ -88,7 +93,7 @@ static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t 
 size_t window_attention_workspace_bytes(int64_t rows, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim)
 {
     WindowShape s;
-    return window_shape(rows, tokens, q_heads, heads, dim, s) ? (size_t)s.bytes : 0;
+    return window_shape(rows, tokens, q_heads, heads, dim, (int64_t)1 << 31, s) ? (size_t)s.bytes : 0;
 }
 
 // ---------------------------------------------------------------- which tokens
@@ -102,25 +107,86 @@ struct Band {
     int steps;
     __device__ __forceinline__ int at(int k, int apart) const { return (k < first_steps ? k : k + skip) * apart; }
 };
+// (positions, queries of a row and steps of tokens stay below 2^31)
 __device__ __forceinline__ Band band_of(int R, int tile, int n, int len, int window, int sinks, int apart)
 {
-    const int64_t queries = (int64_t)n * R;
-    const int64_t q0 = (int64_t)tile * kTile, q1 = queries <= kFewQueries || q0 + kTile > queries ? queries : q0 + kTile;
+    const int shift = apart == kStep ? 5 : 6;
+    const uint32_t queries = (uint32_t)n * (uint32_t)R;
+    const uint32_t q0 = (uint32_t)tile * kTile, q1 = queries <= kFewQueries || q0 + kTile > queries ? queries : q0 + kTile;
     Band b;
-    b.p0 = len - n + (int)(q0 / R);
-    b.p1 = len - n + (int)((q1 - 1) / R);
+    b.p0 = len - n + (int)(q0 / (uint32_t)R);
+    b.p1 = len - n + (int)((q1 - 1) / (uint32_t)R);
     const int hi = b.p1 + 1;                                                   // none sees a token from here on
     if (hi <= 0) { b.first_steps = b.skip = b.steps = 0; return b; }
     const int lo = (b.p0 < 0 ? 0 : b.p0) >= window ? b.p0 - window + 1 : 0;    // none sees one before it, but the first ones
-    const int lo_step = lo / apart, kept = sinks < hi ? sinks : hi;
-    const int kept_steps = (int)(((int64_t)kept + apart - 1) / apart);
+    const int lo_step = lo >> shift, kept = sinks < hi ? sinks : hi;
+    const int kept_steps = (kept + apart - 1) >> shift;
     b.first_steps = kept_steps < lo_step ? kept_steps : lo_step;
     b.skip = lo_step - b.first_steps;
-    b.steps = (int)(((int64_t)hi + apart - 1) / apart) - b.skip;
+    b.steps = ((hi + apart - 1) >> shift) - b.skip;
     return b;
 }
 
 // ---------------------------------------------------------------- plan
+// Places for tiles: a row's lie from place_of_row(row) on, as many as it can have.
+__device__ __forceinline__ int64_t place_of_row(int offset, int R, int row) { return (int64_t)offset * R / kTile + row; }
+
+// f(line, record) for every tile among places [begin, end); offset(row), len(row): the row's first query and tokens.
+template <typename Offset, typename Len, typename F>
+__device__ __forceinline__ void tiles_in(const WindowArgs& a, int R, int64_t begin, int64_t end, Offset offset, Len len_of, F f)
+{
+    if (begin >= end) return;
+    int low = 0, high = a.rows;                                                // the last row whose places begin at or before `begin`
+    while (high - low > 1) {
+        const int mid = (low + high) / 2;
+        if (place_of_row(offset(mid), R, mid) <= begin) low = mid;
+        else high = mid;
+    }
+    for (int r = low; r < a.rows; ++r) {
+        const int off = offset(r), n = offset(r + 1) - off;
+        const int64_t k = place_of_row(off, R, r);
+        if (k >= end) break;
+        if (n <= 0) continue;
+        const int64_t queries = (int64_t)n * R;
+        const int line = queries <= kFewQueries ? kOfWaves : kOfGroups;
+        const int64_t last = k + tiles_of(queries);
+        const int len = len_of(r);
+        for (int64_t u = k > begin ? k : begin; u < last && u < end; ++u) {
+            Work w;
+            w.first = 0; w.row = r; w.tile = (int)(u - k); w.offset = off; w.n = n; w.len = len;
+            w.cost = kCost + band_of(R, w.tile, n, len, a.window, a.sinks, line == kOfWaves ? kStep : kBlock).steps;
+            f(line, w);
+        }
+    }
+}
+
+// Sums over the threads before this one, and over all: steps of both lines; tiles, the waves' in the upper half.
+template <int kOf>
+__device__ __forceinline__ void scan(const int64_t own[3], int64_t before[3], int64_t all[3], int64_t (*lds)[3])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        before[k] = own[k];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t y = __shfl_up(before[k], d);
+            if (lane >= d) before[k] += y;
+        }
+        if (lane == 63) lds[wave][k] = before[k];
+        before[k] -= own[k];
+        all[k] = 0;
+    }
+    __syncthreads();
+    for (int i = 0; i < kOf; ++i)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            if (i < wave) before[k] += lds[i][k];
+            all[k] += lds[i][k];
+        }
+}
+
+// The plan of a large batch, a launch of one workgroup.
 constexpr int kPlanWaves = 16, kPlanLanes = 64 * kPlanWaves, kPlanRows = 8192;
 
 __global__ __launch_bounds__(kPlanLanes)
@@ -128,75 +194,30 @@ void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, c
 {
     __shared__ int offsets_lds[kPlanRows + 1];
     __shared__ int64_t sums[kPlanWaves][3];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const bool in_lds = a.rows <= kPlanRows;
     if (in_lds) {
         for (int i = threadIdx.x; i <= a.rows; i += kPlanLanes) offsets_lds[i] = clamp_len(a.offsets[i], a.tokens);
         __syncthreads();
     }
     auto offset = [&](int r) { return in_lds ? offsets_lds[r] : clamp_len(a.offsets[r], a.tokens); };
-    // Places for tiles: a row's lie from key(row) on, as many as it can have.
-    auto key = [&](int r) { return (int64_t)offset(r) * s.R / kTile + r; };
+    const int64_t visible = table_tokens(a.row_width, page_size);
+    auto len = [&](int r) { return clamp_len(a.row_lens[r], visible); };
     const int64_t places = (int64_t)a.tokens * s.R / kTile + a.rows;
     const int64_t share = (places + kPlanLanes - 1) / kPlanLanes;
     const int64_t begin = threadIdx.x * share, end = begin + share < places ? begin + share : places;
-    const int64_t visible = table_tokens(a.row_width, page_size);
-    // f(line, record) for every tile among the thread's places
-    auto each = [&](auto f) {
-        if (begin >= end) return;
-        int low = 0, high = a.rows;                                            // the last row whose places begin at or before `begin`
-        while (high - low > 1) {
-            const int mid = (low + high) / 2;
-            if (key(mid) <= begin) low = mid;
-            else high = mid;
-        }
-        for (int r = low; r < a.rows && key(r) < end; ++r) {
-            const int off = offset(r), n = offset(r + 1) - off;
-            if (n <= 0) continue;
-            const int64_t k = key(r), queries = (int64_t)n * s.R;
-            const int line = queries <= kFewQueries ? kOfWaves : kOfGroups;
-            const int64_t last = k + tiles_of(queries);
-            const int len = clamp_len(a.row_lens[r], visible);
-            for (int64_t u = k > begin ? k : begin; u < last && u < end; ++u) {
-                Work w;
-                w.first = 0; w.row = r; w.tile = (int)(u - k); w.offset = off; w.n = n; w.len = len;
-                w.cost = kCost + band_of(s.R, w.tile, n, len, a.window, a.sinks, line == kOfWaves ? kStep : kBlock).steps;
-                f(line, w);
-            }
-        }
-    };
-    int64_t own[3] = {0, 0, 0};                                                // steps of both lines; tiles, the waves' in the upper half
-    each([&](int line, const Work& w) {
+    int64_t own[3] = {0, 0, 0}, before[3], all[3];
+    tiles_in(a, s.R, begin, end, offset, len, [&](int line, const Work& w) {
         own[0] += line == 0 ? (int64_t)w.cost * heads : 0;
         own[1] += line == 1 ? (int64_t)w.cost * heads : 0;
         own[2] += line == 1 ? 1ll << 32 : 1;
     });
-    int64_t sum[3], all[3] = {0, 0, 0};
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        sum[k] = own[k];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t y = __shfl_up(sum[k], d);
-            if (lane >= d) sum[k] += y;
-        }
-        if (lane == 63) sums[wave][k] = sum[k];
-        sum[k] -= own[k];
-    }
-    __syncthreads();
-    for (int i = 0; i < kPlanWaves; ++i)
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            if (i < wave) sum[k] += sums[i][k];
-            all[k] += sums[i][k];
-        }
-    int64_t at[2] = {sum[0], sum[1]};
-    int64_t index[2] = {sum[2] & 0xFFFFFFFF, sum[2] >> 32};
-    each([&](int line, Work w) {
-        w.first = line == 0 ? at[0] : at[1];
+    scan<kPlanWaves>(own, before, all, sums);
+    int64_t index[2] = {before[2] & 0xFFFFFFFF, before[2] >> 32};
+    tiles_in(a, s.R, begin, end, offset, len, [&](int line, Work w) {
+        w.first = line == 0 ? before[0] : before[1];
         const int64_t i = line == 0 ? index[0]++ : index[1]++;
-        if (line == 0) at[0] += (int64_t)w.cost * heads;
-        else at[1] += (int64_t)w.cost * heads;
+        if (line == 0) before[0] += (int64_t)w.cost * heads;
+        else before[1] += (int64_t)w.cost * heads;
         if (i < s.most[line]) reinterpret_cast<Work*>(ws + s.at_list[line])[i] = w;
     });
     if (threadIdx.x == 0) {
@@ -205,11 +226,86 @@ void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, c
         const bool fits = (all[2] & 0xFFFFFFFF) <= s.most[0] && (all[2] >> 32) <= s.most[1];
         t.steps[0] = fits ? all[0] : 0;
         t.steps[1] = fits ? all[1] : 0;
-        t.count[0] = (int)(all[2] & 0xFFFFFFFF);
-        t.count[1] = (int)(all[2] >> 32);
+        t.count[0] = fits ? (int)(all[2] & 0xFFFFFFFF) : 0;
+        t.count[1] = fits ? (int)(all[2] >> 32) : 0;
         *reinterpret_cast<Totals*>(ws) = t;
     }
 }
+
+// A batch of few rows and tiles is planned by every workgroup of the attend launch for itself, in LDS: a launch less.  (One row 20.1
+// us with a launch for the plan.)
+constexpr int kOwnPlaces = 640;                 // what fits beside the keys of two workgroups
+struct OwnPlan {
+    int offsets[kOwnPlaces + 1], lens[kOwnPlaces];
+    int64_t first[kOwnPlaces];                  // the line of workgroups, then the line of waves
+    uint32_t row_tile[kOwnPlaces];
+    int64_t sums[kWaves][3];
+};
+__device__ __forceinline__ Totals plan_own(const WindowArgs& a, const WindowShape& s, int heads, int page_size, OwnPlan& p)
+{
+    constexpr int kThreads = 64 * kWaves;
+    const int64_t visible = table_tokens(a.row_width, page_size);
+    for (int i = threadIdx.x; i <= a.rows; i += kThreads) {
+        p.offsets[i] = clamp_len(a.offsets[i], a.tokens);
+        if (i < a.rows) p.lens[i] = clamp_len(a.row_lens[i], visible);
+    }
+    __syncthreads();
+    auto offset = [&](int r) { return p.offsets[r]; };
+    auto len = [&](int r) { return p.lens[r]; };
+    const int places = (int)((int64_t)a.tokens * s.R / kTile) + a.rows;
+    const int share = (places + kThreads - 1) / kThreads;
+    const int begin = (int)threadIdx.x * share, end = begin + share < places ? begin + share : places;
+    int64_t own[3] = {0, 0, 0}, before[3], all[3];
+    tiles_in(a, s.R, begin, end, offset, len, [&](int line, const Work& w) {
+        own[0] += line == 0 ? (int64_t)w.cost * heads : 0;
+        own[1] += line == 1 ? (int64_t)w.cost * heads : 0;
+        own[2] += line == 1 ? 1ll << 32 : 1;
+    });
+    scan<kWaves>(own, before, all, p.sums);
+    Totals t;
+    const int64_t count[2] = {all[2] & 0xFFFFFFFF, all[2] >> 32};
+    const bool fits = count[0] + count[1] <= kOwnPlaces;
+    t.steps[0] = fits ? all[0] : 0;
+    t.steps[1] = fits ? all[1] : 0;
+    t.count[0] = fits ? (int)count[0] : 0;
+    t.count[1] = fits ? (int)count[1] : 0;
+    if (fits) {
+        int index[2] = {(int)(before[2] & 0xFFFFFFFF), (int)(count[0] + (before[2] >> 32))};
+        tiles_in(a, s.R, begin, end, offset, len, [&](int line, const Work& w) {
+            const int i = line == 0 ? index[0]++ : index[1]++;
+            p.first[i] = line == 0 ? before[0] : before[1];
+            p.row_tile[i] = (uint32_t)w.row << 16 | (uint32_t)w.tile;
+            if (line == 0) before[0] += (int64_t)w.cost * heads;
+            else before[1] += (int64_t)w.cost * heads;
+        });
+    }
+    __syncthreads();
+    return t;
+}
+
+// A line's records, in the workspace or in LDS.
+struct InWorkspace {
+    const Work* list;
+    __device__ __forceinline__ int64_t first(int i) const { return list[i].first; }
+    __device__ __forceinline__ Work get(int i) const { return list[i]; }
+};
+template <int kLine>
+struct InLds {
+    const OwnPlan& p;
+    const WindowArgs& a;
+    int R, from;
+    __device__ __forceinline__ int64_t first(int i) const { return p.first[from + i]; }
+    __device__ __forceinline__ Work get(int i) const
+    {
+        Work w;
+        w.first = p.first[from + i];
+        const uint32_t x = p.row_tile[from + i];
+        w.row = (int)(x >> 16); w.tile = (int)(x & 0xFFFFu);
+        w.offset = p.offsets[w.row]; w.n = p.offsets[w.row + 1] - w.offset; w.len = p.lens[w.row];
+        w.cost = kCost + band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kLine == kOfWaves ? kStep : kBlock).steps;
+        return w;
+    }
+};
 
 // How the workgroups and stretches are divided, the same in every launch that asks.
 struct Division {
@@ -238,13 +334,14 @@ __device__ __forceinline__ Division divide_work(const Totals& t, int workgroups)
 }
 
 // The last record that begins at or before a step: every lane looks at a 64th of what is left.
-__device__ __forceinline__ int find_work(const Work* list, int count, int64_t step)
+template <typename List>
+__device__ __forceinline__ int find_work(const List& list, int count, int64_t step)
 {
     const int lane = threadIdx.x & 63;
     int first = 0, left = count;
     while (left > 1) {
         const int apart = (left + 63) / 64, at = lane * apart;
-        const int n = (int)__popcll(__ballot(at < left && list[first + (at < left ? at : 0)].first <= step));
+        const int n = (int)__popcll(__ballot(at < left && list.first(first + (at < left ? at : 0)) <= step));
         const int k = n > 0 ? n - 1 : 0;
         first += k * apart;
         left = left - k * apart < apart ? left - k * apart : apart;
@@ -475,6 +572,7 @@ struct Many {
     static constexpr int kImage = kKeys + kValues;                             // two of them, within the 64 KB that a load into LDS reaches,
     static constexpr int kFactors = 2 * kBlock * 4, kExtra = kFactors + 16;    // then twice factors and four flags
     static constexpr int kLds = 2 * (kImage + kExtra);
+    static_assert(kLds % 16 == 0, "what lies behind it is aligned");
     static constexpr int kElem = kFp8 ? 1 : 2;
     static constexpr int kRow = D * kElem / 16;                                // pieces of a row in the cache
     static constexpr int kLoads = kBlock * kRow / 256;                         // of 16 bytes, a thread's, of K and of V
@@ -890,16 +988,20 @@ struct Many {
 
 // The stretch of worker `part`: f(record, piece, which of the worker's two places, record and head of what lies behind the piece in the stretch,
 // whether that is an item's first steps).
-template <int kLine, typename F>
-__device__ __forceinline__ void along(const Work* list, int count, const Division& d, int heads, int part, Cut* cut, F f)
+template <int kLine, typename List, typename F>
+__device__ __forceinline__ void along(const List& list, int count, const Division& d, int heads, int part, Cut* cut, F f)
 {
-    if (part >= d.parts[kLine]) return;
+    const bool writes = (threadIdx.x & (kLine == kOfGroups ? 255 : 63)) == 0;
+    Cut found{-1, 0, 0, 0, 0, 0, 0, 0};
+    if (part >= d.parts[kLine]) {
+        if (writes) *cut = found;
+        return;
+    }
     int64_t at = begin_of(part, d.steps[kLine], d.parts[kLine]);
     const int64_t end = begin_of(part + 1, d.steps[kLine], d.parts[kLine]);
     int i = find_work(list, count, at);
-    Cut found{-1, 0, 0, 0};
     const int64_t begin = at;
-    Work w = uniform(list[i]);
+    Work w = uniform(list.get(i));
     while (at < end && i < count) {
         const int64_t offset = at - w.first;
         const int head = (int)divide(offset, w.cost), from = (int)(offset - (int64_t)head * w.cost);
@@ -914,38 +1016,51 @@ __device__ __forceinline__ void along(const Work* list, int count, const Divisio
             // the item began before: was its first step the worker's before?
             const int64_t item = at - from;
             if (begin_of(part - 1, d.steps[kLine], d.parts[kLine]) <= item + kCost)
-                found = Cut{i, head, part_of(item + w.cost - 1, d.steps[kLine], d.parts[kLine]), 0};
+                found = Cut{w.row, w.tile, w.offset, w.n, w.len, head, part_of(item + w.cost - 1, d.steps[kLine], d.parts[kLine]), 0};
         }
         // what follows: the same tile's next head, or the next tile
         const bool done = head + 1 == heads && from + n == w.cost;
         Work after = w;
-        if (done && i + 1 < count) after = uniform(list[i + 1]);
+        if (done && i + 1 < count) after = uniform(list.get(i + 1));
         const bool more = at + n < end && from + n == w.cost && (!done || i + 1 < count) && after.cost > kCost && end - (at + n) > kCost;
         if (piece.to > piece.from || (w.cost == kCost && piece.whole)) f(w, piece, from <= kCost ? 1 : 0, after, done ? 0 : head + 1, more);
         at += n;
         if (done) { ++i; w = after; }
     }
-    if ((threadIdx.x & (kLine == kOfGroups ? 255 : 63)) == 0) *cut = found;
+    if (writes) *cut = found;
 }
 
-template <int D, bool kFp8>
+template <int D, bool kFp8, bool kOwn>
 __global__ __launch_bounds__(64 * kWaves, kPerUnit)
 void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
 {
-    __shared__ __align__(16) char lds[Many<D, kFp8>::kLds];
-    const Totals totals = *reinterpret_cast<const Totals*>(ws);
+    // (one array: the blocks are within the 64 KB that a load into LDS reaches)
+    __shared__ __align__(16) char lds[Many<D, kFp8>::kLds + (kOwn ? sizeof(OwnPlan) : 0)];
+    OwnPlan& own = *reinterpret_cast<OwnPlan*>(lds + Many<D, kFp8>::kLds);
+    Totals totals;
+    if constexpr (kOwn) totals = plan_own(a, s, c.heads, c.page_size, own);
+    else totals = *reinterpret_cast<const Totals*>(ws);
     const int workgroups = (int)gridDim.x;
     const Division d = divide_work(totals, workgroups);
+    auto list = [&](auto line) {
+        if constexpr (kOwn) return InLds<decltype(line)::value>{own, a, s.R, decltype(line)::value == kOfGroups ? 0 : uniform(totals.count[kOfGroups])};
+        else return InWorkspace{reinterpret_cast<const Work*>(ws + s.at_list[decltype(line)::value])};
+    };
     Cut* cuts = reinterpret_cast<Cut*>(ws + s.at_cuts);
+    Cut* wave_cuts = cuts + s.workers[kOfGroups];
     float2* ml = reinterpret_cast<float2*>(ws + s.at_ml);
     // Workgroups of one die (dealt in turn to eight) lie next to each other on the line: they read the same keys.
     const int block = (workgroups & 7) == 0 ? (int)(blockIdx.x & 7) * (workgroups >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
+    const int wave = uniform((int)threadIdx.x >> 6);
+    const Cut none{-1, 0, 0, 0, 0, 0, 0, 0};
     if (block < d.groups) {
+        // (the join looks at every worker's cut: waves of these workgroups are no workers of the other line)
+        if ((threadIdx.x & 63) == 0) wave_cuts[(workgroups - d.groups) * kWaves + block * kWaves + wave] = none;
         float* o = reinterpret_cast<float*>(ws + s.at_o[kOfGroups]);
         Many<D, kFp8> x;
         x.begin();
         x.ready = false;
-        along<kOfGroups>(reinterpret_cast<const Work*>(ws + s.at_list[kOfGroups]), uniform(totals.count[kOfGroups]), d, c.heads, block, cuts + block,
+        along<kOfGroups>(list(std::integral_constant<int, kOfGroups>{}), uniform(totals.count[kOfGroups]), d, c.heads, block, cuts + block,
                          [&](const Work& w, const Piece1& piece, int which, const Work& after, int head, bool more) {
                              const int64_t place = (2 * block + which) * (int64_t)kTile;
                              x.run(c, a, s.R, w, piece, {after, head, more}, lds, ml + place, o + place * D);
@@ -953,11 +1068,11 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
         Many<D, kFp8>::landed();
         return;
     }
+    if (s.workers[kOfGroups] > 0 && threadIdx.x == 0) cuts[block] = none;
     // a workgroup's waves lie far apart on their line: few stretches are spread over all workgroups
-    const int wave = uniform((int)threadIdx.x >> 6);
     const int part = wave * (workgroups - d.groups) + block - d.groups;
     float* o = reinterpret_cast<float*>(ws + s.at_o[kOfWaves]);
-    along<kOfWaves>(reinterpret_cast<const Work*>(ws + s.at_list[kOfWaves]), uniform(totals.count[kOfWaves]), d, c.heads, part, cuts + s.workers[0] + part,
+    along<kOfWaves>(list(std::integral_constant<int, kOfWaves>{}), uniform(totals.count[kOfWaves]), d, c.heads, part, wave_cuts + part,
                     [&](const Work& w, const Piece1& piece, int which, const Work&, int, bool) {
                         const int64_t place = (2 * part + which) * (int64_t)kFewQueries;
                         float2* ml_out = ml + 2 * (int64_t)s.workers[0] * kTile + place;
@@ -976,21 +1091,18 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
 // fewer queries than lots of lanes have their parts spread over several.
 template <int D>
 __global__ __launch_bounds__(256, 8)
-void window_join_kernel(WindowArgs a, WindowShape s, int heads, int workgroups, int group_slices, int wave_slices, const char* ws)
+void window_join_kernel(WindowArgs a, WindowShape s, int group_slices, int wave_slices, const char* ws)
 {
     constexpr int kLanes4 = D / 4, kSubs = 256 / kLanes4;
     __shared__ float lds[kSubs][2 + D];
-    const Totals totals = *reinterpret_cast<const Totals*>(ws);
-    const Division d = divide_work(totals, workgroups);
     const int of_groups = s.workers[kOfGroups] * group_slices;
     const bool groups = (int)blockIdx.x < of_groups;
     const int slices = groups ? group_slices : wave_slices;
     const int block = groups ? (int)blockIdx.x : (int)blockIdx.x - of_groups;
     const int part = block / slices, slice = block % slices;
-    if (part >= (groups ? d.parts[kOfGroups] : d.parts[kOfWaves])) return;
     const Cut cut = reinterpret_cast<const Cut*>(ws + s.at_cuts)[(groups ? 0 : s.workers[kOfGroups]) + part];
-    if (cut.work < 0) return;
-    const Work w = reinterpret_cast<const Work*>(ws + s.at_list[groups ? kOfGroups : kOfWaves])[cut.work];
+    if (cut.row < 0) return;
+    const Work w{0, cut.row, cut.tile, cut.offset, cut.n, cut.len, 0};
     const int places = groups ? kTile : kFewQueries, each = places / slices;
     const int64_t base = groups ? (int64_t)w.tile * kTile : 0, queries = (int64_t)w.n * s.R - base;
     const int first = slice * each, end = queries < first + each ? (int)queries : first + each;
@@ -1059,23 +1171,29 @@ void window_join_kernel(WindowArgs a, WindowShape s, int heads, int workgroups, 
 template <int D, bool kFp8>
 static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const WindowShape& s, char* ws, hipStream_t stream)
 {
-    window_plan_kernel<<<1, kPlanLanes, 0, stream>>>(a, s, c.heads, c.page_size, ws);
-    hipError_t err = hipGetLastError();
+    if ((int64_t)a.tokens * s.R / kTile + a.rows <= kOwnPlaces) {
+        window_kernel<D, kFp8, true><<<s.workgroups, 64 * kWaves, 0, stream>>>(c, a, s, ws);
+    } else {
+        window_plan_kernel<<<1, kPlanLanes, 0, stream>>>(a, s, c.heads, c.page_size, ws);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+        window_kernel<D, kFp8, false><<<s.workgroups, 64 * kWaves, 0, stream>>>(c, a, s, ws);
+    }
+    const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    const int workgroups = compute_units() * kPerUnit;
-    window_kernel<D, kFp8><<<workgroups, 64 * kWaves, 0, stream>>>(c, a, s, ws);
-    err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    const int group_slices = 16, wave_slices = 4;
+    // Queries of one workgroup of the join: 32 of a tile's; of a wave's item all, fewer where there are few workers, whose items have
+    // many parts.
+    const int group_slices = kTile / 32, wave_slices = s.workgroups * kPerUnit < compute_units() ? 8 : s.workgroups < compute_units() * kPerUnit ? 4 : 1;
     const int blocks = s.workers[kOfGroups] * group_slices + s.workers[kOfWaves] * wave_slices;
-    window_join_kernel<D><<<blocks, 256, 0, stream>>>(a, s, c.heads, workgroups, group_slices, wave_slices, ws);
+    window_join_kernel<D><<<blocks, 256, 0, stream>>>(a, s, group_slices, wave_slices, ws);
     return hipGetLastError();
 }
 
 hipError_t launch_window_attention(const CacheView& c, const WindowArgs& a, void* workspace, hipStream_t stream)
 {
     WindowShape s;
-    if (!window_shape(a.rows, a.tokens, a.q_heads, c.heads, c.dim, s)) return hipErrorInvalidValue;
+    const int64_t table = (int64_t)a.row_width * c.page_size, band = (int64_t)a.window + a.sinks + a.tokens;
+    if (!window_shape(a.rows, a.tokens, a.q_heads, c.heads, c.dim, table < band ? table : band, s)) return hipErrorInvalidValue;
     char* ws = static_cast<char*>(workspace);
     if (c.dim == 128) return c.fp8 ? launch_window<128, true>(c, a, s, ws, stream) : launch_window<128, false>(c, a, s, ws, stream);
     return c.fp8 ? launch_window<64, true>(c, a, s, ws, stream) : launch_window<64, false>(c, a, s, ws, stream);
