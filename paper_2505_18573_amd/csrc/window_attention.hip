@@ -611,14 +611,13 @@ struct Many {
     {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int64_t row = uniform(page_row(c, head, page[half], at + 32 * half));
+            const int64_t row = page_row(c, head, uniform(page[half]), at + 32 * half);        // scalar arithmetic; the same in both tensors
             keys_at[half] = static_cast<const char*>(c.k) + row * (D * kElem);
             values_at[half] = static_cast<const char*>(c.v) + row * (D * kElem);
-            if (kFp8 && half == 0) {
+            if (kFp8) {
                 const int token = threadIdx.x & 63;
-                scales_row = row + (token & 31);
-            } else if (kFp8) {
-                scales_row = (threadIdx.x & 63) < 32 ? scales_row : row + (threadIdx.x & 31);
+                if (half == 0) scales_row = row + (token & 31);
+                else scales_row = token < 32 ? scales_row : row + (token & 31);
             }
         }
     }
@@ -1181,9 +1180,9 @@ static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const W
     }
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    // Queries of one workgroup of the join: 32 of a tile's; of a wave's item all, fewer where there are few workers, whose items have
+    // Queries of one workgroup of the join: 16 of a tile's; of a wave's item all, fewer where there are few workers, whose items have
     // many parts.
-    const int group_slices = kTile / 32, wave_slices = s.workgroups * kPerUnit < compute_units() ? 8 : s.workgroups < compute_units() * kPerUnit ? 4 : 1;
+    const int group_slices = kTile / 16, wave_slices = s.workgroups * kPerUnit < compute_units() ? 8 : s.workgroups < compute_units() * kPerUnit ? 4 : 1;
     const int blocks = s.workers[kOfGroups] * group_slices + s.workers[kOfWaves] * wave_slices;
     window_join_kernel<D><<<blocks, 256, 0, stream>>>(a, s, group_slices, wave_slices, ws);
     return hipGetLastError();
