@@ -120,11 +120,27 @@ void beam_stream_kernel(BeamArgs a, BeamShape s, float c, char* ws)
     }
     const float up = wave_max(ref);
     const double all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f((ref - up) * c));
+    // The chunks' maxima over the wave: halves trade two chunks each and keep one, rows of sixteen lanes again; what is left is a row's.
     float* tops = reinterpret_cast<float*>(ws) + row * s.chunks + segment * kChunks;
+    float in_half[kChunks / 2], in_row[kChunks / 4];
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const float m = wave_max(top[i]);
-        if (lane == i && segment * kChunks + i < s.chunks) tops[i] = m;
+    for (int i = 0; i < kChunks / 2; ++i) {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[i]), __float_as_uint(top[i + kChunks / 2]), false, false);
+        in_half[i] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));      // lower half: chunk i, upper: i + kChunks / 2
+    }
+#pragma unroll
+    for (int i = 0; i < kChunks / 4; ++i) {
+        const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(in_half[i]), __float_as_uint(in_half[i + kChunks / 4]), false, false);
+        float m = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));         // row r: chunk i + (r & 1) kChunks / 4 + (r >> 1) kChunks / 2
+        m = fmaxf(m, dpp_f<kDppXor1>(m, m));
+        m = fmaxf(m, dpp_f<kDppXor2>(m, m));
+        m = fmaxf(m, dpp_f<kDppHalfMirror>(m, m));
+        in_row[i] = fmaxf(m, dpp_f<kDppMirror>(m, m));
+    }
+#pragma unroll
+    for (int i = 0; i < kChunks / 4; ++i) {
+        const int chunk = i + ((lane >> 4) & 1) * (kChunks / 4) + (lane >> 5) * (kChunks / 2);
+        if ((lane & 15) == i && segment * kChunks + chunk < s.chunks) tops[chunk] = in_row[i];
     }
     if (lane == 0) reinterpret_cast<Partial*>(ws + s.at_partials)[row * s.segments + segment] = Partial{up, 0.0f, all};
 }
@@ -181,19 +197,38 @@ __device__ __forceinline__ float logit_at(const char* row, int64_t col)
     return kBf16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[col] << 16) : reinterpret_cast<const float*>(row)[col];
 }
 
+// Whether a comes before b.
+__device__ __forceinline__ bool before(const Entry& a, const Entry& b) { return a.key > b.key || (a.key == b.key && a.index < b.index); }
+
+constexpr int kGroups = kSelectThreads / 8;     // of eight lanes, whose maxima bound what is kept
+constexpr int kRoom = 256;                      // chunks above the bound
+constexpr int kElements = kMaxKeep * (kMaxKeep + 1) / 2;          // of the r-th best chunk at most keep - r elements
 struct SelectLds {
     double base[kMaxBeams];                     // s_b - ln sum exp, -inf: the beam offers nothing
     double log2_sum[kMaxBeams];
     double sums[kSelectWaves];
     int ends[kMaxBeams];                        // a finished beam
-    Entry of_wave[kSelectWaves + 1][kMaxKeep + 2];
-    Entry chunk[kMaxKeep + 2];
-    double key[kMaxKeep * (kMaxKeep + 1) / 2];  // of chunk r at most keep - r elements
-    int column[kMaxKeep * (kMaxKeep + 1) / 2];
-    int count[kMaxKeep];
-    int chunks_found;
+    alignas(16) float group[kGroups];
+    float bound;
+    int found, elements, chunks_found;
     uint32_t near;                              // beams whose sums decide
+    Entry chunk[kMaxKeep + 2];                  // the best ones, in order
+    Entry some[kRoom + kMaxKeep + 2];           // chunks above the bound
+    Entry element[kElements];
+    Entry best[kMaxKeep + 2];
+    Entry of_wave[kSelectWaves + 1][kMaxKeep + 2];
 };
+
+// to[r] = the r-th of n entries in order, r < most, by counting how many come before each.
+__device__ __forceinline__ void in_order(const Entry* from, int n, Entry* to, int most)
+{
+    for (int i = threadIdx.x; i < n; i += kSelectThreads) {
+        const Entry mine = from[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += before(from[j], mine) ? 1 : 0;
+        if (rank < most) to[rank] = mine;
+    }
+}
 
 template <bool kBf16>
 __global__ __launch_bounds__(kSelectThreads)
@@ -204,7 +239,15 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
     const int64_t seq = blockIdx.x, row0 = seq * a.beams;
     const float* tops = reinterpret_cast<const float*>(ws) + row0 * s.chunks;
     const double per_logit = 1.0 / (double)a.tau, c = kLog2e * per_logit;
-    const int keep = a.keep, most = (int)s.chunks;
+    const int keep = a.keep, need = keep + 1, most = (int)s.chunks;
+    constexpr int kEach = 8;
+    const int entries = a.beams * most;
+    float z[kEach];                                                            // asked for before the sums are
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int e = i * kSelectThreads + (int)threadIdx.x;
+        z[i] = e < entries ? tops[e] : 0.0f;
+    }
 
     for (int b = wave; b < a.beams; b += kSelectWaves) {
         const float score = a.scores[row0 + b];
@@ -232,9 +275,7 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
     __syncthreads();
 
     for (int round = 0; round < 2; ++round) {
-        // the best keep + 1 chunks
-        constexpr int kEach = 8;
-        const int entries = a.beams * most;
+        // ---- the best keep + 1 chunks: thread t's are entries t, t + 1024, ... of eight times as many at a time
         int known = 0;                                                         // in lds.chunk
         for (int from = 0; from < entries; from += kEach * kSelectThreads) {
             double key[kEach];
@@ -244,19 +285,57 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
                 const int e = from + i * kSelectThreads + (int)threadIdx.x;
                 key[i] = kNone;
                 if (e < entries) {
+                    if (from > 0 || round > 0) z[i] = tops[e];
                     const int b = e / most;
                     const double base = lds.base[b];
                     if (base > kNone) {
                         if (lds.ends[b]) {
                             if (e - b * most == a.eos / kChunkCols) key[i] = base;
-                        } else {
-                            const float z = tops[e];
-                            if (z > kNoLogit) key[i] = base + (double)z * per_logit;
+                        } else if (z[i] > kNoLogit) {
+                            key[i] = base + (double)z[i] * per_logit;
                         }
                     }
                 }
                 if (key[i] > mine.key) mine = Entry{key[i], e};
             }
+            // A bound that at least `need` of them reach if so many are there: the need-th of the maxima of eight lanes.  (Rounding to fp32
+            // keeps the order.)
+            float g = (float)mine.key;
+            g = fmaxf(g, dpp_f<kDppXor1>(g, g));
+            g = fmaxf(g, dpp_f<kDppXor2>(g, g));
+            g = fmaxf(g, dpp_f<kDppHalfMirror>(g, g));
+            if ((lane & 7) == 0) lds.group[threadIdx.x >> 3] = g;
+            if (threadIdx.x == 0) { lds.bound = -INFINITY; lds.found = known; }
+            if (wave == 0)
+                for (int i = lane; i < known; i += 64) lds.some[i] = lds.chunk[i];
+            __syncthreads();
+            if (threadIdx.x < kGroups) {
+                const float x = lds.group[threadIdx.x];
+                int above = 0, equal = 0;
+                for (int j = 0; j < kGroups; j += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(&lds.group[j]);
+                    above += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
+                    equal += (y.x == x) + (y.y == x) + (y.z == x) + (y.w == x);
+                }
+                if (above < need && above + equal >= need) lds.bound = x;       // equal ones store the same
+            }
+            __syncthreads();
+            const float bound = lds.bound;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (key[i] > kNone && (float)key[i] >= bound) {
+                    const int at = atomicAdd(&lds.found, 1);
+                    if (at < kRoom + known) lds.some[at] = Entry{key[i], from + i * kSelectThreads + (int)threadIdx.x};
+                }
+            __syncthreads();
+            const int found = lds.found;
+            if (found <= kRoom + known) {                                      // in any order there, in order afterwards
+                in_order(lds.some, found, lds.chunk, need);
+                known = found < need ? found : need;
+                __syncthreads();
+                continue;
+            }
+            // Hundreds of equal ones: one after the other, a list for each wave, then the lists.
             int n = 0;
             for (; n <= keep; ++n) {
                 const int l = first_of(mine);
@@ -277,7 +356,7 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
             if (wave == 0)
                 for (int i = lane; i <= known; i += 64) lds.of_wave[kSelectWaves][i] = i < known ? lds.chunk[i] : Entry{kNone, 0};
             __syncthreads();
-            if (wave == 0) {                                                   // the waves' lists and what is known, in order
+            if (wave == 0) {
                 int at = 0, out = 0;
                 Entry head = lane <= kSelectWaves ? lds.of_wave[lane][0] : Entry{kNone, 0};
                 for (; out <= keep; ++out) {
@@ -293,82 +372,99 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
             __syncthreads();
             known = lds.chunks_found;
         }
-        // their elements
+        // ---- their elements
         const int chunks = known < keep ? known : keep;
         const double border = chunks == keep ? lds.chunk[keep - 1].key : kNone;      // `keep` candidates reach it
+        if (threadIdx.x == 0) lds.elements = 0;
+        __syncthreads();
         for (int r = wave; r < chunks; r += kSelectWaves) {
             const Entry of = lds.chunk[r];
-            const int b = of.index / most, chunk = of.index % most;
-            const int at = r * keep - r * (r - 1) / 2, room = keep - r;
-            int n = 0;
+            const int b = of.index / most, chunk = of.index % most, room = keep - r;
             if (lds.ends[b]) {
-                if (lane == 0) { lds.key[at] = of.key; lds.column[at] = a.eos; }
-                n = 1;
+                if (lane == 0) lds.element[atomicAdd(&lds.elements, 1)] = Entry{of.key, b * (int)a.V + a.eos};
+                continue;
+            }
+            const char* row = row_of(a, row0 + b, kBf16 ? 2 : 4);
+            const int64_t first = (int64_t)chunk * kChunkCols + lane * 8;
+            const double base = lds.base[b];
+            float x[8];
+            if (first + 8 <= a.V) {
+                const u32x4* p = reinterpret_cast<const u32x4*>(row + first * (kBf16 ? 2 : 4));
+                const u32x4 w0 = p[0], w1 = kBf16 ? w0 : p[1];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] = kBf16 ? __uint_as_float((j & 1) ? w0[j >> 1] & 0xFFFF0000u : w0[j >> 1] << 16) : __uint_as_float(j < 4 ? w0[j & 3] : w1[j & 3]);
             } else {
-                const char* row = row_of(a, row0 + b, kBf16 ? 2 : 4);
-                const int64_t first = (int64_t)chunk * kChunkCols + lane * 8;
-                const double base = lds.base[b];
-                float z[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] = first + j < a.V ? logit_at<kBf16>(row, first + j) : -INFINITY;
-                for (; n < room; ++n) {
-                    float best = z[0];
-                    int j0 = 0;
+                for (int j = 0; j < 8; ++j) x[j] = first + j < a.V ? logit_at<kBf16>(row, first + j) : -INFINITY;
+            }
+            int n = 0;
+            unsigned long long reach[8];
 #pragma unroll
-                    for (int j = 1; j < 8; ++j)
-                        if (z[j] > best) { best = z[j]; j0 = j; }
-                    const float top = wave_max(best);
-                    const double key = base + (double)top * per_logit;
-                    if (!(top > kNoLogit) || key < border) break;
-                    const int l = (int)__builtin_ctzll(__ballot(best == top));
-                    if (lane == l) {
-                        lds.key[at + n] = key;
-                        lds.column[at + n] = (int)first + j0;
+            for (int j = 0; j < 8; ++j) {
+                reach[j] = __ballot(x[j] > kNoLogit && base + (double)x[j] * per_logit >= border);
+                n += (int)__popcll(reach[j]);
+            }
+            if (n <= room) {
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&lds.elements, n);
+                at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j == j0) z[j] = -INFINITY;
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    if ((reach[j] >> lane) & 1ull)
+                        lds.element[at + (int)__popcll(reach[j] & ((1ull << lane) - 1ull))] = Entry{base + (double)x[j] * per_logit, b * (int)a.V + (int)first + j};
+                    at += (int)__popcll(reach[j]);
+                }
+                continue;
+            }
+            // more than can be kept (equal values): the first ones, one after the other
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&lds.elements, room);
+            at = __builtin_amdgcn_readfirstlane(at);
+            for (n = 0; n < room; ++n) {
+                float best = x[0];
+                int j0 = 0;
+#pragma unroll
+                for (int j = 1; j < 8; ++j)
+                    if (x[j] > best) { best = x[j]; j0 = j; }
+                const float top = wave_max(best);
+                const int l = (int)__builtin_ctzll(__ballot(best == top));
+                if (lane == l) {
+                    lds.element[at + n] = Entry{base + (double)top * per_logit, b * (int)a.V + (int)first + j0};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j == j0) x[j] = -INFINITY;
                 }
             }
-            if (lane == 0) lds.count[r] = n;
         }
         __syncthreads();
-        if (wave == 0) {
-            // lane r: the elements of chunk r, best first
-            const int at = lane * keep - lane * (lane - 1) / 2, n = lane < chunks ? lds.count[lane] : 0;
-            const int b = lane < chunks ? lds.chunk[lane].index / most : 0;
-            int i = 0;
-            auto head = [&] { return i < n ? Entry{lds.key[at + i], b * (int)a.V + lds.column[at + i]} : Entry{kNone, 0}; };
-            Entry e = head();
-            double before = INFINITY;
-            int beam_before = -1;
-            uint32_t near = 0;
-            int32_t parent = -1, token = -1;
-            double score = kNone;
-            for (int out = 0; out <= keep; ++out) {
-                const int l = first_of(e);
-                Entry best{kNone, 0};
-                if (l >= 0) best = Entry{read_lane(e.key, l), __builtin_amdgcn_readlane(e.index, l)};
-                if (out == keep && known > keep && lds.chunk[keep].key > best.key) best = Entry{lds.chunk[keep].key, lds.chunk[keep].index / most * (int)a.V};
-                if (!(best.key > kNone)) break;
-                const int of = best.index / (int)a.V;
-                if (of != beam_before && beam_before >= 0 && before - best.key < kNear) near |= 1u << of | 1u << beam_before;
-                before = best.key;
-                beam_before = of;
-                if (out == keep) break;
-                if (lane == out) { parent = of; token = best.index % (int)a.V; score = best.key; }
-                if (lane == l) { ++i; e = head(); }
-            }
-            if (round == 0 && lane == 0) lds.near = near;
-            if ((round == 1 || near == 0) && lane < keep) {
-                a.parent_out[seq * keep + lane] = parent;
-                a.token_out[seq * keep + lane] = token;
-                a.score_out[seq * keep + lane] = (float)score;
-            }
+        // ---- in order; behind the last kept one the best that is left out, here or with its chunk
+        const int n = lds.elements, kept = n < keep ? n : keep;
+        in_order(lds.element, n, lds.best, need);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            Entry out = n > keep ? lds.best[keep] : Entry{kNone, 0};
+            if (known > keep && lds.chunk[keep].key > out.key) out = Entry{lds.chunk[keep].key, lds.chunk[keep].index / most * (int)a.V};
+            lds.best[kept] = out;
         }
         __syncthreads();
-        const uint32_t near = lds.near;
-        if (round == 1 || near == 0) return;
+        if (round == 0 && (int)threadIdx.x < kept) {
+            const Entry x = lds.best[threadIdx.x], y = lds.best[threadIdx.x + 1];
+            const int bx = x.index / (int)a.V, by = y.index / (int)a.V;
+            if (y.key > kNone && bx != by && x.key - y.key < kNear) atomicOr(&lds.near, 1u << bx | 1u << by);
+        }
+        __syncthreads();
+        const uint32_t near = round == 0 ? lds.near : 0u;
+        if (near == 0) {
+            if ((int)threadIdx.x < keep) {
+                const Entry x = (int)threadIdx.x < kept ? lds.best[threadIdx.x] : Entry{kNone, 0};
+                const int64_t at = seq * keep + threadIdx.x;
+                a.parent_out[at] = (int)threadIdx.x < kept ? x.index / (int)a.V : -1;
+                a.token_out[at] = (int)threadIdx.x < kept ? x.index % (int)a.V : -1;
+                a.score_out[at] = (float)x.key;
+            }
+            return;
+        }
         for (int b = 0; b < a.beams; ++b) {                                    // uniform
             if (((near >> b) & 1u) == 0 || lds.ends[b]) continue;
             const char* row = row_of(a, row0 + b, kBf16 ? 2 : 4);
