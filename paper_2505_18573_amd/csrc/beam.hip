@@ -28,10 +28,11 @@ constexpr double kNone = -INFINITY;
 
 template <bool kBf16> struct Segment { static constexpr int kCols = kVecs * 64 * (kBf16 ? 8 : 4), kChunks = kCols / kChunkCols; };
 
-struct Partial { float ref; float unused; double sum; };          // sum of 2^((z - ref) c)
+struct Partial { double ref, sum; };            // sum of 2^(z c - ref), c = log2(e) / tau
 
 struct BeamShape {
     int64_t chunks, segments;                   // of a row (segments: of the narrower type)
+    uint32_t per_chunk;                         // ceil(2^32 / chunks): x * per_chunk >> 32 = x / chunks for x * chunks < 2^32 (chunks > 1)
     int64_t at_partials, bytes;
 };
 static BeamShape beam_shape(int64_t rows, int64_t V, bool bf16)
@@ -40,6 +41,7 @@ static BeamShape beam_shape(int64_t rows, int64_t V, bool bf16)
     const int64_t cols = bf16 ? Segment<true>::kCols : Segment<false>::kCols;
     s.chunks = (V + kChunkCols - 1) / kChunkCols;
     s.segments = (V + cols - 1) / cols;
+    s.per_chunk = s.chunks > 1 ? (uint32_t)((((uint64_t)1 << 32) + s.chunks - 1) / s.chunks) : 0;
     s.at_partials = (rows * s.chunks * 4 + 255) / 256 * 256;
     s.bytes = s.at_partials + rows * s.segments * (int64_t)sizeof(Partial);
     return s;
@@ -61,7 +63,7 @@ __device__ __forceinline__ bool takes_part(float score) { return fabsf(score) < 
 // ---------------------------------------------------------------- stream
 template <bool kBf16>
 __global__ __launch_bounds__(64 * kStreamWaves)
-void beam_stream_kernel(BeamArgs a, BeamShape s, float c, char* ws)
+void beam_stream_kernel(BeamArgs a, BeamShape s, float c, double c64, char* ws)
 {
     constexpr int kPer = kBf16 ? 8 : 4, kCols = Segment<kBf16>::kCols, kChunks = Segment<kBf16>::kChunks, kOf = kVecs / kChunks;
     const int lane = threadIdx.x & 63;
@@ -73,53 +75,75 @@ void beam_stream_kernel(BeamArgs a, BeamShape s, float c, char* ws)
     const int64_t first = segment * kCols + lane * kPer;
     const bool tail = (segment + 1) * kCols > a.V;                            // uniform
     u32x4 w[kVecs];
+    if (!tail) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int64_t col = first + (int64_t)i * 64 * kPer;
-        if (!tail || col + kPer <= a.V) {
-            w[i] = stream_load(reinterpret_cast<const u32x4*>(p + col * (kBf16 ? 2 : 4)));
-        } else {                                                               // nothing behind the row is read
-            w[i] = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < kVecs; ++i) w[i] = stream_load(reinterpret_cast<const u32x4*>(p + (first + (int64_t)i * 64 * kPer) * (kBf16 ? 2 : 4)));
+    } else {                                                                   // nothing behind the row is read
 #pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (col + j < a.V) {
-                    if (kBf16) w[i][j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[col + j] << (16 * (j & 1));
-                    else w[i][j & 3] = reinterpret_cast<const uint32_t*>(p)[col + j];
-                }
+        for (int i = 0; i < kVecs; ++i) {
+            const int64_t col = first + (int64_t)i * 64 * kPer;
+            constexpr uint32_t kLow = kBf16 ? 0xFF80FF80u : 0xFF800000u;       // -inf
+            w[i] = u32x4{kLow, kLow, kLow, kLow};
+            if (col + kPer <= a.V) {
+                w[i] = stream_load(reinterpret_cast<const u32x4*>(p + col * (kBf16 ? 2 : 4)));
+            } else {
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (col + j < a.V) {
+                        if (kBf16) {
+                            const uint32_t x = reinterpret_cast<const uint16_t*>(p)[col + j];
+                            w[i][j >> 1] = (j & 1) ? (w[i][j >> 1] & 0xFFFFu) | x << 16 : (w[i][j >> 1] & 0xFFFF0000u) | x;
+                        } else {
+                            w[i][j & 3] = reinterpret_cast<const uint32_t*>(p)[col + j];
+                        }
+                    }
+            }
         }
     }
-    float z[kVecs][kPer], top[kChunks];
+    auto logit = [&](int i, int j) {
+        return kBf16 ? __uint_as_float((j & 1) ? w[i][j >> 1] & 0xFFFF0000u : w[i][j >> 1] << 16) : __uint_as_float(w[i][j & 3]);
+    };
+    float top[kChunks];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
+        float m = fmaxf(logit(i, 0), logit(i, 1));
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            z[i][j] = kBf16 ? __uint_as_float((j & 1) ? w[i][j >> 1] & 0xFFFF0000u : w[i][j >> 1] << 16) : __uint_as_float(w[i][j & 3]);
-            if (tail && first + (int64_t)i * 64 * kPer + j >= a.V) z[i][j] = -INFINITY;
-        }
-        float m = fmaxf(z[i][0], z[i][1]);
-#pragma unroll
-        for (int j = 2; j < kPer; j += 2) m = fmax3(m, z[i][j], z[i][j + 1]);
+        for (int j = 2; j < kPer; j += 2) m = fmax3(m, logit(i, j), logit(i, j + 1));
         top[i / kOf] = i % kOf == 0 ? m : fmaxf(top[i / kOf], m);
     }
     float most = top[0];
 #pragma unroll
     for (int i = 1; i < kChunks; ++i) most = fmaxf(most, top[i]);
-    // Differences first: z c and the reference's would both be rounded, and far apart for masks such as -1e30.
     const float ref = fmaxf(most, kNoLogit);
-    float sum = 0.0f;
+    auto add_up = [&](auto term) {
+        float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        float part[kPer];
+        for (int i = 0; i < kVecs; ++i) {
+            float part[kPer];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) part[j] = __builtin_amdgcn_exp2f((z[i][j] - ref) * c);
+            for (int j = 0; j < kPer; ++j) part[j] = __builtin_amdgcn_exp2f(term(logit(i, j)));
 #pragma unroll
-        for (int d = 1; d < kPer; d <<= 1)
+            for (int d = 1; d < kPer; d <<= 1)
 #pragma unroll
-            for (int j = 0; j < kPer; j += 2 * d) part[j] += part[j + d];
-        sum += part[0];
+                for (int j = 0; j < kPer; j += 2 * d) part[j] += part[j + d];
+            sum += part[0];
+        }
+        return sum;
+    };
+    // One multiply-add a term: the lane's reference is rounded once, in the scaled domain, and is the same in every term.  Not where
+    // it is large (masks of -1e9 throughout): z c there is off its rounded like by more than the exponent holds.
+    double up, all;
+    if (!__any(fabsf(ref) > 4096.0f) && c < 1024.0f) {
+        const float scaled = ref * c, sum = add_up([&](float z) { return fmaf(z, c, -scaled); });
+        const float most_scaled = wave_max(scaled);
+        up = most_scaled;
+        all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f(scaled - most_scaled));
+    } else {
+        const float sum = add_up([&](float z) { return (z - ref) * c; });
+        const float most_ref = wave_max(ref);
+        up = (double)most_ref * c64;
+        all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f((ref - most_ref) * c));
     }
-    const float up = wave_max(ref);
-    const double all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f((ref - up) * c));
     // The chunks' maxima over the wave: halves trade two chunks each and keep one, rows of sixteen lanes again; what is left is a row's.
     float* tops = reinterpret_cast<float*>(ws) + row * s.chunks + segment * kChunks;
     float in_half[kChunks / 2], in_row[kChunks / 4];
@@ -142,7 +166,7 @@ void beam_stream_kernel(BeamArgs a, BeamShape s, float c, char* ws)
         const int chunk = i + ((lane >> 4) & 1) * (kChunks / 4) + (lane >> 5) * (kChunks / 2);
         if ((lane & 15) == i && segment * kChunks + chunk < s.chunks) tops[chunk] = in_row[i];
     }
-    if (lane == 0) reinterpret_cast<Partial*>(ws + s.at_partials)[row * s.segments + segment] = Partial{up, 0.0f, all};
+    if (lane == 0) reinterpret_cast<Partial*>(ws + s.at_partials)[row * s.segments + segment] = Partial{up, all};
 }
 
 // ---------------------------------------------------------------- select
@@ -219,26 +243,32 @@ struct SelectLds {
     Entry of_wave[kSelectWaves + 1][kMaxKeep + 2];
 };
 
-// to[r] = the r-th of n entries in order, r < most, by counting how many come before each.
+// to[r] = the r-th of n entries in order, r < most, by counting how many come before each: eight lanes an entry.
 __device__ __forceinline__ void in_order(const Entry* from, int n, Entry* to, int most)
 {
-    for (int i = threadIdx.x; i < n; i += kSelectThreads) {
-        const Entry mine = from[i];
+    const int part = threadIdx.x & 7;
+    for (int i0 = 0; i0 < n; i0 += kSelectThreads / 8) {
+        const int i = i0 + (int)(threadIdx.x >> 3);
+        const Entry mine = from[i < n ? i : 0];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += before(from[j], mine) ? 1 : 0;
-        if (rank < most) to[rank] = mine;
+#pragma unroll 4
+        for (int j = part; j < n; j += 8) rank += before(from[j], mine) ? 1 : 0;
+        rank += dpp_i<kDppXor1>(rank, rank);
+        rank += dpp_i<kDppXor2>(rank, rank);
+        rank += dpp_i<kDppHalfMirror>(rank, rank);
+        if (part == 0 && i < n && rank < most) to[rank] = mine;
     }
 }
 
 template <bool kBf16>
 __global__ __launch_bounds__(kSelectThreads)
-void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
+void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* ws)
 {
     __shared__ SelectLds lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t seq = blockIdx.x, row0 = seq * a.beams;
     const float* tops = reinterpret_cast<const float*>(ws) + row0 * s.chunks;
-    const double per_logit = 1.0 / (double)a.tau, c = kLog2e * per_logit;
+    const double c = kLog2e * per_logit;                                       // per_logit = 1 / tau
     const int keep = a.keep, need = keep + 1, most = (int)s.chunks;
     constexpr int kEach = 8;
     const int entries = a.beams * most;
@@ -250,6 +280,9 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
     }
 
     for (int b = wave; b < a.beams; b += kSelectWaves) {
+        // (what a beam that takes no part has left is asked for as well, and not used)
+        const Partial* parts = reinterpret_cast<const Partial*>(ws + s.at_partials) + (row0 + b) * s.segments;
+        const Partial mine = parts[lane < s.segments ? lane : 0];
         const float score = a.scores[row0 + b];
         const bool ends = a.finished && a.finished[row0 + b];
         double base = kNone, total = 0.0;
@@ -257,16 +290,16 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
             if (ends) {
                 base = score;
             } else {
-                const Partial* parts = reinterpret_cast<const Partial*>(ws + s.at_partials) + (row0 + b) * s.segments;
-                float up = -INFINITY;
-                for (int64_t i = lane; i < s.segments; i += 64) up = fmaxf(up, parts[i].ref);
-                up = wave_max(up);
-                double sum = 0.0;
-                for (int64_t i = lane; i < s.segments; i += 64) sum += parts[i].sum * exp2_of(fmax(((double)parts[i].ref - (double)up) * c, -1000.0));
+                double up = lane < s.segments ? mine.ref : -INFINITY;
+                for (int64_t i = lane + 64; i < s.segments; i += 64) up = fmax(up, parts[i].ref);
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) up = fmax(up, __shfl_xor(up, d));
+                double sum = lane < s.segments ? mine.sum * exp2_of(fmax(mine.ref - up, -1000.0)) : 0.0;
+                for (int64_t i = lane + 64; i < s.segments; i += 64) sum += parts[i].sum * exp2_of(fmax(parts[i].ref - up, -1000.0));
                 sum = wave_sum(sum);
-                total = (double)up * c + log2(sum);
+                total = up + log2(sum);
                 // NaN and +inf make the sum no number; a row without any probability has none
-                if (sum > 0.0 && sum < INFINITY && fabsf(up) < INFINITY) base = score - total * kLn2;
+                if (sum > 0.0 && sum < INFINITY && fabs(up) < INFINITY) base = score - total * kLn2;
             }
         }
         if (lane == 0) { lds.base[b] = base; lds.log2_sum[b] = total; lds.ends[b] = ends; }
@@ -282,19 +315,15 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
             Entry mine{kNone, 0};
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int e = from + i * kSelectThreads + (int)threadIdx.x;
                 key[i] = kNone;
+                if (from + i * kSelectThreads >= entries) continue;            // uniform
+                const int e = from + i * kSelectThreads + (int)threadIdx.x;
                 if (e < entries) {
                     if (from > 0 || round > 0) z[i] = tops[e];
-                    const int b = e / most;
+                    const int b = most > 1 ? (int)__umulhi((uint32_t)e, s.per_chunk) : e;     // e / most
                     const double base = lds.base[b];
-                    if (base > kNone) {
-                        if (lds.ends[b]) {
-                            if (e - b * most == a.eos / kChunkCols) key[i] = base;
-                        } else if (z[i] > kNoLogit) {
-                            key[i] = base + (double)z[i] * per_logit;
-                        }
-                    }
+                    const bool ends = lds.ends[b] != 0;
+                    if (base > kNone && (ends ? e - b * most == a.eos / kChunkCols : z[i] > kNoLogit)) key[i] = ends ? base : base + (double)z[i] * per_logit;
                 }
                 if (key[i] > mine.key) mine = Entry{key[i], e};
             }
@@ -312,6 +341,7 @@ void beam_select_kernel(BeamArgs a, BeamShape s, const char* ws)
             if (threadIdx.x < kGroups) {
                 const float x = lds.group[threadIdx.x];
                 int above = 0, equal = 0;
+#pragma unroll 8
                 for (int j = 0; j < kGroups; j += 4) {
                     const float4 y = *reinterpret_cast<const float4*>(&lds.group[j]);
                     above += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
@@ -494,12 +524,12 @@ hipError_t launch_beam_select(const BeamArgs& a, bool bf16, void* workspace, hip
     const float c = (float)(kLog2e / (double)a.tau);
     const int64_t items = a.seqs * a.beams * s.segments;
     const dim3 grid((uint32_t)((items + kStreamWaves - 1) / kStreamWaves));
-    if (bf16) beam_stream_kernel<true><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, ws);
-    else beam_stream_kernel<false><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, ws);
+    if (bf16) beam_stream_kernel<true><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, kLog2e / (double)a.tau, ws);
+    else beam_stream_kernel<false><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, kLog2e / (double)a.tau, ws);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    if (bf16) beam_select_kernel<true><<<(uint32_t)a.seqs, kSelectThreads, 0, stream>>>(a, s, ws);
-    else beam_select_kernel<false><<<(uint32_t)a.seqs, kSelectThreads, 0, stream>>>(a, s, ws);
+    if (bf16) beam_select_kernel<true><<<(uint32_t)a.seqs, kSelectThreads, 0, stream>>>(a, s, 1.0 / (double)a.tau, ws);
+    else beam_select_kernel<false><<<(uint32_t)a.seqs, kSelectThreads, 0, stream>>>(a, s, 1.0 / (double)a.tau, ws);
     return hipGetLastError();
 }
 
