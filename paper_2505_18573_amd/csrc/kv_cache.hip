@@ -154,29 +154,49 @@ __device__ __forceinline__ uint32_t deal(uint32_t w, int lane)
     return out;
 }
 
-// A wave's work: the window that starts at token `first`, head (or pair of heads) `head_item`.  turn(x) may change the keys, x[i] being
-// the lane's four columns of token 4 half + i, once all rows are there.
-template <int D, bool kFp8, bool kBf16, typename Turn>
-__device__ __forceinline__ void append_item(const CacheView& c, const TokenRows& k, const TokenRows& v, const int64_t* slots, int64_t tokens,
-                                            int64_t first, int head_item, Turn turn)
+// A wave's work: the window that starts at token `first`, head (or pair of heads) `head_item`.
+struct AppendRows { float k[4][4], v[4][4]; };                    // [token 4 half + i][the lane's four columns]
+template <int D>
+__device__ __forceinline__ int append_head(int head_item)
 {
-    constexpr int kHeads = 128 / D;                               // heads of a wave
+    const int lane = threadIdx.x & 63;
+    return head_item * (128 / D) + ((lane & 31) >> (D == 128 ? 5 : 4));
+}
+// Rows of the window: keys, and values for those whose block is not filled.
+template <int D, bool kBf16>
+__device__ __forceinline__ void append_load(const CacheView& c, const TokenRows& k, const TokenRows& v, int64_t tokens, int64_t first, int head_item,
+                                            AppendRows& rows)
+{
+    constexpr int kIn = kBf16 ? 2 : 4;
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = (lane & (D / 4 - 1)) * 4, head = append_head<D>(head_item);
+    const int safe_head = head < c.heads ? head : 0;
+    auto load = [&](const TokenRows& t, int64_t token, float x[4]) {
+        const int64_t safe = token < tokens ? token : tokens - 1;
+        load4<kBf16>(static_cast<const char*>(t.base) + (safe * t.token_stride + safe_head * t.head_stride + col) * kIn, x);
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load(k, first + 4 * half + i, rows.k[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load(v, first + 4 * half + i, rows.v[i]);
+}
+// What is made of them.  turn(x) may change the keys.
+template <int D, bool kFp8, bool kBf16, typename Turn>
+__device__ __forceinline__ void append_store(const CacheView& c, const TokenRows& v, const int64_t* slots, int64_t tokens,
+                                             int64_t first, int head_item, AppendRows& rows, Turn turn)
+{
     constexpr int kIn = kBf16 ? 2 : 4;
     const int lane = threadIdx.x & 63;
     const int half = lane >> 5, part = lane & (D / 4 - 1), col = part * 4;
-    const int head = head_item * kHeads + ((lane & 31) >> (D == 128 ? 5 : 4));
+    const int head = append_head<D>(head_item);
     const bool live = head < c.heads;
     const int safe_head = live ? head : 0;
     auto load = [&](const TokenRows& t, int64_t token, float x[4]) {
         const int64_t safe = token < tokens ? token : tokens - 1;
         load4<kBf16>(static_cast<const char*>(t.base) + (safe * t.token_stride + safe_head * t.head_stride + col) * kIn, x);
     };
-    // rows of the window: keys, and values for those whose block is not filled.  Requested before the slots are known.
-    float xk[4][4], xv[4][4], xb[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load(k, first + 4 * half + i, xk[i]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load(v, first + 4 * half + i, xv[i]);
+    float (&xk)[4][4] = rows.k;
+    float (&xv)[4][4] = rows.v;
+    float xb[4][4];
     const Window w = look_at(slots, first, tokens, c.num_pages * c.page_size, lane);
     // codes of four rows, and their scale bytes into the cache
     auto quantise = [&](float x[4][4], const int64_t row[4], const bool ok[4], uint8_t* scales, uint32_t code[4]) {
@@ -282,13 +302,17 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
     const int64_t item = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
     if (item >= items) return;
     const int per = (c.heads + kHeads - 1) / kHeads;
-    append_item<D, kFp8, kBf16>(c, k, v, slots, tokens, item / per * kBlockTokens, (int)(item % per), [](float (&)[4][4]) {});
+    const int64_t first = item / per * kBlockTokens;
+    AppendRows rows;                                              // requested before the slots are known
+    append_load<D, kBf16>(c, k, v, tokens, first, (int)(item % per), rows);
+    append_store<D, kFp8, kBf16>(c, v, slots, tokens, first, (int)(item % per), rows, [](float (&)[4][4]) {});
 }
 
 // With rotary positions: a workgroup takes a window of eight tokens and makes sine and cosine of every (token, pair) once, for all
 // heads, in LDS.  Workgroups of grid row 0 write keys and values, a wave per head (two of 64 columns), turned in registers before they
-// are quantised; the other rows turn the queries, a share of the heads each.  A lane's four columns are half of four pairs
-// whose other half another lane of the row holds, or two whole pairs.
+// are quantised: a lane's four columns are half of four pairs whose other half another lane of the row holds, or two whole
+// pairs.  The other rows turn the queries, a share of the heads each: a thread keeps the (cos, sin) of eight pairs of a token and
+// takes head after head.  Either kind asks for its first rows before it makes the angles.
 constexpr int kAppendThreads = 256;
 template <int D, bool kFp8, bool kBf16>
 __global__ __launch_bounds__(kAppendThreads)
@@ -298,14 +322,33 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
     const int64_t first = (int64_t)blockIdx.x * kBlockTokens;
     const int here = tokens - first < kBlockTokens ? (int)(tokens - first) : kBlockTokens;
     const int pairs = r.rot / 2;
-    for (int i = threadIdx.x; i < here * pairs; i += kAppendThreads) turns[i] = turn_of(r, first + i / pairs, i % pairs);
-    __syncthreads();
+    auto make_turns = [&] {
+        for (int i = threadIdx.x; i < kBlockTokens * D / 2; i += kAppendThreads) {
+            const int t = i / (D / 2), pair = i % (D / 2);
+            if (t < here && pair < pairs) turns[i] = turn_of(r, first + t, pair);
+        }
+        __syncthreads();
+    };
     if (blockIdx.y > 0) {
-        const int units = units_of(r.rot, D);
-        const int h0 = ((int)blockIdx.y - 1) * q_heads_each, n = (q.heads - h0 < q_heads_each ? q.heads - h0 : q_heads_each) * here * units;
-        for (int i = threadIdx.x; i < n; i += kAppendThreads) {
-            const int u = i % units, rest = i / units, t = rest % here, h = h0 + rest / here;
-            turn_unit<kBf16>(q, r, first + t, h, u, turns + t * pairs);
+        constexpr int kUnits = D / 16, kAt = kUnits * kBlockTokens, kHeadsAtOnce = kAppendThreads / kAt;
+        const int u = threadIdx.x % kUnits, t = threadIdx.x / kUnits % kBlockTokens;
+        const int h0 = ((int)blockIdx.y - 1) * q_heads_each, h1 = q.heads - h0 < q_heads_each ? q.heads : h0 + q_heads_each;
+        int h = h0 + (int)threadIdx.x / kAt;
+        const bool is = t < here;
+        const int64_t token = first + (is ? t : 0);
+        Unit<kBf16> now;
+        now.load(q, r, token, h < h1 ? h : h0, u);
+        make_turns();
+        float2 by[8];
+        if (u < r.rot / 16) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) by[j] = turns[(is ? t : 0) * (D / 2) + 8 * u + j];
+        }
+        if (!is || h >= h1) return;
+        now.store(q, r, token, h, u, by);
+        for (h += kHeadsAtOnce; h < h1; h += kHeadsAtOnce) {
+            now.load(q, r, token, h, u);
+            now.store(q, r, token, h, u, by);
         }
         return;
     }
@@ -318,7 +361,7 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 4 * half + i < here ? 4 * half + i : here - 1;
-            const float2* of = turns + t * pairs;
+            const float2* of = turns + t * (D / 2);
             if (r.neighbours) {
                 if (mine) {
 #pragma unroll
@@ -343,8 +386,15 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
     };
     constexpr int kHeads = 128 / D;
     const int per = (c.heads + kHeads - 1) / kHeads;
-    for (int item = threadIdx.x >> 6; item < per; item += kAppendThreads / 64)
-        append_item<D, kFp8, kBf16>(c, k, v, slots, tokens, first, item, turn);
+    int item = threadIdx.x >> 6;
+    AppendRows rows;
+    if (item < per) append_load<D, kBf16>(c, k, v, tokens, first, item, rows);
+    make_turns();
+    while (item < per) {
+        append_store<D, kFp8, kBf16>(c, v, slots, tokens, first, item, rows, turn);
+        item += kAppendThreads / 64;
+        if (item < per) append_load<D, kBf16>(c, k, v, tokens, first, item, rows);
+    }
 }
 
 // Reading back: the same windows.  A token whose slot is not in the cache reads as zeros.
@@ -527,9 +577,9 @@ hipError_t launch_cache_append_rotated(const CacheView& c, const TokenRows& k, c
 {
     const int64_t windows = (tokens + kBlockTokens - 1) / kBlockTokens;
     // The queries' heads are spread over as many workgroups as give every compute unit two, and a thread a unit at least.
-    const int units = units_of(r.rot, c.dim) * (int)(tokens < kBlockTokens ? tokens : kBlockTokens);
     int groups = 0, each = 1;
     if (q.heads > 0) {
+        const int units = units_of(r.rot, c.dim) * (int)(tokens < kBlockTokens ? tokens : kBlockTokens);
         const int64_t want = 2 * (int64_t)compute_units() / windows, most = ((int64_t)q.heads * units + kAppendThreads - 1) / kAppendThreads;
         groups = (int)(want < 1 ? 1 : want < most ? want : most);
         each = (q.heads + groups - 1) / groups;

@@ -5,8 +5,10 @@
 // Angles: positions reach millions and f_0 is 1, so 32 bits would leave nothing of the angle behind the comma.  In turns
 // (theta / 2 pi) the whole part drops out, and the product is taken in 64 bits with its own rounding error (fused
 // multiply-add), so a position below 2^52 loses nothing; what is left, at most an eighth of a turn after the quadrant is
-// taken off, goes to fp32 and into the Taylor polynomials of sine and cosine (degree 9 and 10: the next terms are below
-// 2^-29 of the result).
+// taken off, goes into the Taylor polynomials of sine and cosine (degree 9 and 10: the next terms are below 2^-29 of the
+// result).  Their leading terms are taken in 64 bits and the others, at most a tenth of those, in 32, so that either is off by little
+// more than its own rounding to fp32: with all of it in 32 bits the keys that are rounded to eight bits another way were twice
+// as many.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -50,18 +52,17 @@ __device__ __forceinline__ float2 turn_of(const Rotary& r, int64_t token, int i)
     const double p = at * g, p_rest = fma(at, g, -p) + at * g_rest;
     const double turn = (p - rint(p)) + p_rest;                   // in [-1/2, 1/2], and p_rest
     const double quarter = rint(turn * 4.0);
-    const float z = (float)(turn - quarter * 0.25) * 6.28318530717958647693f;     // at most pi / 4
-    const float z2 = z * z;
-    float s = 1.0f / 362880.0f, c = -1.0f / 3628800.0f;
-    s = fmaf(s, z2, -1.0f / 5040.0f);
-    s = fmaf(s, z2, 1.0f / 120.0f);
-    s = fmaf(s, z2, -1.0f / 6.0f);
-    s = fmaf(s * z2, z, z);
-    c = fmaf(c, z2, 1.0f / 40320.0f);
-    c = fmaf(c, z2, -1.0f / 720.0f);
-    c = fmaf(c, z2, 1.0f / 24.0f);
-    c = fmaf(c, z2, -0.5f);
-    c = fmaf(c, z2, 1.0f);
+    const double angle = (turn - quarter * 0.25) * 6.28318530717958647693;        // at most pi / 4
+    const float z = (float)angle, z2 = z * z;
+    float p_s = 1.0f / 362880.0f, p_c = -1.0f / 3628800.0f;
+    p_s = fmaf(p_s, z2, -1.0f / 5040.0f);
+    p_s = fmaf(p_s, z2, 1.0f / 120.0f);
+    p_s = fmaf(p_s, z2, -1.0f / 6.0f);
+    p_c = fmaf(p_c, z2, 1.0f / 40320.0f);
+    p_c = fmaf(p_c, z2, -1.0f / 720.0f);
+    p_c = fmaf(p_c, z2, 1.0f / 24.0f);
+    const float s = (float)(angle + (double)(z2 * z * p_s));
+    const float c = (float)(fma(angle * angle, -0.5, 1.0) + (double)(z2 * z2 * p_c));
     const int q = (int)quarter;
     const float cs = (q & 1) ? s : c, sn = (q & 1) ? c : s;
     return float2{((q + 1) & 2) ? -cs : cs, r.sign * ((q & 2) ? -sn : sn)};
@@ -103,51 +104,56 @@ struct Eight {
 
 __host__ __device__ __forceinline__ int units_of(int rot, int dim) { return rot / 16 + (dim - rot + 15) / 16; }
 
-// Unit u of (token, head): `turns` the token's (cos, sin) of all pairs.
+// Unit u of (token, head), as it comes; `by`: (cos, sin) of pairs 8 u .. 8 u + 7 (any, where the unit is not turned).
 template <bool kBf16>
-__device__ __forceinline__ void turn_unit(const TurnArgs& a, const Rotary& r, int64_t token, int head, int u, const float2* turns)
-{
-    constexpr int kSize = kBf16 ? 2 : 4;
-    const char* x = static_cast<const char*>(a.x.base) + (token * a.x.token_stride + head * a.x.head_stride) * kSize;
-    char* out = static_cast<char*>(a.out) + (token * a.out_token_stride + head * a.out_head_stride) * kSize;
-    const int turned = r.rot / 16;
-    if (u >= turned) {                                            // columns behind the turned ones
-        const int col = r.rot + (u - turned) * 16;
-        Eight<kBf16> v;
-        v.load(x + col * kSize);
-        if (col + 8 < a.dim) {
-            Eight<kBf16> w;
-            w.load(x + (col + 8) * kSize);
-            w.store(out + (col + 8) * kSize);
-        }
-        v.store(out + col * kSize);
-        return;
-    }
-    const int at_a = r.neighbours ? 16 * u : 8 * u, at_b = r.neighbours ? at_a + 8 : at_a + r.rot / 2;
+struct Unit {
     Eight<kBf16> v, w;
-    v.load(x + at_a * kSize);
-    w.load(x + at_b * kSize);
-    if (r.neighbours) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 t = turns[8 * u + j], s = turns[8 * u + 4 + j];
-            const float v0 = v.x[2 * j], w0 = w.x[2 * j];
-            v.x[2 * j] = v0 * t.x - v.x[2 * j + 1] * t.y;
-            v.x[2 * j + 1] = v.x[2 * j + 1] * t.x + v0 * t.y;
-            w.x[2 * j] = w0 * s.x - w.x[2 * j + 1] * s.y;
-            w.x[2 * j + 1] = w.x[2 * j + 1] * s.x + w0 * s.y;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float2 t = turns[8 * u + j];
-            const float v0 = v.x[j];
-            v.x[j] = v0 * t.x - w.x[j] * t.y;
-            w.x[j] = w.x[j] * t.x + v0 * t.y;
-        }
+    static __device__ __forceinline__ void columns(const Rotary& r, int u, int* first, int* second)
+    {
+        const int turned = r.rot / 16;
+        const bool pairs = u < turned && !r.neighbours;           // two vectors half the turned columns apart, else next to each other
+        *first = pairs ? 8 * u : u < turned ? 16 * u : r.rot + (u - turned) * 16;
+        *second = pairs ? *first + r.rot / 2 : *first + 8;
     }
-    v.store(out + at_a * kSize);
-    w.store(out + at_b * kSize);
-}
+    __device__ __forceinline__ void load(const TurnArgs& a, const Rotary& r, int64_t token, int head, int u)
+    {
+        constexpr int kSize = kBf16 ? 2 : 4;
+        const char* x = static_cast<const char*>(a.x.base) + (token * a.x.token_stride + head * a.x.head_stride) * kSize;
+        int first, second;
+        columns(r, u, &first, &second);
+        v.load(x + first * kSize);
+        if (second < a.dim) w.load(x + second * kSize);
+    }
+    __device__ __forceinline__ void store(const TurnArgs& a, const Rotary& r, int64_t token, int head, int u, const float2 by[8])
+    {
+        constexpr int kSize = kBf16 ? 2 : 4;
+        char* out = static_cast<char*>(a.out) + (token * a.out_token_stride + head * a.out_head_stride) * kSize;
+        int first, second;
+        columns(r, u, &first, &second);
+        if (u < r.rot / 16) {
+            if (r.neighbours) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 t = by[j], s = by[4 + j];
+                    const float v0 = v.x[2 * j], w0 = w.x[2 * j];
+                    v.x[2 * j] = v0 * t.x - v.x[2 * j + 1] * t.y;
+                    v.x[2 * j + 1] = v.x[2 * j + 1] * t.x + v0 * t.y;
+                    w.x[2 * j] = w0 * s.x - w.x[2 * j + 1] * s.y;
+                    w.x[2 * j + 1] = w.x[2 * j + 1] * s.x + w0 * s.y;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float2 t = by[j];
+                    const float v0 = v.x[j];
+                    v.x[j] = v0 * t.x - w.x[j] * t.y;
+                    w.x[j] = w.x[j] * t.x + v0 * t.y;
+                }
+            }
+        }
+        v.store(out + first * kSize);
+        if (second < a.dim) w.store(out + second * kSize);
+    }
+};
 
 }  // namespace e3

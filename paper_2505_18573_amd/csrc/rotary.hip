@@ -1,8 +1,9 @@
 // Turning rows of heads by their tokens' positions (formulas: rotary.h).
 //
 // A workgroup takes a few tokens with all their heads: sine and cosine of every (token, pair) are made once, by one thread each,
-// and lie in LDS; then a thread takes units of two 16-byte vectors (bf16) that hold eight pairs.  Each element is read and
-// written once, in place where the caller likes, since a unit's two vectors are read before either is written.
+// and lie in LDS; then a thread keeps those of eight pairs of its token and takes units of two 16-byte vectors (bf16) from head after
+// head.  Each element is read and written once, in place where the caller likes, since a unit's two
+// vectors are read before either is written.
 #include "rotary.h"
 #include "vocab_pass.h"
 
@@ -19,11 +20,25 @@ void rotate_kernel(TurnArgs a, Rotary r, int tokens_each, int heads_each)
     const int64_t first = (int64_t)blockIdx.x * tokens_each;
     const int here = a.tokens - first < tokens_each ? (int)(a.tokens - first) : tokens_each;
     const int pairs = r.rot / 2, units = units_of(r.rot, a.dim);
+    const int u = threadIdx.x % units, t = threadIdx.x / units % tokens_each;
+    int h = threadIdx.x / (units * tokens_each);
+    const bool is = h < heads_each && t < here;
+    const int64_t token = first + (is ? t : 0);
+    Unit<kBf16> now;
+    if (is) now.load(a, r, token, h < a.heads ? h : 0, u);
     for (int i = threadIdx.x; i < here * pairs; i += kTurnThreads) turns[i] = turn_of(r, first + i / pairs, i % pairs);
     __syncthreads();
-    const int u = threadIdx.x % units, t = threadIdx.x / units % tokens_each, h0 = threadIdx.x / (units * tokens_each);
-    if (h0 >= heads_each || t >= here) return;
-    for (int h = h0; h < a.heads; h += heads_each) turn_unit<kBf16>(a, r, first + t, h, u, turns + t * pairs);
+    if (h >= a.heads || !is) return;
+    float2 by[8];
+    if (u < r.rot / 16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) by[j] = turns[t * pairs + 8 * u + j];
+    }
+    now.store(a, r, token, h, u, by);
+    for (h += heads_each; h < a.heads; h += heads_each) {
+        now.load(a, r, token, h, u);
+        now.store(a, r, token, h, u, by);
+    }
 }
 
 hipError_t launch_rotate(const TurnArgs& a, const Rotary& r, bool bf16, hipStream_t stream)
