@@ -456,7 +456,7 @@ int e3_cache_read(const e3_cache* cache, const int64_t* slots, int64_t tokens,
  * axes      1 .. E3_MAX_AXES.
  * neighbours  0: pair i is columns i and i + rot_dim / 2;  1: columns 2 i and 2 i + 1.
  * Positions are int64, [axes][tokens], rows position_stride elements apart, and may be negative; angles are exact to far below fp32's
- * rounding for |position| < 2^52.  Sums in fp32, rounded once.
+ * rounding for |position| < 2^52.
  */
 #define E3_MAX_AXES 8
 typedef struct {
@@ -469,8 +469,8 @@ typedef struct {
  * Turn rows of heads: out = R(theta) x, or with inverse = 1 R(-theta) x, which is R's transpose: the gradient with respect
  * to x where x stands for the gradient with respect to R x.
  *
- * x, out    [tokens][heads][head_dim] of dtype (E3_BF16 / E3_F32), strides in elements, columns next to each other; bases and
- *           strides multiples of 16 bytes (E3_ERR_ALIGN).  out may be x with the same strides (other strides: E3_ERR_VALUE); they may not
+ * x, out    [tokens][heads][head_dim] of dtype (E3_BF16 / E3_F32), strides in elements, columns next to each other (computed in
+ *           fp32 and rounded once); bases and strides multiples of 16 bytes (E3_ERR_ALIGN).  out may be x with the same strides (other strides: E3_ERR_VALUE); they may not
  *           overlap in any other way.
  * tokens at most 2^25, heads at most 65,536, head_dim a multiple of 8 from 16 to 1024 (E3_ERR_SHAPE).
  */
@@ -479,8 +479,8 @@ int e3_rotate(const e3_rotary* rotary, const int64_t* positions, int64_t positio
               void* out, int64_t out_token_stride, int64_t out_head_stride, int inverse, void* hip_stream);
 
 /*
- * e3_cache_append with the keys turned on the way (in fp32, before they are rounded or quantised), and the same tokens' queries
- * turned beside them in the same launch.  Values are stored as they are.
+ * e3_cache_append with the keys turned on the way (in fp64, rounded or quantised once), and the same tokens' queries turned beside them
+ * in the same launch.  Values are stored as they are.
  * q, q_out  [tokens][q_heads][head_dim] of dtype, as x and out of e3_rotate; q_heads == 0: keys and values only, both may be NULL.
  *           The queries of tokens whose slot is outside the cache are turned too.
  * tokens    at most 2^25; other arguments as for e3_cache_append and e3_rotate.

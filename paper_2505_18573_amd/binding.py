@@ -24,6 +24,7 @@ NATIVE_PATH = os.path.join(HERE, "_native.so")
 
 E3_F32, E3_BF16, E3_E4M3 = 0, 1, 2
 E3_OK = 0
+E3_ERR_SHAPE = -2
 E3_TILE_CHUNK, E3_TILE_LANES, E3_TILE_DEPTH = 8, 64, 8
 E3_NOALLOC_MAX_ROWS = 1024
 E3_MAX_DRAFTS = 63
@@ -1055,6 +1056,14 @@ def e3_verify_drafts(logits: torch.Tensor, draft_tokens: Optional[torch.Tensor],
     return (accepted_out, *outs)
 
 
+def _int32(v, name: str) -> int:
+    """An int that C takes as int32_t (ctypes would cut it)."""
+    v = int(v)
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{name} must fit 32 bits")
+    return v
+
+
 def e3_beam_workspace_bytes(seqs: int, beams: int, V: int) -> int:
     """Host-only; 0 for a shape that is not served."""
     return int(lib().e3_beam_workspace_bytes(seqs, beams, V))
@@ -1073,6 +1082,9 @@ def e3_beam_select(logits: torch.Tensor, scores: torch.Tensor, keep: int, tau: f
         raise ValueError("logits must be [seqs, beams, V] on the GPU")
     dt, dev = _float_type(logits.dtype), logits.device
     seqs, beams, V = logits.shape
+    keep, eos_token = _int32(keep, "keep"), _int32(eos_token, "eos_token")
+    if keep < 1 or keep > E3_MAX_KEEP:                             # (before outputs of that size are allocated)
+        raise E3Error(E3_ERR_SHAPE, "e3_beam_select")
     seq_stride, beam_stride = _positions(logits, "logits", logits.dtype, (seqs, beams, V), dev)
     for t, dtype, name in ((scores, torch.float32, "scores"), (finished, torch.uint8, "finished")):
         if t is not None and (t.dtype is not dtype or tuple(t.shape) != (seqs, beams) or t.device != dev or not t.is_contiguous()):
@@ -1080,7 +1092,7 @@ def e3_beam_select(logits: torch.Tensor, scores: torch.Tensor, keep: int, tau: f
     outs = []
     for t, dtype, name in ((parent_out, torch.int32, "parent_out"), (token_out, torch.int32, "token_out"), (score_out, torch.float32, "score_out")):
         if t is None:
-            t = torch.empty((seqs, max(0, int(keep))), dtype=dtype, device=dev)
+            t = torch.empty((seqs, keep), dtype=dtype, device=dev)
         elif t.dtype is not dtype or tuple(t.shape) != (seqs, keep) or t.device != dev or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor [{seqs}, {keep}] on {dev}")
         outs.append(t)
@@ -1088,8 +1100,8 @@ def e3_beam_select(logits: torch.Tensor, scores: torch.Tensor, keep: int, tau: f
         workspace = torch.empty(e3_beam_workspace_bytes(seqs, beams, V), dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
-    rc = lib().e3_beam_select(_ptr(logits), dt, seqs, beams, V, seq_stride, beam_stride, _ptr(scores), int(keep), float(tau), _ptr(finished),
-                              int(eos_token), *(_ptr(t) for t in outs), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
+    rc = lib().e3_beam_select(_ptr(logits), dt, seqs, beams, V, seq_stride, beam_stride, _ptr(scores), keep, float(tau), _ptr(finished),
+                              eos_token, *(_ptr(t) for t in outs), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev))
     if rc != E3_OK:
         raise E3Error(rc, "e3_beam_select")
     return tuple(outs)
@@ -1107,7 +1119,7 @@ def e3_beam_reorder(parent: torch.Tensor, row_pages: torch.Tensor, row_lens: tor
     if parent.dtype is not torch.int32 or parent.dim() != 2 or not parent.is_contiguous() or not parent.is_cuda:
         raise ValueError("parent must be a contiguous int32 tensor [seqs, beams] on the GPU")
     seqs, beams = parent.shape
-    rows = seqs * beams
+    rows, page_size = seqs * beams, _int32(page_size, "page_size")
     width = _table(row_pages, rows, "row_pages", dev)
     _check(row_lens, torch.int32, rows, "row_lens", dev)
     if pages_out is None:
@@ -1121,7 +1133,7 @@ def e3_beam_reorder(parent: torch.Tensor, row_pages: torch.Tensor, row_lens: tor
         else:
             _check(t, torch.int32, rows, name, dev)
         outs.append(t)
-    rc = lib().e3_beam_reorder(_ptr(parent), seqs, beams, _ptr(row_pages), width, _ptr(row_lens), int(page_size), _ptr(pages_out),
+    rc = lib().e3_beam_reorder(_ptr(parent), seqs, beams, _ptr(row_pages), width, _ptr(row_lens), page_size, _ptr(pages_out),
                                *(_ptr(t) for t in outs), _stream(dev))
     if rc != E3_OK:
         raise E3Error(rc, "e3_beam_reorder")

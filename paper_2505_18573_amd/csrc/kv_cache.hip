@@ -318,14 +318,15 @@ template <int D, bool kFp8, bool kBf16>
 __global__ __launch_bounds__(kAppendThreads)
 void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Rotary r, const int64_t* slots, int64_t tokens, int q_heads_each)
 {
-    __shared__ float2 turns[kBlockTokens * D / 2];                // [token][pair]
+    __shared__ double2 exact[kBlockTokens * D / 2];               // [token][pair]
+    float2* const turns = reinterpret_cast<float2*>(exact);       // the queries'
     const int64_t first = (int64_t)blockIdx.x * kBlockTokens;
     const int here = tokens - first < kBlockTokens ? (int)(tokens - first) : kBlockTokens;
     const int pairs = r.rot / 2;
-    auto make_turns = [&] {
+    auto make_turns = [&](auto* to, auto of) {
         for (int i = threadIdx.x; i < kBlockTokens * D / 2; i += kAppendThreads) {
             const int t = i / (D / 2), pair = i % (D / 2);
-            if (t < here && pair < pairs) turns[i] = turn_of(r, first + t, pair);
+            if (t < here && pair < pairs) to[i] = of(r, first + t, pair);
         }
         __syncthreads();
     };
@@ -338,7 +339,7 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
         const int64_t token = first + (is ? t : 0);
         Unit<kBf16> now;
         now.load(q, r, token, h < h1 ? h : h0, u);
-        make_turns();
+        make_turns(turns, turn_of);
         float2 by[8];
         if (u < r.rot / 16) {
 #pragma unroll
@@ -361,15 +362,15 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 4 * half + i < here ? 4 * half + i : here - 1;
-            const float2* of = turns + t * (D / 2);
+            const double2* of = exact + t * (D / 2);
             if (r.neighbours) {
                 if (mine) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float2 w = of[col / 2 + j];
-                        const float a = x[i][2 * j], b = x[i][2 * j + 1];
-                        x[i][2 * j] = a * w.x - b * w.y;
-                        x[i][2 * j + 1] = b * w.x + a * w.y;
+                        const double2 w = of[col / 2 + j];
+                        const double a = x[i][2 * j], b = x[i][2 * j + 1];
+                        x[i][2 * j] = sticky(a * w.x - b * w.y);
+                        x[i][2 * j + 1] = sticky(b * w.x + a * w.y);
                     }
                 }
             } else {
@@ -377,8 +378,8 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
                 for (int j = 0; j < 4; ++j) {
                     const float y = __shfl(x[i][j], other);
                     if (mine) {
-                        const float2 w = of[(upper ? col - pairs : col) + j];
-                        x[i][j] = upper ? x[i][j] * w.x + y * w.y : x[i][j] * w.x - y * w.y;
+                        const double2 w = of[(upper ? col - pairs : col) + j];
+                        x[i][j] = sticky((double)x[i][j] * w.x + (double)y * (upper ? w.y : -w.y));
                     }
                 }
             }
@@ -389,7 +390,7 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
     int item = threadIdx.x >> 6;
     AppendRows rows;
     if (item < per) append_load<D, kBf16>(c, k, v, tokens, first, item, rows);
-    make_turns();
+    make_turns(exact, turn64_of);
     while (item < per) {
         append_store<D, kFp8, kBf16>(c, v, slots, tokens, first, item, rows, turn);
         item += kAppendThreads / 64;

@@ -787,7 +787,7 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         const void* finished = table(a[4], at::kByte);
         const int32_t keep = r.integer32(a[2]), eos = r.integer32(a[5]);
         const double tau = r.number(a[3]);
-        if (!r.ok || keep < 1) return unusual();
+        if (!r.ok || keep < 1 || keep > E3_MAX_KEEP) return unusual();
         const std::array<int64_t, 2> shape = {seqs, keep};
         Output parent, token, score;
         parent.shaped(r, a[6], at::kInt, shape);

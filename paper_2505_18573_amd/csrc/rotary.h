@@ -7,8 +7,9 @@
 // multiply-add), so a position below 2^52 loses nothing; what is left, at most an eighth of a turn after the quadrant is
 // taken off, goes into the Taylor polynomials of sine and cosine (degree 9 and 10: the next terms are below 2^-29 of the
 // result).  Their leading terms are taken in 64 bits and the others, at most a tenth of those, in 32, so that either is off by little
-// more than its own rounding to fp32: with all of it in 32 bits the keys that are rounded to eight bits another way were twice
-// as many.
+// more than its own rounding to fp32.
+// Keys on their way into the cache are turned in 64 bits throughout and rounded once: in eight bits an element that lies next to
+// the border of two codes is a sixteenth larger or smaller by an error of one bit of fp32.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -41,18 +42,35 @@ hipError_t launch_rotate(const TurnArgs& a, const Rotary& r, bool bf16, hipStrea
 hipError_t launch_cache_append_rotated(const CacheView& c, const TokenRows& k, const TokenRows& v, const TurnArgs& q, const Rotary& r,
                                        bool in_bf16, const int64_t* slots, int64_t tokens, hipStream_t stream);
 
-// (cos, sin) of pair i at a token
-__device__ __forceinline__ float2 turn_of(const Rotary& r, int64_t token, int i)
+// The angle of pair i at a token: quarter turns taken off, at most pi / 4 left.  false: the pair goes by no axis and stays as it is.
+__device__ __forceinline__ bool angle_of(const Rotary& r, int64_t token, int i, double* angle, int* quarters)
 {
     const int axis = r.axis == nullptr ? 0 : r.axis[i];
-    if (axis >= r.axes) return float2{1.0f, 0.0f};                // no axis: the pair stays as it is
+    if (axis >= r.axes) return false;
     const double at = (double)r.positions[axis * r.stride + token], f = r.freqs[i];
     constexpr double kHi = 0.15915494309189533577, kLo = -9.839338337591243e-18;    // 1 / (2 pi) in two parts
     const double g = f * kHi, g_rest = fma(f, kHi, -g) + f * kLo;
     const double p = at * g, p_rest = fma(at, g, -p) + at * g_rest;
     const double turn = (p - rint(p)) + p_rest;                   // in [-1/2, 1/2], and p_rest
     const double quarter = rint(turn * 4.0);
-    const double angle = (turn - quarter * 0.25) * 6.28318530717958647693;        // at most pi / 4
+    *angle = (turn - quarter * 0.25) * 6.28318530717958647693;
+    *quarters = (int)quarter;
+    return true;
+}
+template <typename T>
+__device__ __forceinline__ void by_quarters(int q, float sign, T& c, T& s)
+{
+    const T cs = (q & 1) ? s : c, sn = (q & 1) ? c : s;
+    c = ((q + 1) & 2) ? -cs : cs;
+    s = ((q & 2) ? -sn : sn) * (T)sign;
+}
+
+// (cos, sin) of pair i at a token, in 32 bits
+__device__ __forceinline__ float2 turn_of(const Rotary& r, int64_t token, int i)
+{
+    double angle;
+    int quarters;
+    if (!angle_of(r, token, i, &angle, &quarters)) return float2{1.0f, 0.0f};
     const float z = (float)angle, z2 = z * z;
     float p_s = 1.0f / 362880.0f, p_c = -1.0f / 3628800.0f;
     p_s = fmaf(p_s, z2, -1.0f / 5040.0f);
@@ -61,11 +79,50 @@ __device__ __forceinline__ float2 turn_of(const Rotary& r, int64_t token, int i)
     p_c = fmaf(p_c, z2, 1.0f / 40320.0f);
     p_c = fmaf(p_c, z2, -1.0f / 720.0f);
     p_c = fmaf(p_c, z2, 1.0f / 24.0f);
-    const float s = (float)(angle + (double)(z2 * z * p_s));
-    const float c = (float)(fma(angle * angle, -0.5, 1.0) + (double)(z2 * z2 * p_c));
-    const int q = (int)quarter;
-    const float cs = (q & 1) ? s : c, sn = (q & 1) ? c : s;
-    return float2{((q + 1) & 2) ? -cs : cs, r.sign * ((q & 2) ? -sn : sn)};
+    float s = (float)(angle + (double)(z2 * z * p_s));
+    float c = (float)(fma(angle * angle, -0.5, 1.0) + (double)(z2 * z2 * p_c));
+    by_quarters(quarters, r.sign, c, s);
+    return float2{c, s};
+}
+
+// The same in 64 bits (series up to z^15 and z^16: the next terms are below 2^-54).
+__device__ __forceinline__ double2 turn64_of(const Rotary& r, int64_t token, int i)
+{
+    double z;
+    int quarters;
+    if (!angle_of(r, token, i, &z, &quarters)) return double2{1.0, 0.0};
+    const double z2 = z * z;
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+    s = fma(s, z2, 1.0 / 6227020800.0);
+    c = fma(c, z2, -1.0 / 87178291200.0);
+    s = fma(s, z2, -1.0 / 39916800.0);
+    c = fma(c, z2, 1.0 / 479001600.0);
+    s = fma(s, z2, 1.0 / 362880.0);
+    c = fma(c, z2, -1.0 / 3628800.0);
+    s = fma(s, z2, -1.0 / 5040.0);
+    c = fma(c, z2, 1.0 / 40320.0);
+    s = fma(s, z2, 1.0 / 120.0);
+    c = fma(c, z2, -1.0 / 720.0);
+    s = fma(s, z2, -1.0 / 6.0);
+    c = fma(c, z2, 1.0 / 24.0);
+    s = fma(s * z2, z, z);
+    c = fma(c, z2, -0.5);
+    c = fma(c, z2, 1.0);
+    by_quarters(quarters, r.sign, c, s);
+    return double2{c, s};
+}
+
+// x in fp32 such that rounding it on to fewer bits gives what rounding x itself would: towards zero, and odd where that was not exact.
+__device__ __forceinline__ float sticky(double x)
+{
+    const float f = (float)x;
+    const double back = (double)f;
+    uint32_t bits = __float_as_uint(f);
+    if (back != x && fabsf(f) < INFINITY) {                       // (NaN differs from itself, and keeps its bits)
+        if (fabs(back) > fabs(x)) bits -= 1;
+        bits |= 1u;
+    }
+    return __uint_as_float(bits);
 }
 
 // A unit: up to 16 columns of one token and head, in two vectors of eight; those that are turned hold pairs 8 u .. 8 u + 7.

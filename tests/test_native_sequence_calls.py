@@ -1,0 +1,125 @@
+"""The calls of rotary positions, window attention and beam search through the binding's native code against its Python path:
+the same outputs bit for bit, the same errors."""
+import pytest
+import torch
+
+import paper_2505_18573_amd as e3
+from tests.test_native_decode_calls import _outcome, _spoilt
+
+DEV = "cuda:0"
+
+
+def _calls(dev):
+    g = torch.Generator().manual_seed(1)
+    heads, D, page = 2, 64, 32
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+    cache = e3.new_cache(8, page, heads, D, device=dev)
+    plain = e3.new_cache(8, page, heads, D, torch.bfloat16, device=dev)
+    x = torch.randn((40, 6 + 2 * heads, D), generator=g).to(dev)
+    slots = torch.arange(40, device=dev) + 3
+    pos = torch.randint(0, 5000, (3, 40), generator=g).to(dev)
+    one, three = e3.new_rotary(D, device=dev), e3.new_rotary(48, sections=(10, 7, 7), neighbours=True, device=dev)
+    turn = dict(x=x[:, :6], rotary=three, positions=pos)
+    append = dict(cache=cache, q=x[:, :6], k=x[:, 6:8], v=x[:, 8:], rotary=three, positions=pos, slots=slots)
+    half = {k: v.bfloat16() for k, v in append.items() if k in ("q", "k", "v")}
+    q = torch.randn((5, 4, D), generator=g).to(torch.bfloat16).to(dev)
+    window = dict(q=q, cache=cache, query_offsets=i32([0, 1, 1, 5]), row_pages=i32([[0, 1], [2, 3], [4, 5]]), row_lens=i32([40, 3, 64]), window=20,
+                  sinks=2, scale=0.125)
+    z = torch.randn((3, 2, 104), generator=g).to(dev)
+    beam = dict(logits=z[..., :100], scores=torch.zeros((3, 2), device=dev), keep=4)
+    order = dict(parent=i32([[1, 1], [0, 0], [1, 0]]), row_pages=i32(list(range(12))).reshape(6, 2), row_lens=i32([5, 5, 33, 33, 9, 9]), page_size=page)
+    return {
+        "rotate": (e3.e3_rotate, turn),
+        "rotate_back": (e3.e3_rotate, dict(x=x[:, :6].bfloat16(), rotary=one, positions=pos[0], inverse=True)),
+        "rotate_into": (e3.e3_rotate, dict(turn, out=torch.zeros((6, 40, D), device=dev).transpose(0, 1))),
+        "append": (e3.e3_cache_append_rotated, append),
+        "append_bf16": (e3.e3_cache_append_rotated, dict(append, **half, cache=plain, rotary=one, positions=pos[1])),
+        "append_into": (e3.e3_cache_append_rotated, dict(append, q_out=torch.zeros((40, 6, D), device=dev))),
+        "append_keys": (e3.e3_cache_append_rotated, dict(append, q=None)),
+        "window": (e3.e3_window_attention, window),
+        "window_plain": (e3.e3_window_attention, dict(window, cache=plain, want_lse=False, scale=1)),
+        "window_into": (e3.e3_window_attention, dict(window, out=torch.zeros_like(q), lse_out=torch.zeros((5, 4), device=dev),
+                                                     workspace=torch.zeros(e3.e3_window_attention_workspace_bytes(3, 5, 4, heads, D) if dev != "cpu" else 8,
+                                                                           dtype=torch.uint8, device=dev))),
+        "beam": (e3.e3_beam_select, beam),
+        "beam_ends": (e3.e3_beam_select, dict(beam, logits=z.bfloat16()[..., :97], tau=0.5, finished=torch.tensor([[0, 1], [1, 1], [0, 0]], dtype=torch.uint8, device=dev),
+                                              eos_token=7)),
+        "beam_into": (e3.e3_beam_select, dict(beam, parent_out=i32([[0] * 4] * 3), token_out=i32([[0] * 4] * 3), score_out=torch.zeros((3, 4), device=dev),
+                                              workspace=torch.zeros(e3.e3_beam_workspace_bytes(3, 2, 100), dtype=torch.uint8, device=dev))),
+        "reorder": (e3.e3_beam_reorder, order),
+        "reorder_into": (e3.e3_beam_reorder, dict(order, pages_out=torch.zeros((6, 2), dtype=torch.int32, device=dev), lens_out=i32([0] * 6), src_out=i32([0] * 6),
+                                                  dst_out=i32([0] * 6), counts_out=i32([0] * 6))),
+        "copy": (e3.e3_cache_copy, dict(cache=cache, src_pages=i32([0, 1, -1]), dst_pages=i32([5, 6, 7]), counts=i32([32, 9, 4]))),
+    }
+
+
+NAMES = list(_calls("cpu"))
+CACHED = {"append_keys", "copy"}                                 # what they return is nothing: the cache is compared
+
+
+def _run(name, kw, monkeypatch, native):
+    out = _outcome(_calls_of(name), kw, monkeypatch, native)
+    return out
+
+
+def _calls_of(name):
+    f = _calls("cpu")[name][0]
+
+    def call(**kw):
+        out = f(**kw)
+        if torch.is_tensor(out):
+            out = (out,) + (tuple(t for t in kw["cache"] if t is not None) if "cache" in kw else ())
+        return out
+    return call
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", NAMES)
+def test_same_outputs_as_the_python_path(name, monkeypatch):
+    e3.lib()
+    served = []
+    monkeypatch.setattr(e3.binding, "_ordinary", lambda n, *a, keep=e3.binding._ordinary: (lambda r: (served.append((n, r is not None)), r)[1])(keep(n, *a)))
+    want = _run(name, _calls(DEV)[name][1], monkeypatch, native=False)
+    kw = _calls(DEV)[name][1]
+    served.clear()
+    got = _run(name, kw, monkeypatch, native=True)
+    assert served and all(ok for _, ok in served)                # the native call did it
+    assert isinstance(want[0], torch.Tensor) and len(got) == len(want)
+    for a, b in zip(got, want):
+        if b is None:
+            assert a is None
+        else:
+            assert a.dtype is b.dtype and a.device == b.device and a.shape == b.shape and torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def _more_spoilt(kw):
+    for key, v in kw.items():
+        if key == "rotary":
+            f, axis, n = v
+            for bad in ((f.float(), axis, n), (f[:-4], axis, n), (f.cpu(), axis, n) if f.is_cuda else (f[None], axis, n), (f, f, n), (f, None, n)):
+                yield dict(kw, rotary=bad)
+            yield dict(kw, rotary=(f, axis))
+        elif key == "positions":
+            yield dict(kw, positions=v.int())
+            yield dict(kw, positions=torch.cat([v, v], -1)[..., ::2])
+            yield dict(kw, positions=v[..., :-1])
+        elif key in ("window", "sinks", "keep", "page_size", "eos_token"):
+            yield dict(kw, **{key: -7})
+            yield dict(kw, **{key: 1 << 40})
+            yield dict(kw, **{key: "x"})
+        elif key == "tau":
+            yield dict(kw, tau=0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", NAMES)
+def test_same_errors(name, monkeypatch):
+    kw = _calls(DEV)[name][1]
+    plain = {k: v for k, v in kw.items() if k != "rotary"}
+    cases = [dict(bad, **({"rotary": kw["rotary"]} if "rotary" in kw else {})) for bad in _spoilt(plain)] + list(_more_spoilt(kw))
+    for bad in cases:
+        want, got = (_run(name, bad, monkeypatch, native=n) for n in (False, True))
+        if isinstance(want[0], type):
+            assert isinstance(got[0], type) and got == want, (got, want)
+        else:                                                    # not an error after all: the same outputs
+            assert len(got) == len(want)

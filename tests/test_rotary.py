@@ -13,6 +13,7 @@ import pytest
 import torch
 
 import paper_2505_18573_amd as e3
+from tests.test_kv_cache import quantised
 
 DEV = "cuda:0"
 TRIG = 2.0 ** -21
@@ -267,6 +268,30 @@ def test_quarter_turns_are_exact(kind, neighbours):
     assert torch.equal(q.cpu(), y)
     for x, w in zip(one, two):
         assert (x is None and w is None) or torch.equal(x.view(torch.uint8), w.view(torch.uint8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.float8_e4m3fn, torch.bfloat16])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_keys_are_rounded_once(kind, dtype):
+    # turned in 64 bits: every stored key is what rounding the definition's value gives, bit for bit
+    n, heads, D = 300, 4, 128
+    x, g = step_inputs(n, 0, heads, D, dtype, 21)
+    k, v = x[:, :heads], x[:, heads:]
+    pos = torch.randint(0, 1 << 20, (3, n), generator=g)
+    slots = torch.randperm(16 * 32, generator=g)[:n].to(DEV)
+    for neighbours in (False, True):
+        r = rotary_of(D, 3, neighbours, DEV)
+        cache = e3.new_cache(16, 32, heads, D, kind, DEV)
+        e3.e3_cache_append_rotated(cache, None, k.to(DEV), v.to(DEV), r, pos.to(DEV), slots)
+        want = turned(k, r.freqs, r.axis, pos, neighbours)[0].numpy()
+        if kind is torch.bfloat16:
+            step = 2.0 ** (np.floor(np.log2(np.abs(want))) - 7)
+            want = np.rint(want / step) * step
+        else:
+            want = quantised(want)[0]
+        got = e3.e3_cache_read(cache, slots, torch.float32)[0].cpu().double().numpy()
+        assert np.array_equal(got, want)
 
 
 @pytest.mark.gpu
