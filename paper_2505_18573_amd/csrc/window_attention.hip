@@ -57,6 +57,7 @@ struct WindowShape {
     int32_t R;                                  // query heads per key head
     int64_t most[2];                            // records of either line
     int32_t workgroups, workers[2];             // workers: at most
+    int64_t steps;                              // of either line at most
     int64_t at_list[2], at_cuts, at_ml, at_o[2], bytes;
 };
 
@@ -72,8 +73,8 @@ static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t 
     s.most[kOfGroups] = queries > kFewQueries ? queries / kTile + rows : 0;
     s.most[kOfWaves] = rows;
     // no more workers than steps: a small call's launches are small
-    const int64_t steps = rows * heads * (visible / kStep + 3 + kCost);
-    s.workgroups = (int32_t)(s.most[kOfGroups] == 0 && steps < groups ? steps : groups);
+    s.steps = (queries / kTile + rows) * heads * (visible / kStep + 4 + kCost);
+    s.workgroups = (int32_t)(s.most[kOfGroups] == 0 && s.steps < groups ? s.steps : groups);
     s.workers[kOfGroups] = s.most[kOfGroups] > 0 ? s.workgroups : 0;
     s.workers[kOfWaves] = s.workgroups * kWaves;
     int64_t at = up(sizeof(Totals));
@@ -131,7 +132,7 @@ __device__ __forceinline__ Band band_of(int R, int tile, int n, int len, int win
 // Places for tiles: a row's lie from place_of_row(row) on, as many as it can have.
 __device__ __forceinline__ int64_t place_of_row(int offset, int R, int row) { return (int64_t)offset * R / kTile + row; }
 
-// f(line, record) for every tile among places [begin, end); offset(row), len(row): the row's first query and tokens.
+// f(line, record, place) for every tile among places [begin, end); offset(row), len(row): the row's first query and tokens.
 template <typename Offset, typename Len, typename F>
 __device__ __forceinline__ void tiles_in(const WindowArgs& a, int R, int64_t begin, int64_t end, Offset offset, Len len_of, F f)
 {
@@ -155,7 +156,7 @@ __device__ __forceinline__ void tiles_in(const WindowArgs& a, int R, int64_t beg
             Work w;
             w.first = 0; w.row = r; w.tile = (int)(u - k); w.offset = off; w.n = n; w.len = len;
             w.cost = kCost + band_of(R, w.tile, n, len, a.window, a.sinks, line == kOfWaves ? kStep : kBlock).steps;
-            f(line, w);
+            f(line, w, u);
         }
     }
 }
@@ -206,14 +207,14 @@ void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, c
     const int64_t share = (places + kPlanLanes - 1) / kPlanLanes;
     const int64_t begin = threadIdx.x * share, end = begin + share < places ? begin + share : places;
     int64_t own[3] = {0, 0, 0}, before[3], all[3];
-    tiles_in(a, s.R, begin, end, offset, len, [&](int line, const Work& w) {
+    tiles_in(a, s.R, begin, end, offset, len, [&](int line, const Work& w, int64_t) {
         own[0] += line == 0 ? (int64_t)w.cost * heads : 0;
         own[1] += line == 1 ? (int64_t)w.cost * heads : 0;
         own[2] += line == 1 ? 1ll << 32 : 1;
     });
     scan<kPlanWaves>(own, before, all, sums);
     int64_t index[2] = {before[2] & 0xFFFFFFFF, before[2] >> 32};
-    tiles_in(a, s.R, begin, end, offset, len, [&](int line, Work w) {
+    tiles_in(a, s.R, begin, end, offset, len, [&](int line, Work w, int64_t) {
         w.first = line == 0 ? before[0] : before[1];
         const int64_t i = line == 0 ? index[0]++ : index[1]++;
         if (line == 0) before[0] += (int64_t)w.cost * heads;
@@ -232,79 +233,94 @@ void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, c
     }
 }
 
-// A batch of few rows and tiles is planned by every workgroup of the attend launch for itself, in LDS: a launch less.  (One row 20.1
-// us with a launch for the plan.)
+// A batch of few rows, tiles and steps is planned by every workgroup of the attend launch for itself, in LDS and 32 bits: a launch less.
+// (One row 20.1 us with a launch for the plan.)  The list has an entry for every place; one without a tile of a line has the
+// beginning of the line's next one.
 constexpr int kOwnPlaces = 640;                 // what fits beside the keys of two workgroups
 struct OwnPlan {
     int offsets[kOwnPlaces + 1], lens[kOwnPlaces];
-    int64_t first[kOwnPlaces];                  // the line of workgroups, then the line of waves
+    int first[2][kOwnPlaces];
     uint32_t row_tile[kOwnPlaces];
-    int64_t sums[kWaves][3];
+    int sums[kWaves][2];
 };
 __device__ __forceinline__ Totals plan_own(const WindowArgs& a, const WindowShape& s, int heads, int page_size, OwnPlan& p)
 {
     constexpr int kThreads = 64 * kWaves;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t visible = table_tokens(a.row_width, page_size);
     for (int i = threadIdx.x; i <= a.rows; i += kThreads) {
         p.offsets[i] = clamp_len(a.offsets[i], a.tokens);
         if (i < a.rows) p.lens[i] = clamp_len(a.row_lens[i], visible);
     }
     __syncthreads();
-    auto offset = [&](int r) { return p.offsets[r]; };
-    auto len = [&](int r) { return p.lens[r]; };
-    const int places = (int)((int64_t)a.tokens * s.R / kTile) + a.rows;
+    const int places = (int)((int64_t)a.tokens * s.R / kTile) + a.rows;        // at most kOwnPlaces
     const int share = (places + kThreads - 1) / kThreads;
     const int begin = (int)threadIdx.x * share, end = begin + share < places ? begin + share : places;
-    int64_t own[3] = {0, 0, 0}, before[3], all[3];
-    tiles_in(a, s.R, begin, end, offset, len, [&](int line, const Work& w) {
-        own[0] += line == 0 ? (int64_t)w.cost * heads : 0;
-        own[1] += line == 1 ? (int64_t)w.cost * heads : 0;
-        own[2] += line == 1 ? 1ll << 32 : 1;
+    for (int u = begin; u < end; ++u) { p.first[0][u] = 0; p.first[1][u] = 0; }
+    tiles_in(a, s.R, begin, end, [&](int r) { return p.offsets[r]; }, [&](int r) { return p.lens[r]; }, [&](int line, const Work& w, int64_t u) {
+        p.first[line][u] = w.cost * heads;
+        p.first[1 - line][u] = 0;
+        p.row_tile[u] = (uint32_t)w.row << 16 | (uint32_t)w.tile;
     });
-    scan<kWaves>(own, before, all, p.sums);
-    Totals t;
-    const int64_t count[2] = {all[2] & 0xFFFFFFFF, all[2] >> 32};
-    const bool fits = count[0] + count[1] <= kOwnPlaces;
-    t.steps[0] = fits ? all[0] : 0;
-    t.steps[1] = fits ? all[1] : 0;
-    t.count[0] = fits ? (int)count[0] : 0;
-    t.count[1] = fits ? (int)count[1] : 0;
-    if (fits) {
-        int index[2] = {(int)(before[2] & 0xFFFFFFFF), (int)(count[0] + (before[2] >> 32))};
-        tiles_in(a, s.R, begin, end, offset, len, [&](int line, const Work& w) {
-            const int i = line == 0 ? index[0]++ : index[1]++;
-            p.first[i] = line == 0 ? before[0] : before[1];
-            p.row_tile[i] = (uint32_t)w.row << 16 | (uint32_t)w.tile;
-            if (line == 0) before[0] += (int64_t)w.cost * heads;
-            else before[1] += (int64_t)w.cost * heads;
-        });
+    int own[2] = {0, 0}, before[2];
+    for (int u = begin; u < end; ++u) { own[0] += p.first[0][u]; own[1] += p.first[1][u]; }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        before[k] = own[k];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(before[k], d);
+            if (lane >= d) before[k] += y;
+        }
+        if (lane == 63) p.sums[wave][k] = before[k];
+        before[k] -= own[k];
     }
+    __syncthreads();
+    Totals t{{0, 0}, {places, places}};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (i < wave) before[k] += p.sums[i][k];
+            t.steps[k] += p.sums[i][k];
+        }
+    for (int u = begin; u < end; ++u)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int cost = p.first[k][u];
+            p.first[k][u] = before[k];
+            before[k] += cost;
+        }
     __syncthreads();
     return t;
 }
 
-// A line's records, in the workspace or in LDS.
+// A line's records, in the workspace or in LDS; next(i, step): the record behind record i, which begins at that step.
 struct InWorkspace {
     const Work* list;
+    int count;
     __device__ __forceinline__ int64_t first(int i) const { return list[i].first; }
-    __device__ __forceinline__ Work get(int i) const { return list[i]; }
+    __device__ __forceinline__ Work get(int i) const { return list[i < count ? i : count - 1]; }
+    __device__ __forceinline__ int next(int i, int64_t) const { return i + 1; }
 };
+template <typename List> __device__ __forceinline__ int find_work(const List& list, int count, int64_t step);
 template <int kLine>
 struct InLds {
     const OwnPlan& p;
     const WindowArgs& a;
-    int R, from;
-    __device__ __forceinline__ int64_t first(int i) const { return p.first[from + i]; }
+    int R, count;
+    __device__ __forceinline__ int64_t first(int i) const { return p.first[kLine][i]; }
     __device__ __forceinline__ Work get(int i) const
     {
         Work w;
-        w.first = p.first[from + i];
-        const uint32_t x = p.row_tile[from + i];
-        w.row = (int)(x >> 16); w.tile = (int)(x & 0xFFFFu);
-        w.offset = p.offsets[w.row]; w.n = p.offsets[w.row + 1] - w.offset; w.len = p.lens[w.row];
+        w.first = p.first[kLine][i];
+        const uint32_t x = p.row_tile[i];
+        w.row = uniform((int)(x >> 16)); w.tile = uniform((int)(x & 0xFFFFu));
+        w.offset = uniform(p.offsets[w.row]); w.n = uniform(p.offsets[w.row + 1]) - w.offset; w.len = uniform(p.lens[w.row]);
         w.cost = kCost + band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kLine == kOfWaves ? kStep : kBlock).steps;
         return w;
     }
+    __device__ __forceinline__ int next(int, int64_t step) const { return find_work(*this, count, step); }
 };
 
 // How the workgroups and stretches are divided, the same in every launch that asks.
@@ -988,7 +1004,7 @@ struct Many {
 // The stretch of worker `part`: f(record, piece, which of the worker's two places, record and head of what lies behind the piece in the stretch,
 // whether that is an item's first steps).
 template <int kLine, typename List, typename F>
-__device__ __forceinline__ void along(const List& list, int count, const Division& d, int heads, int part, Cut* cut, F f)
+__device__ __forceinline__ void along(const List& list, const Division& d, int heads, int part, Cut* cut, F f)
 {
     const bool writes = (threadIdx.x & (kLine == kOfGroups ? 255 : 63)) == 0;
     Cut found{-1, 0, 0, 0, 0, 0, 0, 0};
@@ -998,10 +1014,10 @@ __device__ __forceinline__ void along(const List& list, int count, const Divisio
     }
     int64_t at = begin_of(part, d.steps[kLine], d.parts[kLine]);
     const int64_t end = begin_of(part + 1, d.steps[kLine], d.parts[kLine]);
-    int i = find_work(list, count, at);
+    int i = find_work(list, list.count, at);
     const int64_t begin = at;
     Work w = uniform(list.get(i));
-    while (at < end && i < count) {
+    while (at < end) {
         const int64_t offset = at - w.first;
         const int head = (int)divide(offset, w.cost), from = (int)(offset - (int64_t)head * w.cost);
         const int n = end - at < w.cost - from ? (int)(end - at) : w.cost - from;
@@ -1020,11 +1036,14 @@ __device__ __forceinline__ void along(const List& list, int count, const Divisio
         // what follows: the same tile's next head, or the next tile
         const bool done = head + 1 == heads && from + n == w.cost;
         Work after = w;
-        if (done && i + 1 < count) after = uniform(list.get(i + 1));
-        const bool more = at + n < end && from + n == w.cost && (!done || i + 1 < count) && after.cost > kCost && end - (at + n) > kCost;
+        if (done && at + n < end) {
+            i = list.next(i, at + n);
+            after = uniform(list.get(i));
+        }
+        const bool more = at + n < end && from + n == w.cost && after.cost > kCost && end - (at + n) > kCost;
         if (piece.to > piece.from || (w.cost == kCost && piece.whole)) f(w, piece, from <= kCost ? 1 : 0, after, done ? 0 : head + 1, more);
         at += n;
-        if (done) { ++i; w = after; }
+        if (done) w = after;
     }
     if (writes) *cut = found;
 }
@@ -1042,8 +1061,8 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
     const int workgroups = (int)gridDim.x;
     const Division d = divide_work(totals, workgroups);
     auto list = [&](auto line) {
-        if constexpr (kOwn) return InLds<decltype(line)::value>{own, a, s.R, decltype(line)::value == kOfGroups ? 0 : uniform(totals.count[kOfGroups])};
-        else return InWorkspace{reinterpret_cast<const Work*>(ws + s.at_list[decltype(line)::value])};
+        if constexpr (kOwn) return InLds<decltype(line)::value>{own, a, s.R, uniform(totals.count[0])};
+        else return InWorkspace{reinterpret_cast<const Work*>(ws + s.at_list[decltype(line)::value]), uniform(totals.count[decltype(line)::value])};
     };
     Cut* cuts = reinterpret_cast<Cut*>(ws + s.at_cuts);
     Cut* wave_cuts = cuts + s.workers[kOfGroups];
@@ -1059,7 +1078,7 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
         Many<D, kFp8> x;
         x.begin();
         x.ready = false;
-        along<kOfGroups>(list(std::integral_constant<int, kOfGroups>{}), uniform(totals.count[kOfGroups]), d, c.heads, block, cuts + block,
+        along<kOfGroups>(list(std::integral_constant<int, kOfGroups>{}), d, c.heads, block, cuts + block,
                          [&](const Work& w, const Piece1& piece, int which, const Work& after, int head, bool more) {
                              const int64_t place = (2 * block + which) * (int64_t)kTile;
                              x.run(c, a, s.R, w, piece, {after, head, more}, lds, ml + place, o + place * D);
@@ -1071,7 +1090,7 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
     // a workgroup's waves lie far apart on their line: few stretches are spread over all workgroups
     const int part = wave * (workgroups - d.groups) + block - d.groups;
     float* o = reinterpret_cast<float*>(ws + s.at_o[kOfWaves]);
-    along<kOfWaves>(list(std::integral_constant<int, kOfWaves>{}), uniform(totals.count[kOfWaves]), d, c.heads, part, wave_cuts + part,
+    along<kOfWaves>(list(std::integral_constant<int, kOfWaves>{}), d, c.heads, part, wave_cuts + part,
                     [&](const Work& w, const Piece1& piece, int which, const Work&, int, bool) {
                         const int64_t place = (2 * part + which) * (int64_t)kFewQueries;
                         float2* ml_out = ml + 2 * (int64_t)s.workers[0] * kTile + place;
@@ -1170,7 +1189,7 @@ void window_join_kernel(WindowArgs a, WindowShape s, int group_slices, int wave_
 template <int D, bool kFp8>
 static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const WindowShape& s, char* ws, hipStream_t stream)
 {
-    if ((int64_t)a.tokens * s.R / kTile + a.rows <= kOwnPlaces) {
+    if ((int64_t)a.tokens * s.R / kTile + a.rows <= kOwnPlaces && s.steps < (int64_t)1 << 31) {
         window_kernel<D, kFp8, true><<<s.workgroups, 64 * kWaves, 0, stream>>>(c, a, s, ws);
     } else {
         window_plan_kernel<<<1, kPlanLanes, 0, stream>>>(a, s, c.heads, c.page_size, ws);
