@@ -81,15 +81,15 @@ struct Window {
 
 // What the wave needs to know about its window: the slots of 7 tokens before it, its own 8 and 7 after it, and from
 // them which blocks are filled.  (Block starts lie at least eight tokens apart: a window holds one at most.)
-__device__ __forceinline__ Window look_at(const int64_t* slots, int64_t first, int64_t tokens, int64_t capacity, int lane)
+__device__ __forceinline__ int64_t ask_slot(const int64_t* slots, int64_t first, int64_t tokens, int lane)
+{
+    const int64_t at = first - 7 + lane;
+    return lane < 22 && at >= 0 && at < tokens ? slots[at] : -1;
+}
+__device__ __forceinline__ Window look_at(int64_t slot, int64_t capacity, int lane)
 {
     Window w;
-    const int64_t at = first - 7 + lane;
-    w.slot = -1;
-    if (lane < 22 && at >= 0 && at < tokens) {
-        const int64_t s = slots[at];
-        w.slot = s >= 0 && s < capacity ? s : -1;
-    }
+    w.slot = slot >= 0 && slot < capacity ? slot : -1;
     const int64_t next = __shfl_down(w.slot, 1);
     const uint32_t follows = (uint32_t)__ballot(lane < 21 && w.slot >= 0 && next == w.slot + 1);
     const uint32_t aligned = (uint32_t)__ballot(lane < 22 && w.slot >= 0 && (w.slot & 7) == 0);
@@ -179,9 +179,9 @@ __device__ __forceinline__ void append_load(const CacheView& c, const TokenRows&
 #pragma unroll
     for (int i = 0; i < 4; ++i) load(v, first + 4 * half + i, rows.v[i]);
 }
-// What is made of them.  turn(x) may change the keys.
+// What is made of them; w: the window's slots.  turn(x) may change the keys.
 template <int D, bool kFp8, bool kBf16, typename Turn>
-__device__ __forceinline__ void append_store(const CacheView& c, const TokenRows& v, const int64_t* slots, int64_t tokens,
+__device__ __forceinline__ void append_store(const CacheView& c, const TokenRows& v, const Window& w, int64_t tokens,
                                              int64_t first, int head_item, AppendRows& rows, Turn turn)
 {
     constexpr int kIn = kBf16 ? 2 : 4;
@@ -197,7 +197,6 @@ __device__ __forceinline__ void append_store(const CacheView& c, const TokenRows
     float (&xk)[4][4] = rows.k;
     float (&xv)[4][4] = rows.v;
     float xb[4][4];
-    const Window w = look_at(slots, first, tokens, c.num_pages * c.page_size, lane);
     // codes of four rows, and their scale bytes into the cache
     auto quantise = [&](float x[4][4], const int64_t row[4], const bool ok[4], uint8_t* scales, uint32_t code[4]) {
 #pragma unroll
@@ -305,7 +304,8 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
     const int64_t first = item / per * kBlockTokens;
     AppendRows rows;                                              // requested before the slots are known
     append_load<D, kBf16>(c, k, v, tokens, first, (int)(item % per), rows);
-    append_store<D, kFp8, kBf16>(c, v, slots, tokens, first, (int)(item % per), rows, [](float (&)[4][4]) {});
+    const Window w = look_at(ask_slot(slots, first, tokens, threadIdx.x & 63), c.num_pages * c.page_size, threadIdx.x & 63);
+    append_store<D, kFp8, kBf16>(c, v, w, tokens, first, (int)(item % per), rows, [](float (&)[4][4]) {});
 }
 
 // With rotary positions: a workgroup takes a window of eight tokens and makes sine and cosine of every (token, pair) once, for all
@@ -390,9 +390,11 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
     int item = threadIdx.x >> 6;
     AppendRows rows;
     if (item < per) append_load<D, kBf16>(c, k, v, tokens, first, item, rows);
+    const int64_t slot = ask_slot(slots, first, tokens, lane);
     make_turns(exact, turn64_of);
+    const Window w = look_at(slot, c.num_pages * c.page_size, lane);
     while (item < per) {
-        append_store<D, kFp8, kBf16>(c, v, slots, tokens, first, item, rows, turn);
+        append_store<D, kFp8, kBf16>(c, v, w, tokens, first, item, rows, turn);
         item += kAppendThreads / 64;
         if (item < per) append_load<D, kBf16>(c, k, v, tokens, first, item, rows);
     }
@@ -428,7 +430,7 @@ void cache_read_kernel(CacheView c, const int64_t* slots, int64_t tokens, int64_
     const int head = (int)(item % per) * kHeads + ((lane & 31) >> (D == 128 ? 5 : 4));
     const bool live = head < c.heads;
     const int safe_head = live ? head : 0;
-    const Window w = look_at(slots, first, tokens, c.num_pages * c.page_size, lane);
+    const Window w = look_at(ask_slot(slots, first, tokens, lane), c.num_pages * c.page_size, lane);
 
     float x[4];
     auto put = [&](char* out, int64_t token, const float v[4]) {
