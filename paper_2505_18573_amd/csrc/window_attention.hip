@@ -723,6 +723,8 @@ struct Many {
         return z;
     }
 
+    static __device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
     // What the workgroup has ahead of it: pages of the next two blocks and the image that the next one is in; `ready`: it is on its way.
     int page[2], after[2];
     int image_of;
@@ -860,25 +862,16 @@ struct Many {
                     for (int i = 0; i < 16; ++i) t[b][i] *= factors[32 * b + 16 * (i >> 3) + 8 * h + (i & 7)];
             }
             if (edge) {
-                // Token 32 b + 16 (i >> 3) + (i & 7) behind the lane's first one: in the window if from `from` on by less than `n`, else
-                // among the first ones.
-                const int base = at + 8 * h;
-                const int from = x.lo - base, n = x.hi - x.lo;
-                if (at < a.sinks) {                                            // uniform
-                    const int kept = (a.sinks < x.hi ? a.sinks : x.hi) - base;
+                // A bit for every token from the lane's first one on; token 32 b + 16 (i >> 3) + (i & 7) is the lane's number i of half b.
+                const int base = at + 8 * h, kept = a.sinks < x.hi ? a.sinks : x.hi;
+                const uint64_t seen = (below(x.hi - base) & ~below(x.lo - base)) | below(kept - base);
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t bits = there[b] ? (uint32_t)(seen >> (32 * b)) : 0u;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int k = 32 * b + 16 * (i >> 3) + (i & 7);
-                            t[b][i] = there[b] && ((uint32_t)(k - from) < (uint32_t)n || k < kept) ? t[b][i] : -INFINITY;
-                        }
-                } else {
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const uint32_t most = there[b] ? (uint32_t)n : 0u;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) t[b][i] = (uint32_t)(32 * b + 16 * (i >> 3) + (i & 7) - from) < most ? t[b][i] : -INFINITY;
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 16 * (i >> 3) + (i & 7), 1);
+                        t[b][i] = __uint_as_float((__float_as_uint(t[b][i]) & all) | (0xFF800000u & ~all));
                     }
                 }
             }
