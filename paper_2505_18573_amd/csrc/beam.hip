@@ -9,9 +9,9 @@
 //            chunks holds one that comes before it (chunks are runs of columns, so this is also right for equal values, where the
 //            lower index comes first).  So the chunks' maxima are ranked first and only `keep` chunks are read again, 1 KB each.
 // Scores are compared in fp64.  Sums taken in fp32 leave ln sum exp off by 1e-7 as a rule (1e-6 at worst), the same for all tokens
-// of a beam, so only the order between beams is in question: where two neighbours of different beams among the results (or the best one left
-// out) are within 2e-6 of each other, the beams' sums are taken again in fp64, by the sequence's workgroup, and the
-// selection is made once more.  (One sequence in some hundreds; it takes 10 us and more for a beam.)
+// of a beam, so only the order between beams is in question: where two neighbours of different beams among the results, or one that is
+// kept and one that is left out, are within 2e-6 of each other, the beams' sums are taken again in fp64, by the sequence's
+// workgroup, and the selection is made once more.  (One sequence in some hundreds; it takes 10 us and more for a beam.)
 #include "beam.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
@@ -404,7 +404,8 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
         }
         // ---- their elements
         const int chunks = known < keep ? known : keep;
-        const double border = chunks == keep ? lds.chunk[keep - 1].key : kNone;      // `keep` candidates reach it
+        // `keep` candidates reach the last of these chunks' best; those a little below it tell where beams are near each other
+        const double border = chunks == keep ? lds.chunk[keep - 1].key - kNear : kNone;
         if (threadIdx.x == 0) lds.elements = 0;
         __syncthreads();
         for (int r = wave; r < chunks; r += kSelectWaves) {
@@ -468,20 +469,39 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
             }
         }
         __syncthreads();
-        // ---- in order; behind the last kept one the best that is left out, here or with its chunk
+        // ---- in order
         const int n = lds.elements, kept = n < keep ? n : keep;
-        in_order(lds.element, n, lds.best, need);
+        in_order(lds.element, n, lds.best, keep);
         __syncthreads();
-        if (threadIdx.x == 0) {
-            Entry out = n > keep ? lds.best[keep] : Entry{kNone, 0};
-            if (known > keep && lds.chunk[keep].key > out.key) out = Entry{lds.chunk[keep].key, lds.chunk[keep].index / most * (int)a.V};
-            lds.best[kept] = out;
-        }
-        __syncthreads();
-        if (round == 0 && (int)threadIdx.x < kept) {
-            const Entry x = lds.best[threadIdx.x], y = lds.best[threadIdx.x + 1];
-            const int bx = x.index / (int)a.V, by = y.index / (int)a.V;
-            if (y.key > kNone && bx != by && x.key - y.key < kNear) atomicOr(&lds.near, 1u << bx | 1u << by);
+        if (round == 0) {
+            const auto beam_of = [&](int i) { return lds.best[i].index / (int)a.V; };
+            if ((int)threadIdx.x + 1 < kept) {
+                const int x = beam_of(threadIdx.x), y = beam_of(threadIdx.x + 1);
+                if (x != y && lds.best[threadIdx.x].key - lds.best[threadIdx.x + 1].key < kNear) atomicOr(&lds.near, 1u << x | 1u << y);
+            }
+            // a candidate that is left out, or the best of a chunk that is, against the last ones that are kept
+            const Entry last = lds.best[keep - 1];                             // (of `keep` chunks there are `keep` candidates)
+            const auto left_out = [&](double key, int beam) {
+                for (int i = keep - 1; i >= 0 && lds.best[i].key - key < kNear; --i)
+                    if (beam_of(i) != beam) atomicOr(&lds.near, 1u << beam_of(i) | 1u << beam);
+            };
+            if (kept == keep) {
+                for (int i = (int)threadIdx.x; i < n; i += kSelectThreads) {
+                    const Entry e = lds.element[i];
+                    if (last.key - e.key < kNear && before(last, e)) left_out(e.key, e.index / (int)a.V);
+                }
+                if (known > keep && last.key - lds.chunk[keep].key < kNear) {
+                    const Entry border_chunk = lds.chunk[keep - 1];
+                    for (int e = (int)threadIdx.x; e < entries; e += kSelectThreads) {
+                        const int b = e / most;
+                        const double base = lds.base[b];
+                        const bool ends = lds.ends[b] != 0;
+                        if (!(base > kNone) || (ends && e - b * most != a.eos / kChunkCols)) continue;
+                        const Entry of{ends ? base : base + (double)tops[e] * per_logit, e};
+                        if (last.key - of.key < kNear && before(border_chunk, of)) left_out(of.key, b);
+                    }
+                }
+            }
         }
         __syncthreads();
         const uint32_t near = round == 0 ? lds.near : 0u;

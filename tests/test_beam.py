@@ -162,6 +162,24 @@ def test_near_scores_of_two_beams():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("apart", [3, 300, 4000])
+def test_near_scores_behind_equal_ones(dtype, apart):
+    # Beam 0 has its best logit twice, in one chunk of columns or two; beam 1 the same logits in another order, its score 2^-29 above
+    # or below: with the last place taken by one of the equal ones, the candidate next to it is the other, and beam 1's lies behind that.
+    g, n, V = torch.Generator().manual_seed(apart), 128, 8192
+    z = (torch.randn((n, 2, V), generator=g) * 3).clamp(max=9.0).to(dtype)
+    for i in range(n):
+        z[i, 0, 17], z[i, 0, 17 + apart] = 10.0, 10.0
+        z[i, 1] = z[i, 0, torch.randperm(V, generator=g)]
+    scores = torch.zeros((n, 2))
+    scores[:, 1] = 2.0 ** -29 * (2 * torch.randint(0, 2, (n,), generator=g) - 1)
+    want = reference(z, scores, 3, 1.0)
+    for keep in (1, 2, 3):
+        check(e3.e3_beam_select(z.to(DEV), scores.to(DEV), keep), [w[:, :keep] for w in want])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_masks_and_values_that_are_no_numbers(dtype):
     g, V = torch.Generator().manual_seed(4), 5000
     z = (torch.randn((6, 4, V), generator=g) * 2).to(dtype)
