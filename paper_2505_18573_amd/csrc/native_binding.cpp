@@ -155,6 +155,16 @@ struct Output {
         object = THPVariable_Wrap(t);
         if (object == nullptr) { PyErr_Clear(); r.ok = false; }
     }
+    // n elements of a vector, from `from` on: several small outputs are one allocation (0.9 us of the calling thread each)
+    void part(Reader& r, const at::Tensor& of, int64_t from, int64_t n)
+    {
+        const at::Tensor t = at::detail::make_tensor<at::TensorImpl>(at::TensorImpl::VIEW, at::Storage(of.storage()), of.key_set(), of.dtype());
+        t.unsafeGetTensorImpl()->set_storage_offset(from);
+        t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+        p = t.data_ptr();
+        object = THPVariable_Wrap(t);
+        if (object == nullptr) { PyErr_Clear(); r.ok = false; }
+    }
     void take(PyObject* given) { Py_INCREF(given); object = given; }
     void take_or_make(Reader& r, PyObject* given, at::ScalarType type, int64_t n)
     {
@@ -821,7 +831,13 @@ PyObject* beam_reorder(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         if (!r.ok) return unusual();
         Output out_pages, out[4];
         out_pages.shaped(r, a[4], at::kInt, std::array<int64_t, 2>{rows, width});
-        for (int i = 0; i < 4; ++i) out[i].take_or_make(r, a[5 + i], at::kInt, rows);
+        if (r.ok && a[5] == Py_None && a[6] == Py_None && a[7] == Py_None && a[8] == Py_None) {
+            const int64_t apart = (rows + 15) / 16 * 16;                       // aligned like allocations for any vector load
+            const at::Tensor all = at::empty({4 * apart}, at::TensorOptions().dtype(at::kInt).device(r.dev));
+            for (int i = 0; i < 4; ++i) out[i].part(r, all, i * apart, rows);
+        }
+        else
+            for (int i = 0; i < 4; ++i) out[i].take_or_make(r, a[5 + i], at::kInt, rows);
         return run(r, [&](void* s) {
                        return p_beam_reorder((const int32_t*)parent->data_ptr(), seqs, (int32_t)beams, (const int32_t*)pages->data_ptr(), width,
                                              (const int32_t*)lens, page, (int32_t*)out_pages.p, (int32_t*)out[0].p, (int32_t*)out[1].p,

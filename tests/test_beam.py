@@ -330,6 +330,18 @@ def test_copies_that_are_none():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,B", [(1, 1), (5, 3), (7, 32), (0, 4)])
+def test_reordered_tensors_are_apart(n, B):
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=DEV)
+    outs = e3.e3_beam_reorder(i32(n, B), i32(n * B, 3), i32(n * B), 32)
+    assert [tuple(t.shape) for t in outs] == [(n * B, 3)] + 4 * [(n * B,)]
+    assert all(t.dtype is torch.int32 and t.is_contiguous() and t.device == torch.device(DEV) and not t.requires_grad for t in outs)
+    for i, t in enumerate(outs):                                  # written one by one, none changes another
+        t.fill_(i + 1)
+    assert all(bool((t == i + 1).all()) for i, t in enumerate(outs)) and all(torch.equal(t.clone(), t) and t.data_ptr() % 16 == 0 for t in outs)
+
+
+@pytest.mark.gpu
 def test_reorder_into_given_tensors_and_a_graph():
     i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
     parent, table, lens = i32([[1, 1, 0], [2, 2, 2]]), i32(list(range(12))).reshape(6, 2).contiguous(), i32([5, 5, 5, 40, 40, 40])
