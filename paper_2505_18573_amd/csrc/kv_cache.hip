@@ -324,10 +324,15 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
     const int here = tokens - first < kBlockTokens ? (int)(tokens - first) : kBlockTokens;
     const int pairs = r.rot / 2;
     auto make_turns = [&](auto* to, auto of) {
-        for (int i = threadIdx.x; i < kBlockTokens * D / 2; i += kAppendThreads) {
-            const int t = i / (D / 2), pair = i % (D / 2);
-            if (t < here && pair < pairs) to[i] = of(r, first + t, pair);
+        constexpr int kEach = kBlockTokens * (D / 2) / kAppendThreads;
+        Place places[kEach];                                      // all asked for first; those behind the last token or pair are not used
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int i = j * kAppendThreads + (int)threadIdx.x, t = i / (D / 2), pair = i % (D / 2);
+            places[j] = place_of(r, first + (t < here ? t : here - 1), pair < pairs ? pair : pairs - 1);
         }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) to[j * kAppendThreads + (int)threadIdx.x] = of(places[j], r.sign);
         __syncthreads();
     };
     if (blockIdx.y > 0) {

@@ -42,20 +42,27 @@ hipError_t launch_rotate(const TurnArgs& a, const Rotary& r, bool bf16, hipStrea
 hipError_t launch_cache_append_rotated(const CacheView& c, const TokenRows& k, const TokenRows& v, const TurnArgs& q, const Rotary& r,
                                        bool in_bf16, const int64_t* slots, int64_t tokens, hipStream_t stream);
 
-// The angle of pair i at a token: quarter turns taken off, at most pi / 4 left.  false: the pair goes by no axis and stays as it is.
-__device__ __forceinline__ bool angle_of(const Rotary& r, int64_t token, int i, double* angle, int* quarters)
+// What the angle of pair i at a token is made of.  is: false where the pair goes by no axis and stays as it is.
+struct Place {
+    double at, freq;
+    bool is;
+};
+__device__ __forceinline__ Place place_of(const Rotary& r, int64_t token, int i)
 {
     const int axis = r.axis == nullptr ? 0 : r.axis[i];
-    if (axis >= r.axes) return false;
-    const double at = (double)r.positions[axis * r.stride + token], f = r.freqs[i];
+    const bool is = axis < r.axes;
+    return Place{(double)r.positions[(is ? axis : 0) * r.stride + token], r.freqs[i], is};
+}
+// The angle: quarter turns taken off, at most pi / 4 left.
+__device__ __forceinline__ double angle_of(const Place& p, int* quarters)
+{
     constexpr double kHi = 0.15915494309189533577, kLo = -9.839338337591243e-18;    // 1 / (2 pi) in two parts
-    const double g = f * kHi, g_rest = fma(f, kHi, -g) + f * kLo;
-    const double p = at * g, p_rest = fma(at, g, -p) + at * g_rest;
-    const double turn = (p - rint(p)) + p_rest;                   // in [-1/2, 1/2], and p_rest
+    const double g = p.freq * kHi, g_rest = fma(p.freq, kHi, -g) + p.freq * kLo;
+    const double x = p.at * g, x_rest = fma(p.at, g, -x) + p.at * g_rest;
+    const double turn = (x - rint(x)) + x_rest;                   // in [-1/2, 1/2], and x_rest
     const double quarter = rint(turn * 4.0);
-    *angle = (turn - quarter * 0.25) * 6.28318530717958647693;
     *quarters = (int)quarter;
-    return true;
+    return (turn - quarter * 0.25) * 6.28318530717958647693;
 }
 template <typename T>
 __device__ __forceinline__ void by_quarters(int q, float sign, T& c, T& s)
@@ -65,12 +72,12 @@ __device__ __forceinline__ void by_quarters(int q, float sign, T& c, T& s)
     s = ((q & 2) ? -sn : sn) * (T)sign;
 }
 
-// (cos, sin) of pair i at a token, in 32 bits
-__device__ __forceinline__ float2 turn_of(const Rotary& r, int64_t token, int i)
+// (cos, sin) at a place, in 32 bits
+__device__ __forceinline__ float2 turn_of(const Place& p, float sign)
 {
-    double angle;
+    if (!p.is) return float2{1.0f, 0.0f};
     int quarters;
-    if (!angle_of(r, token, i, &angle, &quarters)) return float2{1.0f, 0.0f};
+    const double angle = angle_of(p, &quarters);
     const float z = (float)angle, z2 = z * z;
     float p_s = 1.0f / 362880.0f, p_c = -1.0f / 3628800.0f;
     p_s = fmaf(p_s, z2, -1.0f / 5040.0f);
@@ -81,16 +88,16 @@ __device__ __forceinline__ float2 turn_of(const Rotary& r, int64_t token, int i)
     p_c = fmaf(p_c, z2, 1.0f / 24.0f);
     float s = (float)(angle + (double)(z2 * z * p_s));
     float c = (float)(fma(angle * angle, -0.5, 1.0) + (double)(z2 * z2 * p_c));
-    by_quarters(quarters, r.sign, c, s);
+    by_quarters(quarters, sign, c, s);
     return float2{c, s};
 }
 
 // The same in 64 bits (series up to z^15 and z^16: the next terms are below 2^-54).
-__device__ __forceinline__ double2 turn64_of(const Rotary& r, int64_t token, int i)
+__device__ __forceinline__ double2 turn64_of(const Place& p, float sign)
 {
-    double z;
+    if (!p.is) return double2{1.0, 0.0};
     int quarters;
-    if (!angle_of(r, token, i, &z, &quarters)) return double2{1.0, 0.0};
+    const double z = angle_of(p, &quarters);
     const double z2 = z * z;
     double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
     s = fma(s, z2, 1.0 / 6227020800.0);
@@ -108,7 +115,7 @@ __device__ __forceinline__ double2 turn64_of(const Rotary& r, int64_t token, int
     s = fma(s * z2, z, z);
     c = fma(c, z2, -0.5);
     c = fma(c, z2, 1.0);
-    by_quarters(quarters, r.sign, c, s);
+    by_quarters(quarters, sign, c, s);
     return double2{c, s};
 }
 

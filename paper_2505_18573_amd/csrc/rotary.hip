@@ -26,7 +26,7 @@ void rotate_kernel(TurnArgs a, Rotary r, int tokens_each, int heads_each)
     const int64_t token = first + (is ? t : 0);
     Unit<kBf16> now;
     if (is) now.load(a, r, token, h < a.heads ? h : 0, u);
-    for (int i = threadIdx.x; i < here * pairs; i += kTurnThreads) turns[i] = turn_of(r, first + i / pairs, i % pairs);
+    for (int i = threadIdx.x; i < here * pairs; i += kTurnThreads) turns[i] = turn_of(place_of(r, first + i / pairs, i % pairs), r.sign);
     __syncthreads();
     if (h >= a.heads || !is) return;
     float2 by[8];
