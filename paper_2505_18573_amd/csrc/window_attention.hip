@@ -904,7 +904,7 @@ struct Many {
                 for (int g = 0; g < 2; ++g) {
                     const float y = t[n >> 1][8 * (n & 1) + 2 * j + g];
                     const float e = __builtin_amdgcn_exp2f(kFp8 ? y - m : fmaf(y, scale, -m));
-                    sum[g] += e;
+                    t[n >> 1][8 * (n & 1) + 2 * j + g] = e;
                     u[g] = kFp8 ? e * factors[kBlock + 16 * n + 8 * h + 2 * j + g] : e;
                 }
                 uint32_t w2 = pack2(u[0], u[1]);
@@ -928,6 +928,11 @@ struct Many {
                     if (n < 3) {
                         if (d < kCols) ask(n + 1, d);
                         if (d % (kCols / 2) == kCols / 2 - 1) weigh(n + 1, d / (kCols / 2));
+                    } else {                                                   // the weights' sum between the last products
+                        constexpr int kAdds = 32 / (2 * kCols);
+#pragma unroll
+                        for (int j = d * kAdds; j < (d + 1) * kAdds; ++j) sum[j & 1] += t[j >> 4][j & 15];
+                        asm volatile("" : "+v"(sum[0]), "+v"(sum[1]));         // (or they all come behind)
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
