@@ -56,6 +56,8 @@ hipError_t launch_rotate(const TurnArgs& a, const Rotary& r, bool bf16, hipStrea
     const int64_t of_token = (int64_t)units * a.heads;
     int each = a.tokens <= 4 * (int64_t)compute_units() ? 1 : (int)((kTurnUnits + of_token - 1) / of_token);
     if (each > kTurnMostTokens) each = kTurnMostTokens;
+    const int least = (int)((a.tokens + (1 << 23) - 1) >> 23);                // threads of a launch below 2^32; 4 at most
+    if (each < least) each = least;
     if (each > kTurnThreads / units) each = kTurnThreads / units;
     const int heads_each = kTurnThreads / (each * units);
     const dim3 grid((uint32_t)((a.tokens + each - 1) / each));
