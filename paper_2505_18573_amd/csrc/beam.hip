@@ -12,6 +12,10 @@
 // of a beam, so only the order between beams is in question: where two neighbours of different beams among the results, or one that is
 // kept and one that is left out, are within 2e-6 of each other, the beams' sums are taken again in fp64, by the sequence's
 // workgroup, and the selection is made once more.  (One sequence in some hundreds; it takes 10 us and more for a beam.)
+//
+// Measured: 64 sequences x 8 beams, V = 151,936, bf16, keep 16: 38.7 us; the stream 27 (5.8 TB/s), the selection 11, a chain of phases with
+// barriers between (the beams' sums, the bound, chunks in order, their elements, these in order).  One sequence x 4, V = 32,000, fp32: 12.3 us, two
+// launches of latency.  A selection by the stream's last workgroup would need counters that start at zero.
 #include "beam.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
@@ -608,7 +612,8 @@ hipError_t launch_beam_reorder(const ReorderArgs& a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// A workgroup per page and head: its keys, values and scale bytes are four runs next to each other each.
+// A workgroup per page and head: its keys, values and scale bytes are four runs next to each other each.  (64 sequences x 8 beams, 4 heads of 128
+// in 8 bits: 6.8 us for 23 MB in and out, the tables before it 3.5; what bounds both is the start and a chain of two loads.)
 __global__ __launch_bounds__(256)
 void cache_copy_kernel(CacheView c, const int32_t* src, const int32_t* dst, const int32_t* counts)
 {

@@ -1,5 +1,8 @@
 """The calls of rotary positions, window attention and beam search through the binding's native code against its Python path:
 the same outputs bit for bit, the same errors."""
+import re
+from pathlib import Path
+
 import pytest
 import torch
 
@@ -7,6 +10,13 @@ import paper_2505_18573_amd as e3
 from tests.test_native_decode_calls import _outcome, _spoilt
 
 DEV = "cuda:0"
+
+
+def test_the_binding_repeats_the_header_s_constants():
+    text = (Path(e3.__file__).parent.parent / "include" / "e3.h").read_text()
+    header = {m[1]: int(m[2]) for m in re.finditer(r"(E3_\w+) *=? +\(?(-?\d+)\)?", text)}
+    for name in ("E3_ERR_SHAPE", "E3_MAX_AXES", "E3_MAX_BEAMS", "E3_MAX_KEEP"):
+        assert getattr(e3.binding, name) == header[name], name
 
 
 def _calls(dev):
