@@ -83,7 +83,8 @@ static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t 
     s.most[kOfWaves] = rows;
     // no more workers than steps: a small call's launches are small
     s.steps = (queries / kTile + rows) * heads * (visible / kStep + 4 + kCost);
-    s.workgroups = (int32_t)(s.most[kOfGroups] == 0 && s.steps < groups ? s.steps : groups);
+    const int64_t enough = s.most[kOfGroups] == 0 ? s.steps : s.steps / 2 + 2;
+    s.workgroups = (int32_t)(enough < groups ? enough : groups);
     s.workers[kOfGroups] = s.most[kOfGroups] > 0 ? s.workgroups : 0;
     s.workers[kOfWaves] = s.workgroups * kWaves;
     int64_t at = up(sizeof(Totals));
@@ -351,7 +352,7 @@ __device__ __forceinline__ Division divide_work(const Totals& t, int workgroups)
     const int64_t most[2] = {d.groups, (int64_t)(workgroups - d.groups) * kWaves};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int least = k == kOfGroups ? 4 : d.steps[k] < 512 ? 1 : d.steps[k] < 1024 ? 2 : 4;
+        const int least = d.steps[k] < 512 ? 1 : d.steps[k] < 1024 ? 2 : 4;
         const int64_t enough = (d.steps[k] + least - 1) / least;
         d.parts[k] = (int)(enough < most[k] ? enough : most[k]);
     }
@@ -389,11 +390,12 @@ struct Query {
     int lo, hi;                                 // tokens lo .. hi - 1, and the first ones
     bool is;
 };
-__device__ __forceinline__ Query query_of(const WindowArgs& a, int R, const Work& w, int head, int64_t index)
+// (a row's queries of a key head stay below 2^31: divided in 32 bits, a 64-bit division takes a hundred instructions more)
+__device__ __forceinline__ Query query_of(const WindowArgs& a, int R, const Work& w, int head, uint32_t index)
 {
     Query q;
-    q.is = index < (int64_t)w.n * R;
-    const int t = q.is ? (int)(index / R) : 0, h = q.is ? (int)(index % R) : 0;
+    q.is = index < (uint32_t)w.n * (uint32_t)R;
+    const int t = q.is ? (int)(index / (uint32_t)R) : 0, h = q.is ? (int)(index - (uint32_t)t * (uint32_t)R) : 0;
     const int p = w.len - w.n + t;
     q.token = w.offset + t;
     q.head = head * R + h;
@@ -757,10 +759,10 @@ struct Many {
         const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
         const Band band = band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kBlock);
         // the wave's queries
-        const int64_t first = (int64_t)w.tile * kTile + wave * 32, queries = (int64_t)w.n * R;
+        const uint32_t first = (uint32_t)w.tile * kTile + (uint32_t)wave * 32, queries = (uint32_t)w.n * (uint32_t)R;
         const bool busy = first < queries;
-        const int64_t end = first + 32 < queries ? first + 32 : queries;
-        const int p0 = w.len - w.n + (int)(first / R), p1 = w.len - w.n + (int)((end - 1) / R);
+        const uint32_t end = first + 32 < queries ? first + 32 : queries;
+        const int p0 = w.len - w.n + (int)(first / (uint32_t)R), p1 = w.len - w.n + (int)((end - 1) / (uint32_t)R);
         const int wave_hi = p1 + 1, wave_lo = p0 >= a.window ? p0 - a.window + 1 : 0;          // what any of them sees
         const int sure_hi = p0 + 1, sure_lo = p1 >= a.window ? p1 - a.window + 1 : 0;          // what all of them see
         const int tile_sure_hi = band.p0 + 1, tile_sure_lo = band.p1 >= a.window ? band.p1 - a.window + 1 : 0;
