@@ -247,6 +247,7 @@ void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, c
 // (A mixed batch 37.1 us, with a launch for the plan 43.0; 512 rows 303.8, 308.4.)  The list has an entry for every place; one without
 // a tile of a line has the beginning of the line's next one.
 constexpr int kOwnPlaces = 640;                 // what fits beside the keys of two workgroups
+constexpr int kOwnSteps = 1 << 20;              // times 4095 stretches: below 2^32
 struct OwnPlan {
     int offsets[kOwnPlaces + 1], lens[kOwnPlaces];
     int first[2][kOwnPlaces];
@@ -307,19 +308,21 @@ __device__ __forceinline__ Totals plan_own(const WindowArgs& a, const WindowShap
 
 // A line's records, in the workspace or in LDS; next(i, step): the record behind record i, which begins at that step.
 struct InWorkspace {
+    using Step = int64_t;
     const Work* list;
     int count;
     __device__ __forceinline__ int64_t first(int i) const { return list[i].first; }
     __device__ __forceinline__ Work get(int i) const { return list[i < count ? i : count - 1]; }
-    __device__ __forceinline__ int next(int i, int64_t) const { return i + 1; }
+    __device__ __forceinline__ int next(int i, Step) const { return i + 1; }
 };
-template <typename List> __device__ __forceinline__ int find_work(const List& list, int count, int64_t step);
+template <typename List> __device__ __forceinline__ int find_work(const List& list, int count, typename List::Step step);
 template <int kLine>
 struct InLds {
+    using Step = int32_t;
     const OwnPlan& p;
     const WindowArgs& a;
     int R, count;
-    __device__ __forceinline__ int64_t first(int i) const { return p.first[kLine][i]; }
+    __device__ __forceinline__ Step first(int i) const { return p.first[kLine][i]; }
     __device__ __forceinline__ Work get(int i) const
     {
         Work w;
@@ -330,7 +333,7 @@ struct InLds {
         w.cost = kCost + band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kLine == kOfWaves ? kStep : kBlock).steps;
         return w;
     }
-    __device__ __forceinline__ int next(int, int64_t step) const { return find_work(*this, count, step); }
+    __device__ __forceinline__ int next(int, Step step) const { return find_work(*this, count, step); }
 };
 
 // How the workgroups and stretches are divided, the same in every launch that asks.
@@ -352,8 +355,8 @@ __device__ __forceinline__ Division divide_work(const Totals& t, int workgroups)
     const int64_t most[2] = {d.groups, (int64_t)(workgroups - d.groups) * kWaves};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int least = d.steps[k] < 512 ? 1 : d.steps[k] < 1024 ? 2 : 4;
-        const int64_t enough = (d.steps[k] + least - 1) / least;
+        const int shift = d.steps[k] < 512 ? 0 : d.steps[k] < 1024 ? 1 : 2;    // a stretch has one step, two, four at least
+        const int64_t enough = (d.steps[k] + (1 << shift) - 1) >> shift;
         d.parts[k] = (int)(enough < most[k] ? enough : most[k]);
     }
     return d;
@@ -361,7 +364,7 @@ __device__ __forceinline__ Division divide_work(const Totals& t, int workgroups)
 
 // The last record that begins at or before a step: every lane looks at a 64th of what is left.
 template <typename List>
-__device__ __forceinline__ int find_work(const List& list, int count, int64_t step)
+__device__ __forceinline__ int find_work(const List& list, int count, typename List::Step step)
 {
     const int lane = threadIdx.x & 63;
     int first = 0, left = count;
@@ -1016,20 +1019,24 @@ struct Many {
 template <int kLine, typename List, typename F>
 __device__ __forceinline__ void along(const List& list, const Division& d, int heads, int part, Cut* cut, F f)
 {
+    using Step = typename List::Step;
     const bool writes = (threadIdx.x & (kLine == kOfGroups ? 255 : 63)) == 0;
     Cut found{-1, 0, 0, 0, 0, 0, 0, 0};
     if (part >= d.parts[kLine]) {
         if (writes) *cut = found;
         return;
     }
-    int64_t at = begin_of(part, d.steps[kLine], d.parts[kLine]);
-    const int64_t end = begin_of(part + 1, d.steps[kLine], d.parts[kLine]);
+    const Step steps = (Step)d.steps[kLine];
+    const int parts = d.parts[kLine];
+    auto begin_at = [&](int w) { return sizeof(Step) == 4 ? (Step)((uint32_t)w * (uint32_t)steps / (uint32_t)parts) : (Step)begin_of(w, steps, parts); };
+    Step at = begin_at(part);
+    const Step end = begin_at(part + 1), begin = at;
     int i = find_work(list, list.count, at);
-    const int64_t begin = at;
     Work w = uniform(list.get(i));
     while (at < end) {
-        const int64_t offset = at - w.first;
-        const int head = (int)divide(offset, w.cost), from = (int)(offset - (int64_t)head * w.cost);
+        const Step offset = at - (Step)w.first;
+        const int head = sizeof(Step) == 4 ? (int)((uint32_t)offset / (uint32_t)w.cost) : (int)divide(offset, w.cost);
+        const int from = (int)(offset - (Step)head * w.cost);
         const int n = end - at < w.cost - from ? (int)(end - at) : w.cost - from;
         Piece1 piece;
         piece.head = head;
@@ -1039,9 +1046,10 @@ __device__ __forceinline__ void along(const List& list, const Division& d, int h
         if (piece.to < 0) piece.to = 0;
         if (at == begin && from > kCost) {
             // the item began before: was its first step the worker's before?
-            const int64_t item = at - from;
-            if (begin_of(part - 1, d.steps[kLine], d.parts[kLine]) <= item + kCost)
-                found = Cut{w.row, w.tile, w.offset, w.n, w.len, head, part_of(item + w.cost - 1, d.steps[kLine], d.parts[kLine]), 0};
+            const Step item = at - from, last = item + w.cost - 1;
+            const int last_part = sizeof(Step) == 4 ? (int)((((uint32_t)last + 1) * (uint32_t)parts + (uint32_t)steps - 1) / (uint32_t)steps) - 1
+                                                    : part_of(last, steps, parts);
+            if (begin_at(part - 1) <= item + kCost) found = Cut{w.row, w.tile, w.offset, w.n, w.len, head, last_part, 0};
         }
         // what follows: the same tile's next head, or the next tile
         const bool done = head + 1 == heads && from + n == w.cost;
@@ -1199,7 +1207,7 @@ void window_join_kernel(WindowArgs a, WindowShape s, int group_slices, int wave_
 template <int D, bool kFp8>
 static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const WindowShape& s, char* ws, hipStream_t stream)
 {
-    if ((int64_t)a.tokens * s.R / kTile + a.rows <= kOwnPlaces && s.steps < (int64_t)1 << 31) {
+    if ((int64_t)a.tokens * s.R / kTile + a.rows <= kOwnPlaces && s.steps < kOwnSteps && s.workers[kOfWaves] < 4096) {
         window_kernel<D, kFp8, true><<<s.workgroups, 64 * kWaves, 0, stream>>>(c, a, s, ws);
     } else {
         window_plan_kernel<<<1, kPlanLanes, 0, stream>>>(a, s, c.heads, c.page_size, ws);
