@@ -19,14 +19,15 @@
 // Weights times values.  For few queries the weights enter as three bf16 numbers, all 24 bits of an fp32 weight, as memory is what
 // is waited for.  For tiles of prompts they enter as two, 16 bits and more: a weight is off by 2^-17 of itself at most, far below the output's own
 // rounding (2^-9 at best) unless an output's terms cancel to less than a hundredth, while one number alone (2^-9)
-// would add as much error as the output's rounding (and save a tenth of the time); the third product would cost a quarter more time.
+// would add as much error as the output's rounding (prompts 392 us for 465); the third product would cost a quarter more time.
 //
 // Measured, with the plan where there is one and the join: 512 rows of one query, 28 heads over 4 of 128, 8 bits, window 4096 of up to 7000
-// tokens 303 us, 5.1 TB/s: memory.  Prompts of 1000 to 4001 tokens, the same heads, 16 bits, window 1024: 445 us, 234 GFLOP of scores and
-// values, 350 with the second bf16 number of the weights, so 0.8 PFLOP/s (a large product of the library: 1.26): the matrix instructions of
-// the two waves on a SIMD are half of the time, the vector instructions the other half, at the 1.6 to 1.8 GHz that were
-// measured under this load.  A mixed batch of 33 rows of 1 to 300 queries, 12 heads over 2 of 64: 37 us; a workgroup has 1.3 items and
-// 7 steps, 6 us pass before the first item, 1.5 in a step, 3.5 into and out of an item, 8 in the join.  One row: 11 us, two launches.
+// tokens 303 us, 5.1 TB/s: memory.  Prompts of 1000 to 4001 tokens, the same heads, 16 bits, window 1024: 436 to 465 us from card to card, 234
+// GFLOP of scores and values, 350 with the second bf16 number of the weights, so 0.8 PFLOP/s (a large product of the library: 1.26):
+// the matrix instructions of the two waves on a SIMD are half of the time, the vector instructions the other half, at the 1.6 to 1.8
+// GHz that were measured under this load.  A mixed batch of 33 rows of 1 to 300 queries, 12 heads over 2 of 64: 35.5 us; a workgroup has
+// 1.3 items and 7 steps, 5 us pass before the first item, 1.5 in a step, 3.5 into and out of an item, 8 in the join.  One row: 10.7
+// us, two launches.  (The figures at the constants below are of these four.)
 #include "attention_step.h"
 #include "stretch.h"
 #include "vocab_pass.h"
@@ -40,11 +41,11 @@ constexpr int kWaves = 4;                       // of a workgroup
 constexpr int kFewQueries = 32;                 // an item of so many is a wave's
 constexpr int kTile = 128;                      // queries of a workgroup's item
 constexpr int kBlock = 64;                      // tokens of a workgroup's step
-// What an item costs besides its steps, in steps of either kind (prompts 440 us; with 1: 483, with 4: 436; 512 rows 303.8, 307.9, 302.5; one
-// row 11.1, 11.3, 11.3; mixed 37.1, 38.8, 37.0).
+// What an item costs besides its steps, in steps of either kind (prompts 465 us; with 1: 496, with 4: 456; 512 rows 303.2, 307.5, 302.9;
+// mixed 35.5, 36.5, 36.6).
 constexpr int kCost = 2;
 constexpr int kPerUnit = 2;                     // workgroups per compute unit, as registers and LDS allow
-constexpr float kBlockCost = 1.0f;              // a workgroup's step against four steps of its waves (mixed 37.1 us; 0.7: 38.7, 1.4: 37.9)
+constexpr float kBlockCost = 1.0f;              // a workgroup's step against four steps of its waves (mixed 35.5 us; 0.7: 37.4, 1.4: 35.6)
 
 enum { kOfGroups = 0, kOfWaves = 1 };           // the two lines
 
@@ -81,7 +82,8 @@ static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t 
     const int64_t queries = tokens * s.R;
     s.most[kOfGroups] = queries > kFewQueries ? queries / kTile + rows : 0;
     s.most[kOfWaves] = rows;
-    // no more workers than steps: a small call's launches are small
+    // No more workgroups than steps, half as many where there may be tiles, whose workgroups are four workers each of the other line too: a
+    // small call's launches are small (3 rows of 2 to 8 queries, 8 heads of 128: 14.8 us in kernels, with all workgroups 19.7).
     s.steps = (queries / kTile + rows) * heads * (visible / kStep + 4 + kCost);
     const int64_t enough = s.most[kOfGroups] == 0 ? s.steps : s.steps / 2 + 2;
     s.workgroups = (int32_t)(enough < groups ? enough : groups);
@@ -244,7 +246,7 @@ void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, c
 }
 
 // A batch of few rows, tiles and steps is planned by every workgroup of the attend launch for itself, in LDS and 32 bits: a launch less.
-// (A mixed batch 37.1 us, with a launch for the plan 43.0; 512 rows 303.8, 308.4.)  The list has an entry for every place; one without
+// (Mixed 35.5 us, with a launch for the plan 42.0; 512 rows 303.2, 309.0.)  The list has an entry for every place; one without
 // a tile of a line has the beginning of the line's next one.
 constexpr int kOwnPlaces = 640;                 // what fits beside the keys of two workgroups
 constexpr int kOwnSteps = 1 << 20;              // times 4095 stretches: below 2^32
@@ -355,7 +357,8 @@ __device__ __forceinline__ Division divide_work(const Totals& t, int workgroups)
     const int64_t most[2] = {d.groups, (int64_t)(workgroups - d.groups) * kWaves};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int shift = d.steps[k] < 512 ? 0 : d.steps[k] < 1024 ? 1 : 2;    // a stretch has one step, two, four at least
+        // a stretch has one step at least, two, four (one row 10.7 us; four: 12.8)
+        const int shift = d.steps[k] < 512 ? 0 : d.steps[k] < 1024 ? 1 : 2;
         const int64_t enough = (d.steps[k] + (1 << shift) - 1) >> shift;
         d.parts[k] = (int)(enough < most[k] ? enough : most[k]);
     }
@@ -841,14 +844,14 @@ struct Many {
             image_at = lds_at + image_of * kImage;
             meet();                                                            // all waves' parts are there, and the other image is done with
             // Of two workgroups on a compute unit the older one's waves go first and it would end earlier, the other then being alone:
-            // they take turns (prompts 440 us, without 449).
+            // they take turns (prompts 465 us, without 473).
             if (((s >> 2) ^ (int)(blockIdx.x / (gridDim.x / kPerUnit))) & 1) __builtin_amdgcn_s_setprio(1);
             else __builtin_amdgcn_s_setprio(0);
             const bool edge = !(whole && at + kBlock <= sure_hi && (at >= sure_lo || at + kBlock <= a.sinks));
             const u32x4* values = reinterpret_cast<const u32x4*>(image + kKeys) + h * D + col;
             const float* factors = reinterpret_cast<const float*>(extra);
             // Pieces of the keys are asked for six products ahead (left to itself the compiler asks for each right before its product
-            // and waits; three ahead: 443 us for 440), the next block's loads, which take the memory units 500 cycles a workgroup, one every other
+            // and waits; three ahead measured the same), the next block's loads, which take the memory units 500 cycles a workgroup, one every other
             // product.
             static_assert(kAll <= kDeep, "a load every other product");
             f32x16 t[2] = {zero(), zero()};
@@ -1218,7 +1221,7 @@ static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const W
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     // Queries of one workgroup of the join: 16 of a tile's; of a wave's item all, fewer where there are few workers, whose items have
-    // many parts (one row 11.1 us with 8, 11.8 with 4, 11.4 with 1; 512 rows, 512 workgroups, 310 with 4, 303 with 1).
+    // many parts (one row 10.7 us with 8, 11.3 with 4, 11.1 with 1; 512 rows, 512 workgroups, 311 with 4, 303 with 1).
     const int group_slices = kTile / 16, wave_slices = s.workgroups * kPerUnit < compute_units() ? 8 : s.workgroups < compute_units() * kPerUnit ? 4 : 1;
     const int blocks = s.workers[kOfGroups] * group_slices + s.workers[kOfWaves] * wave_slices;
     window_join_kernel<D><<<blocks, 256, 0, stream>>>(a, s, group_slices, wave_slices, ws);
