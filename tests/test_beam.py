@@ -254,6 +254,27 @@ def test_select_strides_outputs_graph_and_streams():
     assert e3.e3_beam_select(part[:0], scores[:0], 6)[0].shape == (0, 6)
 
 
+@pytest.mark.gpu
+def test_logits_and_pages_behind_four_gigabytes():
+    g, V, apart = torch.Generator().manual_seed(8), 1000, (1 << 31) + 8
+    z = (torch.randn((2, 3, V), generator=g) * 3).to(torch.bfloat16)
+    room = torch.empty(apart + 3 * V, dtype=torch.bfloat16, device=DEV)
+    far = room.as_strided((2, 3, V), (apart, V, 1))
+    far.copy_(z.to(DEV))
+    scores = -torch.rand((2, 3), generator=g)
+    check(e3.e3_beam_select(far, scores.to(DEV), 6), reference(z, scores, 6, 1.0))
+    del far, room
+    pages = 1_060_000
+    cache = e3.new_cache(pages, 64, 1, 64, device=DEV)
+    for t in cache:
+        t[pages - 3].view(torch.uint8).random_(1, 100)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    e3.e3_cache_copy(cache, i32([pages - 3]), i32([pages - 1]), i32([64]))
+    for t in cache:
+        a, b, c = (t[p].view(torch.uint8) for p in (pages - 3, pages - 1, pages - 2))
+        assert torch.equal(a, b) and bool((a > 0).all()) and not bool((c > 0).any())
+
+
 # ---------------------------------------------------------------- pages
 def reordered(parent, table, lens, page):
     """Lists: the new tables and lengths, and (source, destination, tokens) of the copies."""

@@ -169,6 +169,22 @@ def test_rotate_strides_and_places(dtype):
 
 
 @pytest.mark.gpu
+def test_more_than_four_gigabytes():
+    n, H, D = (1 << 21) + 5, 9, 128                               # of bf16, in place
+    r = rotary_of(D, 1, False, DEV)
+    g = torch.Generator().manual_seed(11)
+    x = torch.zeros((n, H, D), dtype=torch.bfloat16, device=DEV)
+    assert x.numel() * 2 > 1 << 32
+    pos = torch.arange(n, device=DEV)
+    some = torch.tensor([0, 1, (1 << 20) + 3, n - 2, n - 1])
+    part = torch.randn((len(some), H, D), generator=g).to(torch.bfloat16)
+    x[some.to(DEV)] = part.to(DEV)
+    assert e3.e3_rotate(x, r, pos, x) is x
+    want, size = turned(part, r.freqs, r.axis, some[None], False)
+    check(x[some.to(DEV)], want, size, torch.bfloat16)
+
+
+@pytest.mark.gpu
 def test_far_positions():
     # the angle of a position near 2^50, taken in rational numbers
     pi = Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798")

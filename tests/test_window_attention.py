@@ -215,6 +215,26 @@ def test_pages_that_do_not_exist_hide_their_tokens(cache_type):
 
 
 @pytest.mark.gpu
+def test_few_rows_in_a_wide_table():
+    # so wide that their steps might not fit the short plan
+    b = Batch([1, 0, 30, 200, 5], [40, 9, 64, 300, 5], 2, 8, 64, 32, FP8, 1 << 40, 0)
+    cache, offsets, table, lens, *rest = b.args()
+    b.check(*e3.e3_window_attention(b.q.to(DEV), cache, offsets, table, lens, *rest))
+    wide = torch.full((5, 40_000), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    b.check(*e3.e3_window_attention(b.q.to(DEV), cache, offsets, wide, lens, *rest))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cache_type,D,spare", [(BF16, 128, 270_000), (FP8, 64, 1_060_000)])
+def test_pages_behind_four_gigabytes(cache_type, D, spare):
+    b = Batch([1, 40, 3], [200, 500, 64], 4, 1, D, 64, cache_type, 100, 4, spare=spare)
+    assert spare * 64 * D * b.cache.k.element_size() > 1 << 32
+    # a stray page may be any, but those before the spare ones hold what others do
+    b.check(*e3.e3_window_attention(b.q.to(DEV), *b.args()))
+
+
+@pytest.mark.gpu
 def test_strides_outputs_and_queries_behind_the_last_row():
     b = Batch([3, 40, 1], [100, 77, 50], 4, 2, 128, 64, FP8, 60, 1)
     want, want_lse = e3.e3_window_attention(b.q.to(DEV), *b.args())
