@@ -11,11 +11,11 @@
 // Scores are compared in fp64.  Sums taken in fp32 leave ln sum exp off by 1e-7 as a rule (1e-6 at worst), the same for all tokens
 // of a beam, so only the order between beams is in question: where two neighbours of different beams among the results, or one that is
 // kept and one that is left out, are within 2e-6 of each other, the beams' sums are taken again in fp64, by the sequence's
-// workgroup, and the selection is made once more.  (One sequence in some hundreds; it takes 10 us and more for a beam.)
+// workgroup, and the selection is made once more.  (One sequence in some hundreds; V = 151,936 takes 19 us for a beam.)
 //
-// Measured: 64 sequences x 8 beams, V = 151,936, bf16, keep 16: 38.7 us; the stream 27 (5.8 TB/s), the selection 11, a chain of phases with
-// barriers between (the beams' sums, the bound, chunks in order, their elements, these in order).  One sequence x 4, V = 32,000, fp32: 12.3 us, two
-// launches of latency.  A selection by the stream's last workgroup would need counters that start at zero.
+// Measured: 64 sequences x 8 beams, V = 151,936, bf16, keep 16: 36.7 us; the stream 27 (5.8 TB/s), the selection 9.5, a chain of phases with
+// barriers between (the beams' sums 1.8, the bound 2, chunks in order 1, their elements 1.8, these in order and out 1.2).  One sequence x 4, V
+// = 32,000, fp32: 10.7 us, two launches of latency.  A selection by the stream's last workgroup would need counters that start at zero.
 #include "beam.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
@@ -247,6 +247,13 @@ struct SelectLds {
     Entry of_wave[kSelectWaves + 1][kMaxKeep + 2];
 };
 
+__device__ __forceinline__ int sum_of_eight(int x)              // over eight lanes
+{
+    x += dpp_i<kDppXor1>(x, x);
+    x += dpp_i<kDppXor2>(x, x);
+    return x + dpp_i<kDppHalfMirror>(x, x);
+}
+
 // to[r] = the r-th of n entries in order, r < most, by counting how many come before each: eight lanes an entry.
 __device__ __forceinline__ void in_order(const Entry* from, int n, Entry* to, int most)
 {
@@ -257,9 +264,7 @@ __device__ __forceinline__ void in_order(const Entry* from, int n, Entry* to, in
         int rank = 0;
 #pragma unroll 4
         for (int j = part; j < n; j += 8) rank += before(from[j], mine) ? 1 : 0;
-        rank += dpp_i<kDppXor1>(rank, rank);
-        rank += dpp_i<kDppXor2>(rank, rank);
-        rank += dpp_i<kDppHalfMirror>(rank, rank);
+        rank = sum_of_eight(rank);
         if (part == 0 && i < n && rank < most) to[rank] = mine;
     }
 }
@@ -274,7 +279,9 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
     const float* tops = reinterpret_cast<const float*>(ws) + row0 * s.chunks;
     const double c = kLog2e * per_logit;                                       // per_logit = 1 / tau
     const int keep = a.keep, need = keep + 1, most = (int)s.chunks;
-    constexpr int kEach = 8;
+    // Chunks a thread holds.  A pass over 1024 times as many costs 2.5 us, instructions that are not used cost their fetch: 16 beams of 297
+    // chunks 18.2 us with five, 20.6 with four, 18.3 with eight; 4 beams of 63 11.7, 11.6, 12.3.
+    constexpr int kEach = 5;
     const int entries = a.beams * most;
     float z[kEach];                                                            // asked for before the sums are
 #pragma unroll
@@ -342,16 +349,19 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
             if (wave == 0)
                 for (int i = lane; i < known; i += 64) lds.some[i] = lds.chunk[i];
             __syncthreads();
-            if (threadIdx.x < kGroups) {
-                const float x = lds.group[threadIdx.x];
+            {                                                                  // eight lanes a group
+                const int part = threadIdx.x & 7;
+                const float x = lds.group[threadIdx.x >> 3];
                 int above = 0, equal = 0;
-#pragma unroll 8
-                for (int j = 0; j < kGroups; j += 4) {
+#pragma unroll
+                for (int j = 4 * part; j < kGroups; j += 32) {
                     const float4 y = *reinterpret_cast<const float4*>(&lds.group[j]);
                     above += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
                     equal += (y.x == x) + (y.y == x) + (y.z == x) + (y.w == x);
                 }
-                if (above < need && above + equal >= need) lds.bound = x;       // equal ones store the same
+                above = sum_of_eight(above);
+                equal = sum_of_eight(equal);
+                if (part == 0 && above < need && above + equal >= need) lds.bound = x;          // equal ones store the same
             }
             __syncthreads();
             const float bound = lds.bound;
