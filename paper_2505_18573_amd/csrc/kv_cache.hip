@@ -199,18 +199,27 @@ __device__ __forceinline__ void append_store(const CacheView& c, const TokenRows
     float xb[4][4];
     // codes of four rows, and their scale bytes into the cache
     auto quantise = [&](float x[4][4], const int64_t row[4], const bool ok[4], uint8_t* scales, uint32_t code[4]) {
+        float most[4];                                            // (row by row each would wait for its own exchanges)
+        int e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float a = 0.0f;
+            most[i] = 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 x[i][j] = finite_or_nan(x[i][j]);
-                a = fmaxf(a, fabsf(x[i][j]));                     // NaN is passed over
+                most[i] = fmaxf(most[i], fabsf(x[i][j]));         // NaN is passed over
             }
-            const int e = exponent_for(row_max<D>(a));
-            code[i] = to_codes(x[i], e);
-            if (part == 0 && live && ok[i]) scales[row[i]] = (uint8_t)(e + 127);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most[i] = row_max<D>(most[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e[i] = exponent_for(most[i]);
+            code[i] = to_codes(x[i], e[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (part == 0 && live && ok[i]) scales[row[i]] = (uint8_t)(e[i] + 127);
     };
 
     int64_t row[4], brow[4];
@@ -365,31 +374,39 @@ void append_rotated_kernel(CacheView c, TokenRows k, TokenRows v, TurnArgs q, Ro
     const int base = lane & ~(D / 4 - 1);
     auto turn = [&](float (&x)[4][4]) {
         const bool mine = col < r.rot, upper = col >= pairs;
+        auto of_token = [&](int i) { return exact + (4 * half + i < here ? 4 * half + i : here - 1) * (D / 2); };
+        if (r.neighbours) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double2* of = of_token(i) + (mine ? col / 2 : 0);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const double2 w = of[j];
+                    const double a = x[i][2 * j], b = x[i][2 * j + 1];
+                    const float c0 = sticky(a * w.x - b * w.y), c1 = sticky(b * w.x + a * w.y);
+                    x[i][2 * j] = mine ? c0 : x[i][2 * j];
+                    x[i][2 * j + 1] = mine ? c1 : x[i][2 * j + 1];
+                }
+            }
+            return;
+        }
         // halves: pair of column c is c or c - pairs, its other column pairs away
         const int other = base + (upper ? part - pairs / 4 : part + pairs / 4);
+        float y[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[i][j] = __shfl(x[i][j], other);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = 4 * half + i < here ? 4 * half + i : here - 1;
-            const double2* of = exact + t * (D / 2);
-            if (r.neighbours) {
-                if (mine) {
+            const double2* of = of_token(i) + (!mine ? 0 : upper ? col - pairs : col);
+            double2 w[4];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const double2 w = of[col / 2 + j];
-                        const double a = x[i][2 * j], b = x[i][2 * j + 1];
-                        x[i][2 * j] = sticky(a * w.x - b * w.y);
-                        x[i][2 * j + 1] = sticky(b * w.x + a * w.y);
-                    }
-                }
-            } else {
+            for (int j = 0; j < 4; ++j) w[j] = of[j];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float y = __shfl(x[i][j], other);
-                    if (mine) {
-                        const double2 w = of[(upper ? col - pairs : col) + j];
-                        x[i][j] = sticky((double)x[i][j] * w.x + (double)y * (upper ? w.y : -w.y));
-                    }
-                }
+            for (int j = 0; j < 4; ++j) {
+                const float z = sticky((double)x[i][j] * w[j].x + (double)y[i][j] * (upper ? w[j].y : -w[j].y));
+                x[i][j] = mine ? z : x[i][j];
             }
         }
     };
