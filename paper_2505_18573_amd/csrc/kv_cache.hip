@@ -323,7 +323,7 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
 // pairs.  The other rows turn the queries, a share of the heads each: a thread keeps the (cos, sin) of eight pairs of a token and
 // takes head after head.  Either kind asks for its first rows, and for all that the angles are made of, before it makes them.
 // Bound by memory: 30,001 tokens, 28 query and 4 key heads of 128, bf16 in, 8 bits kept: 122 us, 525 MB, 4.3 TB/s; the fp64 turns of the
-// keys lie in its shadow.  512 tokens 8.8 us (without turning and queries 5.4): two chains of loads, the angles, the exchange of codes.
+// keys lie in its shadow.  512 tokens 8.0 us (without turning and queries 5.4): two chains of loads, the angles, the exchange of codes.
 // Queries in a launch of their own, five workgroups' waves per SIMD, and a thread asking for its next head early were slower.
 constexpr int kAppendThreads = 256;
 template <int D, bool kFp8, bool kBf16>
