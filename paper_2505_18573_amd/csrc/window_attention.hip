@@ -30,6 +30,7 @@
 // us, two launches.  (The figures at the constants below are of these four.)
 #include "attention_step.h"
 #include "stretch.h"
+#include "vocab_common.h"
 #include "vocab_pass.h"
 #include "window_attention.h"
 
@@ -173,6 +174,27 @@ __device__ __forceinline__ void tiles_in(const WindowArgs& a, int R, int64_t beg
     }
 }
 
+// The sum over the lanes up to this one: rows of sixteen, then the rows before.
+constexpr int kDppUp = 0x110;                   // + n: from n lanes before
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int from_before(int x) { return dpp_i<kCtrl, kRows>(0, x); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int64_t from_before(int64_t x)
+{
+    const uint32_t lo = (uint32_t)dpp_i<kCtrl, kRows>(0, (int)(uint32_t)x), hi = (uint32_t)dpp_i<kCtrl, kRows>(0, (int)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+template <typename T>
+__device__ __forceinline__ T sum_up_to(T x)
+{
+    x += from_before<kDppUp + 1, 0xF>(x);                                           // 1, 2, 4, 8 lanes before, in the row
+    x += from_before<kDppUp + 2, 0xF>(x);
+    x += from_before<kDppUp + 4, 0xF>(x);
+    x += from_before<kDppUp + 8, 0xF>(x);
+    x += from_before<kDppBcast15, 0xA>(x);                                           // the last lane of the row before, for odd rows
+    return x + from_before<kDppBcast31, 0xC>(x);                                     // lane 31, for the upper half
+}
+
 // Sums over the threads before this one, and over all: steps of both lines; tiles, the waves' in the upper half.
 template <int kOf>
 __device__ __forceinline__ void scan(const int64_t own[3], int64_t before[3], int64_t all[3], int64_t (*lds)[3])
@@ -180,12 +202,7 @@ __device__ __forceinline__ void scan(const int64_t own[3], int64_t before[3], in
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        before[k] = own[k];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t y = __shfl_up(before[k], d);
-            if (lane >= d) before[k] += y;
-        }
+        before[k] = sum_up_to(own[k]);
         if (lane == 63) lds[wave][k] = before[k];
         before[k] -= own[k];
         all[k] = 0;
@@ -279,12 +296,7 @@ __device__ __forceinline__ Totals plan_own(const WindowArgs& a, const WindowShap
     for (int u = begin; u < end; ++u) { own[0] += p.first[0][u]; own[1] += p.first[1][u]; }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        before[k] = own[k];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(before[k], d);
-            if (lane >= d) before[k] += y;
-        }
+        before[k] = sum_up_to(own[k]);
         if (lane == 63) p.sums[wave][k] = before[k];
         before[k] -= own[k];
     }
