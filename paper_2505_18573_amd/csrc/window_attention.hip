@@ -1142,19 +1142,19 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
 // fewer queries than lots of lanes have their parts spread over several.
 template <int D>
 __global__ __launch_bounds__(256, 8)
-void window_join_kernel(WindowArgs a, WindowShape s, int group_slices, int wave_slices, const char* ws)
+void window_join_kernel(WindowArgs a, WindowShape s, int group_shift, int wave_shift, const char* ws)
 {
     constexpr int kLanes4 = D / 4, kSubs = 256 / kLanes4;
     __shared__ float lds[kSubs][2 + D];
-    const int of_groups = s.workers[kOfGroups] * group_slices;
+    const int of_groups = s.workers[kOfGroups] << group_shift;
     const bool groups = (int)blockIdx.x < of_groups;
-    const int slices = groups ? group_slices : wave_slices;
+    const int shift = groups ? group_shift : wave_shift;                       // of the number of slices
     const int block = groups ? (int)blockIdx.x : (int)blockIdx.x - of_groups;
-    const int part = block / slices, slice = block % slices;
+    const int part = block >> shift, slice = block & ((1 << shift) - 1);
     const Cut cut = reinterpret_cast<const Cut*>(ws + s.at_cuts)[(groups ? 0 : s.workers[kOfGroups]) + part];
     if (cut.row < 0) return;
     const Work w{0, cut.row, cut.tile, cut.offset, cut.n, cut.len, 0};
-    const int places = groups ? kTile : kFewQueries, each = places / slices;
+    const int places = groups ? kTile : kFewQueries, each = places >> shift;
     const int64_t base = groups ? (int64_t)w.tile * kTile : 0, queries = (int64_t)w.n * s.R - base;
     const int first = slice * each, end = queries < first + each ? (int)queries : first + each;
     if (first >= end) return;
@@ -1162,14 +1162,15 @@ void window_join_kernel(WindowArgs a, WindowShape s, int group_slices, int wave_
     const float* o = reinterpret_cast<const float*>(ws + s.at_o[groups ? kOfGroups : kOfWaves]);
     const int sub = threadIdx.x / kLanes4, col = (threadIdx.x % kLanes4) * 4;
     const int parts = cut.last - part + 2;
-    const int wide = end - first < kSubs ? end - first : kSubs, spread = kSubs / wide;         // uniform
+    const int wide = end - first < kSubs ? end - first : kSubs;                                // uniform
+    const int spread_shift = 31 - __builtin_clz(kSubs) - (wide > 1 ? 32 - __builtin_clz(wide - 1) : 0), spread = 1 << spread_shift;
     for (int q0 = first; q0 < end; q0 += wide) {
-        const int query = q0 + sub / spread;
-        const bool is = sub / spread < wide && query < end;
+        const int query = q0 + (sub >> spread_shift);
+        const bool is = (sub >> spread_shift) < wide && query < end;
         float m = kNoScore, l = 0.0f;
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
         if (is) {
-            for (int i = sub % spread; i < parts; i += 4 * spread) {
+            for (int i = (sub & (spread - 1)); i < parts; i += 4 * spread) {
                 float2 pw[4];
                 f32x4 po[4];
 #pragma unroll
@@ -1197,7 +1198,7 @@ void window_join_kernel(WindowArgs a, WindowShape s, int group_slices, int wave_
 #pragma unroll
             for (int j = 0; j < 4; ++j) lds[sub][2 + col + j] = x[j];
             __syncthreads();
-            if (is && sub % spread == 0) {
+            if (is && (sub & (spread - 1)) == 0) {
                 for (int k = sub + 1; k < sub + spread; ++k) {
                     const float to = fmaxf(m, lds[k][0]);
                     const float f = __builtin_amdgcn_exp2f(m - to), g = __builtin_amdgcn_exp2f(lds[k][0] - to);
@@ -1208,7 +1209,7 @@ void window_join_kernel(WindowArgs a, WindowShape s, int group_slices, int wave_
                 }
             }
         }
-        if (is && sub % spread == 0) {
+        if (is && (sub & (spread - 1)) == 0) {
             const Query t = query_of(a, s.R, w, cut.head, base + query);
             const int64_t where = (int64_t)t.token * a.q_heads + t.head;
             const bool none = l == 0.0f && m == kNoScore;
@@ -1234,9 +1235,9 @@ static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const W
     if (err != hipSuccess) return err;
     // Queries of one workgroup of the join: 16 of a tile's; of a wave's item all, fewer where there are few workers, whose items have
     // many parts (one row 10.7 us with 8, 11.3 with 4, 11.1 with 1; 512 rows, 512 workgroups, 311 with 4, 303 with 1).
-    const int group_slices = kTile / 16, wave_slices = s.workgroups * kPerUnit < compute_units() ? 8 : s.workgroups < compute_units() * kPerUnit ? 4 : 1;
-    const int blocks = s.workers[kOfGroups] * group_slices + s.workers[kOfWaves] * wave_slices;
-    window_join_kernel<D><<<blocks, 256, 0, stream>>>(a, s, group_slices, wave_slices, ws);
+    const int group_shift = 3, wave_shift = s.workgroups * kPerUnit < compute_units() ? 3 : s.workgroups < compute_units() * kPerUnit ? 2 : 0;
+    const int blocks = (s.workers[kOfGroups] << group_shift) + (s.workers[kOfWaves] << wave_shift);
+    window_join_kernel<D><<<blocks, 256, 0, stream>>>(a, s, group_shift, wave_shift, ws);
     return hipGetLastError();
 }
 
