@@ -27,7 +27,7 @@
 // the matrix instructions of the two waves on a SIMD are half of the time, the vector instructions the other half, at the 1.6 to 1.8
 // GHz that were measured under this load.  A mixed batch of 33 rows of 1 to 300 queries, 12 heads over 2 of 64: 34.5 us; a workgroup has
 // 1.3 items and 7 steps, 5 us pass before the first item, 1.5 in a step, 3.5 into and out of an item, 8 in the join.  One row: 10.2
-// us, two launches.  (The figures at the constants below are of these four, a step or two before the last.)
+// us, two launches.  (The figures at the constants below compare builds that differ in nothing else, on these four.)
 #include "attention_step.h"
 #include "stretch.h"
 #include "vocab_common.h"
