@@ -68,7 +68,7 @@ struct WindowShape {
     int32_t R;                                  // query heads per key head
     int64_t most[2];                            // records of either line
     int32_t workgroups, workers[2];             // workers: at most
-    int64_t steps;                              // of either line at most
+    int64_t steps, most_cost;                   // of either line, of an item at most
     int64_t at_list[2], at_cuts, at_ml, at_o[2], bytes;
 };
 
@@ -85,7 +85,8 @@ static bool window_shape(int64_t rows, int64_t tokens, int64_t q_heads, int64_t 
     s.most[kOfWaves] = rows;
     // No more workgroups than steps, half as many where there may be tiles, whose workgroups are four workers each of the other line too: a
     // small call's launches are small (3 rows of 2 to 8 queries, 8 heads of 128: 14.8 us in kernels, with all workgroups 19.7).
-    s.steps = (queries / kTile + rows) * heads * (visible / kStep + 4 + kCost);
+    s.most_cost = visible / kStep + 4 + kCost;
+    s.steps = (queries / kTile + rows) * heads * s.most_cost;
     const int64_t enough = s.most[kOfGroups] == 0 ? s.steps : s.steps / 2 + 2;
     s.workgroups = (int32_t)(enough < groups ? enough : groups);
     s.workers[kOfGroups] = s.most[kOfGroups] > 0 ? s.workgroups : 0;
@@ -266,11 +267,13 @@ void window_plan_kernel(WindowArgs a, WindowShape s, int heads, int page_size, c
 // (Mixed 35.5 us, with a launch for the plan 42.0; 512 rows 303.2, 309.0.)  The list has an entry for every place; one without
 // a tile of a line has the beginning of the line's next one.
 constexpr int kOwnPlaces = 640;                 // what fits beside the keys of two workgroups
-constexpr int kOwnSteps = 1 << 20;              // times 4095 stretches: below 2^32
+constexpr int kOwnSteps = 1 << 20;              // of all; what may have more takes long enough for another launch not to count
+constexpr int kOwnCost = 1 << 16;               // of an item
 struct OwnPlan {
     int offsets[kOwnPlaces + 1], lens[kOwnPlaces];
     int first[2][kOwnPlaces];
     uint32_t row_tile[kOwnPlaces];
+    uint16_t cost[kOwnPlaces];
     int sums[kWaves][2];
 };
 __device__ __forceinline__ Totals plan_own(const WindowArgs& a, const WindowShape& s, int heads, int page_size, OwnPlan& p)
@@ -291,6 +294,7 @@ __device__ __forceinline__ Totals plan_own(const WindowArgs& a, const WindowShap
         p.first[line][u] = w.cost * heads;
         p.first[1 - line][u] = 0;
         p.row_tile[u] = (uint32_t)w.row << 16 | (uint32_t)w.tile;
+        p.cost[u] = (uint16_t)w.cost;
     });
     int own[2] = {0, 0}, before[2];
     for (int u = begin; u < end; ++u) { own[0] += p.first[0][u]; own[1] += p.first[1][u]; }
@@ -334,8 +338,7 @@ template <int kLine>
 struct InLds {
     using Step = int32_t;
     const OwnPlan& p;
-    const WindowArgs& a;
-    int R, count;
+    int count;
     __device__ __forceinline__ Step first(int i) const { return p.first[kLine][i]; }
     __device__ __forceinline__ Work get(int i) const
     {
@@ -344,17 +347,34 @@ struct InLds {
         const uint32_t x = p.row_tile[i];
         w.row = uniform((int)(x >> 16)); w.tile = uniform((int)(x & 0xFFFFu));
         w.offset = uniform(p.offsets[w.row]); w.n = uniform(p.offsets[w.row + 1]) - w.offset; w.len = uniform(p.lens[w.row]);
-        w.cost = kCost + band_of(R, w.tile, w.n, w.len, a.window, a.sinks, kLine == kOfWaves ? kStep : kBlock).steps;
+        w.cost = p.cost[i];
         return w;
     }
     __device__ __forceinline__ int next(int, Step step) const { return find_work(*this, count, step); }
 };
 
-// How the workgroups and stretches are divided, the same in every launch that asks.
+// How workgroups and steps are divided.
 struct Division {
     int64_t steps[2];
     int groups;                                 // workgroups of the line of workgroups
     int parts[2];                               // stretches
+};
+// The stretches of a line: the first `longer` of them have each + 1 steps, the others `each`.
+template <typename Step>
+struct Stretches {
+    Step each;
+    int longer;
+    __device__ __forceinline__ Stretches(Step steps, int parts)
+    {
+        each = sizeof(Step) == 4 ? (Step)((uint32_t)steps / (uint32_t)parts) : (Step)divide(steps, parts);
+        longer = (int)(steps - each * parts);
+    }
+    __device__ __forceinline__ Step begin(int w) const { return w * each + (w < longer ? w : longer); }
+    __device__ __forceinline__ int of(Step step) const
+    {
+        const Step first = longer * (each + 1), x = step < first ? step : step - first, by = step < first ? each + 1 : each;
+        return (step < first ? 0 : longer) + (sizeof(Step) == 4 ? (int)((uint32_t)x / (uint32_t)by) : (int)divide(x, by));
+    }
 };
 __device__ __forceinline__ Division divide_work(const Totals& t, int workgroups)
 {
@@ -1041,11 +1061,9 @@ __device__ __forceinline__ void along(const List& list, const Division& d, int h
         if (writes) *cut = found;
         return;
     }
-    const Step steps = (Step)d.steps[kLine];
-    const int parts = d.parts[kLine];
-    auto begin_at = [&](int w) { return sizeof(Step) == 4 ? (Step)((uint32_t)w * (uint32_t)steps / (uint32_t)parts) : (Step)begin_of(w, steps, parts); };
-    Step at = begin_at(part);
-    const Step end = begin_at(part + 1), begin = at;
+    const Stretches<Step> stretches((Step)d.steps[kLine], d.parts[kLine]);
+    Step at = stretches.begin(part);
+    const Step end = stretches.begin(part + 1), begin = at;
     int i = find_work(list, list.count, at);
     Work w = uniform(list.get(i));
     while (at < end) {
@@ -1061,10 +1079,8 @@ __device__ __forceinline__ void along(const List& list, const Division& d, int h
         if (piece.to < 0) piece.to = 0;
         if (at == begin && from > kCost) {
             // the item began before: was its first step the worker's before?
-            const Step item = at - from, last = item + w.cost - 1;
-            const int last_part = sizeof(Step) == 4 ? (int)((((uint32_t)last + 1) * (uint32_t)parts + (uint32_t)steps - 1) / (uint32_t)steps) - 1
-                                                    : part_of(last, steps, parts);
-            if (begin_at(part - 1) <= item + kCost) found = Cut{w.row, w.tile, w.offset, w.n, w.len, head, last_part, 0};
+            const Step item = at - from;
+            if (stretches.begin(part - 1) <= item + kCost) found = Cut{w.row, w.tile, w.offset, w.n, w.len, head, stretches.of(item + w.cost - 1), 0};
         }
         // what follows: the same tile's next head, or the next tile
         const bool done = head + 1 == heads && from + n == w.cost;
@@ -1094,7 +1110,7 @@ void window_kernel(CacheView c, WindowArgs a, WindowShape s, char* ws)
     const int workgroups = (int)gridDim.x;
     const Division d = divide_work(totals, workgroups);
     auto list = [&](auto line) {
-        if constexpr (kOwn) return InLds<decltype(line)::value>{own, a, s.R, uniform(totals.count[0])};
+        if constexpr (kOwn) return InLds<decltype(line)::value>{own, uniform(totals.count[0])};
         else return InWorkspace{reinterpret_cast<const Work*>(ws + s.at_list[decltype(line)::value]), uniform(totals.count[decltype(line)::value])};
     };
     Cut* cuts = reinterpret_cast<Cut*>(ws + s.at_cuts);
@@ -1223,7 +1239,7 @@ void window_join_kernel(WindowArgs a, WindowShape s, int group_shift, int wave_s
 template <int D, bool kFp8>
 static hipError_t launch_window(const CacheView& c, const WindowArgs& a, const WindowShape& s, char* ws, hipStream_t stream)
 {
-    if ((int64_t)a.tokens * s.R / kTile + a.rows <= kOwnPlaces && s.steps < kOwnSteps && s.workers[kOfWaves] < 4096) {
+    if ((int64_t)a.tokens * s.R / kTile + a.rows <= kOwnPlaces && s.steps < kOwnSteps && s.most_cost < kOwnCost) {
         window_kernel<D, kFp8, true><<<s.workgroups, 64 * kWaves, 0, stream>>>(c, a, s, ws);
     } else {
         window_plan_kernel<<<1, kPlanLanes, 0, stream>>>(a, s, c.heads, c.page_size, ws);
