@@ -651,10 +651,15 @@ struct Many {
         return piece ^ (kPieces == 16 ? token & 15 : (token >> 1) & 7);
     }
     // 16 bytes a lane from memory, `offset` behind `from`, into LDS, lane after lane from `to` on (from and to the same in all of them).
+    // A load into LDS needs a wait state behind a write of m0, or it may go by the place of the load before; nothing adds it to assembly.
+    // (m0 is named as lost so that no value of the compiler's own is kept in it; the warning is that it does not save it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
     static __device__ __forceinline__ void to_lds(const char* from, uint32_t offset, uint32_t to)
     {
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(from), "s"(to) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(from), "s"(to) : "memory", "m0");
     }
+#pragma clang diagnostic pop
     static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
     // Writes to LDS are there for all waves.  Loads from memory stay on their way.
     static __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
