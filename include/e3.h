@@ -631,10 +631,10 @@ int e3_verify_drafts(const void* logits, int dtype, int64_t rows, int32_t drafts
  * tau           host, finite and > 0 (E3_ERR_VALUE).
  * finished      [seqs][beams] uint8 or NULL, with eos_token in [0, V) (E3_ERR_VALUE).
  * parent_out, token_out [seqs][keep] int32, score_out [seqs][keep] fp32.  Places without a candidate: -1, -1, -inf.
- * A logit of -inf, or of -1e30 and less, has no probability and is never chosen.  A beam whose logits hold NaN or +inf (or z / tau beyond
- * fp32) offers nothing.
+ * A logit of -inf, or of -1e30 and less, has no probability and is never chosen.  A beam whose logits hold NaN or +inf offers nothing, nor
+ * does any that is not finished where log2(e) / tau is beyond fp32.
  * Scores are compared in fp64.  Where the order between two beams lies within 2e-6 the sums over their vocabularies are taken in
- * fp64 as well; beyond, fp32 sums decide, whose error is below that but for rows built to add up roundings.
+ * fp64 as well; beyond, fp32 sums decide, whose error is below that, wherever the logits lie, but for rows built to add up roundings.
  * workspace     device, 256-byte aligned (E3_ERR_ALIGN), at least e3_beam_workspace_bytes() (else E3_ERR_WORKSPACE); contents on entry ignored, no
  *               state between calls, to be used by one call at a time.
  */

@@ -4,11 +4,12 @@
 //
 // Two launches.
 //   stream   Every wave takes a segment of a row, eight 16-byte loads a lane, and leaves sum exp2 (fp32 in a lane, fp64 over the
-//            lanes) and the largest logit of every chunk of 512 columns.  The logits are read once; that is what bounds the call.
+//            lanes) relative to its largest logit, and the largest logit of every chunk of 512 columns.  The logits are read once; that is what bounds the call.
 //   select   A workgroup per sequence.  No element outside the `keep` best chunks can be among the `keep` best: each of those
 //            chunks holds one that comes before it (chunks are runs of columns, so this is also right for equal values, where the
 //            lower index comes first).  So the chunks' maxima are ranked first and only `keep` chunks are read again, 1 KB each.
-// Scores are compared in fp64.  Sums taken in fp32 leave ln sum exp off by 1e-7 as a rule (1e-6 at worst), the same for all tokens
+// Scores are compared in fp64, as differences of logits: base_b + (z - largest z) / tau.  Sums taken in fp32 leave ln sum exp off by 1e-7
+// as a rule (4e-7 the most of 27,648 beams: tau 0.02 to 3, logits around 0 to +-4000, 1000 to 151,936 columns), the same for all tokens
 // of a beam, so only the order between beams is in question: where two neighbours of different beams among the results, or one that is
 // kept and one that is left out, are within 2e-6 of each other, the beams' sums are taken again in fp64, by the sequence's
 // workgroup, and the selection is made once more.  (One sequence in some hundreds; V = 151,936 takes 19 us for a beam.)
@@ -32,7 +33,7 @@ constexpr double kNone = -INFINITY;
 
 template <bool kBf16> struct Segment { static constexpr int kCols = kVecs * 64 * (kBf16 ? 8 : 4), kChunks = kCols / kChunkCols; };
 
-struct Partial { double ref, sum; };            // sum of 2^(z c - ref), c = log2(e) / tau
+struct Partial { double ref, sum; };            // the largest logit, and the sum of 2^((z - ref) c), c = log2(e) / tau
 
 struct BeamShape {
     int64_t chunks, segments;                   // of a row (segments: of the narrower type)
@@ -67,7 +68,7 @@ __device__ __forceinline__ bool takes_part(float score) { return fabsf(score) < 
 // ---------------------------------------------------------------- stream
 template <bool kBf16>
 __global__ __launch_bounds__(64 * kStreamWaves)
-void beam_stream_kernel(BeamArgs a, BeamShape s, float c, double c64, char* ws)
+void beam_stream_kernel(BeamArgs a, BeamShape s, float c, char* ws)
 {
     constexpr int kPer = kBf16 ? 8 : 4, kCols = Segment<kBf16>::kCols, kChunks = Segment<kBf16>::kChunks, kOf = kVecs / kChunks;
     const int lane = threadIdx.x & 63;
@@ -134,20 +135,19 @@ void beam_stream_kernel(BeamArgs a, BeamShape s, float c, double c64, char* ws)
         }
         return sum;
     };
-    // One multiply-add a term: the lane's reference is rounded once, in the scaled domain, and is the same in every term.  Not where
-    // it is large (masks of -1e9 throughout): z c there is off its rounded like by more than the exponent holds.
-    double up, all;
+    // One multiply-add a term: the lane's reference is rounded once, in the scaled domain, and by how much (fused: exactly) is made up
+    // for in the lane's factor, so that everything is relative to a logit: c is off by 2^-25 of itself, and only differences of logits may see
+    // that.  Not where the reference is large (masks of -1e9 throughout): its rounding there is more than the exponent holds.
+    const float most_ref = wave_max(ref), below = ref - most_ref;
+    float sum, off = 0.0f;
     if (!__any(fabsf(ref) > 4096.0f) && c < 1024.0f) {
-        const float scaled = ref * c, sum = add_up([&](float z) { return fmaf(z, c, -scaled); });
-        const float most_scaled = wave_max(scaled);
-        up = most_scaled;
-        all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f(scaled - most_scaled));
+        const float scaled = ref * c;
+        off = fmaf(ref, c, -scaled);
+        sum = add_up([&](float z) { return fmaf(z, c, -scaled); });
     } else {
-        const float sum = add_up([&](float z) { return (z - ref) * c; });
-        const float most_ref = wave_max(ref);
-        up = (double)most_ref * c64;
-        all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f((ref - most_ref) * c));
+        sum = add_up([&](float z) { return (z - ref) * c; });
     }
+    const double all = wave_sum((double)sum * (double)__builtin_amdgcn_exp2f(fmaf(below, c, -off)));
     // The chunks' maxima over the wave: halves trade two chunks each and keep one, rows of sixteen lanes again; what is left is a row's.
     float* tops = reinterpret_cast<float*>(ws) + row * s.chunks + segment * kChunks;
     float in_half[kChunks / 2], in_row[kChunks / 4];
@@ -170,7 +170,7 @@ void beam_stream_kernel(BeamArgs a, BeamShape s, float c, double c64, char* ws)
         const int chunk = i + ((lane >> 4) & 1) * (kChunks / 4) + (lane >> 5) * (kChunks / 2);
         if ((lane & 15) == i && segment * kChunks + chunk < s.chunks) tops[chunk] = in_row[i];
     }
-    if (lane == 0) reinterpret_cast<Partial*>(ws + s.at_partials)[row * s.segments + segment] = Partial{up, all};
+    if (lane == 0) reinterpret_cast<Partial*>(ws + s.at_partials)[row * s.segments + segment] = Partial{(double)most_ref, all};
 }
 
 // ---------------------------------------------------------------- select
@@ -232,7 +232,9 @@ constexpr int kGroups = kSelectThreads / 8;     // of eight lanes, whose maxima 
 constexpr int kRoom = 256;                      // chunks above the bound
 constexpr int kElements = kMaxKeep * (kMaxKeep + 1) / 2;          // of the r-th best chunk at most keep - r elements
 struct SelectLds {
-    double base[kMaxBeams];                     // s_b - ln sum exp, -inf: the beam offers nothing
+    // score(b, v) = base + (z - top) / tau: relative to the beam's largest logit, or logits far from zero would cost the score its last digits
+    double base[kMaxBeams];                     // s_b - ln sum exp((z - top) / tau), a finished beam's s_b, -inf: the beam offers nothing
+    double top[kMaxBeams];
     double log2_sum[kMaxBeams];
     double sums[kSelectWaves];
     int ends[kMaxBeams];                        // a finished beam
@@ -296,24 +298,24 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
         const Partial mine = parts[lane < s.segments ? lane : 0];
         const float score = a.scores[row0 + b];
         const bool ends = a.finished && a.finished[row0 + b];
-        double base = kNone, total = 0.0;
+        double base = kNone, total = 0.0, up = 0.0;
         if (takes_part(score)) {
             if (ends) {
                 base = score;
             } else {
-                double up = lane < s.segments ? mine.ref : -INFINITY;
+                up = lane < s.segments ? mine.ref : -INFINITY;
                 for (int64_t i = lane + 64; i < s.segments; i += 64) up = fmax(up, parts[i].ref);
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) up = fmax(up, __shfl_xor(up, d));
-                double sum = lane < s.segments ? mine.sum * exp2_of(fmax(mine.ref - up, -1000.0)) : 0.0;
-                for (int64_t i = lane + 64; i < s.segments; i += 64) sum += parts[i].sum * exp2_of(fmax(parts[i].ref - up, -1000.0));
+                double sum = lane < s.segments ? mine.sum * exp2_of(fmax((mine.ref - up) * c, -1000.0)) : 0.0;
+                for (int64_t i = lane + 64; i < s.segments; i += 64) sum += parts[i].sum * exp2_of(fmax((parts[i].ref - up) * c, -1000.0));
                 sum = wave_sum(sum);
-                total = up + log2(sum);
+                total = log2(sum);
                 // NaN and +inf make the sum no number; a row without any probability has none
                 if (sum > 0.0 && sum < INFINITY && fabs(up) < INFINITY) base = score - total * kLn2;
             }
         }
-        if (lane == 0) { lds.base[b] = base; lds.log2_sum[b] = total; lds.ends[b] = ends; }
+        if (lane == 0) { lds.base[b] = base; lds.top[b] = up; lds.log2_sum[b] = total; lds.ends[b] = ends; }
     }
     if (threadIdx.x == 0) lds.near = 0;
     __syncthreads();
@@ -332,9 +334,9 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
                 if (e < entries) {
                     if (from > 0 || round > 0) z[i] = tops[e];
                     const int b = most > 1 ? (int)__umulhi((uint32_t)e, s.per_chunk) : e;     // e / most
-                    const double base = lds.base[b];
+                    const double base = lds.base[b], top = lds.top[b];
                     const bool ends = lds.ends[b] != 0;
-                    if (base > kNone && (ends ? e - b * most == a.eos / kChunkCols : z[i] > kNoLogit)) key[i] = ends ? base : base + (double)z[i] * per_logit;
+                    if (base > kNone && (ends ? e - b * most == a.eos / kChunkCols : z[i] > kNoLogit)) key[i] = ends ? base : base + ((double)z[i] - top) * per_logit;
                 }
                 if (key[i] > mine.key) mine = Entry{key[i], e};
             }
@@ -431,7 +433,8 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
             }
             const char* row = row_of(a, row0 + b, kBf16 ? 2 : 4);
             const int64_t first = (int64_t)chunk * kChunkCols + lane * 8;
-            const double base = lds.base[b];
+            const double base = lds.base[b], top_logit = lds.top[b];
+            const auto key_of = [&](float z) { return base + ((double)z - top_logit) * per_logit; };
             float x[8];
             if (first + 8 <= a.V) {
                 const u32x4* p = reinterpret_cast<const u32x4*>(row + first * (kBf16 ? 2 : 4));
@@ -447,7 +450,7 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
             unsigned long long reach[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                reach[j] = __ballot(x[j] > kNoLogit && base + (double)x[j] * per_logit >= border);
+                reach[j] = __ballot(x[j] > kNoLogit && key_of(x[j]) >= border);
                 n += (int)__popcll(reach[j]);
             }
             if (n <= room) {
@@ -457,7 +460,7 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     if ((reach[j] >> lane) & 1ull)
-                        lds.element[at + (int)__popcll(reach[j] & ((1ull << lane) - 1ull))] = Entry{base + (double)x[j] * per_logit, b * (int)a.V + (int)first + j};
+                        lds.element[at + (int)__popcll(reach[j] & ((1ull << lane) - 1ull))] = Entry{key_of(x[j]), b * (int)a.V + (int)first + j};
                     at += (int)__popcll(reach[j]);
                 }
                 continue;
@@ -475,7 +478,7 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
                 const float top = wave_max(best);
                 const int l = (int)__builtin_ctzll(__ballot(best == top));
                 if (lane == l) {
-                    lds.element[at + n] = Entry{base + (double)top * per_logit, b * (int)a.V + (int)first + j0};
+                    lds.element[at + n] = Entry{key_of(top), b * (int)a.V + (int)first + j0};
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         if (j == j0) x[j] = -INFINITY;
@@ -511,7 +514,7 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
                         const double base = lds.base[b];
                         const bool ends = lds.ends[b] != 0;
                         if (!(base > kNone) || (ends && e - b * most != a.eos / kChunkCols)) continue;
-                        const Entry of{ends ? base : base + (double)tops[e] * per_logit, e};
+                        const Entry of{ends ? base : base + ((double)tops[e] - lds.top[b]) * per_logit, e};
                         if (last.key - of.key < kNear && before(border_chunk, of)) left_out(of.key, b);
                     }
                 }
@@ -532,10 +535,10 @@ void beam_select_kernel(BeamArgs a, BeamShape s, double per_logit, const char* w
         for (int b = 0; b < a.beams; ++b) {                                    // uniform
             if (((near >> b) & 1u) == 0 || lds.ends[b]) continue;
             const char* row = row_of(a, row0 + b, kBf16 ? 2 : 4);
-            const double total = lds.log2_sum[b];
+            const double total = lds.log2_sum[b], top = lds.top[b];
             double sum = 0.0;
             for (int64_t col = threadIdx.x; col < a.V; col += kSelectThreads) {
-                const double x = fma((double)logit_at<kBf16>(row, col), c, -total);
+                const double x = fma((double)logit_at<kBf16>(row, col) - top, c, -total);
                 if (x > -1000.0) sum += exp2_of(x);
             }
             sum = wave_sum(sum);
@@ -558,8 +561,8 @@ hipError_t launch_beam_select(const BeamArgs& a, bool bf16, void* workspace, hip
     const float c = (float)(kLog2e / (double)a.tau);
     const int64_t items = a.seqs * a.beams * s.segments;
     const dim3 grid((uint32_t)((items + kStreamWaves - 1) / kStreamWaves));
-    if (bf16) beam_stream_kernel<true><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, kLog2e / (double)a.tau, ws);
-    else beam_stream_kernel<false><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, kLog2e / (double)a.tau, ws);
+    if (bf16) beam_stream_kernel<true><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, ws);
+    else beam_stream_kernel<false><<<grid, 64 * kStreamWaves, 0, stream>>>(a, s, c, ws);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     if (bf16) beam_select_kernel<true><<<(uint32_t)a.seqs, kSelectThreads, 0, stream>>>(a, s, 1.0 / (double)a.tau, ws);

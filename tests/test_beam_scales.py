@@ -1,0 +1,68 @@
+"""Beam search's scores and order wherever a beam's logits lie: softmax does not change under a shift, neither may the selection.
+
+A score is within 2e-6 (the sums in fp32: about log2 V roundings of exponents below log2 V and of the sums, 2^-24 each, most of which cancel
+over thousands of terms) and its own rounding, 2^-24 of it; candidates that are further apart than that keep their order."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_18573_amd as e3
+from tests.test_beam import check, reference
+
+DEV = "cuda:0"
+
+
+def shifted_reference(z, scores, keep, tau, *rest):
+    """The definition with each beam's largest logit taken off first, which is exact in 64 bits."""
+    x = z.double()
+    x = torch.where(x <= -1e30, torch.full_like(x, -math.inf), x)
+    return reference(x - x.amax(-1, keepdim=True), scores, keep, float(np.float32(tau)), *rest)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tau", [0.02, 0.1, 0.3, 0.9, 1.0, 3.0])
+@pytest.mark.parametrize("offset", [20.0, 100.0, 1000.0, 4000.0, 1e6])
+def test_scores_of_shifted_logits(dtype, tau, offset):
+    g, n, V = torch.Generator().manual_seed(int(offset)), 6, 8000
+    z = torch.randn((n, 4, V), generator=g) * 3
+    z = (z + torch.tensor([offset, -offset, 0.0, offset / 3])[:, None]).to(dtype)
+    scores = -torch.rand((n, 4), generator=g)
+    # in bf16 many logits are equal far from zero; ties and what lies nearer than fp32's rounding of z / tau go by the definition all the same
+    check(e3.e3_beam_select(z.to(DEV), scores.to(DEV), 40, tau), shifted_reference(z, scores, 40, tau))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tau", [0.02, 0.1, 0.5, 0.9, 1.0])
+@pytest.mark.parametrize("offset", [2.0, 64.0, 256.0, 1024.0, 4000.0])
+def test_order_of_beams_that_differ_by_a_shift(tau, offset):
+    # the same logits in every beam, in another order and shifted (steps of 2^-10: the shift is exact); scores 3e-6 and more apart
+    g, n, V = torch.Generator().manual_seed(int(offset)), 32, 20_000
+    one = torch.round(torch.randn((n, V), generator=g) * 3 * 1024) / 1024
+    z = torch.stack([torch.stack([one[i, torch.randperm(V, generator=g)] for _ in range(3)]) for i in range(n)])
+    z = z + offset * torch.stack([torch.randperm(3, generator=g) - 1 for _ in range(n)])[..., None]
+    scores = torch.stack([torch.randperm(3, generator=g) for _ in range(n)]) * 3e-6
+    want = shifted_reference(z, scores, 12, tau)
+    check(e3.e3_beam_select(z.to(DEV), scores.to(DEV), 12, tau), want)
+    check(e3.e3_beam_select(z.to(DEV), scores.to(DEV), 1, tau), [w[:, :1] for w in want])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tau", [1e-3, 1.0, 1e20, 1e27])
+def test_very_large_logits(tau):
+    # a score is a difference of two logits, not of two numbers of 1e29 / tau
+    g, V = torch.Generator().manual_seed(9), 3000
+    z = torch.randn((4, 3, V), generator=g) * 1e29
+    z[1, :, 100:2900] = -math.inf
+    scores = -torch.rand((4, 3), generator=g)
+    check(e3.e3_beam_select(z.to(DEV), scores.to(DEV), 20, tau), shifted_reference(z, scores, 20, tau))
+
+
+@pytest.mark.gpu
+def test_a_temperature_whose_inverse_is_beyond_fp32():
+    z, scores = torch.randn((1, 2, 800), device=DEV), torch.tensor([[-1.0, -2.0]], device=DEV)
+    assert [t.tolist() for t in e3.e3_beam_select(z, scores, 3, 1e-39)] == [[[-1] * 3], [[-1] * 3], [[-math.inf] * 3]]
+    finished = torch.tensor([[0, 1]], dtype=torch.uint8, device=DEV)
+    assert [t.tolist() for t in e3.e3_beam_select(z, scores, 2, 1e-39, finished, 5)] == [[[1, -1]], [[5, -1]], [[-2.0, -math.inf]]]
