@@ -66,3 +66,21 @@ def test_a_temperature_whose_inverse_is_beyond_fp32():
     assert [t.tolist() for t in e3.e3_beam_select(z, scores, 3, 1e-39)] == [[[-1] * 3], [[-1] * 3], [[-math.inf] * 3]]
     finished = torch.tensor([[0, 1]], dtype=torch.uint8, device=DEV)
     assert [t.tolist() for t in e3.e3_beam_select(z, scores, 2, 1e-39, finished, 5)] == [[[1, -1]], [[5, -1]], [[-2.0, -math.inf]]]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tau", [0.01, 1.0, 1e10, 1e28, 1e30, 3e38])
+def test_masks_at_any_temperature(dtype, tau):
+    # at or below -1e30 there is no probability, whatever tau makes of it
+    g, V = torch.Generator().manual_seed(10), 6000
+    z = (torch.randn((4, 4, V), generator=g) * (1.0 if tau < 1e28 else 3e28)).to(dtype)
+    low = torch.tensor(-1e30).to(dtype)
+    low = low if low <= -1e30 else torch.tensor(-1.01e30).to(dtype)
+    z[0, :, 7:] = low                                             # a few tokens allowed
+    z[1, 2] = low                                                 # none
+    z[2, :, ::2] = low
+    z[2, 0, 5000:] = -math.inf
+    z[3, :, 100:5900] = -3e38
+    scores = -torch.rand((4, 4), generator=g)
+    check(e3.e3_beam_select(z.to(DEV), scores.to(DEV), 16, tau), shifted_reference(z, scores, 16, tau))
