@@ -651,6 +651,9 @@ int e3_beam_select(const void* logits, int dtype, int64_t seqs, int32_t beams, i
  * full and own the one that their next token goes to (entry row_lens[r] / page_size).  A parent's first child goes on in
  * that page; every other child takes over the page of a beam without children (there are as many), into which the parent's tokens are to be
  * copied: by e3_cache_copy, once for every layer's cache.
+ * All other entries are the parent's, those behind that page too: rows with the same parent name the same pages there.  Where tables are
+ * filled ahead they have to be set anew before a row's tokens reach them, to pages that no other row names (if a sequence's rows have the
+ * same length: to those that the row had there before the call).
  *
  * parent        [seqs][beams] int32, within the sequence; an entry outside [0, beams) stands for the row itself.
  * row_pages     [seqs * beams][row_width] int32, row_lens [seqs * beams] int32 (tokens): before.

@@ -1111,7 +1111,8 @@ def e3_beam_reorder(parent: torch.Tensor, row_pages: torch.Tensor, row_lens: tor
                     pages_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None, src_out: Optional[torch.Tensor] = None,
                     dst_out: Optional[torch.Tensor] = None, counts_out: Optional[torch.Tensor] = None):
     """The beams' page tables after a selection: parent int32 [seqs, beams], row_pages int32 [seqs * beams, width], row_lens int32
-    [seqs * beams].  Returns (row_pages, row_lens, src, dst, counts), the last three (int32 [seqs * beams]) for e3_cache_copy."""
+    [seqs * beams].  Returns (row_pages, row_lens, src, dst, counts), the last three (int32 [seqs * beams]) for e3_cache_copy.  Entries behind
+    the page of a row's next token are its parent's, the same in all of the parent's children: set them anew where tables are filled ahead."""
     res = _ordinary("beam_reorder", parent, row_pages, row_lens, page_size, pages_out, lens_out, src_out, dst_out, counts_out)
     if res is not None:
         return res

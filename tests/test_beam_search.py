@@ -72,3 +72,41 @@ def test_beams_pages_attention_and_selection(cache_type, beams, window, sinks):
 def test_the_example_runs(capsys):
     example().main(3)
     assert capsys.readouterr().out.count("best beam") == 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("beams", [1, 3, 8])
+def test_tables_that_are_filled_ahead(beams):
+    # Every row has all the pages that it can need from the start.  Behind the page of the next token a table is the parent's after a
+    # reordering; with the row's own entries set there again no page that is written to has two names, and pages hold the beams' tokens.
+    g = torch.Generator().manual_seed(beams)
+    seqs, page, width, D = 4, 32, 4, 64
+    rows = seqs * beams
+    cache = e3.new_cache(rows * width, page, 1, D, torch.bfloat16, DEV)
+    table = torch.randperm(rows * width, generator=g).reshape(rows, width).to(torch.int32).to(DEV)
+    lens = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    held = torch.zeros((rows, 0), dtype=torch.int64)              # the numbers that stand for a row's tokens
+    index = torch.arange(width, device=DEV)
+    for step in range(width * page - 1):
+        new = torch.randint(0, 200, (rows,), generator=g)         # exact in bf16
+        held = torch.cat([held, new[:, None]], 1)
+        slots = table.gather(1, (lens // page).long()[:, None])[:, 0].long() * page + lens % page
+        x = new.to(DEV).to(torch.bfloat16)[:, None, None].expand(rows, 1, D).contiguous()
+        e3.e3_cache_append(cache, x, x, slots)
+        lens = lens + 1
+        parent = torch.randint(0, beams, (seqs, beams), generator=g).to(torch.int32)
+        before = table
+        table, lens, src, dst, counts = e3.e3_beam_reorder(parent.to(DEV), before, lens, page)
+        e3.e3_cache_copy(cache, src, dst, counts)
+        of = (torch.arange(seqs)[:, None] * beams + parent).reshape(-1)
+        held = held[of]
+        behind = index > (lens // page)[:, None]
+        assert torch.equal(table[behind], before[of.to(DEV)][behind])
+        table = torch.where(behind, before, table)
+        written = table[index >= (lens // page)[:, None]]
+        assert written.unique().numel() == written.numel()
+        if step % 31 == 30 or step == width * page - 2:
+            at = torch.arange(step + 1, device=DEV)
+            for r in range(rows):
+                k, v = e3.e3_cache_read(cache, table[r].long()[at // page] * page + at % page)
+                assert torch.equal(k[:, 0, 0].long().cpu(), held[r]) and torch.equal(v[:, 0, D - 1].long().cpu(), held[r])
