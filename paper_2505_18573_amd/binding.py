@@ -777,6 +777,22 @@ def e3_cache_read(cache: E3Cache, slots: torch.Tensor, dtype: torch.dtype = torc
     return outs[0], outs[1]
 
 
+def _integer(v, bits: int, name: str) -> int:
+    """An int that C takes in so many bits (ctypes would cut it)."""
+    v = int(v)
+    if not -(1 << (bits - 1)) <= v < 1 << (bits - 1):
+        raise ValueError(f"{name} must fit {bits} bits")
+    return v
+
+
+def _int32(v, name: str) -> int:
+    return _integer(v, 32, name)
+
+
+def _int64(v, name: str) -> int:
+    return _integer(v, 64, name)
+
+
 class E3Rotary(NamedTuple):
     """Rotary positions (e3_rotary in include/e3.h): freqs fp64 [pairs], radians per position; axis uint8 [pairs] or None (one axis);
     neighbours: pairs of columns (2 i, 2 i + 1) instead of (i, i + pairs)."""
@@ -961,6 +977,7 @@ def e3_window_attention(q: torch.Tensor, cache: E3Cache, query_offsets: torch.Te
         return res
     c = _cache(cache)
     dev = cache[0].device
+    window, sinks = _int64(window, "window"), _int64(sinks, "sinks")
     if q.dim() != 3:
         raise ValueError(f"q must be [tokens, q_heads, {c.head_dim}]")
     tokens, q_heads, D = q.shape
@@ -982,7 +999,7 @@ def e3_window_attention(q: torch.Tensor, cache: E3Cache, query_offsets: torch.Te
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
     rc = lib().e3_window_attention(C.byref(c), _ptr(q), tokens, q_heads, _step(q, 0), _step(q, 1), _ptr(query_offsets), rows, _ptr(row_pages),
-                                   row_width, _ptr(row_lens), int(window), int(sinks), float(scale), _ptr(out), _ptr(lse_out), _ptr(workspace),
+                                   row_width, _ptr(row_lens), window, sinks, float(scale), _ptr(out), _ptr(lse_out), _ptr(workspace),
                                    workspace.numel() * workspace.element_size(), _stream(dev))
     if rc != E3_OK:
         raise E3Error(rc, "e3_window_attention")
@@ -1054,14 +1071,6 @@ def e3_verify_drafts(logits: torch.Tensor, draft_tokens: Optional[torch.Tensor],
     if rc != E3_OK:
         raise E3Error(rc, "e3_verify_drafts")
     return (accepted_out, *outs)
-
-
-def _int32(v, name: str) -> int:
-    """An int that C takes as int32_t (ctypes would cut it)."""
-    v = int(v)
-    if not -(1 << 31) <= v < 1 << 31:
-        raise ValueError(f"{name} must fit 32 bits")
-    return v
 
 
 def e3_beam_workspace_bytes(seqs: int, beams: int, V: int) -> int:

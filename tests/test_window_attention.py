@@ -295,3 +295,21 @@ def test_agrees_with_prefix_attention():
     args = b.args()
     want, want_lse = e3.e3_prefix_attention(b.q.to(DEV)[:, None], b.cache, None, None, None, args[2], args[3], b.scale)
     assert bool((out.float() - want[:, 0].float()).abs().max() <= 2.0 ** -7) and bool((lse - want_lse[:, 0]).abs().max() <= 4e-5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("far", [1 << 63, 1 << 64, (1 << 64) + 5, -(1 << 64) + 7])
+def test_numbers_that_64_bits_do_not_hold(far):
+    # cut to 64 bits they would be other windows; the largest that they hold is plain causal attention
+    cache = e3.new_cache(4, 32, 1, 64, torch.bfloat16, DEV)
+    for t in cache[:2]:
+        t.normal_()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    q = torch.randn((3, 2, 64), device=DEV).to(torch.bfloat16)
+    args = q, cache, i32([0, 3]), i32([[0, 1, 2]]), i32([70])
+    for window, sinks in ((far, 0), (5, far)):
+        with pytest.raises(ValueError, match="64 bits"):
+            e3.e3_window_attention(*args, window, sinks, 0.125)
+    want = e3.e3_window_attention(*args, 70, 0, 0.125)
+    for window, sinks in (((1 << 63) - 1, 0), (1, (1 << 63) - 1)):
+        assert all(torch.equal(a, b) for a, b in zip(e3.e3_window_attention(*args, window, sinks, 0.125), want))
