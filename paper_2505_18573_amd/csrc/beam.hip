@@ -14,9 +14,9 @@
 // kept and one that is left out, are within 2e-6 of each other, the beams' sums are taken again in fp64, by the sequence's
 // workgroup, and the selection is made once more.  (One sequence in some hundreds; V = 151,936 takes 19 us for a beam.)
 //
-// Measured: 64 sequences x 8 beams, V = 151,936, bf16, keep 16: 36.7 us; the stream 27 (5.8 TB/s), the selection 9.5, a chain of phases with
+// Measured: 64 sequences x 8 beams, V = 151,936, bf16, keep 16: 36.5 us; the stream 27.3 (5.7 TB/s), the selection 9.7, a chain of phases with
 // barriers between (the beams' sums 1.8, the bound 2, chunks in order 1, their elements 1.8, these in order and out 1.2).  One sequence x 4, V
-// = 32,000, fp32: 10.7 us, two launches of latency.  A selection by the stream's last workgroup would need counters that start at zero.
+// = 32,000, fp32: 10.6 us, two launches of latency.  A selection by the stream's last workgroup would need counters that start at zero.
 #include "beam.h"
 #include "vocab_common.h"
 #include "vocab_pass.h"
@@ -634,7 +634,8 @@ hipError_t launch_beam_reorder(const ReorderArgs& a, hipStream_t stream)
 }
 
 // A workgroup per page and head: its keys, values and scale bytes are four runs next to each other each.  (64 sequences x 8 beams, 4 heads of 128
-// in 8 bits: 6.8 us for 23 MB in and out, the tables before it 3.5; what bounds both is the start and a chain of two loads.)
+// in 16 bits: 7.4 us for 23 MB in and out, in 8 bits 5.1 for 11.6, the tables before it 3.5; what bounds both is the start and a chain of two
+// loads.)
 __global__ __launch_bounds__(256)
 void cache_copy_kernel(CacheView c, const int32_t* src, const int32_t* dst, const int32_t* counts)
 {

@@ -18,7 +18,7 @@
 //
 // What bounds it: memory for prompts (60,001 tokens x 4 heads of 128: 123 MB of bf16 into 62 MB of codes 42 us, 4.4 TB/s; back
 // 31 us, 6.0 TB/s, part of the codes still in the memory-side cache), the launch and its chain of two loads (slot, row) for a step's
-// tokens (512: 5.4 us in, 4.3 us back).
+// tokens (512: 4.9 us in, 4.3 us back).
 #include "kv_cache.h"
 #include "rotary.h"
 #include "vocab_common.h"
@@ -322,8 +322,10 @@ void cache_append_kernel(CacheView c, TokenRows k, TokenRows v, const int64_t* s
 // are quantised: a lane's four columns are half of four pairs whose other half another lane of the row holds, or two whole
 // pairs.  The other rows turn the queries, a share of the heads each: a thread keeps the (cos, sin) of eight pairs of a token and
 // takes head after head.  Either kind asks for its first rows, and for all that the angles are made of, before it makes them.
-// Bound by memory: 30,001 tokens, 28 query and 4 key heads of 128, bf16 in, 8 bits kept: 122 us, 525 MB, 4.3 TB/s; the fp64 turns of the
-// keys lie in its shadow.  512 tokens 8.0 us (without turning and queries 5.4): two chains of loads, the angles, the exchange of codes.
+// Bound by memory: 30,001 tokens, 28 query and 4 key heads of 128, bf16 in, 8 bits kept: 120 to 132 us from card to card, 525 MB, 4.0 to 4.4 TB/s;
+// the fp64 turns of the keys lie in its shadow.  512 tokens 8.3 us (without turning and queries 4.9): 64 workgroups on 256 compute units make
+// two fp64 angles a thread, then turn, reduce and quantise four rows a lane, behind two or three dependent loads; into 16 bits 9.9, values
+// that are stored one by one.
 // Queries in a launch of their own, five workgroups' waves per SIMD, and a thread asking for its next head early were slower.
 constexpr int kAppendThreads = 256;
 template <int D, bool kFp8, bool kBf16>

@@ -22,11 +22,11 @@
 // would add as much error as the output's rounding (prompts 392 us for 465); the third product would cost a quarter more time.
 //
 // Measured, with the plan where there is one and the join: 512 rows of one query, 28 heads over 4 of 128, 8 bits, window 4096 of up to 7000
-// tokens 303 us, 5.1 TB/s: memory.  Prompts of 1000 to 4001 tokens, the same heads, 16 bits, window 1024: 434 to 465 us from card to card, 234
+// tokens 303 us, 5.1 TB/s: memory.  Prompts of 1000 to 4001 tokens, the same heads, 16 bits, window 1024: 434 to 467 us from card to card, 234
 // GFLOP of scores and values, 350 with the second bf16 number of the weights, so 0.8 PFLOP/s (a large product of the library: 1.26):
 // the matrix instructions of the two waves on a SIMD are half of the time, the vector instructions the other half, at the 1.6 to 1.8
-// GHz that were measured under this load.  A mixed batch of 33 rows of 1 to 300 queries, 12 heads over 2 of 64: 34.5 us; a workgroup has
-// 1.3 items and 7 steps, 5 us pass before the first item, 1.5 in a step, 3.5 into and out of an item, 8 in the join.  One row: 10.2
+// GHz that were measured under this load.  A mixed batch of 33 rows of 1 to 300 queries, 12 heads over 2 of 64: 33.9 us; a workgroup has
+// 1.3 items and 7 steps, 5 us pass before the first item, 1.5 in a step, 3.5 into and out of an item, 8 in the join.  One row: 10.3
 // us, two launches.  (The figures at the constants below compare builds that differ in nothing else, on these four.)
 #include "attention_step.h"
 #include "stretch.h"
